@@ -549,6 +549,76 @@ int loip_k_lm_head(const float* x, const uint16_t* g_final, const uint16_t* lm_h
                    int32_t V, float eps, float* z, float* logits, int32_t* tokens, void* scratch, void* stream);
 uint64_t loip_k_lm_head_scratch_bytes(int32_t B, int32_t V);
 
+/* ---------------------------------------------------------------------------
+ * Windowed serving over the paged cache: the append, and the attention of
+ * single tokens and of prompts behind a sliding window with sinks.  With a
+ * window the cache of a request stops growing: pages that hold neither sinks
+ * nor positions of the window are never read (nor are their page-table
+ * entries), so their memory can go to new pages instead of to further weight
+ * offloading (the KV thresholds of Sec. III-E).
+ *
+ * Cache layout and page table as for loip_k_attention (page_tokens = 64; page
+ * offsets, kv_base and layer_page_bytes multiples of 16).  `dtype` is the type
+ * of the activations (queries in, outputs out): LOIP_F32 or LOIP_BF16; sums,
+ * softmax states and norms are fp32, an fp32 query is not rounded on its way to
+ * the tensor cores, and each output is rounded once.  d = 64 or 128; any
+ * Hq / Hkv.  Zero rows are allowed and launch nothing.  Every call is async on
+ * `stream`, allocates nothing and can be captured in a CUDA graph; a refusal
+ * (LOIP_ERR_INVALID, message in loip_last_error(NULL)) comes before anything
+ * is enqueued.
+ * ------------------------------------------------------------------------- */
+enum { LOIP_F32 = 0, LOIP_BF16 = 1 };
+
+/* Norm of queries and keys for each head, position rotation, append.  Row t of
+ * qkv (T rows of (Hq + 2 Hkv) * d elements, row_stride elements apart: query
+ * heads, key heads, value heads; 16-byte aligned rows) is the token of request
+ * row_req[t] (row t when row_req is NULL) at position positions[t] (dev int32).
+ *   g_q, g_k (bf16 [d], both or neither): y = x / sqrt(mean(x^2) + eps) * g
+ *   theta >= 1: pairs (i, i + d/2) turn by position * theta^(-2i/d); 0: none
+ * The query goes to q_out ([T, Hq * d], dtype), key and value as bf16 into the
+ * request's page of that position.  The page table has n_req rows.  A row whose
+ * position is negative or past max_pages * 64, or whose request is not in
+ * [0, n_req), is padding: its q_out is zero and the cache keeps what it holds.
+ * Two rows for the same position of a request race. */
+int loip_k_qk_append(const void* qkv, int32_t dtype, int64_t row_stride, int32_t T, int32_t Hq, int32_t Hkv,
+                     int32_t d, const uint16_t* g_q, const uint16_t* g_k, float eps, float theta,
+                     const int32_t* positions, const int32_t* row_req, int32_t n_req, void* q_out, void* kv_base,
+                     const int64_t* page_offsets, int32_t max_pages, int32_t page_tokens, int32_t layer,
+                     uint64_t layer_page_bytes, void* stream);
+
+/* Attention of one new token of each of B requests: request b holds ctx_lens[b]
+ * cached positions (dev int32, the new token's included) and its query sees the
+ * last `window` of them and the first `sinks` (window >= the context: all of
+ * them).  A request that sees nothing (no context, or window and sinks zero)
+ * gets zeros.  ctx_lens[b] <= max_ctx <= max_pages * 64 (a larger one is read
+ * as max_ctx).  o [B, Hq * d].  `scratch` (dev, 16-byte aligned, scratch_bytes
+ * >= loip_k_window_attention_scratch_bytes(...)) holds partial softmax states
+ * and completion counters: zero-filled once by the caller, left usable by every
+ * call; calls that may overlap on the GPU need a scratch each. */
+int loip_k_window_attention(const void* q, int32_t dtype, const void* kv_base, const int64_t* page_offsets,
+                            int32_t max_pages, const int32_t* ctx_lens, int32_t B, int32_t Hq, int32_t Hkv, int32_t d,
+                            int32_t page_tokens, int32_t layer, uint64_t layer_page_bytes, int32_t window,
+                            int32_t sinks, int32_t max_ctx, void* scratch, uint64_t scratch_bytes, void* o,
+                            void* stream);
+uint64_t loip_k_window_attention_scratch_bytes(int32_t B, int32_t Hq, int32_t Hkv, int32_t d, int32_t window,
+                                               int32_t sinks, int32_t max_ctx);
+
+/* The same attention for the M rows of n_prompts prompts or chunks of prompts:
+ * prompt i's rows are row_starts[i] .. row_starts[i + 1] - 1 (dev int32
+ * [n_prompts + 1], from 0 to M, not decreasing) at positions first_pos[i], ...
+ * (dev int32 [n_prompts], NULL = 0) of request i, whose keys and values up to
+ * the last row are in the cache.  The row at position p sees the cached
+ * positions j <= p with j > p - window or j < sinks; a row that sees nothing
+ * gets zeros.  No position reaches max_ctx (<= max_pages * 64; keys past it are
+ * not read).  o [M, Hq * d].  Scratch as for loip_k_window_attention. */
+int loip_k_window_prefill(const void* q, int32_t dtype, const void* kv_base, const int64_t* page_offsets,
+                          int32_t max_pages, const int32_t* row_starts, const int32_t* first_pos, int32_t n_prompts,
+                          int32_t M, int32_t Hq, int32_t Hkv, int32_t d, int32_t page_tokens, int32_t layer,
+                          uint64_t layer_page_bytes, int32_t window, int32_t sinks, int32_t max_ctx, void* scratch,
+                          uint64_t scratch_bytes, void* o, void* stream);
+uint64_t loip_k_window_prefill_scratch_bytes(int32_t M, int32_t n_prompts, int32_t Hq, int32_t Hkv, int32_t d,
+                                             int32_t window, int32_t sinks, int32_t max_ctx);
+
 #ifdef __cplusplus
 }
 #endif

@@ -176,6 +176,11 @@ int attention_tc_tile_positions(int Hq, int Hkv);
 cudaError_t launch_attention_tc(const float* q, KvView kv, const int4* tiles, int n_tiles, int M, int Hq, int Hkv,
                                 int d, uint16_t* o, cudaStream_t st);
 cudaError_t attention_tc_error(int* code);
+// Status of a kernel-level entry point that has no context: a refusal or a failed
+// launch leaves its message for loip_last_error(NULL).  Never throws.
+int kernel_refused(const char* why);
+int kernel_status(cudaError_t e);
+
 cudaError_t launch_gather_rows(const float* x, const int32_t* rows, int n, int H, float* out, cudaStream_t st);
 
 }  // namespace loip

@@ -2500,6 +2500,23 @@ static int cerr(cudaError_t e) {
     return LOIP_ERR_CUDA;
 }
 
+namespace loip {
+int kernel_refused(const char* why) {
+    try {
+        g_create_error = why;
+    } catch (...) {  // no memory for the message: the status alone
+    }
+    return LOIP_ERR_INVALID;
+}
+int kernel_status(cudaError_t e) {
+    try {
+        return cerr(e);
+    } catch (...) {
+        return LOIP_ERR_CUDA;
+    }
+}
+}  // namespace loip
+
 extern "C" int loip_k_generate(uint16_t* out, uint64_t n, uint64_t first, uint64_t seed, uint32_t tensor_id,
                                int32_t kind, void* stream) {
     if ((!out && n) || (kind != 0 && kind != 1) || first + n > (1ull << 40)) return LOIP_ERR_INVALID;

@@ -1,0 +1,387 @@
+// window.cu -- windowed serving over the paged cache: the append of new tokens
+// (norm of queries and keys for each head, position rotation, keys and values
+// into their pages) and the attention behind a sliding window with sinks.
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include "../../include/loip.h"
+#include "internal.h"
+#include "window.h"
+
+namespace loip {
+namespace {
+
+// ---------------------------------------------------------------------------
+// Append.
+//
+// y = x / sqrt(mean(x^2) + eps) * g for each query and key head (optional), then
+// (y_i, y_{i + d/2}) turns by position * theta^(-2i/d).
+//
+// The angle is kept in turns, as a 64-bit fixed-point fraction: turn_i =
+// theta^(-2i/d) / (2 pi) rounded to 2^-64, and position * turn_i modulo 2^64 is
+// the fraction of a turn itself -- one integer product, exact up to position *
+// 2^-65, where a floating-point angle would have to be reduced modulo 2 pi.  Its
+// top 32 bits, as a signed number, are an angle in [-pi, pi) for sincospif.
+// ---------------------------------------------------------------------------
+struct RopeTurns {
+    uint64_t turn[64];
+};
+
+RopeTurns rope_turns(float theta, int d) {
+    RopeTurns r{};
+    for (int i = 0; i < d / 2; ++i)  // below 1 / (2 pi) of 2^64, so the conversion is in range
+        r.turn[i] = theta == 0.f ? 0 : (uint64_t)ldexp(pow((double)theta, -2.0 * i / d) * 0.15915494309189535, 64);
+    return r;
+}
+
+struct AppendArgs {
+    const void* qkv;
+    int64_t row_stride;
+    const __nv_bfloat16 *g_q, *g_k;
+    float eps;
+    const int32_t *positions, *row_req;
+    int n_req, Hq, Hkv;
+    void* q_out;
+    KvView kv;
+    RopeTurns rope;
+};
+
+__device__ __forceinline__ void load8(const float* p, float (&v)[8]) {
+    const float4 a = __ldg(reinterpret_cast<const float4*>(p)), b = __ldg(reinterpret_cast<const float4*>(p) + 1);
+    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+}
+__device__ __forceinline__ void load8(const __nv_bfloat16* p, float (&v)[8]) {
+    const uint4 w = __ldg(reinterpret_cast<const uint4*>(p));
+    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        v[2 * i] = __uint_as_float(u[i] << 16);
+        v[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
+    }
+}
+__device__ __forceinline__ void store8(float* p, const float (&v)[8]) {
+    reinterpret_cast<float4*>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
+    reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+}
+__device__ __forceinline__ void store8(__nv_bfloat16* p, const float (&v)[8]) {
+    uint32_t u[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+        u[i] = *reinterpret_cast<const uint32_t*>(&h);
+    }
+    *reinterpret_cast<uint4*>(p) = make_uint4(u[0], u[1], u[2], u[3]);
+}
+
+// One block per token and group of heads; D / 16 lanes per head, each holding
+// the elements 8l .. 8l + 7 of the head and their partners D / 2 further on.
+template <int D, typename T>
+__global__ void __launch_bounds__(256) qk_append_kernel(const __grid_constant__ AppendArgs p) {
+    constexpr int LANES = D / 16, HEADS = 256 / LANES;
+    __shared__ __align__(16) float2 turn[D / 2];  // cos, sin
+    const int t = blockIdx.x, l = threadIdx.x % LANES, head = blockIdx.y * HEADS + threadIdx.x / LANES;
+    const bool live = head < p.Hq + 2 * p.Hkv;
+    const int pos = p.positions[t], req = p.row_req ? p.row_req[t] : t;
+    const bool padding = pos < 0 || pos / kPageTokens >= p.kv.max_pages || req < 0 || req >= p.n_req;
+    float a[8], b[8];
+    if (live) {
+        const T* x = static_cast<const T*>(p.qkv) + (int64_t)t * p.row_stride + head * D + 8 * l;
+        load8(x, a);
+        load8(x + D / 2, b);
+    }
+    if (threadIdx.x < D / 2) {
+        const int32_t turns = (int32_t)((uint64_t)pos * p.rope.turn[threadIdx.x] >> 32);
+        float s, c;
+        sincospif((float)turns * 0x1p-31f, &s, &c);
+        turn[threadIdx.x] = make_float2(c, s);
+    }
+    __syncthreads();
+    const bool is_q = head < p.Hq, is_v = head >= p.Hq + p.Hkv;
+    if (p.g_q) {  // the sum is fp32, over a head's lanes
+        float ss = 0.f;
+        if (live) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) ss = fmaf(a[i], a[i], fmaf(b[i], b[i], ss));
+        }
+#pragma unroll
+        for (int m = 1; m < LANES; m *= 2) ss += __shfl_xor_sync(0xffffffffu, ss, m);
+        if (live && !is_v) {
+            const float r = 1.0f / sqrtf(ss * (1.0f / D) + p.eps);
+            const __nv_bfloat16* g = (is_q ? p.g_q : p.g_k) + 8 * l;
+            float ga[8], gb[8];
+            load8(g, ga);
+            load8(g + D / 2, gb);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                a[i] *= r * ga[i];
+                b[i] *= r * gb[i];
+            }
+        }
+    }
+    if (!live) return;
+    if (!is_v) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float2 cs = turn[8 * l + i];
+            const float x = a[i], y = b[i];
+            a[i] = x * cs.x - y * cs.y;
+            b[i] = y * cs.x + x * cs.y;
+        }
+    }
+    if (is_q) {
+        T* o = static_cast<T*>(p.q_out) + ((int64_t)t * p.Hq + head) * D + 8 * l;
+        if (padding) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) a[i] = b[i] = 0.f;
+        }
+        store8(o, a);
+        store8(o + D / 2, b);
+    } else if (!padding) {
+        // keys, then values, of the layer: [Hkv][64][D] each
+        char* page = p.kv.base + p.kv.page_offsets[(int64_t)req * p.kv.max_pages + pos / kPageTokens] +
+                     (uint64_t)p.kv.layer * p.kv.layer_page_bytes;
+        __nv_bfloat16* o = reinterpret_cast<__nv_bfloat16*>(page) +
+                           ((int64_t)(head - p.Hq) * kPageTokens + pos % kPageTokens) * D + 8 * l;
+        store8(o, a);
+        store8(o + D / 2, b);
+    }
+}
+
+template <int D, typename T>
+cudaError_t launch_append(const AppendArgs& a, int rows, cudaStream_t st) {
+    constexpr int HEADS = 256 / (D / 16);
+    const int heads = a.Hq + 2 * a.Hkv;
+    qk_append_kernel<D, T><<<dim3(rows, (heads + HEADS - 1) / HEADS), 256, 0, st>>>(a);
+    return cudaGetLastError();
+}
+
+// ---------------------------------------------------------------------------
+// Attention, the simple form: one warp per (row, query head) walks the visible
+// positions with the running maximum and sum of its softmax.
+// ---------------------------------------------------------------------------
+__device__ __forceinline__ float rows_load(const float* p) { return *p; }
+__device__ __forceinline__ float rows_load(const __nv_bfloat16* p) { return __bfloat162float(*p); }
+__device__ __forceinline__ void rows_store(float* p, float v) { *p = v; }
+__device__ __forceinline__ void rows_store(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
+
+template <int D, typename T>
+__global__ void __launch_bounds__(128) attn_rows_kernel(const WindowArgs a) {
+    const int lane = threadIdx.x % 32;
+    const int64_t unit = (int64_t)blockIdx.x * 4 + threadIdx.x / 32;
+    if (unit >= (int64_t)a.rows * a.Hq) return;
+    const int row = (int)(unit / a.Hq), h = (int)(unit % a.Hq), g = h / (a.Hq / a.Hkv);
+    int req = row, pos;
+    if (a.ctx_lens) {
+        pos = min(a.ctx_lens[row], a.max_ctx) - 1;
+    } else {
+        int lo = 0, hi = a.n_prompts;  // the last prompt that starts at or before the row
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) / 2;
+            if (a.row_starts[mid] <= row) lo = mid; else hi = mid;
+        }
+        req = lo;
+        pos = (a.first_pos ? a.first_pos[req] : 0) + row - a.row_starts[req];
+    }
+    const T* q = static_cast<const T*>(a.q) + ((int64_t)row * a.Hq + h) * D;
+    T* out = static_cast<T*>(a.o) + ((int64_t)row * a.Hq + h) * D;
+    float qv[D / 32], o[D / 32], m = -INFINITY, l = 0.f;
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) {
+        qv[i] = rows_load(q + i * 32 + lane);
+        o[i] = 0.f;
+    }
+    const float scale = 1.0f / sqrtf((float)D);
+    const int last = min(pos, a.max_ctx - 1);
+    for (int j = 0; j <= last; ++j) {
+        if (j >= a.sinks && j <= pos - a.window) {  // to the window's first position
+            j = pos - a.window;
+            continue;
+        }
+        const __nv_bfloat16* k =
+            reinterpret_cast<const __nv_bfloat16*>(
+                a.kv.base + a.kv.page_offsets[(int64_t)req * a.kv.max_pages + j / kPageTokens] +
+                (uint64_t)a.kv.layer * a.kv.layer_page_bytes) +
+            ((int64_t)g * kPageTokens + j % kPageTokens) * D;
+        const __nv_bfloat16* v = k + (int64_t)a.Hkv * kPageTokens * D;
+        float s = 0.f;
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) s = fmaf(qv[i], __bfloat162float(k[i * 32 + lane]), s);
+#pragma unroll
+        for (int x = 16; x; x /= 2) s += __shfl_xor_sync(0xffffffffu, s, x);
+        s *= scale;
+        const float m_new = fmaxf(m, s), alpha = expf(m - m_new), w = expf(s - m_new);
+        l = l * alpha + w;
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) o[i] = fmaf(w, __bfloat162float(v[i * 32 + lane]), o[i] * alpha);
+        m = m_new;
+    }
+    const float inv = l > 0.f ? 1.0f / l : 0.f;
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) rows_store(out + i * 32 + lane, o[i] * inv);
+}
+
+template <int D, typename T>
+cudaError_t launch_attn_rows(const WindowArgs& a, cudaStream_t st) {
+    const int64_t units = (int64_t)a.rows * a.Hq;
+    attn_rows_kernel<D, T><<<(unsigned)((units + 3) / 4), 128, 0, st>>>(a);
+    return cudaGetLastError();
+}
+
+cudaError_t launch_attn(const WindowArgs& a, bool f32, cudaStream_t st) {
+    if (a.d == 128) return f32 ? launch_attn_rows<128, float>(a, st) : launch_attn_rows<128, __nv_bfloat16>(a, st);
+    return f32 ? launch_attn_rows<64, float>(a, st) : launch_attn_rows<64, __nv_bfloat16>(a, st);
+}
+
+bool aligned(const void* p, uintptr_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
+
+// What every call on the cache has in common; null if it is in order.
+const char* cache_refusal(int dtype, int rows, int Hq, int Hkv, int d, const void* kv_base, const int64_t* page_offsets,
+                          int max_pages, int page_tokens, int layer, uint64_t layer_page_bytes) {
+    if (dtype != LOIP_F32 && dtype != LOIP_BF16) return "dtype is LOIP_F32 or LOIP_BF16";
+    if (rows < 0) return "a negative number of rows";
+    if (Hkv < 1 || Hq < 1 || Hq % Hkv) return "the query heads are a multiple of the kv heads";
+    if ((int64_t)Hq + 2 * (int64_t)Hkv > 65535) return "more heads than the kernels take";
+    if (d != 64 && d != 128) return "the head size is 64 or 128";
+    if (page_tokens != kPageTokens) return "pages hold 64 tokens";
+    if (max_pages < 1 || layer < 0) return "no pages, or a negative layer";
+    if (!kv_base || !aligned(kv_base, 16) || layer_page_bytes % 16) return "the cache is 16-byte aligned";
+    if (!page_offsets || !aligned(page_offsets, 8)) return "the page table is an 8-byte aligned device array";
+    return nullptr;
+}
+
+const char* window_refusal(const void* q, const void* o, int max_pages, int window, int sinks, int max_ctx,
+                           const void* scratch, uint64_t scratch_bytes, uint64_t scratch_need) {
+    if (!q || !o || !aligned(q, 16) || !aligned(o, 16)) return "queries and outputs are 16-byte aligned";
+    if (window < 0 || sinks < 0) return "a negative window or number of sinks";
+    if (max_ctx < 1 || (int64_t)max_pages * kPageTokens < max_ctx) return "max_ctx is 1 to max_pages * 64";
+    if (!scratch || !aligned(scratch, 16) || scratch_bytes < scratch_need)
+        return "the scratch is 16-byte aligned and as large as its size function says";
+    return nullptr;
+}
+
+}  // namespace
+}  // namespace loip
+
+using namespace loip;
+
+extern "C" int loip_k_qk_append(const void* qkv, int32_t dtype, int64_t row_stride, int32_t T, int32_t Hq, int32_t Hkv,
+                                int32_t d, const uint16_t* g_q, const uint16_t* g_k, float eps, float theta,
+                                const int32_t* positions, const int32_t* row_req, int32_t n_req, void* q_out,
+                                void* kv_base, const int64_t* page_offsets, int32_t max_pages, int32_t page_tokens,
+                                int32_t layer, uint64_t layer_page_bytes, void* stream) {
+    if (const char* why = cache_refusal(dtype, T, Hq, Hkv, d, kv_base, page_offsets, max_pages, page_tokens, layer,
+                                        layer_page_bytes))
+        return kernel_refused(why);
+    if (T == 0) return LOIP_OK;
+    const int64_t width = (int64_t)(Hq + 2 * Hkv) * d;
+    if (!qkv || !q_out || !aligned(qkv, 16) || !aligned(q_out, 16) || row_stride < width ||
+        row_stride % (dtype == LOIP_F32 ? 4 : 8))
+        return kernel_refused("the rows of qkv and q_out are 16-byte aligned and do not overlap");
+    if (!positions || !aligned(positions, 4) || !aligned(row_req, 4) || n_req < 1)
+        return kernel_refused("positions (and requests) are device int32 arrays, the page table has a row");
+    if (!g_q != !g_k || !aligned(g_q, 16) || !aligned(g_k, 16))
+        return kernel_refused("both gains or neither, 16-byte aligned");
+    if (!(theta == 0.f || (theta >= 1.f && isfinite(theta))) || !(eps >= 0.f && isfinite(eps)))
+        return kernel_refused("theta is 0 or at least 1, eps is not negative");
+    AppendArgs a{};
+    a.qkv = qkv;
+    a.row_stride = row_stride;
+    a.g_q = reinterpret_cast<const __nv_bfloat16*>(g_q);
+    a.g_k = reinterpret_cast<const __nv_bfloat16*>(g_k);
+    a.eps = eps;
+    a.positions = positions;
+    a.row_req = row_req;
+    a.n_req = n_req;
+    a.Hq = Hq;
+    a.Hkv = Hkv;
+    a.q_out = q_out;
+    a.kv = KvView{(char*)kv_base, page_offsets, max_pages, page_tokens, layer, layer_page_bytes};
+    a.rope = rope_turns(theta, d);
+    cudaStream_t st = (cudaStream_t)stream;
+    if (d == 128)
+        return kernel_status(dtype == LOIP_F32 ? launch_append<128, float>(a, T, st)
+                                               : launch_append<128, __nv_bfloat16>(a, T, st));
+    return kernel_status(dtype == LOIP_F32 ? launch_append<64, float>(a, T, st)
+                                           : launch_append<64, __nv_bfloat16>(a, T, st));
+}
+
+extern "C" uint64_t loip_k_window_attention_scratch_bytes(int32_t B, int32_t Hq, int32_t Hkv, int32_t d,
+                                                          int32_t window, int32_t sinks, int32_t max_ctx) {
+    if (B < 0 || Hq < 1 || Hkv < 1 || Hq % Hkv || (d != 64 && d != 128) || window < 0 || sinks < 0 || max_ctx < 1)
+        return 0;
+    return 16;
+}
+
+extern "C" int loip_k_window_attention(const void* q, int32_t dtype, const void* kv_base, const int64_t* page_offsets,
+                                       int32_t max_pages, const int32_t* ctx_lens, int32_t B, int32_t Hq, int32_t Hkv,
+                                       int32_t d, int32_t page_tokens, int32_t layer, uint64_t layer_page_bytes,
+                                       int32_t window, int32_t sinks, int32_t max_ctx, void* scratch,
+                                       uint64_t scratch_bytes, void* o, void* stream) {
+    if (const char* why = cache_refusal(dtype, B, Hq, Hkv, d, kv_base, page_offsets, max_pages, page_tokens, layer,
+                                        layer_page_bytes))
+        return kernel_refused(why);
+    if (B == 0) return LOIP_OK;
+    if (const char* why = window_refusal(q, o, max_pages, window, sinks, max_ctx, scratch, scratch_bytes,
+                                         loip_k_window_attention_scratch_bytes(B, Hq, Hkv, d, window, sinks, max_ctx)))
+        return kernel_refused(why);
+    if (!ctx_lens || !aligned(ctx_lens, 4)) return kernel_refused("ctx_lens is a device int32 array");
+    WindowArgs a{};
+    a.q = q;
+    a.o = o;
+    a.kv = KvView{(char*)kv_base, page_offsets, max_pages, page_tokens, layer, layer_page_bytes};
+    a.ctx_lens = ctx_lens;
+    a.rows = B;
+    a.Hq = Hq;
+    a.Hkv = Hkv;
+    a.d = d;
+    a.window = window;
+    a.sinks = sinks;
+    a.max_ctx = max_ctx;
+    a.scratch = scratch;
+    return kernel_status(launch_attn(a, dtype == LOIP_F32, (cudaStream_t)stream));
+}
+
+extern "C" uint64_t loip_k_window_prefill_scratch_bytes(int32_t M, int32_t n_prompts, int32_t Hq, int32_t Hkv,
+                                                        int32_t d, int32_t window, int32_t sinks, int32_t max_ctx) {
+    if (M < 0 || n_prompts < 0 || Hq < 1 || Hkv < 1 || Hq % Hkv || (d != 64 && d != 128) || window < 0 || sinks < 0 ||
+        max_ctx < 1)
+        return 0;
+    return 16;
+}
+
+extern "C" int loip_k_window_prefill(const void* q, int32_t dtype, const void* kv_base, const int64_t* page_offsets,
+                                     int32_t max_pages, const int32_t* row_starts, const int32_t* first_pos,
+                                     int32_t n_prompts, int32_t M, int32_t Hq, int32_t Hkv, int32_t d,
+                                     int32_t page_tokens, int32_t layer, uint64_t layer_page_bytes, int32_t window,
+                                     int32_t sinks, int32_t max_ctx, void* scratch, uint64_t scratch_bytes, void* o,
+                                     void* stream) {
+    if (const char* why = cache_refusal(dtype, M, Hq, Hkv, d, kv_base, page_offsets, max_pages, page_tokens, layer,
+                                        layer_page_bytes))
+        return kernel_refused(why);
+    if (M == 0) return LOIP_OK;
+    if (n_prompts < 1) return kernel_refused("rows without a prompt");
+    if (const char* why = window_refusal(q, o, max_pages, window, sinks, max_ctx, scratch, scratch_bytes,
+                                         loip_k_window_prefill_scratch_bytes(M, n_prompts, Hq, Hkv, d, window, sinks,
+                                                                             max_ctx)))
+        return kernel_refused(why);
+    if (!row_starts || !aligned(row_starts, 4) || !aligned(first_pos, 4))
+        return kernel_refused("row_starts (and first_pos) are device int32 arrays");
+    WindowArgs a{};
+    a.q = q;
+    a.o = o;
+    a.kv = KvView{(char*)kv_base, page_offsets, max_pages, page_tokens, layer, layer_page_bytes};
+    a.row_starts = row_starts;
+    a.first_pos = first_pos;
+    a.n_prompts = n_prompts;
+    a.rows = M;
+    a.Hq = Hq;
+    a.Hkv = Hkv;
+    a.d = d;
+    a.window = window;
+    a.sinks = sinks;
+    a.max_ctx = max_ctx;
+    a.scratch = scratch;
+    return kernel_status(launch_attn(a, dtype == LOIP_F32, (cudaStream_t)stream));
+}

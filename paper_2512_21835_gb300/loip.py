@@ -120,6 +120,14 @@ _SIGS = {
     "loip_k_pack": (C.c_int, [P, U64, P, P, C.c_uint32, C.c_uint32, P]),
     "loip_k_unpack": (C.c_int, [P, U64, P, P]),
     "loip_k_tc_status": (C.c_int, []),
+    "loip_k_qk_append": (C.c_int, [P, I32, C.c_int64, I32, I32, I32, I32, P, P, F32, F32, P, P, I32, P, P, P, I32, I32,
+                                   I32, U64, P]),
+    "loip_k_window_attention": (C.c_int, [P, I32, P, P, I32, P, I32, I32, I32, I32, I32, I32, U64, I32, I32, I32, P,
+                                          U64, P, P]),
+    "loip_k_window_attention_scratch_bytes": (C.c_uint64, [I32] * 7),
+    "loip_k_window_prefill": (C.c_int, [P, I32, P, P, I32, P, P, I32, I32, I32, I32, I32, I32, I32, U64, I32, I32, I32,
+                                        P, U64, P, P]),
+    "loip_k_window_prefill_scratch_bytes": (C.c_uint64, [I32] * 8),
 }
 
 _lib = None
@@ -510,3 +518,66 @@ def loip_k_lm_head(x, g_final, lm_head, eps, z, logits, tokens, scratch, stream=
     B, H = x.shape
     _check(lib().loip_k_lm_head(_ptr(x), _ptr(g_final), _ptr(lm_head), B, H, lm_head.shape[0], eps, _ptr(z),
                                 _ptr(logits), _ptr(tokens), _ptr(scratch), _s(stream)))
+
+
+F32_ROWS, BF16_ROWS = 0, 1  # `dtype` of the windowed operators' activations
+
+
+def _dtype(x, like=None):
+    """LOIP_F32 / LOIP_BF16 of a tensor; `like`, if given, has to be of the same type."""
+    import torch
+    if like is not None and like.dtype != x.dtype:
+        raise LoipError(ERR_INVALID, f"input of {x.dtype} with an output of {like.dtype}")
+    if x.dtype == torch.float32:
+        return F32_ROWS
+    if x.dtype == torch.bfloat16:
+        return BF16_ROWS
+    raise LoipError(ERR_INVALID, f"activations are float32 or bfloat16, not {x.dtype}")
+
+
+def loip_k_qk_append(qkv, g_q, g_k, Hq, Hkv, d, eps, theta, positions, row_req, q_out, kv_base, page_offsets,
+                     max_pages, page_tokens, layer, layer_page_bytes, stream=None):
+    """Norm of queries and keys (g_q, g_k or None), rotation (theta 0: none), append.  qkv [T, (Hq + 2 Hkv) * d]
+    float32 or bfloat16 with any row stride; page_offsets [requests, max_pages]."""
+    if qkv.stride(-1) != 1 or not q_out.is_contiguous():
+        raise LoipError(ERR_INVALID, "rows of qkv have to be contiguous, and q_out as a whole")
+    T = qkv.shape[0]
+    if positions.numel() < T or q_out.numel() != T * Hq * d or qkv.shape[1] != (Hq + 2 * Hkv) * d:
+        raise LoipError(ERR_INVALID, "qkv, positions and q_out do not fit together")
+    _check(lib().loip_k_qk_append(_ptr(qkv), _dtype(qkv, q_out), qkv.stride(0), T, Hq, Hkv, d, _ptr(g_q), _ptr(g_k),
+                                  eps, theta, _ptr(positions), _ptr(row_req), page_offsets.shape[0], _ptr(q_out),
+                                  _ptr(kv_base), _ptr(page_offsets), max_pages, page_tokens, layer, layer_page_bytes,
+                                  _s(stream)))
+
+
+def loip_k_window_attention_scratch_bytes(B, Hq, Hkv, d, window, sinks, max_ctx) -> int:
+    return int(lib().loip_k_window_attention_scratch_bytes(B, Hq, Hkv, d, window, sinks, max_ctx))
+
+
+def loip_k_window_attention(q, kv_base, page_offsets, max_pages, ctx_lens, Hq, Hkv, d, page_tokens, layer,
+                            layer_page_bytes, window, sinks, max_ctx, scratch, o, stream=None):
+    """Attention of one new token per request behind a window with sinks.  scratch: a uint8 tensor of
+    loip_k_window_attention_scratch_bytes(...), zero-filled once."""
+    B = q.shape[0]
+    if not (q.is_contiguous() and o.is_contiguous()) or q.numel() != B * Hq * d or o.numel() != q.numel():
+        raise LoipError(ERR_INVALID, "q and o are contiguous [B, Hq * d]")
+    _check(lib().loip_k_window_attention(_ptr(q), _dtype(q, o), _ptr(kv_base), _ptr(page_offsets), max_pages,
+                                         _ptr(ctx_lens), B, Hq, Hkv, d, page_tokens, layer, layer_page_bytes, window,
+                                         sinks, max_ctx, _ptr(scratch), scratch.nbytes, _ptr(o), _s(stream)))
+
+
+def loip_k_window_prefill_scratch_bytes(M, n_prompts, Hq, Hkv, d, window, sinks, max_ctx) -> int:
+    return int(lib().loip_k_window_prefill_scratch_bytes(M, n_prompts, Hq, Hkv, d, window, sinks, max_ctx))
+
+
+def loip_k_window_prefill(q, kv_base, page_offsets, max_pages, row_starts, first_pos, Hq, Hkv, d, page_tokens, layer,
+                          layer_page_bytes, window, sinks, max_ctx, scratch, o, stream=None):
+    """The same attention for the rows of prompts: row_starts (device int32 [prompts + 1]), first_pos (device int32
+    [prompts] or None = 0)."""
+    M = q.shape[0]
+    if not (q.is_contiguous() and o.is_contiguous()) or q.numel() != M * Hq * d or o.numel() != q.numel():
+        raise LoipError(ERR_INVALID, "q and o are contiguous [M, Hq * d]")
+    _check(lib().loip_k_window_prefill(_ptr(q), _dtype(q, o), _ptr(kv_base), _ptr(page_offsets), max_pages,
+                                       _ptr(row_starts), _ptr(first_pos), row_starts.numel() - 1, M, Hq, Hkv, d,
+                                       page_tokens, layer, layer_page_bytes, window, sinks, max_ctx, _ptr(scratch),
+                                       scratch.nbytes, _ptr(o), _s(stream)))
