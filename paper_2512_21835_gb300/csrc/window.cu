@@ -172,18 +172,12 @@ __global__ void __launch_bounds__(128) attn_rows_kernel(const WindowArgs a) {
     const int64_t unit = (int64_t)blockIdx.x * 4 + threadIdx.x / 32;
     if (unit >= (int64_t)a.rows * a.Hq) return;
     const int row = (int)(unit / a.Hq), h = (int)(unit % a.Hq), g = h / (a.Hq / a.Hkv);
-    int req = row, pos;
-    if (a.ctx_lens) {
-        pos = min(a.ctx_lens[row], a.max_ctx) - 1;
-    } else {
-        int lo = 0, hi = a.n_prompts;  // the last prompt that starts at or before the row
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) / 2;
-            if (a.row_starts[mid] <= row) lo = mid; else hi = mid;
-        }
-        req = lo;
-        pos = (a.first_pos ? a.first_pos[req] : 0) + row - a.row_starts[req];
+    int req = 0, hi = a.n_prompts;  // the last prompt that starts at or before the row
+    while (hi - req > 1) {
+        const int mid = (req + hi) / 2;
+        if (a.row_starts[mid] <= row) req = mid; else hi = mid;
     }
+    const int pos = (a.first_pos ? a.first_pos[req] : 0) + row - a.row_starts[req];
     const T* q = static_cast<const T*>(a.q) + ((int64_t)row * a.Hq + h) * D;
     T* out = static_cast<T*>(a.o) + ((int64_t)row * a.Hq + h) * D;
     float qv[D / 32], o[D / 32], m = -INFINITY, l = 0.f;
@@ -255,7 +249,8 @@ const char* window_refusal(const void* q, const void* o, int max_pages, int wind
                            const void* scratch, uint64_t scratch_bytes, uint64_t scratch_need) {
     if (!q || !o || !aligned(q, 16) || !aligned(o, 16)) return "queries and outputs are 16-byte aligned";
     if (window < 0 || sinks < 0) return "a negative window or number of sinks";
-    if (max_ctx < 1 || (int64_t)max_pages * kPageTokens < max_ctx) return "max_ctx is 1 to max_pages * 64";
+    if (max_ctx < 1 || max_ctx > 1 << 30 || (int64_t)max_pages * kPageTokens < max_ctx)
+        return "max_ctx is 1 to max_pages * 64, and at most 2^30";
     if (!scratch || !aligned(scratch, 16) || scratch_bytes < scratch_need)
         return "the scratch is 16-byte aligned and as large as its size function says";
     return nullptr;
@@ -311,7 +306,7 @@ extern "C" uint64_t loip_k_window_attention_scratch_bytes(int32_t B, int32_t Hq,
                                                           int32_t window, int32_t sinks, int32_t max_ctx) {
     if (B < 0 || Hq < 1 || Hkv < 1 || Hq % Hkv || (d != 64 && d != 128) || window < 0 || sinks < 0 || max_ctx < 1)
         return 0;
-    return 16;
+    return window_decode_scratch(B, Hq, Hkv, d, window, sinks, max_ctx);
 }
 
 extern "C" int loip_k_window_attention(const void* q, int32_t dtype, const void* kv_base, const int64_t* page_offsets,
@@ -340,7 +335,7 @@ extern "C" int loip_k_window_attention(const void* q, int32_t dtype, const void*
     a.sinks = sinks;
     a.max_ctx = max_ctx;
     a.scratch = scratch;
-    return kernel_status(launch_attn(a, dtype == LOIP_F32, (cudaStream_t)stream));
+    return kernel_status(launch_window_decode(a, dtype == LOIP_F32, (cudaStream_t)stream));
 }
 
 extern "C" uint64_t loip_k_window_prefill_scratch_bytes(int32_t M, int32_t n_prompts, int32_t Hq, int32_t Hkv,

@@ -26,4 +26,9 @@ struct WindowArgs {
     void* scratch;
 };
 
+// Attention of single tokens (window_decode.cu).  The scratch starts with completion
+// counters that a call leaves at zero; its size follows from the sizes alone.
+uint64_t window_decode_scratch(int B, int Hq, int Hkv, int d, int window, int sinks, int max_ctx);
+cudaError_t launch_window_decode(const WindowArgs& a, bool f32, cudaStream_t st);
+
 }  // namespace loip

@@ -54,7 +54,7 @@ CACHE_BAD = [dict(dtype=2), dict(dtype=-1), dict(Hq=5), dict(Hkv=0), dict(Hq=0),
              dict(page_tokens=16), dict(page_tokens=0), dict(max_pages=0), dict(layer=-1), dict(kv=None),
              dict(kv=A + 8), dict(table=None), dict(table=A + 4), dict(lpb=24)]
 WINDOW_BAD = [dict(q=None), dict(q=A + 8), dict(o=None), dict(o=A + 4), dict(window=-1), dict(sinks=-1),
-              dict(max_ctx=0), dict(max_ctx=257), dict(scratch=None), dict(scratch=A + 8), dict(nbytes=0)]
+              dict(max_ctx=0), dict(max_ctx=257), dict(max_ctx=(1 << 30) + 1, max_pages=1 << 25), dict(scratch=None), dict(scratch=A + 8), dict(nbytes=0)]
 
 
 @pytest.mark.parametrize("bad", CACHE_BAD + [
