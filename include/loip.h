@@ -475,8 +475,8 @@ int loip_k_prefill_attention(const float* q, const void* kv_base, const int64_t*
                              int32_t Hkv, int32_t d, int32_t page_tokens, int32_t layer, uint64_t layer_page_bytes,
                              void* tiles, uint16_t* o2, void* stream);
 
-/* 0 if no tensor-core attention launch has recorded a failure (a bounded wait
- * that ran out); otherwise the first failure code.  -1 if unreadable. */
+/* 0 if no tensor-core attention launch (this one and loip_k_window_prefill) has
+ * recorded a failure (a bounded wait that ran out); otherwise the first failure code.  -1 if unreadable. */
 int loip_k_attention_tc_status(void);
 
 /* x += wo o  (output projection with the residual add); o fp32 [B, Hq*d].  As in

@@ -31,6 +31,7 @@
 #include "hostpool.h"
 #include "internal.h"
 #include "plan.h"
+#include "window.h"
 
 using namespace loip;
 
@@ -2595,6 +2596,7 @@ extern "C" int loip_k_prefill_attention(const float* q, const void* kv_base, con
 extern "C" int loip_k_attention_tc_status(void) {
     int code = 0;
     if (attention_tc_error(&code) != cudaSuccess) return -1;
+    if (!code && window_prefill_error(&code) != cudaSuccess) return -1;
     return code;
 }
 

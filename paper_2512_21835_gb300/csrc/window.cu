@@ -157,77 +157,6 @@ cudaError_t launch_append(const AppendArgs& a, int rows, cudaStream_t st) {
     return cudaGetLastError();
 }
 
-// ---------------------------------------------------------------------------
-// Attention, the simple form: one warp per (row, query head) walks the visible
-// positions with the running maximum and sum of its softmax.
-// ---------------------------------------------------------------------------
-__device__ __forceinline__ float rows_load(const float* p) { return *p; }
-__device__ __forceinline__ float rows_load(const __nv_bfloat16* p) { return __bfloat162float(*p); }
-__device__ __forceinline__ void rows_store(float* p, float v) { *p = v; }
-__device__ __forceinline__ void rows_store(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
-
-template <int D, typename T>
-__global__ void __launch_bounds__(128) attn_rows_kernel(const WindowArgs a) {
-    const int lane = threadIdx.x % 32;
-    const int64_t unit = (int64_t)blockIdx.x * 4 + threadIdx.x / 32;
-    if (unit >= (int64_t)a.rows * a.Hq) return;
-    const int row = (int)(unit / a.Hq), h = (int)(unit % a.Hq), g = h / (a.Hq / a.Hkv);
-    int req = 0, hi = a.n_prompts;  // the last prompt that starts at or before the row
-    while (hi - req > 1) {
-        const int mid = (req + hi) / 2;
-        if (a.row_starts[mid] <= row) req = mid; else hi = mid;
-    }
-    const int pos = (a.first_pos ? a.first_pos[req] : 0) + row - a.row_starts[req];
-    const T* q = static_cast<const T*>(a.q) + ((int64_t)row * a.Hq + h) * D;
-    T* out = static_cast<T*>(a.o) + ((int64_t)row * a.Hq + h) * D;
-    float qv[D / 32], o[D / 32], m = -INFINITY, l = 0.f;
-#pragma unroll
-    for (int i = 0; i < D / 32; ++i) {
-        qv[i] = rows_load(q + i * 32 + lane);
-        o[i] = 0.f;
-    }
-    const float scale = 1.0f / sqrtf((float)D);
-    const int last = min(pos, a.max_ctx - 1);
-    for (int j = 0; j <= last; ++j) {
-        if (j >= a.sinks && j <= pos - a.window) {  // to the window's first position
-            j = pos - a.window;
-            continue;
-        }
-        const __nv_bfloat16* k =
-            reinterpret_cast<const __nv_bfloat16*>(
-                a.kv.base + a.kv.page_offsets[(int64_t)req * a.kv.max_pages + j / kPageTokens] +
-                (uint64_t)a.kv.layer * a.kv.layer_page_bytes) +
-            ((int64_t)g * kPageTokens + j % kPageTokens) * D;
-        const __nv_bfloat16* v = k + (int64_t)a.Hkv * kPageTokens * D;
-        float s = 0.f;
-#pragma unroll
-        for (int i = 0; i < D / 32; ++i) s = fmaf(qv[i], __bfloat162float(k[i * 32 + lane]), s);
-#pragma unroll
-        for (int x = 16; x; x /= 2) s += __shfl_xor_sync(0xffffffffu, s, x);
-        s *= scale;
-        const float m_new = fmaxf(m, s), alpha = expf(m - m_new), w = expf(s - m_new);
-        l = l * alpha + w;
-#pragma unroll
-        for (int i = 0; i < D / 32; ++i) o[i] = fmaf(w, __bfloat162float(v[i * 32 + lane]), o[i] * alpha);
-        m = m_new;
-    }
-    const float inv = l > 0.f ? 1.0f / l : 0.f;
-#pragma unroll
-    for (int i = 0; i < D / 32; ++i) rows_store(out + i * 32 + lane, o[i] * inv);
-}
-
-template <int D, typename T>
-cudaError_t launch_attn_rows(const WindowArgs& a, cudaStream_t st) {
-    const int64_t units = (int64_t)a.rows * a.Hq;
-    attn_rows_kernel<D, T><<<(unsigned)((units + 3) / 4), 128, 0, st>>>(a);
-    return cudaGetLastError();
-}
-
-cudaError_t launch_attn(const WindowArgs& a, bool f32, cudaStream_t st) {
-    if (a.d == 128) return f32 ? launch_attn_rows<128, float>(a, st) : launch_attn_rows<128, __nv_bfloat16>(a, st);
-    return f32 ? launch_attn_rows<64, float>(a, st) : launch_attn_rows<64, __nv_bfloat16>(a, st);
-}
-
 bool aligned(const void* p, uintptr_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
 
 // What every call on the cache has in common; null if it is in order.
@@ -343,7 +272,7 @@ extern "C" uint64_t loip_k_window_prefill_scratch_bytes(int32_t M, int32_t n_pro
     if (M < 0 || n_prompts < 0 || Hq < 1 || Hkv < 1 || Hq % Hkv || (d != 64 && d != 128) || window < 0 || sinks < 0 ||
         max_ctx < 1)
         return 0;
-    return 16;
+    return window_prefill_scratch(M, n_prompts, Hq, Hkv, d, window, sinks, max_ctx);
 }
 
 extern "C" int loip_k_window_prefill(const void* q, int32_t dtype, const void* kv_base, const int64_t* page_offsets,
@@ -378,5 +307,5 @@ extern "C" int loip_k_window_prefill(const void* q, int32_t dtype, const void* k
     a.sinks = sinks;
     a.max_ctx = max_ctx;
     a.scratch = scratch;
-    return kernel_status(launch_attn(a, dtype == LOIP_F32, (cudaStream_t)stream));
+    return kernel_status(launch_window_prefill(a, dtype == LOIP_F32, (cudaStream_t)stream));
 }

@@ -31,4 +31,9 @@ struct WindowArgs {
 uint64_t window_decode_scratch(int B, int Hq, int Hkv, int d, int window, int sinks, int max_ctx);
 cudaError_t launch_window_decode(const WindowArgs& a, bool f32, cudaStream_t st);
 
+// Attention of prompt rows (window_prefill.cu).
+uint64_t window_prefill_scratch(int M, int n_prompts, int Hq, int Hkv, int d, int window, int sinks, int max_ctx);
+cudaError_t launch_window_prefill(const WindowArgs& a, bool f32, cudaStream_t st);
+cudaError_t window_prefill_error(int* code);  // first failure code of any launch (0 = none)
+
 }  // namespace loip

@@ -383,6 +383,27 @@ def test_prefill_many_prompts(torch, L):
     _check_prefill(torch, L, runs, 2, 1, 64, 30, 2, "bf16", 131)
 
 
+# enough row tiles that a block takes two of them (bf16): the second one empty, partly
+# filled, full, or with key tiles of its own behind the first one's window
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("window,sinks", [(1 << 30, 0), (40, 3), (150, 70), (0, 2)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_prefill_many_tiles(torch, L, d, window, sinks, dtype):
+    runs = [(300, 0), (129, 70), (128, 500), (0, 9)] + [(1 + i, 30 * i) for i in range(18)]
+    _check_prefill(torch, L, runs, 16, 16, d, window, sinks, dtype, 161)
+
+
+def test_prefill_two_tiles_and_values_that_later_rows_alone_see(torch, L):
+    def edit(c):
+        bits = c.bits[c.slot(0, 133, 1)].copy()
+        bits[:, 7] = 0xFF80  # minus infinity
+        c.bits[c.slot(0, 133, 1)] = bits
+
+    runs = [(280, 0)] + [(2, 5)] * 20
+    got = _check_prefill(torch, L, runs, 16, 16, 64, 100, 1, "bf16", 171, edit=edit)
+    assert np.all(np.isfinite(got[:133])) and np.all(np.isneginf(got[133:233, :, 7])) and np.all(np.isfinite(got[233:]))
+
+
 def test_prefill_equals_decode(torch, L):
     """A prompt of one row is a decode step: both agree to the sum of their bounds."""
     ctx, Hq, Hkv, d = (500, 1, 77), 8, 2, 128
