@@ -29,10 +29,18 @@ struct RopeTurns {
     uint64_t turn[64];
 };
 
-RopeTurns rope_turns(float theta, int d) {
-    RopeTurns r{};
-    for (int i = 0; i < d / 2; ++i)  // below 1 / (2 pi) of 2^64, so the conversion is in range
-        r.turn[i] = theta == 0.f ? 0 : (uint64_t)ldexp(pow((double)theta, -2.0 * i / d) * 0.15915494309189535, 64);
+// The table of a base and head size; the thread's last one is kept (64 powers take longer
+// than the launch).
+const RopeTurns& rope_turns(float theta, int d) {
+    thread_local RopeTurns r;
+    thread_local float of_theta = -1.f;
+    thread_local int of_d = 0;
+    if (theta != of_theta || d != of_d) {
+        for (int i = 0; i < d / 2; ++i)  // below 1 / (2 pi) of 2^64, so the conversion is in range
+            r.turn[i] = theta == 0.f ? 0 : (uint64_t)ldexp(pow((double)theta, -2.0 * i / d) * 0.15915494309189535, 64);
+        of_theta = theta;
+        of_d = d;
+    }
     return r;
 }
 

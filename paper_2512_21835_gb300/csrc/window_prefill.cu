@@ -137,9 +137,15 @@ __device__ __forceinline__ bool warp_wait(Ctl* c, uint64_t* b, uint32_t parity, 
 }
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+// The MMA warp runs as a whole; its issuing instructions are predicated on the elected
+// lane inside one asm block, so that addresses and descriptors stay warp-uniform.  Issued
+// from a lane's own branch they took 130 cycles each, twice what an MMA of 128 columns
+// takes the tensor core.
 __device__ __forceinline__ void commit(uint64_t* b) {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_u32(b))
-                 : "memory");
+    asm volatile(
+        "{\n .reg .pred e;\n elect.sync _|e, 0xffffffff;\n"
+        " @e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n}\n" ::"r"(smem_u32(b))
+        : "memory");
 }
 // kind::f16, fp32 accumulator, bf16 A and B, M = 128, N = n; B with its N contiguous when `b_mn`
 __host__ __device__ constexpr uint32_t idesc(int n, bool b_mn) {
@@ -152,17 +158,31 @@ __device__ __forceinline__ uint64_t sdesc(uint32_t addr, uint32_t lbo) {
     return (uint64_t)((addr >> 4) & 0x3FFFu) | ((uint64_t)(lbo >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) |
            ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
 }
-__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t id, uint32_t acc) {
+// Four MMAs (64 of K): both operands in shared memory, 32 bytes a step along their rows;
+__device__ __forceinline__ void mma_ss4(uint32_t d, uint64_t a, uint64_t b, uint32_t id, uint32_t acc) {
     asm volatile(
-        "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(
-            d),
+        "{\n .reg .pred e, p, t;\n .reg .b64 a1, a2, a3, b1, b2, b3;\n"
+        " elect.sync _|e, 0xffffffff;\n setp.ne.b32 p, %4, 0;\n setp.eq.b32 t, %4, %4;\n"
+        " add.s64 a1, %1, 2;\n add.s64 a2, %1, 4;\n add.s64 a3, %1, 6;\n"
+        " add.s64 b1, %2, 2;\n add.s64 b2, %2, 4;\n add.s64 b3, %2, 6;\n"
+        " @e tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n"
+        " @e tcgen05.mma.cta_group::1.kind::f16 [%0], a1, b1, %3, t;\n"
+        " @e tcgen05.mma.cta_group::1.kind::f16 [%0], a2, b2, %3, t;\n"
+        " @e tcgen05.mma.cta_group::1.kind::f16 [%0], a3, b3, %3, t;\n}\n" ::"r"(d),
         "l"(a), "l"(b), "r"(id), "r"(acc)
         : "memory");
 }
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t id, uint32_t acc) {
+// A in tensor memory, 8 columns a step; B 16 rows of 128 bytes a step.
+__device__ __forceinline__ void mma_ts4(uint32_t d, uint32_t a, uint64_t b, uint32_t id, uint32_t acc) {
     asm volatile(
-        "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n" ::"r"(
-            d),
+        "{\n .reg .pred e, p, t;\n .reg .b32 a1, a2, a3;\n .reg .b64 b1, b2, b3;\n"
+        " elect.sync _|e, 0xffffffff;\n setp.ne.b32 p, %4, 0;\n setp.eq.b32 t, %4, %4;\n"
+        " add.s32 a1, %1, 8;\n add.s32 a2, %1, 16;\n add.s32 a3, %1, 24;\n"
+        " add.s64 b1, %2, 128;\n add.s64 b2, %2, 256;\n add.s64 b3, %2, 384;\n"
+        " @e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n"
+        " @e tcgen05.mma.cta_group::1.kind::f16 [%0], [a1], b1, %3, t;\n"
+        " @e tcgen05.mma.cta_group::1.kind::f16 [%0], [a2], b2, %3, t;\n"
+        " @e tcgen05.mma.cta_group::1.kind::f16 [%0], [a3], b3, %3, t;\n}\n" ::"r"(d),
         "r"(a), "l"(b), "r"(id), "r"(acc)
         : "memory");
 }
@@ -374,22 +394,24 @@ __global__ void __launch_bounds__(kThreads, 1) window_prefill_kernel(const __gri
     // the rows of stream w: its row tile's
     auto stream_pos = [&](int w) { return QT == 2 ? pos0 + w * p.tok : pos0; };
     auto stream_tokens = [&](int w) { return QT == 2 ? min(max(tokens - w * p.tok, 0), p.tok) : tokens; };
-    // whether stream w computes key tile t
-    auto takes = [&](int w, int t) {
-        if (QT == 1) return (t & 1) == w;
-        if (stream_tokens(w) == 0) return false;
-        const Pages mine(a, stream_pos(w), stream_pos(w) + stream_tokens(w) - 1);
-        bool any = false;
-#pragma unroll
-        for (int x = 0; x < C::PPT; ++x) {
-            const int v = t * C::PPT + x, pg = pages.at(v);
-            any |= v < pages.n && pg < mine.end && (pg < mine.sink || pg >= mine.win);
-        }
-        return any;
+    // the key tiles that stream w computes: [0, sink) and [lo, hi)
+    struct Takes {
+        int sink, lo, hi;
+        __device__ bool operator()(int t) const { return t < sink || (t >= lo && t < hi); }
     };
-    // place in the ring's order: LEAD key tiles, then values and keys in turn
-    auto k_place = [&](int t) { return t < C::LEAD ? t : 2 * t - C::LEAD + 1; };
-    auto v_place = [&](int t) { return t + min(n, C::LEAD + t); };
+    auto takes_of = [&](int w) {
+        Takes k{0, 0, 0};
+        if (stream_tokens(w) > 0) {
+            const Pages mine(a, stream_pos(w), stream_pos(w) + stream_tokens(w) - 1);
+            const int shift = pages.sink - pages.win;  // of a window page in the list
+            k.sink = (min(mine.sink, pages.sink) + C::PPT - 1) / C::PPT;
+            if (mine.end > max(mine.win, pages.win)) {
+                k.lo = (max(mine.win, pages.win) + shift) / C::PPT;
+                k.hi = (mine.end + shift + C::PPT - 1) / C::PPT;
+            }
+        }
+        return k;
+    };
 
     if (warp >= 8) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
@@ -456,23 +478,33 @@ __global__ void __launch_bounds__(kThreads, 1) window_prefill_kernel(const __gri
                 bar_arrive(&c->full[at % C::SLOTS]);
             };
             const int total = 2 * n;
-            int at = 0;
+            const int step = RPP * D * 2;  // a pass further in the page; RPP is a multiple of 8: the swizzle stays
+            static_assert(RPP % 8 == 0, "");
+            int at = 0, slot = 0;
+            uint32_t free_phase = 1;  // of the ring's previous round; none for the first
             for (; at < total; ++at) {
-                if (at >= C::SLOTS && !bar_wait(c, &c->empty[at % C::SLOTS], (at / C::SLOTS - 1) & 1, 1)) break;
+                if (at >= C::SLOTS && !bar_wait(c, &c->empty[slot], free_phase, 1)) break;
                 bool is_v;
                 const int t = tile_of(at, is_v);
-                const uint32_t slot = ring + (uint32_t)(at % C::SLOTS) * C::SLOT;
 #pragma unroll
                 for (int x = 0; x < C::PPT; ++x) {
                     const int v = t * C::PPT + x;
-                    const bool live = v < pages.n;
-                    const int pg = live ? pages.at(v) : 0;
+                    const int pg = v < pages.n ? pages.at(v) : 0, b = pg * kPageTokens;
+                    const uint32_t dst = place(ring + (uint32_t)slot * C::SLOT, x, r0);
                     const char* src = layer;
-                    if (live) src += __ldg(table + pg) + ((int64_t)(is_v ? a.Hkv : 0) + kvh) * (kPageTokens * D * 2);
-#pragma unroll 4
-                    for (int r = r0; r < kPageTokens; r += RPP) {
-                        const bool ok = live && seen(pg * kPageTokens + r);
-                        cp_async16(place(slot, x, r), ok ? src + (r * D + chunk * 8) * 2 : layer, ok ? 16u : 0u);
+                    if (v < pages.n)
+                        src += __ldg(table + pg) + ((int64_t)(is_v ? a.Hkv : 0) + kvh) * (kPageTokens * D * 2) +
+                               (r0 * D + chunk * 8) * 2;
+                    if (v < pages.n && b + kPageTokens <= pages.last &&
+                        ((b >= win0 && a.window > 0) || b + kPageTokens <= a.sinks)) {  // the whole page
+#pragma unroll
+                        for (int k = 0; k < kPageTokens / RPP; ++k) cp_async16(dst + k * RPP * 128, src + k * step, 16u);
+                    } else {
+#pragma unroll
+                        for (int k = 0; k < kPageTokens / RPP; ++k) {
+                            const bool ok = v < pages.n && seen(b + r0 + k * RPP);
+                            cp_async16(dst + k * RPP * 128, ok ? src + k * step : layer, ok ? 16u : 0u);
+                        }
                     }
                 }
                 asm volatile("cp.async.commit_group;" ::: "memory");
@@ -480,77 +512,103 @@ __global__ void __launch_bounds__(kThreads, 1) window_prefill_kernel(const __gri
                     asm volatile("cp.async.wait_group %0;" ::"n"(C::LAG) : "memory");
                     signal(at - C::LAG);
                 }
+                if (++slot == C::SLOTS) {
+                    slot = 0;
+                    free_phase ^= 1;
+                }
             }
             asm volatile("cp.async.wait_all;" ::: "memory");
             if (at == total)
                 for (int i = max(0, total - C::LAG); i < total; ++i) signal(i);
-        } else if (warp == 12 && lane == 0 && n > 0) {
+        } else if (warp == 12 && n > 0) {
             // ---------------------------------------------------------------- MMA issue
             uint32_t pv_n[2] = {0, 0};  // products P V issued per stream
-            bool ok = bar_wait(c, &c->q_full, 0, 2);
-            auto wait_tile = [&](int at) {
-                return bar_wait(c, &c->full[at % C::SLOTS], (uint32_t)(at / C::SLOTS) & 1, 3);
+            bool ok = warp_wait(c, &c->q_full, 0, 2);
+            // the ring is used in its own order: a cursor and the phase of its round
+            int slot = 0;
+            uint32_t phase = 0;
+            auto advance = [&] {
+                commit(&c->empty[slot]);
+                if (++slot == C::SLOTS) {
+                    slot = 0;
+                    phase ^= 1;
+                }
             };
-            auto issue_s = [&](int w, int t) {  // S of key tile t; P of the stream's last tile has been used
-                if (!wait_tile(k_place(t))) return false;
-                if (pv_n[w] && !bar_wait(c, &c->pv_done[w], (pv_n[w] - 1) & 1, 4)) return false;
+            const uint64_t q_desc = sdesc(q_smem, 16), k_desc = sdesc(ring, 16), v_desc = sdesc(ring, C::KV_SLAB);
+            auto issue_s = [&](int w) {  // S of the keys at the cursor; P of the stream's last tile has been used
+                if (!warp_wait(c, &c->full[slot], phase, 3)) return false;
+                if (pv_n[w] && !warp_wait(c, &c->pv_done[w], (pv_n[w] - 1) & 1, 4)) return false;
                 fence_after();
-                const uint32_t q = q_smem + (QT == 2 ? (uint32_t)w * NP * C::Q_PLANE : 0u);
-                const uint32_t k = ring + (uint32_t)(k_place(t) % C::SLOTS) * C::SLOT;
-                uint32_t acc = 0;
+                const uint64_t q = q_desc + (QT == 2 ? (uint32_t)w * (NP * C::Q_PLANE / 16) : 0u);
+                const uint64_t k = k_desc + (uint32_t)slot * (C::SLOT / 16);
+                const uint32_t d = tmem + 256u * w + C::S;
 #pragma unroll
                 for (int pl = NP - 1; pl >= 0; --pl)
 #pragma unroll
-                    for (int x = 0; x < D / 16; ++x) {
-                        mma_ss(tmem + 256u * w + C::S,
-                               sdesc(q + pl * C::Q_PLANE + (x >> 2) * C::Q_SLAB, 16) + 2 * (x & 3),
-                               sdesc(k + (x >> 2) * C::KV_SLAB, 16) + 2 * (x & 3), idesc(KT, false), acc);
-                        acc = 1;
-                    }
+                    for (int x = 0; x < D / 64; ++x)
+                        mma_ss4(d, q + (pl * C::Q_PLANE + x * C::Q_SLAB) / 16, k + x * C::KV_SLAB / 16,
+                                idesc(KT, false), pl != NP - 1 || x != 0);
                 commit(&c->s_full[w]);
                 return true;
             };
-            auto issue_pv = [&](int w, int t) {
-                if (!bar_wait(c, &c->p_full[w], pv_n[w] & 1, 5) || !wait_tile(v_place(t))) return false;
+            auto issue_pv = [&](int w) {  // O += P V of the values at the cursor
+                if (!warp_wait(c, &c->p_full[w], pv_n[w] & 1, 5) || !warp_wait(c, &c->full[slot], phase, 3)) return false;
                 fence_after();
-                const uint32_t v = ring + (uint32_t)(v_place(t) % C::SLOTS) * C::SLOT;
-                uint32_t acc = NP == 1 && pv_n[w] ? 1u : 0u;  // drained per tile, or kept
+                const uint64_t v = v_desc + (uint32_t)slot * (C::SLOT / 16);
+                const uint32_t d = tmem + 256u * w + C::O, pa = tmem + 256u * w;
+                const uint32_t first = NP == 1 && pv_n[w] ? 1u : 0u;  // O is kept, or drained per tile
 #pragma unroll
                 for (int pl = NP - 1; pl >= 0; --pl)
 #pragma unroll
-                    for (int x = 0; x < KT / 16; ++x) {
-                        const uint32_t pa = tmem + 256u * w + (pl == 0 ? C::P0 : pl == 1 ? C::P1 : C::P2) + 8 * x;
-                        mma_ts(tmem + 256u * w + C::O, pa, sdesc(v + x * 2048, C::KV_SLAB), idesc(D, true), acc);
-                        acc = 1;
-                    }
+                    for (int x = 0; x < KT / 64; ++x)
+                        mma_ts4(d, pa + (pl == 0 ? C::P0 : pl == 1 ? C::P1 : C::P2) + 32 * x, v + x * (64 * 128 / 16),
+                                idesc(D, true), pl != NP - 1 || x != 0 ? 1u : first);
                 ++pv_n[w];
                 commit(&c->pv_done[w]);
                 return true;
             };
-            auto release = [&](int at) { commit(&c->empty[at % C::SLOTS]); };
             if (QT == 2) {
-                for (int w = 0; w < 2 && ok; ++w)
-                    if (takes(w, 0)) ok = issue_s(w, 0);
-                release(k_place(0));
+                const Takes k0 = takes_of(0), k1 = takes_of(1);
+                if (ok && k0(0)) ok = issue_s(0);
+                if (ok && k1(0)) ok = issue_s(1);
+                advance();
                 for (int t = 0; t < n && ok; ++t) {
-                    for (int w = 0; w < 2 && ok; ++w) {
-                        if (takes(w, t)) ok = issue_pv(w, t);
-                        if (w) release(v_place(t));
-                        if (ok && t + 1 < n && takes(w, t + 1)) ok = issue_s(w, t + 1);
-                        if (w && t + 1 < n) release(k_place(t + 1));
+                    // cursor on V_t; K_(t+1) is the next one
+                    const int v_slot = slot;
+                    const uint32_t v_phase = phase;
+                    const bool more = t + 1 < n;
+                    auto to_k = [&] {
+                        if (++slot == C::SLOTS) {
+                            slot = 0;
+                            phase ^= 1;
+                        }
+                    };
+                    auto to_v = [&] {
+                        slot = v_slot;
+                        phase = v_phase;
+                    };
+                    if (k0(t)) ok = issue_pv(0);
+                    if (ok && more && k0(t + 1)) {
+                        to_k();
+                        ok = issue_s(0);
+                        to_v();
                     }
+                    if (ok && k1(t)) ok = issue_pv(1);
+                    advance();
+                    if (ok && more && k1(t + 1)) ok = issue_s(1);
+                    if (more) advance();
                 }
             } else {
                 for (int t = 0; t < min(2, n) && ok; ++t) {
-                    ok = issue_s(t, t);
-                    release(k_place(t));
+                    ok = issue_s(t);
+                    advance();
                 }
                 for (int t = 0; t < n && ok; ++t) {
-                    ok = issue_pv(t & 1, t);
-                    release(v_place(t));
+                    ok = issue_pv(t & 1);
+                    advance();
                     if (ok && t + 2 < n) {
-                        ok = issue_s(t & 1, t + 2);
-                        release(k_place(t + 2));
+                        ok = issue_s(t & 1);
+                        advance();
                     }
                 }
             }
@@ -567,29 +625,40 @@ __global__ void __launch_bounds__(kThreads, 1) window_prefill_kernel(const __gri
         auto row_at = [&](int tok, int head) {  // element offset of a row of q and o
             return ((int64_t)(row0 + tok) * a.Hq + kvh * G + head0 + head) * D;
         };
-        // ---- queries -> shared memory, bf16 planes, swizzled
-        for (int i = tid; i < QT * 128 * (D / 8); i += 256) {
-            const int ch = i % (D / 8), r = i / (D / 8) % 128, tile = i / (D / 8) / 128;
-            const int tk = r / heads, tok = tile * p.tok + tk;
-            uint8_t* dst = sm + tile * NP * C::Q_PLANE + (ch >> 3) * C::Q_SLAB + r * 128 + (((ch & 7) ^ (r & 7)) << 4);
-            const bool live = tk < p.tok && tok < tokens;
-            const T* src = qg + row_at(live ? tok : 0, live ? r % heads : 0) + ch * 8;
-            if constexpr (NP == 1) {
-                *reinterpret_cast<uint4*>(dst) =
-                    live ? __ldg(reinterpret_cast<const uint4*>(src)) : make_uint4(0u, 0u, 0u, 0u);
-            } else {
-                float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-                if (live) {
-                    const float4 x = __ldg(reinterpret_cast<const float4*>(src));
-                    const float4 y = __ldg(reinterpret_cast<const float4*>(src) + 1);
-                    v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w; v[4] = y.x; v[5] = y.y; v[6] = y.z; v[7] = y.w;
+        // ---- queries -> shared memory, bf16 planes, swizzled; eight loads in flight per thread
+        constexpr int CPR = D / 8, EACH = QT * 128 * CPR / 256, MOST = NP == 1 ? 8 : 4, BATCH = EACH < MOST ? EACH : MOST;
+        static_assert(EACH % BATCH == 0, "");
+        for (int i0 = tid; i0 < QT * 128 * CPR; i0 += 256 * BATCH) {
+            uint4 x[BATCH], y[NP == 1 ? 1 : BATCH];
+#pragma unroll
+            for (int k = 0; k < BATCH; ++k) {
+                const int i = i0 + 256 * k, r = i / CPR % 128, tile = i / CPR / 128;
+                const int tk = r / heads, tok = tile * p.tok + tk;
+                x[k] = make_uint4(0u, 0u, 0u, 0u);
+                if constexpr (NP > 1) y[k] = x[k];
+                if (tk < p.tok && tok < tokens) {
+                    const uint4* src = reinterpret_cast<const uint4*>(qg + row_at(tok, r - tk * heads) + i % CPR * 8);
+                    x[k] = __ldg(src);
+                    if constexpr (NP > 1) y[k] = __ldg(src + 1);
                 }
+            }
 #pragma unroll
-                for (int pl = 0; pl < NP; ++pl) {
-                    uint32_t u[4];
+            for (int k = 0; k < BATCH; ++k) {
+                const int i = i0 + 256 * k, ch = i % CPR, r = i / CPR % 128, tile = i / CPR / 128;
+                uint8_t* dst =
+                    sm + tile * NP * C::Q_PLANE + (ch >> 3) * C::Q_SLAB + r * 128 + (((ch & 7) ^ (r & 7)) << 4);
+                if constexpr (NP == 1) {
+                    *reinterpret_cast<uint4*>(dst) = x[k];
+                } else {
+                    float v[8] = {asf(x[k].x), asf(x[k].y), asf(x[k].z), asf(x[k].w),
+                                  asf(y[k].x), asf(y[k].y), asf(y[k].z), asf(y[k].w)};
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) u[e] = peel(v[2 * e], v[2 * e + 1]);
-                    *reinterpret_cast<uint4*>(dst + pl * C::Q_PLANE) = make_uint4(u[0], u[1], u[2], u[3]);
+                    for (int pl = 0; pl < NP; ++pl) {
+                        uint32_t u[4];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) u[e] = peel(v[2 * e], v[2 * e + 1]);
+                        *reinterpret_cast<uint4*>(dst + pl * C::Q_PLANE) = make_uint4(u[0], u[1], u[2], u[3]);
+                    }
                 }
             }
         }
@@ -611,8 +680,9 @@ __global__ void __launch_bounds__(kThreads, 1) window_prefill_kernel(const __gri
             for (int i = 0; i < D; ++i) o[i] = 0.f;
         }
         bool ok = true;
-        for (int t = 0; t < n; ++t) {
-            if (!takes(w, t)) continue;
+        const Takes takes = takes_of(w);
+        for (int t = QT == 1 ? w : 0; t < n; t += QT == 1 ? 2 : 1) {
+            if (QT == 2 && !takes(t)) continue;
             // which positions of the tile this row sees, one bit each
             bool masked = false;
             uint32_t see[KT / 32];
