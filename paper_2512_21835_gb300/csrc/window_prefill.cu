@@ -7,17 +7,24 @@
 // and a window costs little more than its own length.
 //
 // Keys.  The pages that some row of the block sees, those of the sinks and then
-// those of the window, are a list without a gap; KT consecutive positions of it (one
-// page or two) are a key tile.  Positions that no row of the block sees are not read:
-// their rows in shared memory are zero-filled.
+// those of the window, are a list without a gap; a page is a key tile.  Positions
+// that no row of the block sees are not read: their rows in shared memory are
+// zero-filled.
 //
 // Per key tile:  S = Q K^T -> tensor memory -> softmax in registers, one row per
-// thread -> P back into tensor memory -> O += P V, V in its cache layout (the MMA
-// takes B with d contiguous).  Two streams w = 0, 1 of this chain run in turn, so that
-// the tensor core works for one while the other is in its softmax:
+// thread -> P back into tensor memory -> O += P V, V in its cache layout
+// (the MMA takes B with d contiguous).  Two streams w = 0, 1 of this chain share the
+// tensor core:
 //   QT = 2: two row tiles over the same key tiles
 //   QT = 1: one row tile, even and odd key tiles; the two partial softmax states are
-//           joined at the end.  For fewer row tiles than the card has places.
+//           joined at the end.  For fewer row tiles than the card has places; with
+//           fewer still, a row tile's pages are split over several blocks, which
+//           leave their states in scratch for the last one to join.
+// S and P have columns of their own (P twice for bf16 rows), so the next tile's S is
+// computed while this one's weights are, and neither waits for P V.  (With P over S, in
+// tiles of 128 keys, the chain softmax - P V - S took 4000 cycles per 128 keys and two
+// streams, of which the tensor core worked 2048: an isolated group of eight MMAs answers
+// after 840.)  The price is N = 64 for S, 48 cycles an MMA instead of 32: 2560 cycles.
 //
 // Precision.  bf16 rows: one MMA per product, weights rounded to bf16, O stays in
 // tensor memory; it is rescaled only when a row's maximum has grown by 2^8 (weights
@@ -30,17 +37,23 @@
 // tiles that not all rows see in full, the loader looks for such values, zeroes them
 // and flags the block, whose rows are then walked one by one (walk_row).
 //
-// Roles (512 threads): warps 0-3 and 4-7 softmax of stream 0 and 1 (one row per
-// thread), warps 8-11 load (cp.async, 128-byte swizzle), warp 12 issues the MMAs.
+// Roles (384 threads): warps 0-3 and 4-7 softmax of stream 0 and 1 (one row per
+// thread), warps 8 and 9 load (cp.async, 128-byte swizzle), warps 10 and 11 issue the
+// MMAs of a stream each.  Beside the softmax a barrier operation of an issuing warp takes
+// 130 cycles, even a wait for a phase that is complete, and the tensor core's queue is
+// two MMAs deep; so the keys of a tile share a slot and a barrier with the values that
+// are used in the same step, and each stream has a warp.
 // Every wait is bounded (2 s); one that runs out records an error, the block stops,
 // lets its copies and MMAs finish, frees its tensor memory and returns.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <math.h>
+#include <stddef.h>
 #include <stdint.h>
 
 #include <algorithm>
 #include <atomic>
+#include <type_traits>
 
 #include "internal.h"
 #include "window.h"
@@ -51,37 +64,45 @@ __device__ int g_window_error;  // first failure code of any launch (0 = none)
 
 namespace {
 
-constexpr int kThreads = 512;
+constexpr int kThreads = 384;
+constexpr int kLoaders = 64;                     // threads of warps 8 and 9
 constexpr int kSms = 152;
-constexpr int kSoftRegs = 192, kOtherRegs = 64;  // 2 x 128 x 192 + 2 x 128 x 64 = 512 x 128
+constexpr int kSoftRegs = 208, kOtherRegs = 88;  // 256 x 208 + 128 x 88 = 384 x 168
+constexpr int kMaxUnits = 256;                   // counters and flags at the start of the scratch
+constexpr int KT = kPageTokens;                  // keys per tile
 
 template <int D, int NP, int QT>
 struct Cfg {
-    static constexpr int KT = NP == 1 ? 128 : 64;      // keys per tile
-    static constexpr int PPT = KT / kPageTokens;       // pages per tile
     static constexpr int SLABS = D / 64;               // 128-byte columns of a row
     static constexpr int Q_SLAB = 128 * 128;
     static constexpr int Q_PLANE = SLABS * Q_SLAB;
     static constexpr int Q_BYTES = QT * NP * Q_PLANE;  // [tile][plane][slab][row]
     static constexpr int KV_SLAB = KT * 128;
-    static constexpr int SLOT = SLABS * KV_SLAB;       // one tile of keys or of values
+    static constexpr int TILE = SLABS * KV_SLAB;       // one tile of keys or of values
+    static constexpr int SLOT = 2 * TILE;              // the keys of one tile, the values of an earlier one
     static constexpr int ROOM = 227 * 1024 - 1024 - 512 - Q_BYTES;
-    static constexpr int SLOTS = ROOM / SLOT < 8 ? ROOM / SLOT : 8;
-    static constexpr int LAG = 2;                      // tiles in flight behind the newest
-    static constexpr int LEAD = QT == 2 ? 1 : 2;       // key tiles ahead of the values
+    static constexpr int SLOTS = ROOM / SLOT < 12 ? ROOM / SLOT : 12;
+    static constexpr int AHEAD = 3 - QT;                 // slot i: keys of tile i, values of tile i - AHEAD
     static constexpr int CTL = Q_BYTES + SLOTS * SLOT;
     static constexpr int BYTES = CTL + 512 + 1024;     // + alignment of the window
-    static_assert(SLOTS >= LAG + 2, "the loader signals a tile LAG tiles late");
-    static_assert(QT == 2 || SLOTS * SLOT >= 128 * D * 4, "the join goes through the ring");
-    // tensor memory of stream w, from column 256 w
-    static constexpr uint32_t S = 0, O = 128;
-    static constexpr uint32_t P0 = NP == 1 ? 0 : 64, P1 = 0, P2 = 96;  // columns that S has been read from, or free
+    static_assert(SLOTS >= 3, "the loader may signal a slot after it has filled the next");
+    static_assert(QT == 2 || SLOTS * SLOT >= 128 * D * 4 + 2048, "the join goes through the ring");
+    // Tensor memory.  bf16: per stream S, two P buffers and O.  fp32: one O, drained after
+    // every tile, then per stream S and the planes of P.
+    __host__ __device__ static constexpr uint32_t s_col(int w) { return NP == 1 ? 256 * w : 128 + 160 * w; }
+    __host__ __device__ static constexpr uint32_t o_col(int w) { return NP == 1 ? 256 * w + 128 : 0; }
+    __host__ __device__ static constexpr uint32_t p_col(int w, int buf, int pl) {
+        return s_col(w) + 64 + 32 * (NP == 1 ? buf : pl);
+    }
 };
 
 struct Ctl {  // control words behind the ring
-    uint64_t full[8], empty[8], s_full[2], p_full[2], pv_done[2], q_full, end;
+    uint64_t full[12], empty[12];      // of the ring's slots
+    uint64_t s_full[2], s_free[2];     // per stream
+    uint64_t p_full[4], pv_done[4];    // per stream and P buffer: for even and odd tiles, no wait is ever two phases behind
+    uint64_t o_free, q_full, end;
     uint32_t tmem;
-    int abort, bad;
+    int abort, bad, last;
     int row0, tokens, req, pos0;
 };
 static_assert(sizeof(Ctl) <= 512, "");
@@ -90,7 +111,11 @@ struct PrefillArgs {
     WindowArgs a;
     int heads, groups;  // query heads per row tile, groups per kv head
     int tok;            // positions per row tile
+    int splits;         // blocks per row tile (QT = 1)
     float scale;        // log2(e) / sqrt(d)
+    unsigned *arrived, *flagged;  // [kMaxUnits]: blocks done, whether one met values that are not finite
+    float4* part;       // [row tile and unit][split][d / 4][128 rows], not normalised
+    float2* ml;         // [row tile and unit][split][128 rows]: maximum (log2), sum
 };
 
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -99,52 +124,60 @@ __device__ __forceinline__ uint64_t now_ns() {
     asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
     return t;
 }
-__device__ __forceinline__ void bar_init(uint64_t* b, uint32_t n) {
-    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(b)), "r"(n) : "memory");
+// Barriers by their address in shared memory.
+__device__ __forceinline__ void bar_init(uint32_t b, uint32_t n) {
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(b), "r"(n) : "memory");
 }
-__device__ __forceinline__ void bar_arrive(uint64_t* b) {
-    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(b)) : "memory");
+__device__ __forceinline__ void bar_arrive(uint32_t b) {
+    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(b) : "memory");
 }
-__device__ __forceinline__ bool bar_try(uint64_t* b, uint32_t parity) {
+// Whether the phase of that parity is complete; waits for it up to a millisecond, asleep.
+// (Without the hint the wait ended after some hundred cycles, and the waiting warps'
+// polls took issue slots and shared memory from the others.)
+__device__ __forceinline__ bool bar_try(uint32_t b, uint32_t parity) {
     uint32_t ok;
     asm volatile(
-        "{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}\n"
+        "{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n selp.u32 %0, 1, 0, p;\n}\n"
         : "=r"(ok)
-        : "r"(smem_u32(b)), "r"(parity)
+        : "r"(b), "r"(parity), "r"(1000000u)
         : "memory");
     return ok != 0;
 }
-// Waits for the phase of that parity; false if the block is to stop.  (Inlined: a call
-// would take part in the register split.)
-__device__ __forceinline__ bool bar_wait_slow(Ctl* c, uint64_t* b, uint32_t parity, int code) {
-    const uint64_t t0 = now_ns();
-    while (!bar_try(b, parity)) {
-        if (*(volatile int*)&c->abort) return false;
-        if (now_ns() - t0 > 2000000000ull) {
-            *(volatile int*)&c->abort = 1;
-            atomicCAS(&g_window_error, 0, code);
-            return false;
+// A thread's waits.  One that runs out (2 s), or the flag of another thread's that did,
+// ends all further ones: the thread goes on to its end with whatever it finds, within
+// its own buffers, and nothing it makes is stored.  (No way out in between: a warp stays
+// together, and the code of a wait is one instruction and a branch.)
+struct Waiter {
+    Ctl* c;
+    bool dead;
+    __device__ __forceinline__ void operator()(uint32_t b, uint32_t parity, int code) {
+        if (!dead && !bar_try(b, parity)) slow(b, parity, code);
+    }
+    __device__ __forceinline__ void slow(uint32_t b, uint32_t parity, int code) {
+        const uint64_t t0 = now_ns();
+        while (!bar_try(b, parity)) {
+            dead = *(volatile int*)&c->abort != 0;
+            if (!dead && now_ns() - t0 > 2000000000ull) {
+                *(volatile int*)&c->abort = 1;
+                atomicCAS(&g_window_error, 0, code);
+                dead = true;
+            }
+            if (dead) return;
         }
     }
-    return true;
-}
-__device__ __forceinline__ bool bar_wait(Ctl* c, uint64_t* b, uint32_t parity, int code) {
-    return bar_try(b, parity) || bar_wait_slow(c, b, parity, code);
-}
-// The same for a whole warp, which leaves it converged.
-__device__ __forceinline__ bool warp_wait(Ctl* c, uint64_t* b, uint32_t parity, int code) {
-    return __all_sync(0xffffffffu, bar_wait(c, b, parity, code));
-}
+};
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+// Copies that have arrived at a barrier, made visible to the tensor core's reads.
+__device__ __forceinline__ void fence_loaded() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 // The MMA warp runs as a whole; its issuing instructions are predicated on the elected
 // lane inside one asm block, so that addresses and descriptors stay warp-uniform.  Issued
 // from a lane's own branch they took 130 cycles each, twice what an MMA of 128 columns
 // takes the tensor core.
-__device__ __forceinline__ void commit(uint64_t* b) {
+__device__ __forceinline__ void commit(uint32_t b) {
     asm volatile(
         "{\n .reg .pred e;\n elect.sync _|e, 0xffffffff;\n"
-        " @e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n}\n" ::"r"(smem_u32(b))
+        " @e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n}\n" ::"r"(b)
         : "memory");
 }
 // kind::f16, fp32 accumulator, bf16 A and B, M = 128, N = n; B with its N contiguous when `b_mn`
@@ -172,17 +205,14 @@ __device__ __forceinline__ void mma_ss4(uint32_t d, uint64_t a, uint64_t b, uint
         "l"(a), "l"(b), "r"(id), "r"(acc)
         : "memory");
 }
-// A in tensor memory, 8 columns a step; B 16 rows of 128 bytes a step.
-__device__ __forceinline__ void mma_ts4(uint32_t d, uint32_t a, uint64_t b, uint32_t id, uint32_t acc) {
+// Two MMAs (32 of K): A in tensor memory, 8 columns a step; B 16 rows of 128 bytes a step.
+__device__ __forceinline__ void mma_ts2(uint32_t d, uint32_t a, uint64_t b, uint32_t id, uint32_t acc) {
     asm volatile(
-        "{\n .reg .pred e, p, t;\n .reg .b32 a1, a2, a3;\n .reg .b64 b1, b2, b3;\n"
+        "{\n .reg .pred e, p, t;\n .reg .b32 a1;\n .reg .b64 b1;\n"
         " elect.sync _|e, 0xffffffff;\n setp.ne.b32 p, %4, 0;\n setp.eq.b32 t, %4, %4;\n"
-        " add.s32 a1, %1, 8;\n add.s32 a2, %1, 16;\n add.s32 a3, %1, 24;\n"
-        " add.s64 b1, %2, 128;\n add.s64 b2, %2, 256;\n add.s64 b3, %2, 384;\n"
+        " add.s32 a1, %1, 8;\n add.s64 b1, %2, 128;\n"
         " @e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n"
-        " @e tcgen05.mma.cta_group::1.kind::f16 [%0], [a1], b1, %3, t;\n"
-        " @e tcgen05.mma.cta_group::1.kind::f16 [%0], [a2], b2, %3, t;\n"
-        " @e tcgen05.mma.cta_group::1.kind::f16 [%0], [a3], b3, %3, t;\n}\n" ::"r"(d),
+        " @e tcgen05.mma.cta_group::1.kind::f16 [%0], [a1], b1, %3, t;\n}\n" ::"r"(d),
         "r"(a), "l"(b), "r"(id), "r"(acc)
         : "memory");
 }
@@ -230,6 +260,23 @@ __device__ __forceinline__ float ex2(float x) {
     return y;
 }
 __device__ __forceinline__ float asf(uint32_t u) { return __uint_as_float(u); }
+// two fp32 lanes in one instruction
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+    float2 r;
+    asm("{\n .reg .b64 a, b, c;\n mov.b64 a, {%2, %3};\n mov.b64 b, {%4, %5};\n mov.b64 c, {%6, %7};\n"
+        " fma.rn.f32x2 a, a, b, c;\n mov.b64 {%0, %1}, a;\n}\n"
+        : "=f"(r.x), "=f"(r.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
+    return r;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+    float2 r;
+    asm("{\n .reg .b64 a, b;\n mov.b64 a, {%2, %3};\n mov.b64 b, {%4, %5};\n"
+        " add.rn.f32x2 a, a, b;\n mov.b64 {%0, %1}, a;\n}\n"
+        : "=f"(r.x), "=f"(r.y)
+        : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return r;
+}
 __device__ __forceinline__ uint32_t pack(float lo, float hi) {
     const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
     return *reinterpret_cast<const uint32_t*>(&h);
@@ -305,26 +352,33 @@ struct Pages {
 template <int D, int NP, int QT, typename T>
 __global__ void __launch_bounds__(kThreads, 1) window_prefill_kernel(const __grid_constant__ PrefillArgs p) {
     using C = Cfg<D, NP, QT>;
-    constexpr int KT = C::KT;
     const WindowArgs& a = p.a;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* sm = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     Ctl* c = reinterpret_cast<Ctl*>(sm + C::CTL);
-    const uint32_t q_smem = smem_u32(sm), ring = q_smem + C::Q_BYTES;
+    const uint32_t q_smem = smem_u32(sm), ring = q_smem + C::Q_BYTES, ctl = q_smem + C::CTL;
+    const uint32_t bar_full = ctl + offsetof(Ctl, full), bar_empty = ctl + offsetof(Ctl, empty),
+                   bar_s = ctl + offsetof(Ctl, s_full), bar_s_free = ctl + offsetof(Ctl, s_free),
+                   bar_p = ctl + offsetof(Ctl, p_full), bar_pv = ctl + offsetof(Ctl, pv_done),
+                   bar_o_free = ctl + offsetof(Ctl, o_free), bar_q = ctl + offsetof(Ctl, q_full),
+                   bar_end = ctl + offsetof(Ctl, end);
     const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
 
-    // ---- which rows: block units are kv heads (and groups of their heads) fastest, prompts
-    // and row tiles from the last, whose rows see the most
+    // ---- which rows: splits fastest, then kv heads (and groups of their heads), then
+    // prompts and row tiles from the last, whose rows see the most
     const int units = a.Hkv * p.groups;
-    const int kvh = blockIdx.x % units / p.groups, head0 = blockIdx.x % units % p.groups * p.heads;
+    const int split = QT == 1 ? blockIdx.x % p.splits : 0;
+    const int unit = QT == 1 ? blockIdx.x / p.splits : blockIdx.x;  // row tile and kv head (and group)
+    const int kvh = unit % units / p.groups, head0 = unit % units % p.groups * p.heads;
     const int G = a.Hq / a.Hkv, heads = min(p.heads, G - head0);
     if (warp == 0) {
-        int left = blockIdx.x / units;  // row tiles from the end
+        int left = unit / units;  // row tiles from the end
         int row0 = 0, tokens = 0, req = 0, pos0 = 0;
         for (int top = a.n_prompts - 1; top >= 0; top -= 32) {
             const int i = top - lane;
-            int lo = 0, hi = 0;
+            int lo = 0, hi = 0, at = 0;
             if (i >= 0) {
+                if (a.first_pos) at = a.first_pos[i];
                 lo = min(max(a.row_starts[i], 0), a.rows);
                 hi = min(max(a.row_starts[i + 1], lo), a.rows);
             }
@@ -343,7 +397,7 @@ __global__ void __launch_bounds__(kThreads, 1) window_prefill_kernel(const __gri
                     row0 = lo + first;
                     tokens = min(QT * p.tok, hi - lo - first);
                     req = i;
-                    pos0 = min(max(a.first_pos ? a.first_pos[i] : 0, -(1 << 30)), 1 << 30) + first;
+                    pos0 = min(max(at, -(1 << 30)), 1 << 30) + first;
                 }
                 row0 = __shfl_sync(0xffffffffu, row0, src);
                 tokens = __shfl_sync(0xffffffffu, tokens, src);
@@ -358,26 +412,29 @@ __global__ void __launch_bounds__(kThreads, 1) window_prefill_kernel(const __gri
             c->tokens = tokens;
             c->req = req;
             c->pos0 = pos0;
+        }
+    } else if (warp == 8) {
+        if (lane == 0) {
             c->abort = 0;
             c->bad = 0;
             for (int i = 0; i < C::SLOTS; ++i) {
-                bar_init(&c->full[i], 128);
-                bar_init(&c->empty[i], 1);
+                bar_init(bar_full + 8 * i, kLoaders);
+                bar_init(bar_empty + 8 * i, QT);
             }
             for (int w = 0; w < 2; ++w) {
-                bar_init(&c->s_full[w], 1);
-                bar_init(&c->p_full[w], 128);
-                bar_init(&c->pv_done[w], 1);
+                bar_init(bar_s + 8 * w, 1);
+                bar_init(bar_s_free + 8 * w, 128);
             }
-            bar_init(&c->q_full, 256);
-            bar_init(&c->end, 1);
+            for (int i = 0; i < 4; ++i) {
+                bar_init(bar_p + 8 * i, 128);
+                bar_init(bar_pv + 8 * i, 1);
+            }
+            bar_init(bar_o_free, 128);
+            bar_init(bar_q, 256);
+            bar_init(bar_end, 2);
             asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         }
-    }
-    __syncthreads();
-    const int row0 = c->row0, tokens = c->tokens, req = c->req, pos0 = c->pos0;
-    if (tokens == 0) return;  // the grid is an upper bound
-    if (warp == 12) {
+    } else if (warp == 10) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&c->tmem)),
                      "r"(512u)
                      : "memory");
@@ -387,14 +444,18 @@ __global__ void __launch_bounds__(kThreads, 1) window_prefill_kernel(const __gri
     __syncthreads();
     fence_after();
     const uint32_t tmem = c->tmem;
+    const int row0 = c->row0, tokens = c->tokens, req = c->req, pos0 = c->pos0;
 
     const int pos1 = pos0 + tokens - 1;
     const Pages pages(a, pos0, pos1);
-    const int n = (pages.n + C::PPT - 1) / C::PPT;  // key tiles
+    // this block's part of the list (the grid is an upper bound: blocks without rows have none)
+    const int begin = tokens == 0 ? 0 : (int)((int64_t)pages.n * split / p.splits);
+    const int n = tokens == 0 ? 0 : (int)((int64_t)pages.n * (split + 1) / p.splits) - begin;
+    auto page_at = [&](int t) { return pages.at(begin + t); };
     // the rows of stream w: its row tile's
     auto stream_pos = [&](int w) { return QT == 2 ? pos0 + w * p.tok : pos0; };
     auto stream_tokens = [&](int w) { return QT == 2 ? min(max(tokens - w * p.tok, 0), p.tok) : tokens; };
-    // the key tiles that stream w computes: [0, sink) and [lo, hi)
+    // the key tiles that stream w computes (QT = 2): [0, sink) and [lo, hi)
     struct Takes {
         int sink, lo, hi;
         __device__ bool operator()(int t) const { return t < sink || (t >= lo && t < hi); }
@@ -404,21 +465,21 @@ __global__ void __launch_bounds__(kThreads, 1) window_prefill_kernel(const __gri
         if (stream_tokens(w) > 0) {
             const Pages mine(a, stream_pos(w), stream_pos(w) + stream_tokens(w) - 1);
             const int shift = pages.sink - pages.win;  // of a window page in the list
-            k.sink = (min(mine.sink, pages.sink) + C::PPT - 1) / C::PPT;
-            if (mine.end > max(mine.win, pages.win)) {
-                k.lo = (max(mine.win, pages.win) + shift) / C::PPT;
-                k.hi = (mine.end + shift + C::PPT - 1) / C::PPT;
-            }
+            k.sink = min(mine.sink, pages.sink);
+            k.lo = max(mine.win, pages.win) + shift;
+            k.hi = mine.end + shift;
         }
         return k;
     };
 
+    Waiter wait{c, false};
     if (warp >= 8) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
-        if (warp < 12) {
+        if (warp < 10) {
             // ---------------------------------------------------------------- loader
             const int lt = tid - 256;
-            constexpr int CPR = D / 8, RPP = 128 / CPR;  // 16-byte chunks per row, rows per pass
+            constexpr int CPR = D / 8, RPP = kLoaders / CPR;  // 16-byte chunks per row, rows per pass
+            constexpr int PASSES = KT / RPP;
             const int chunk = lt % CPR, r0 = lt / CPR;
             const char* layer = a.kv.base + (uint64_t)a.kv.layer * a.kv.layer_page_bytes;
             const int64_t* table = a.kv.page_offsets + (int64_t)req * a.kv.max_pages;
@@ -426,198 +487,138 @@ __global__ void __launch_bounds__(kThreads, 1) window_prefill_kernel(const __gri
             auto seen = [&](int pos) {
                 return pos < pages.last && ((pos >= win0 && a.window > 0) || pos < a.sinks);
             };
-            auto place = [&](uint32_t slot, int x, int r) {
-                return slot + (uint32_t)((chunk >> 3) * C::KV_SLAB + (x * kPageTokens + r) * 128 +
-                                         (((chunk & 7) ^ (r & 7)) << 4));
-            };
-            // the tile at a place of the order: its index, and whether it holds values
-            auto tile_of = [&](int at, bool& is_v) {
-                is_v = false;
-                if (at < min(n, C::LEAD)) return at;
-                const int x = at - min(n, C::LEAD);  // V0 K_LEAD V1 K_(LEAD+1) ... then values alone
-                const int both = max(n - C::LEAD, 0);
-                if (x < 2 * both) {
-                    is_v = (x & 1) == 0;
-                    return is_v ? x / 2 : x / 2 + C::LEAD;
-                }
-                is_v = true;
-                return x - both;
-            };
-            // tiles that some row does not see in full: values that are not finite are taken out
-            auto check = [&](int at) {
-                bool is_v;
-                const int t = tile_of(at, is_v);
-                if (!is_v) return;
-                const uint32_t slot = ring + (uint32_t)(at % C::SLOTS) * C::SLOT;
-                for (int x = 0; x < C::PPT; ++x) {
-                    const int v = t * C::PPT + x, b = pages.at(v) * kPageTokens;
-                    if (v >= pages.n) break;
-                    if (b + kPageTokens - 1 <= pos0 &&
-                        (b > pos1 - a.window || b + kPageTokens <= a.sinks)) continue;  // all rows see all of it
-                    for (int r = r0; r < kPageTokens; r += RPP) {
-                        const uint32_t w = place(slot, x, r);
-                        uint32_t u[4];
-                        asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];"
-                                     : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3])
-                                     : "r"(w)
-                                     : "memory");
-                        bool bad = false;
+            // place in a slot of this thread's chunk of pass k: row r0 + k RPP, chunk ^ row % 8
+            static_assert(RPP == 4 || RPP == 8, "");
+            const uint32_t place0 = (uint32_t)((chunk >> 3) * C::KV_SLAB + r0 * 128 + (((chunk & 7) ^ (r0 & 7)) << 4));
+            const uint32_t place1 = RPP == 8 ? place0 : place0 ^ 64;  // odd passes: row % 8 differs by 4
+            auto place = [&](int k) { return (k & 1 ? place1 : place0) + k * RPP * 128; };
+            // Slots arrive at their barrier by themselves, except with values of a page that not all rows
+            // see in full: of those, the ones that are not finite are taken out first, one slot later.
+            auto checked = [&](uint32_t slot) {
+                for (int k = 0; k < PASSES; ++k) {
+                    const uint32_t w = ring + slot * C::SLOT + C::TILE + place(k);
+                    uint32_t u[4];
+                    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];"
+                                 : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3])
+                                 : "r"(w)
+                                 : "memory");
+                    bool bad = false;
 #pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            bad |= (u[i] & 0x7F80u) == 0x7F80u || (u[i] & 0x7F800000u) == 0x7F800000u;
-                        if (bad) {
-                            asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(w), "r"(0u) : "memory");
-                            *(volatile int*)&c->bad = 1;
-                        }
+                    for (int i = 0; i < 4; ++i)
+                        bad |= (u[i] & 0x7F80u) == 0x7F80u || (u[i] & 0x7F800000u) == 0x7F800000u;
+                    if (bad) {
+                        asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(w), "r"(0u) : "memory");
+                        *(volatile int*)&c->bad = 1;
+                    }
+                }
+                bar_arrive(bar_full + 8 * slot);
+            };
+            constexpr int STEP = RPP * D * 2;  // bytes from a pass to the next in the page
+            auto load = [&](int t, bool is_v, uint32_t dst) {
+                const int pg = page_at(t), b = pg * KT;
+                const char* src = layer + __ldg(table + pg) + ((int64_t)(is_v ? a.Hkv : 0) + kvh) * (KT * D * 2) +
+                                  (r0 * D + chunk * 8) * 2;
+                if (b + KT <= pages.last && ((b >= win0 && a.window > 0) || b + KT <= a.sinks)) {  // the whole page
+#pragma unroll
+                    for (int k = 0; k < PASSES; ++k) cp_async16(dst + place(k), src + k * STEP, 16u);
+                } else {
+#pragma unroll 2
+                    for (int k = 0; k < PASSES; ++k) {
+                        const bool ok = seen(b + r0 + k * RPP);
+                        cp_async16(dst + place(k), ok ? src + k * STEP : layer, ok ? 16u : 0u);
                     }
                 }
             };
-            auto signal = [&](int at) {
-                check(at);
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                bar_arrive(&c->full[at % C::SLOTS]);
-            };
-            const int total = 2 * n;
-            const int step = RPP * D * 2;  // a pass further in the page; RPP is a multiple of 8: the swizzle stays
-            static_assert(RPP % 8 == 0, "");
-            int at = 0, slot = 0;
-            uint32_t free_phase = 1;  // of the ring's previous round; none for the first
-            for (; at < total; ++at) {
-                if (at >= C::SLOTS && !bar_wait(c, &c->empty[slot], free_phase, 1)) break;
-                bool is_v;
-                const int t = tile_of(at, is_v);
-#pragma unroll
-                for (int x = 0; x < C::PPT; ++x) {
-                    const int v = t * C::PPT + x;
-                    const int pg = v < pages.n ? pages.at(v) : 0, b = pg * kPageTokens;
-                    const uint32_t dst = place(ring + (uint32_t)slot * C::SLOT, x, r0);
-                    const char* src = layer;
-                    if (v < pages.n)
-                        src += __ldg(table + pg) + ((int64_t)(is_v ? a.Hkv : 0) + kvh) * (kPageTokens * D * 2) +
-                               (r0 * D + chunk * 8) * 2;
-                    if (v < pages.n && b + kPageTokens <= pages.last &&
-                        ((b >= win0 && a.window > 0) || b + kPageTokens <= a.sinks)) {  // the whole page
-#pragma unroll
-                        for (int k = 0; k < kPageTokens / RPP; ++k) cp_async16(dst + k * RPP * 128, src + k * step, 16u);
-                    } else {
-#pragma unroll
-                        for (int k = 0; k < kPageTokens / RPP; ++k) {
-                            const bool ok = v < pages.n && seen(b + r0 + k * RPP);
-                            cp_async16(dst + k * RPP * 128, ok ? src + k * step : layer, ok ? 16u : 0u);
-                        }
-                    }
+            int slot = 0, late = -1;  // late: the slot before, if it is yet to be checked
+            uint32_t free_phase = 1;  // of the ring's previous round (before the first one: complete)
+#pragma unroll 1
+            for (int i = 0; i < n + C::AHEAD && n > 0; ++i) {
+                const int t = i - C::AHEAD;  // whose values
+                const uint32_t dst = ring + (uint32_t)slot * C::SLOT;
+                wait(bar_empty + 8 * slot, free_phase, 1);
+                if (i < n) load(i, false, dst);
+                bool some = false;
+                if (t >= 0) {
+                    load(t, true, dst + C::TILE);
+                    const int b = page_at(t) * KT;
+                    some = !(b + KT - 1 <= pos0 && (b > pos1 - a.window || b + KT <= a.sinks));
                 }
                 asm volatile("cp.async.commit_group;" ::: "memory");
-                if (at >= C::LAG) {
-                    asm volatile("cp.async.wait_group %0;" ::"n"(C::LAG) : "memory");
-                    signal(at - C::LAG);
+                if (!some)
+                    asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar_full + 8 * slot)
+                                 : "memory");
+                if (late >= 0) {
+                    asm volatile("cp.async.wait_group 1;" ::: "memory");
+                    checked(late);
                 }
+                late = some ? slot : -1;
                 if (++slot == C::SLOTS) {
                     slot = 0;
                     free_phase ^= 1;
                 }
             }
             asm volatile("cp.async.wait_all;" ::: "memory");
-            if (at == total)
-                for (int i = max(0, total - C::LAG); i < total; ++i) signal(i);
-        } else if (warp == 12 && n > 0) {
+            if (late >= 0) checked(late);
+        } else if (n > 0) {
             // ---------------------------------------------------------------- MMA issue
-            uint32_t pv_n[2] = {0, 0};  // products P V issued per stream
-            bool ok = warp_wait(c, &c->q_full, 0, 2);
-            // the ring is used in its own order: a cursor and the phase of its round
-            int slot = 0;
-            uint32_t phase = 0;
-            auto advance = [&] {
-                commit(&c->empty[slot]);
+            const int w = warp - 10;  // the stream
+            const Takes takes = takes_of(w);
+            auto mine = [&](int t) { return t >= 0 && t < n && (QT == 1 ? (t & 1) == w : takes(t)); };
+            const uint64_t q_desc = sdesc(q_smem + (QT == 2 ? w * NP * C::Q_PLANE : 0), 16), k_desc = sdesc(ring, 16),
+                           v_desc = sdesc(ring + C::TILE, C::KV_SLAB);
+            uint32_t slot = 0, phase = 0;     // a cursor in the ring, and the phase of its round
+            uint32_t free = 1;                // of S (before the first tile: complete)
+            uint32_t done = 0;                // products P V
+            wait(bar_q, 0, 2);
+#pragma unroll 1
+            for (int i = 0; i < n + C::AHEAD; ++i) {
+                if (QT == 2 || (i & 1) == w) {  // (a slot's keys and values are of one stream, or of both)
+                    wait(bar_full + 8 * slot, phase, 3);
+                    fence_loaded();
+                    if (mine(i)) {  // S = Q K^T, once the softmax has read the last one
+                        wait(bar_s_free + 8 * w, free, 4);
+                        free ^= 1;
+                        fence_after();
+                        const uint64_t k = k_desc + slot * (C::SLOT / 16);
+#pragma unroll
+                        for (int pl = NP - 1; pl >= 0; --pl)
+#pragma unroll
+                            for (int x = 0; x < D / 64; ++x)
+                                mma_ss4(tmem + C::s_col(w), q_desc + (pl * C::Q_PLANE + x * C::Q_SLAB) / 16,
+                                        k + x * C::KV_SLAB / 16, idesc(KT, false), pl != NP - 1 || x != 0);
+                        commit(bar_s + 8 * w);
+                    }
+                    if (mine(i - C::AHEAD)) {  // O += P V
+                        const uint32_t buf = done & 1;
+                        wait(bar_p + 16 * w + 8 * buf, done / 2 & 1, 5);
+                        // O is one for both streams: the other one's last tile has been drained.  (This
+                        // stream's own last one has, as its P is here, so the phase is the right one.)
+                        if (NP > 1) wait(bar_o_free, (i - C::AHEAD + 1) & 1, 9);
+                        fence_after();
+                        const uint64_t v = v_desc + slot * (C::SLOT / 16);
+#pragma unroll
+                        for (int pl = NP - 1; pl >= 0; --pl)
+#pragma unroll
+                            for (int x = 0; x < 2; ++x)  // O is kept (bf16), or drained after every tile
+                                mma_ts2(tmem + C::o_col(w), tmem + C::p_col(w, buf, pl) + 16 * x,
+                                        v + x * (32 * 128 / 16), idesc(D, true),
+                                        pl != NP - 1 || x != 0 || (NP == 1 && done) ? 1u : 0u);
+                        commit(bar_pv + 16 * w + 8 * buf);
+                        ++done;
+                    }
+                    commit(bar_empty + 8 * slot);
+                }
                 if (++slot == C::SLOTS) {
                     slot = 0;
                     phase ^= 1;
                 }
-            };
-            const uint64_t q_desc = sdesc(q_smem, 16), k_desc = sdesc(ring, 16), v_desc = sdesc(ring, C::KV_SLAB);
-            auto issue_s = [&](int w) {  // S of the keys at the cursor; P of the stream's last tile has been used
-                if (!warp_wait(c, &c->full[slot], phase, 3)) return false;
-                if (pv_n[w] && !warp_wait(c, &c->pv_done[w], (pv_n[w] - 1) & 1, 4)) return false;
-                fence_after();
-                const uint64_t q = q_desc + (QT == 2 ? (uint32_t)w * (NP * C::Q_PLANE / 16) : 0u);
-                const uint64_t k = k_desc + (uint32_t)slot * (C::SLOT / 16);
-                const uint32_t d = tmem + 256u * w + C::S;
-#pragma unroll
-                for (int pl = NP - 1; pl >= 0; --pl)
-#pragma unroll
-                    for (int x = 0; x < D / 64; ++x)
-                        mma_ss4(d, q + (pl * C::Q_PLANE + x * C::Q_SLAB) / 16, k + x * C::KV_SLAB / 16,
-                                idesc(KT, false), pl != NP - 1 || x != 0);
-                commit(&c->s_full[w]);
-                return true;
-            };
-            auto issue_pv = [&](int w) {  // O += P V of the values at the cursor
-                if (!warp_wait(c, &c->p_full[w], pv_n[w] & 1, 5) || !warp_wait(c, &c->full[slot], phase, 3)) return false;
-                fence_after();
-                const uint64_t v = v_desc + (uint32_t)slot * (C::SLOT / 16);
-                const uint32_t d = tmem + 256u * w + C::O, pa = tmem + 256u * w;
-                const uint32_t first = NP == 1 && pv_n[w] ? 1u : 0u;  // O is kept, or drained per tile
-#pragma unroll
-                for (int pl = NP - 1; pl >= 0; --pl)
-#pragma unroll
-                    for (int x = 0; x < KT / 64; ++x)
-                        mma_ts4(d, pa + (pl == 0 ? C::P0 : pl == 1 ? C::P1 : C::P2) + 32 * x, v + x * (64 * 128 / 16),
-                                idesc(D, true), pl != NP - 1 || x != 0 ? 1u : first);
-                ++pv_n[w];
-                commit(&c->pv_done[w]);
-                return true;
-            };
-            if (QT == 2) {
-                const Takes k0 = takes_of(0), k1 = takes_of(1);
-                if (ok && k0(0)) ok = issue_s(0);
-                if (ok && k1(0)) ok = issue_s(1);
-                advance();
-                for (int t = 0; t < n && ok; ++t) {
-                    // cursor on V_t; K_(t+1) is the next one
-                    const int v_slot = slot;
-                    const uint32_t v_phase = phase;
-                    const bool more = t + 1 < n;
-                    auto to_k = [&] {
-                        if (++slot == C::SLOTS) {
-                            slot = 0;
-                            phase ^= 1;
-                        }
-                    };
-                    auto to_v = [&] {
-                        slot = v_slot;
-                        phase = v_phase;
-                    };
-                    if (k0(t)) ok = issue_pv(0);
-                    if (ok && more && k0(t + 1)) {
-                        to_k();
-                        ok = issue_s(0);
-                        to_v();
-                    }
-                    if (ok && k1(t)) ok = issue_pv(1);
-                    advance();
-                    if (ok && more && k1(t + 1)) ok = issue_s(1);
-                    if (more) advance();
-                }
-            } else {
-                for (int t = 0; t < min(2, n) && ok; ++t) {
-                    ok = issue_s(t);
-                    advance();
-                }
-                for (int t = 0; t < n && ok; ++t) {
-                    ok = issue_pv(t & 1);
-                    advance();
-                    if (ok && t + 2 < n) {
-                        ok = issue_s(t & 1);
-                        advance();
-                    }
-                }
             }
             // nothing may be in flight when the tensor memory is released
-            commit(&c->end);
+            commit(bar_end);
             const uint64_t t0 = now_ns();
-            while (!bar_try(&c->end, 0) && now_ns() - t0 < 2000000000ull) {}
+            while (!bar_try(bar_end, 0) && now_ns() - t0 < 2000000000ull) {}
         }
-    } else {
+    } else if (tokens > 0) {
         // -------------------------------------------------------------------- softmax
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftRegs));
         const T* qg = static_cast<const T*>(a.q);
@@ -625,8 +626,8 @@ __global__ void __launch_bounds__(kThreads, 1) window_prefill_kernel(const __gri
         auto row_at = [&](int tok, int head) {  // element offset of a row of q and o
             return ((int64_t)(row0 + tok) * a.Hq + kvh * G + head0 + head) * D;
         };
-        // ---- queries -> shared memory, bf16 planes, swizzled; eight loads in flight per thread
-        constexpr int CPR = D / 8, EACH = QT * 128 * CPR / 256, MOST = NP == 1 ? 8 : 4, BATCH = EACH < MOST ? EACH : MOST;
+        // ---- queries -> shared memory, bf16 planes, swizzled; all of a thread's loads in flight
+        constexpr int CPR = D / 8, EACH = QT * 128 * CPR / 256, MOST = NP == 1 ? 16 : 8, BATCH = EACH < MOST ? EACH : MOST;
         static_assert(EACH % BATCH == 0, "");
         for (int i0 = tid; i0 < QT * 128 * CPR; i0 += 256 * BATCH) {
             uint4 x[BATCH], y[NP == 1 ? 1 : BATCH];
@@ -663,7 +664,7 @@ __global__ void __launch_bounds__(kThreads, 1) window_prefill_kernel(const __gri
             }
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        bar_arrive(&c->q_full);
+        bar_arrive(bar_q);
 
         const int w = warp / 4, r = tid % 128;
         const int base_tok = QT == 2 ? w * p.tok : 0, mine = stream_tokens(w);
@@ -671,44 +672,50 @@ __global__ void __launch_bounds__(kThreads, 1) window_prefill_kernel(const __gri
         const bool live = tk < min(p.tok, mine);
         const int pos = live ? pos0 + base_tok + tk : -1;
         const int first = pos0 + base_tok, final = first + mine - 1;  // positions of the stream's rows
-        const uint32_t t_row = tmem + 256u * w + ((uint32_t)(warp % 4) << 21);
+        // key tiles [full0, full1) of the window are seen in full by all of the stream's rows
+        const int list0 = pages.sink - pages.win - begin;  // tile of page 0, were it in the window's part
+        const int full0 = max(pages.win, final - a.window < 0 ? 0 : (final - a.window) / KT + 1) + list0;
+        const int full1 = max(min(first + 1, pages.last), 0) / KT + list0;
+        const uint32_t lanes = (uint32_t)(warp % 4) << 21;  // this warp's lanes of tensor memory
         float m = -INFINITY, l = 0.f;  // m: the maximum that the weights are relative to
         uint32_t done = 0;             // tiles computed
+        // P V of the stream's tile j is complete (j the last or the last but one whose P is handed over,
+        // or -2 or -1: complete)
+        auto pv_wait = [&](uint32_t j, int code) { wait(bar_pv + 16 * w + 8 * (j & 1), (uint32_t)((int)j >> 1) & 1, code); };
         float o[NP == 1 ? 1 : D];
         if constexpr (NP > 1) {
 #pragma unroll
             for (int i = 0; i < D; ++i) o[i] = 0.f;
         }
-        bool ok = true;
         const Takes takes = takes_of(w);
         for (int t = QT == 1 ? w : 0; t < n; t += QT == 1 ? 2 : 1) {
             if (QT == 2 && !takes(t)) continue;
-            // which positions of the tile this row sees, one bit each
-            bool masked = false;
-            uint32_t see[KT / 32];
-#pragma unroll
-            for (int x = 0; x < C::PPT; ++x) {
-                const int v = t * C::PPT + x, b = pages.at(v) * kPageTokens;
-                const bool all = v < pages.n && b + kPageTokens - 1 <= first &&
-                                 (b > final - a.window || b + kPageTokens <= a.sinks);
-                masked |= !all;
-                uint64_t bits = ~0ull;
-                if (!all)
-                    bits = v < pages.n && live ? low_bits(min(pos, a.max_ctx - 1) - b + 1) &
-                                                     (~low_bits(pos - a.window + 1 - b) | low_bits(a.sinks - b))
-                                               : 0ull;
-                see[2 * x] = (uint32_t)bits;
-                see[2 * x + 1] = (uint32_t)(bits >> 32);
+            // which positions of the page this row sees, one bit each
+            const bool masked = t < full0 || t >= full1;
+            uint32_t see[2] = {0xffffffffu, 0xffffffffu};
+            if (masked) {
+                const int b = page_at(t) * KT;
+                const uint64_t bits =
+                    live ? low_bits(min(pos, a.max_ctx - 1) - b + 1) &
+                               (~low_bits(pos - a.window + 1 - b) | low_bits(a.sinks - b))
+                         : 0ull;
+                see[0] = (uint32_t)bits;
+                see[1] = (uint32_t)(bits >> 32);
             }
-            if (!(ok = warp_wait(c, &c->s_full[w], done & 1, 6))) break;
+            const uint32_t buf = done & 1;
+            wait(bar_s + 8 * w, done & 1, 6);
+            __syncwarp();
             fence_after();
+            const uint32_t s_at = tmem + lanes + C::s_col(w);
             if constexpr (NP == 1) {
                 uint32_t s[KT];
-                tmem_ld32<0>(t_row + C::S, s);
-                tmem_ld32<32>(t_row + C::S + 32, s);
-                tmem_ld32<64>(t_row + C::S + 64, s);
-                tmem_ld32<96>(t_row + C::S + 96, s);
+                tmem_ld32<0>(s_at, s);
+                tmem_ld32<32>(s_at + 32, s);
                 tmem_landed(s);
+                fence_before();
+                bar_arrive(bar_s_free + 8 * w);
+                pv_wait(done - 2, 8);  // P of that tile is free
+                __syncwarp();
                 if (masked) {
 #pragma unroll
                     for (int i = 0; i < KT; ++i)
@@ -721,8 +728,7 @@ __global__ void __launch_bounds__(kThreads, 1) window_prefill_kernel(const __gri
                     x1 = fmaxf(x1, fmaxf(asf(s[i + 2]), asf(s[i + 3])));
                 }
                 const float mx = fmaxf(x0, x1) * p.scale;
-                // O is rescaled when a row's maximum has outgrown the one in use by 2^8; P V of
-                // the stream's last tile is complete (S of this one was issued after it)
+                // O is rescaled when a row's maximum has outgrown the one in use by 2^8
                 const bool grown = mx > m + 8.f;  // the first time too: m is -inf
                 if (__any_sync(0xffffffffu, grown)) {
                     const float m_new = grown ? mx : m;
@@ -730,191 +736,334 @@ __global__ void __launch_bounds__(kThreads, 1) window_prefill_kernel(const __gri
                     m = m_new;
                     l *= alpha;
                     if (done) {
+                        pv_wait(done - 1, 8);
+                        __syncwarp();
+                        fence_after();
 #pragma unroll
                         for (int i = 0; i < D; i += 32) {
                             uint32_t y[32];
-                            tmem_ld32<0>(t_row + C::O + i, y);
+                            tmem_ld32<0>(tmem + lanes + C::o_col(w) + i, y);
                             tmem_landed(y);
 #pragma unroll
                             for (int e = 0; e < 32; ++e) y[e] = __float_as_uint(asf(y[e]) * alpha);
-                            tmem_st16<0>(t_row + C::O + i, y);
-                            tmem_st16<16>(t_row + C::O + i + 16, y);
+                            tmem_st16<0>(tmem + lanes + C::o_col(w) + i, y);
+                            tmem_st16<16>(tmem + lanes + C::o_col(w) + i + 16, y);
                         }
                     }
                 }
                 const float base = m == -INFINITY ? 0.f : m;
-                float l0 = 0.f, l1 = 0.f;
+                const float2 scale2 = make_float2(p.scale, p.scale), base2 = make_float2(-base, -base);
+                float2 l0 = make_float2(0.f, 0.f), l1 = l0;
 #pragma unroll
                 for (int i = 0; i < KT; i += 32) {
                     uint32_t pk[16];
 #pragma unroll
-                    for (int e = 0; e < 32; e += 2) {
-                        const float y0 = ex2(fmaf(asf(s[i + e]), p.scale, -base));
-                        const float y1 = ex2(fmaf(asf(s[i + e + 1]), p.scale, -base));
-                        l0 += y0;
-                        l1 += y1;
-                        pk[e / 2] = pack(y0, y1);
+                    for (int e = 0; e < 32; e += 4) {
+                        float2 y = fma2(make_float2(asf(s[i + e]), asf(s[i + e + 1])), scale2, base2);
+                        float2 z = fma2(make_float2(asf(s[i + e + 2]), asf(s[i + e + 3])), scale2, base2);
+                        y.x = ex2(y.x); y.y = ex2(y.y); z.x = ex2(z.x); z.y = ex2(z.y);
+                        l0 = add2(l0, y);
+                        l1 = add2(l1, z);
+                        pk[e / 2] = pack(y.x, y.y);
+                        pk[e / 2 + 1] = pack(z.x, z.y);
                     }
-                    tmem_st16<0>(t_row + C::P0 + i / 2, pk);
+                    tmem_st16<0>(tmem + lanes + C::p_col(w, buf, 0) + i / 2, pk);
                 }
-                l += l0 + l1;
+                l0 = add2(l0, l1);
+                l += l0.x + l0.y;
                 tmem_stored();
                 fence_before();
-                bar_arrive(&c->p_full[w]);
+                bar_arrive(bar_p + 16 * w + 8 * buf);
                 ++done;
             } else {
                 float mx = -INFINITY;
 #pragma unroll
-                for (int i = 0; i < KT; i += 32) {
+                for (int h = 0; h < 2; ++h) {
                     uint32_t s[32];
-                    tmem_ld32<0>(t_row + C::S + i, s);
+                    tmem_ld32<0>(s_at + 32 * h, s);
                     tmem_landed(s);
+                    if (masked) {
 #pragma unroll
-                    for (int e = 0; e < 32; ++e)
-                        if (see[i / 32] >> e & 1u) mx = fmaxf(mx, asf(s[e]));
+                        for (int e = 0; e < 32; ++e)
+                            if (!(see[h] >> e & 1u)) s[e] = 0xff800000u;
+                    }
+                    float x0 = -INFINITY, x1 = -INFINITY;
+#pragma unroll
+                    for (int e = 0; e < 32; e += 4) {
+                        x0 = fmaxf(x0, fmaxf(asf(s[e]), asf(s[e + 1])));
+                        x1 = fmaxf(x1, fmaxf(asf(s[e + 2]), asf(s[e + 3])));
+                    }
+                    mx = fmaxf(mx, fmaxf(x0, x1));
                 }
                 const float m_new = fmaxf(m, mx * p.scale);
                 const float alpha = m == -INFINITY ? 0.f : ex2(m - m_new);
                 m = m_new;
                 const float base = m == -INFINITY ? 0.f : m;
-                float sum = 0.f;
+                const float2 scale2 = make_float2(p.scale, p.scale), base2 = make_float2(-base, -base);
+                float2 sum = make_float2(0.f, 0.f);
 #pragma unroll
-                for (int i = 0; i < KT; i += 32) {
+                for (int h = 0; h < 2; ++h) {
                     uint32_t s[32], pk[16];
-                    tmem_ld32<0>(t_row + C::S + i, s);
+                    tmem_ld32<0>(s_at + 32 * h, s);
                     tmem_landed(s);
+                    if (h == 1) {
+                        fence_before();
+                        bar_arrive(bar_s_free + 8 * w);
+                    }
+                    if (masked) {
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) {
-                        const float y = see[i / 32] >> e & 1u ? ex2(fmaf(asf(s[e]), p.scale, -base)) : 0.f;
-                        sum += y;
-                        s[e] = __float_as_uint(y);
+                        for (int e = 0; e < 32; ++e)
+                            if (!(see[h] >> e & 1u)) s[e] = 0xff800000u;
+                    }
+#pragma unroll
+                    for (int e = 0; e < 32; e += 2) {
+                        float2 y = fma2(make_float2(asf(s[e]), asf(s[e + 1])), scale2, base2);
+                        y.x = ex2(y.x); y.y = ex2(y.y);
+                        sum = add2(sum, y);
+                        s[e] = __float_as_uint(y.x);
+                        s[e + 1] = __float_as_uint(y.y);
                     }
 #pragma unroll
                     for (int pl = 0; pl < 3; ++pl) {
 #pragma unroll
                         for (int e = 0; e < 32; e += 2) {
                             float y0 = asf(s[e]), y1 = asf(s[e + 1]);
-                            pk[e / 2] = peel(y0, y1);
+                            pk[e / 2] = pl < 2 ? peel(y0, y1) : pack(y0, y1);
                             s[e] = __float_as_uint(y0);
                             s[e + 1] = __float_as_uint(y1);
                         }
-                        tmem_st16<0>(t_row + (pl == 0 ? C::P0 : pl == 1 ? C::P1 : C::P2) + i / 2, pk);
+                        tmem_st16<0>(tmem + lanes + C::p_col(w, 0, pl) + 16 * h, pk);
                     }
                 }
-                l = fmaf(l, alpha, sum);
+                l = fmaf(l, alpha, sum.x + sum.y);
                 tmem_stored();
                 fence_before();
-                bar_arrive(&c->p_full[w]);
+                bar_arrive(bar_p + 16 * w + 8 * buf);
                 // ---- O of this tile, added in fp32
-                if (!(ok = warp_wait(c, &c->pv_done[w], done & 1, 7))) break;
+                pv_wait(done, 7);
+                __syncwarp();
                 ++done;
                 fence_after();
 #pragma unroll
                 for (int i = 0; i < D; i += 32) {
                     uint32_t y[32];
-                    tmem_ld32<0>(t_row + C::O + i, y);
+                    tmem_ld32<0>(tmem + lanes + C::o_col(w) + i, y);
                     tmem_landed(y);
 #pragma unroll
                     for (int e = 0; e < 32; ++e) o[i + e] = fmaf(o[i + e], alpha, asf(y[e]));
                 }
+                fence_before();
+                bar_arrive(bar_o_free);
             }
         }
-        if (NP == 1 && ok && done) {
-            ok = warp_wait(c, &c->pv_done[w], (done - 1) & 1, 8);
+        if constexpr (NP == 1) {
+            pv_wait(done - 2, 8);
+            pv_wait(done - 1, 8);
+            __syncwarp();
             fence_after();
         }
-        // ---- QT = 1: stream 1 hands its state to stream 0 through the ring, which nothing uses
-        // any more once both streams' last products are complete
-        float keep = 1.f, take = 0.f;
-        float* join = reinterpret_cast<float*>(sm + C::Q_BYTES);  // [D][128]
-        float* join_ml = reinterpret_cast<float*>(sm);            // [2][128], where the queries were
-        if constexpr (QT == 1) {
-            asm volatile("bar.sync 1, 256;" ::: "memory");
-            if (w == 1) {
-                join_ml[r] = m;
-                join_ml[128 + r] = l;
+        // the row's 32 elements from i of O as it stands
+        auto o_part = [&](int i, uint32_t (&y)[32]) {
+            if constexpr (NP == 1) {
+                if (done) {  // the same for a warp: all its lanes load
+                    tmem_ld32<0>(tmem + lanes + C::o_col(w) + i, y);
+                    tmem_landed(y);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) y[e] = 0u;
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < 32; ++e) y[e] = __float_as_uint(o[i + e]);
+            }
+        };
+        // The finished 32 elements from i of the row, through shared memory where the stream's queries
+        // were (same swizzle, so that neither side has bank conflicts), to leave in whole rows.
+        uint8_t* stage = sm + (QT == 2 ? w * C::Q_PLANE : 0);
+        constexpr int OPR = D * (int)sizeof(T) / 16;  // 16-byte chunks of an output row
+        auto stage_at = [&](int row, int ch) { return stage + (ch >> 3) * C::Q_SLAB + row * 128 + (((ch & 7) ^ (row & 7)) << 4); };
+        auto put = [&](int i, const uint32_t (&y)[32], float f) {
+#pragma unroll
+            for (int e = 0; e < 32; e += 16 / (int)sizeof(T)) {
+                uint4 u;
+                if constexpr (NP == 1)
+                    u = make_uint4(pack(asf(y[e]) * f, asf(y[e + 1]) * f), pack(asf(y[e + 2]) * f, asf(y[e + 3]) * f),
+                                   pack(asf(y[(e + 4) % 32]) * f, asf(y[(e + 5) % 32]) * f),
+                                   pack(asf(y[(e + 6) % 32]) * f, asf(y[(e + 7) % 32]) * f));
+                else
+                    u = make_uint4(__float_as_uint(asf(y[e]) * f), __float_as_uint(asf(y[e + 1]) * f),
+                                   __float_as_uint(asf(y[e + 2]) * f), __float_as_uint(asf(y[e + 3]) * f));
+                *reinterpret_cast<uint4*>(stage_at(r, (i + e) * (int)sizeof(T) / 16)) = u;
+            }
+        };
+        auto leave = [&](int thread, int threads) {
+            const int n_rows = min(p.tok, mine) * heads;
+            for (int i = thread; i < n_rows * OPR; i += threads) {
+                const int row = i / OPR, ch = i % OPR, t_row = row / heads;
+                reinterpret_cast<uint4*>(og + row_at(base_tok + t_row, row - t_row * heads))[ch] =
+                    *reinterpret_cast<const uint4*>(stage_at(row, ch));
+            }
+        };
+        if constexpr (QT == 2) {
+            {
+                const float inv = l == 0.f ? 0.f : 1.0f / l;  // a row that sees nothing: zeros
 #pragma unroll
                 for (int i = 0; i < D; i += 32) {
                     uint32_t y[32];
-                    if constexpr (NP == 1) {
-                        if (done) {
-                            tmem_ld32<0>(t_row + C::O + i, y);
-                            tmem_landed(y);
-                        }
-                    }
-#pragma unroll
-                    for (int e = 0; e < 32; ++e) {
-                        float v;
-                        if constexpr (NP == 1) v = done ? asf(y[e]) : 0.f; else v = o[i + e];
-                        join[(i + e) * 128 + r] = v;
-                    }
+                    o_part(i, y);
+                    put(i, y, inv);
                 }
             }
-            asm volatile("bar.sync 1, 256;" ::: "memory");
-            if (w == 0) {
-                const float m1 = join_ml[r], mt = fmaxf(m, m1);
-                keep = m == -INFINITY ? 0.f : ex2(m - mt);
-                take = m1 == -INFINITY ? 0.f : ex2(m1 - mt);
-                l = l * keep + join_ml[128 + r] * take;
-            }
-        }
-        if (ok && (QT == 2 || w == 0)) {
-            const float inv = l == 0.f ? 0.f : 1.0f / l;  // a row that sees nothing: zeros
-            T* out = og + row_at(live ? base_tok + tk : 0, live ? r % heads : 0);
+            if (w == 0)
+                asm volatile("bar.sync 1, 128;" ::: "memory");
+            else
+                asm volatile("bar.sync 2, 128;" ::: "memory");
+            if (!wait.dead) leave(r, 128);
+        } else {
+            // ---- join the streams through the ring, which nothing uses any more once both streams'
+            // last products are complete: each gives the other half of its columns
+            float* join = reinterpret_cast<float*>(sm + C::Q_BYTES);   // [2][D / 2][128]
+            float2* join_ml = reinterpret_cast<float2*>(join + D * 128);  // [2][128]
+            auto give = [&](auto which) {
+                constexpr int half = decltype(which)::value;
 #pragma unroll
-            for (int i = 0; i < D; i += 32) {
-                uint32_t y[32];
-                if constexpr (NP == 1) {
-                    if (done) {  // the same for a warp: all its lanes load
-                        tmem_ld32<0>(t_row + C::O + i, y);
-                        tmem_landed(y);
-                    } else {
+                for (int i = 0; i < D / 2; i += 32) {
+                    uint32_t y[32];
+                    o_part(half * (D / 2) + i, y);
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) y[e] = 0u;
-                    }
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 32; ++e) y[e] = __float_as_uint(o[i + e]);
+                    for (int e = 0; e < 32; ++e) join[(half * (D / 2) + i + e) * 128 + r] = asf(y[e]);
                 }
-                if (live) {
-                    if constexpr (QT == 1) {
+            };
+            const int64_t part = ((int64_t)unit * p.splits + split) * 128;
+            auto finish = [&](auto which, float keep, float take, float f) {
+                constexpr int half = decltype(which)::value;
 #pragma unroll
-                        for (int e = 0; e < 32; ++e)
-                            y[e] = __float_as_uint(asf(y[e]) * keep + join[(i + e) * 128 + r] * take);
-                    }
-                    if constexpr (NP == 1) {
+                for (int i = half * (D / 2); i < (half + 1) * (D / 2); i += 32) {
+                    uint32_t y[32];
+                    o_part(i, y);
 #pragma unroll
-                        for (int e = 0; e < 32; e += 8) {
-                            uint32_t u[4];
-#pragma unroll
-                            for (int x = 0; x < 4; ++x)
-                                u[x] = pack(asf(y[e + 2 * x]) * inv, asf(y[e + 2 * x + 1]) * inv);
-                            *reinterpret_cast<uint4*>(out + i + e) = make_uint4(u[0], u[1], u[2], u[3]);
-                        }
-                    } else {
+                    for (int e = 0; e < 32; ++e)
+                        y[e] = __float_as_uint(asf(y[e]) * keep + join[(i + e) * 128 + r] * take);
+                    if (p.splits > 1) {
 #pragma unroll
                         for (int e = 0; e < 32; e += 4)
-                            *reinterpret_cast<float4*>(out + i + e) = make_float4(
-                                asf(y[e]) * inv, asf(y[e + 1]) * inv, asf(y[e + 2]) * inv, asf(y[e + 3]) * inv);
+                            __stcg(p.part + part * (D / 4) + (i + e) / 4 * 128 + r,
+                                   make_float4(asf(y[e]), asf(y[e + 1]), asf(y[e + 2]), asf(y[e + 3])));
+                    } else {
+                        put(i, y, f);
                     }
                 }
-                __syncwarp();
+            };
+            asm volatile("bar.sync 1, 256;" ::: "memory");
+            join_ml[w * 128 + r] = make_float2(m, l);
+            if (w == 0) give(std::integral_constant<int, 1>{}); else give(std::integral_constant<int, 0>{});
+            asm volatile("bar.sync 1, 256;" ::: "memory");
+            const float2 his = join_ml[(1 - w) * 128 + r];
+            const float mt = fmaxf(m, his.x);
+            const float keep = m == -INFINITY ? 0.f : ex2(m - mt), take = his.x == -INFINITY ? 0.f : ex2(his.x - mt);
+            const float lt = l * keep + his.y * take, inv = lt == 0.f ? 0.f : 1.0f / lt;
+            if (p.splits > 1 && w == 0) __stcg(p.ml + part + r, make_float2(mt, lt));
+            if (w == 0) finish(std::integral_constant<int, 0>{}, keep, take, inv);
+            else finish(std::integral_constant<int, 1>{}, keep, take, inv);
+            if (p.splits == 1) {
+                asm volatile("bar.sync 1, 256;" ::: "memory");
+                if (!wait.dead) leave(tid, 256);
             }
         }
+    } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftRegs));
     }
     __syncwarp();
     fence_before();
+    if (QT == 1 && p.splits > 1) __threadfence();
     __syncthreads();
-    if (warp == 12) {
+    if (warp == 10) {
         fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
     }
-    if (c->bad && warp < 8 && !c->abort) {
+    if (tokens == 0 || warp >= 8) return;
+    bool bad = false;
+    if (QT == 1 && p.splits > 1) {
+        // ---- the last block of the row tile to arrive joins the parts, in their order; the
+        // counter wraps to zero with that arrival, the flag is taken back by it
+        if (tid == 0) {
+            if (c->bad && !c->abort) atomicOr(p.flagged + unit, 1u);
+            __threadfence();
+            c->last = atomicInc(p.arrived + unit, (unsigned)p.splits - 1u) == (unsigned)p.splits - 1u;
+            __threadfence();
+            if (c->last) c->bad = (int)atomicExch(p.flagged + unit, 0u);
+        }
+        asm volatile("bar.sync 1, 256;" ::: "memory");
+        if (!c->last) return;
+        bad = c->bad;
+        const int r = tid % 128, tk = r / heads;
+        if (tk < min(p.tok, tokens)) {
+            const int64_t part = (int64_t)unit * p.splits * 128 + r;
+            float mt = -INFINITY, lt = 0.f;
+            for (int x = 0; x < p.splits; ++x) mt = fmaxf(mt, __ldcg(p.ml + part + x * 128).x);
+            for (int x = 0; x < p.splits; ++x) {
+                const float2 ml = __ldcg(p.ml + part + x * 128);
+                lt += ml.x == -INFINITY ? 0.f : ml.y * ex2(ml.x - mt);
+            }
+            const float inv = lt == 0.f ? 0.f : 1.0f / lt;
+            T* out = static_cast<T*>(a.o) +
+                     ((int64_t)(row0 + tk) * a.Hq + kvh * G + head0 + r - tk * heads) * D;
+            for (int i = tid / 128 * (D / 8); i < (tid / 128 + 1) * (D / 8); i += 2) {  // half of the row per thread
+                float4 y[2] = {make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)};
+#pragma unroll 4
+                for (int x = 0; x < p.splits; ++x) {
+                    const float mx = __ldcg(p.ml + part + x * 128).x;
+                    const float f = mx == -INFINITY ? 0.f : ex2(mx - mt);
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const float4 v = __ldcg(p.part + ((int64_t)unit * p.splits + x) * 128 * (D / 4) + (i + e) * 128 + r);
+                        y[e].x = fmaf(f, v.x, y[e].x); y[e].y = fmaf(f, v.y, y[e].y);
+                        y[e].z = fmaf(f, v.z, y[e].z); y[e].w = fmaf(f, v.w, y[e].w);
+                    }
+                }
+                if constexpr (NP == 1) {
+                    *reinterpret_cast<uint4*>(out + 4 * i) =
+                        make_uint4(pack(y[0].x * inv, y[0].y * inv), pack(y[0].z * inv, y[0].w * inv),
+                                   pack(y[1].x * inv, y[1].y * inv), pack(y[1].z * inv, y[1].w * inv));
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 2; ++e)
+                        *reinterpret_cast<float4*>(out + 4 * (i + e)) =
+                            make_float4(y[e].x * inv, y[e].y * inv, y[e].z * inv, y[e].w * inv);
+                }
+            }
+        }
+        asm volatile("bar.sync 1, 256;" ::: "memory");
+    } else {
+        bad = c->bad && !c->abort;
+    }
+    if (bad) {
         for (int i = warp; i < tokens * heads; i += 8) {
             const int64_t at = ((int64_t)(row0 + i / heads) * a.Hq + kvh * G + head0 + i % heads) * D;
             walk_row<D, T>(a, req, kvh, pos0 + i / heads, static_cast<const T*>(a.q) + at, static_cast<T*>(a.o) + at);
         }
     }
+}
+
+// Row tiles of a call, at most, and the blocks that share one.
+struct Plan {
+    int heads, groups, tok, splits;
+    int64_t tiles;  // of one row tile per block, over all prompts and units
+};
+
+// A row tile is split when there are fewer row tiles than SMs, into parts of two pages
+// (one per stream) or more.
+Plan make_plan(int M, int n_prompts, int Hq, int Hkv, int window, int sinks, int max_ctx) {
+    Plan p{};
+    const int G = Hq / Hkv;
+    p.groups = (G + 127) / 128;
+    p.heads = (G + p.groups - 1) / p.groups;
+    p.tok = 128 / p.heads;
+    p.tiles = std::min<int64_t>((int64_t)M / p.tok + n_prompts, M) * Hkv * p.groups;
+    const int64_t pages = std::min<int64_t>(((int64_t)max_ctx + KT - 1) / KT,
+                                            ((int64_t)window + p.tok + KT - 1) / KT + 1 + ((int64_t)sinks + KT - 1) / KT);
+    p.splits = p.tiles < kSms ? (int)std::max<int64_t>(1, std::min<int64_t>(kSms / std::max<int64_t>(p.tiles, 1), pages / 2)) : 1;
+    return p;
 }
 
 template <int D, int NP, int QT, typename T>
@@ -931,37 +1080,46 @@ cudaError_t launch_t(const PrefillArgs& p, cudaStream_t st) {
         if (dev < 64) ready.fetch_or(1ull << dev);
     }
     const int64_t tiles = p.a.rows / (QT * p.tok) + p.a.n_prompts;  // at least the sum over prompts
-    const int64_t blocks = std::min<int64_t>(tiles, p.a.rows) * p.a.Hkv * p.groups;
+    const int64_t blocks = std::min<int64_t>(tiles, p.a.rows) * p.a.Hkv * p.groups * p.splits;
     if (blocks > 0x7fffffff) return cudaErrorInvalidValue;
     window_prefill_kernel<D, NP, QT, T><<<(unsigned)blocks, kThreads, C::BYTES, st>>>(p);
     return cudaGetLastError();
 }
 
 template <int D>
-cudaError_t launch_d(const PrefillArgs& p, bool f32, cudaStream_t st) {
+cudaError_t launch_d(const PrefillArgs& p, bool f32, int64_t tiles, cudaStream_t st) {
     if (f32) return launch_t<D, 3, 1, float>(p, st);
     // two row tiles per block once that leaves no SM without a block
-    const int64_t tiles = ((int64_t)p.a.rows / p.tok + p.a.n_prompts) * p.a.Hkv * p.groups;
     return tiles >= 2 * kSms ? launch_t<D, 1, 2, __nv_bfloat16>(p, st) : launch_t<D, 1, 1, __nv_bfloat16>(p, st);
 }
 
 }  // namespace
 
 uint64_t window_prefill_scratch(int M, int n_prompts, int Hq, int Hkv, int d, int window, int sinks, int max_ctx) {
-    return 16;
+    uint64_t n = 2 * kMaxUnits * sizeof(unsigned);
+    if (M > 0) {
+        const Plan p = make_plan(M, n_prompts, Hq, Hkv, window, sinks, max_ctx);
+        if (p.splits > 1) n += (uint64_t)p.tiles * p.splits * 128 * (d + 2) * sizeof(float);
+    }
+    return n;
 }
 
 cudaError_t launch_window_prefill(const WindowArgs& a, bool f32, cudaStream_t st) {
+    const Plan plan = make_plan(a.rows, a.n_prompts, a.Hq, a.Hkv, a.window, a.sinks, a.max_ctx);
     PrefillArgs p{};
     p.a = a;
     p.a.window = std::min(a.window, 1 << 30);  // positions are below max_ctx <= 2^30
     p.a.sinks = std::min(a.sinks, 1 << 30);
-    const int G = a.Hq / a.Hkv;
-    p.groups = (G + 127) / 128;
-    p.heads = (G + p.groups - 1) / p.groups;
-    p.tok = 128 / p.heads;
+    p.heads = plan.heads;
+    p.groups = plan.groups;
+    p.tok = plan.tok;
+    p.splits = plan.splits;
     p.scale = (float)(1.4426950408889634 / sqrt((double)a.d));
-    return a.d == 128 ? launch_d<128>(p, f32, st) : launch_d<64>(p, f32, st);
+    p.arrived = static_cast<unsigned*>(a.scratch);
+    p.flagged = p.arrived + kMaxUnits;
+    p.part = reinterpret_cast<float4*>(p.flagged + kMaxUnits);
+    p.ml = reinterpret_cast<float2*>(p.part + plan.tiles * plan.splits * 128 * (a.d / 4));
+    return a.d == 128 ? launch_d<128>(p, f32, plan.tiles, st) : launch_d<64>(p, f32, plan.tiles, st);
 }
 
 cudaError_t window_prefill_error(int* code) { return cudaMemcpyFromSymbol(code, g_window_error, sizeof(int)); }
