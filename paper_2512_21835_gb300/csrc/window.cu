@@ -6,6 +6,8 @@
 #include <math.h>
 #include <stdint.h>
 
+#include <algorithm>
+
 #include "../../include/loip.h"
 #include "internal.h"
 #include "window.h"
@@ -50,25 +52,36 @@ struct AppendArgs {
     const __nv_bfloat16 *g_q, *g_k;
     float eps;
     const int32_t *positions, *row_req;
-    int n_req, Hq, Hkv;
+    int rows, n_req, Hq, Hkv;
+    int heads;  // per block
     void* q_out;
     KvView kv;
     RopeTurns rope;
 };
 
-__device__ __forceinline__ void load8(const float* p, float (&v)[8]) {
-    const float4 a = __ldg(reinterpret_cast<const float4*>(p)), b = __ldg(reinterpret_cast<const float4*>(p) + 1);
-    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-}
-__device__ __forceinline__ void load8(const __nv_bfloat16* p, float (&v)[8]) {
-    const uint4 w = __ldg(reinterpret_cast<const uint4*>(p));
-    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+// Eight elements as they lie in memory, and their values.
+template <typename T>
+struct Raw8 {
+    uint4 u[sizeof(T) / 2];
+    __device__ __forceinline__ void load(const T* p) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        v[2 * i] = __uint_as_float(u[i] << 16);
-        v[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) u[i] = __ldg(reinterpret_cast<const uint4*>(p) + i);
     }
-}
+    __device__ __forceinline__ void values(float (&v)[8]) const {
+        if constexpr (sizeof(T) == 4) {
+            v[0] = __uint_as_float(u[0].x); v[1] = __uint_as_float(u[0].y); v[2] = __uint_as_float(u[0].z);
+            v[3] = __uint_as_float(u[0].w); v[4] = __uint_as_float(u[1].x); v[5] = __uint_as_float(u[1].y);
+            v[6] = __uint_as_float(u[1].z); v[7] = __uint_as_float(u[1].w);
+        } else {
+            const uint32_t w[4] = {u[0].x, u[0].y, u[0].z, u[0].w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                v[2 * i] = __uint_as_float(w[i] << 16);
+                v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+            }
+        }
+    }
+};
 __device__ __forceinline__ void store8(float* p, const float (&v)[8]) {
     reinterpret_cast<float4*>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
     reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
@@ -83,22 +96,38 @@ __device__ __forceinline__ void store8(__nv_bfloat16* p, const float (&v)[8]) {
     *reinterpret_cast<uint4*>(p) = make_uint4(u[0], u[1], u[2], u[3]);
 }
 
-// One block per token and group of heads; D / 16 lanes per head, each holding
-// the elements 8l .. 8l + 7 of the head and their partners D / 2 further on.
+// A block takes a group of heads of one token; D / 16 lanes per head, each holding the
+// elements 8l .. 8l + 7 of the head and their partners D / 2 further on.  Bound by memory:
+// short blocks with all their loads issued at once, the gains' among them, and as many of
+// them per SM as the registers can be held to (8191 fp32 tokens of 120 heads of 128: 119.6
+// us, 7.0 TB/s; 1999 bf16 tokens of 80 heads, with norms: 18.3 us, 4.5 TB/s, where six or
+// four blocks per SM take 20.7 and 19.7 us, two tokens per block 19.9 us, and one wave of
+// blocks that walk over the tokens with the next one's loads in flight 28.7 us).
 template <int D, typename T>
-__global__ void __launch_bounds__(256) qk_append_kernel(const __grid_constant__ AppendArgs p) {
-    constexpr int LANES = D / 16, HEADS = 256 / LANES;
+__global__ void __launch_bounds__(256, sizeof(T) == 2 ? 8 : 6) qk_append_kernel(const __grid_constant__ AppendArgs p) {
+    constexpr int LANES = D / 16;
     __shared__ __align__(16) float2 turn[D / 2];  // cos, sin
-    const int t = blockIdx.x, l = threadIdx.x % LANES, head = blockIdx.y * HEADS + threadIdx.x / LANES;
-    const bool live = head < p.Hq + 2 * p.Hkv;
+    pdl_trigger();
+    pdl_wait();
+    const int t = blockIdx.x, l = threadIdx.x % LANES, head = blockIdx.y * p.heads + threadIdx.x / LANES;
+    const bool live = head < min(p.Hq + 2 * p.Hkv, (int)(blockIdx.y + 1) * p.heads);
+    const bool is_q = head < p.Hq, is_v = head >= p.Hq + p.Hkv;
     const int pos = p.positions[t], req = p.row_req ? p.row_req[t] : t;
-    const bool padding = pos < 0 || pos / kPageTokens >= p.kv.max_pages || req < 0 || req >= p.n_req;
-    float a[8], b[8];
+    Raw8<T> ra, rb;
+    Raw8<__nv_bfloat16> ga, gb;
     if (live) {
         const T* x = static_cast<const T*>(p.qkv) + (int64_t)t * p.row_stride + head * D + 8 * l;
-        load8(x, a);
-        load8(x + D / 2, b);
+        ra.load(x);
+        rb.load(x + D / 2);
+        if (p.g_q && !is_v) {
+            const __nv_bfloat16* g = (is_q ? p.g_q : p.g_k) + 8 * l;
+            ga.load(g);
+            gb.load(g + D / 2);
+        }
     }
+    const bool padding = pos < 0 || pos / kPageTokens >= p.kv.max_pages || req < 0 || req >= p.n_req;
+    int64_t page = 0;
+    if (live && !is_q && !padding) page = p.kv.page_offsets[(int64_t)req * p.kv.max_pages + pos / kPageTokens];
     if (threadIdx.x < D / 2) {
         const int32_t turns = (int32_t)((uint64_t)pos * p.rope.turn[threadIdx.x] >> 32);
         float s, c;
@@ -106,7 +135,11 @@ __global__ void __launch_bounds__(256) qk_append_kernel(const __grid_constant__ 
         turn[threadIdx.x] = make_float2(c, s);
     }
     __syncthreads();
-    const bool is_q = head < p.Hq, is_v = head >= p.Hq + p.Hkv;
+    float a[8], b[8];
+    if (live) {
+        ra.values(a);
+        rb.values(b);
+    }
     if (p.g_q) {  // the sum is fp32, over a head's lanes
         float ss = 0.f;
         if (live) {
@@ -117,15 +150,13 @@ __global__ void __launch_bounds__(256) qk_append_kernel(const __grid_constant__ 
         for (int m = 1; m < LANES; m *= 2) ss += __shfl_xor_sync(0xffffffffu, ss, m);
         if (live && !is_v) {
             const float r = 1.0f / sqrtf(ss * (1.0f / D) + p.eps);
-            const __nv_bfloat16* g = (is_q ? p.g_q : p.g_k) + 8 * l;
-            float ga[8], gb[8];
-            load8(g, ga);
-            load8(g + D / 2, gb);
+            float g[8];
+            ga.values(g);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                a[i] *= r * ga[i];
-                b[i] *= r * gb[i];
-            }
+            for (int i = 0; i < 8; ++i) a[i] *= r * g[i];
+            gb.values(g);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) b[i] *= r * g[i];
         }
     }
     if (!live) return;
@@ -148,21 +179,22 @@ __global__ void __launch_bounds__(256) qk_append_kernel(const __grid_constant__ 
         store8(o + D / 2, b);
     } else if (!padding) {
         // keys, then values, of the layer: [Hkv][64][D] each
-        char* page = p.kv.base + p.kv.page_offsets[(int64_t)req * p.kv.max_pages + pos / kPageTokens] +
-                     (uint64_t)p.kv.layer * p.kv.layer_page_bytes;
-        __nv_bfloat16* o = reinterpret_cast<__nv_bfloat16*>(page) +
-                           ((int64_t)(head - p.Hq) * kPageTokens + pos % kPageTokens) * D + 8 * l;
+        __nv_bfloat16* o =
+            reinterpret_cast<__nv_bfloat16*>(p.kv.base + page + (uint64_t)p.kv.layer * p.kv.layer_page_bytes) +
+            ((int64_t)(head - p.Hq) * kPageTokens + pos % kPageTokens) * D + 8 * l;
         store8(o, a);
         store8(o + D / 2, b);
     }
 }
 
+// Heads in equal groups of at most a block's 256 threads.
 template <int D, typename T>
-cudaError_t launch_append(const AppendArgs& a, int rows, cudaStream_t st) {
-    constexpr int HEADS = 256 / (D / 16);
-    const int heads = a.Hq + 2 * a.Hkv;
-    qk_append_kernel<D, T><<<dim3(rows, (heads + HEADS - 1) / HEADS), 256, 0, st>>>(a);
-    return cudaGetLastError();
+cudaError_t launch_append(AppendArgs& a, cudaStream_t st) {
+    constexpr int LANES = D / 16, MOST = 256 / LANES;
+    const int heads = a.Hq + 2 * a.Hkv, groups = (heads + MOST - 1) / MOST;
+    a.heads = (heads + groups - 1) / groups;
+    const unsigned threads = std::max((a.heads * LANES + 31) / 32 * 32, D / 2);
+    return launch_pdl(qk_append_kernel<D, T>, dim3(a.rows, groups), threads, 0, st, a);
 }
 
 bool aligned(const void* p, uintptr_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
@@ -225,6 +257,7 @@ extern "C" int loip_k_qk_append(const void* qkv, int32_t dtype, int64_t row_stri
     a.eps = eps;
     a.positions = positions;
     a.row_req = row_req;
+    a.rows = T;
     a.n_req = n_req;
     a.Hq = Hq;
     a.Hkv = Hkv;
@@ -233,10 +266,10 @@ extern "C" int loip_k_qk_append(const void* qkv, int32_t dtype, int64_t row_stri
     a.rope = rope_turns(theta, d);
     cudaStream_t st = (cudaStream_t)stream;
     if (d == 128)
-        return kernel_status(dtype == LOIP_F32 ? launch_append<128, float>(a, T, st)
-                                               : launch_append<128, __nv_bfloat16>(a, T, st));
-    return kernel_status(dtype == LOIP_F32 ? launch_append<64, float>(a, T, st)
-                                           : launch_append<64, __nv_bfloat16>(a, T, st));
+        return kernel_status(dtype == LOIP_F32 ? launch_append<128, float>(a, st)
+                                               : launch_append<128, __nv_bfloat16>(a, st));
+    return kernel_status(dtype == LOIP_F32 ? launch_append<64, float>(a, st)
+                                           : launch_append<64, __nv_bfloat16>(a, st));
 }
 
 extern "C" uint64_t loip_k_window_attention_scratch_bytes(int32_t B, int32_t Hq, int32_t Hkv, int32_t d,

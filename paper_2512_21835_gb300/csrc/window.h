@@ -10,6 +10,29 @@ namespace loip {
 
 constexpr int kPageTokens = 64;
 
+// Programmatic dependent launch: a kernel of this family lets its successor in the stream
+// be launched as soon as all its own blocks are, and reads or writes global memory only
+// after pdl_wait, which returns when the predecessor is complete.  What overlaps is the
+// launch and the set-up of a block.
+#ifdef __CUDACC__
+__device__ __forceinline__ void pdl_trigger() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+template <typename Args>
+cudaError_t launch_pdl(void (*kernel)(Args), dim3 grid, unsigned threads, size_t smem, cudaStream_t st, const Args& args) {
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t c{};
+    c.gridDim = grid;
+    c.blockDim = dim3(threads);
+    c.dynamicSmemBytes = smem;
+    c.stream = st;
+    c.attrs = at;
+    c.numAttrs = 1;
+    return cudaLaunchKernelEx(&c, kernel, args);
+}
+#endif
+
 // Attention of query rows over the paged cache behind a window with sinks: the
 // query at position p sees the cached positions j <= p with j > p - window or
 // j < sinks.

@@ -9,19 +9,20 @@
 // MMAs (m16n8k16) have it to spare, and their fragments can be loaded from global
 // memory directly, so there is no shared-memory staging and no barrier in the loop.
 //
-// A tile is 16 consecutive positions (a quarter of a page), one warp's step:
-//   S [R x 16] = Q K^T   A = Q rows, B = keys; the contraction index d is permuted so
-//                        that a lane's B registers are 16 contiguous bytes of its key:
-//                        lane 4 n + c holds, of key n, the elements 32 i + 8 c .. + 7
-//   O [R x d] += P V     A = P straight from the accumulator layout of S; a lane
-//                        loads 16 contiguous bytes of four value rows and pairs
-//                        adjacent rows with byte permutes (columns of O permuted
-//                        likewise: lane 4 n + c, register m: element 64 i + 8 n + m)
+// A tile is 16 consecutive positions (a quarter of a page), one warp's step.  The heads
+// are the MMA's eight columns, the cache its sixteen rows:
+//   S^T [16 x 8] = K Q^T     a lane's A registers are 16 contiguous bytes of two keys:
+//                            lane 4 n + c holds, of keys n and n + 8, the elements
+//                            32 i + 8 c .. + 7 (the contraction index d is permuted)
+//   O^T [d x 8] += V^T P^T   a lane loads 16 contiguous bytes of four value rows and pairs
+//                            adjacent rows with byte permutes (rows of O^T permuted
+//                            likewise); P^T is S^T's accumulator, transposed 8 x 8
+// With the heads as rows instead, half of every MMA and of O's registers were empty.
 //
-// Precision.  The MMA's 16 rows hold 8 heads twice.  An fp32 query is the exact sum
-// of three bf16 planes: the first two go to rows 0-7 and 8-15 of one MMA, the third
-// to rows 0-7 of another; the row pairs are added in fp32.  Weights likewise (two
-// planes, 2^-17, for bf16 activations: the second plane's rows are there anyway).
+// Precision.  An fp32 query is the exact sum of three bf16 planes, and so are the
+// weights of fp32 activations: three MMAs per product, a tile's product added to O in
+// fp32 (the MMA's own sums truncate: 4e-6 over 150 tiles).  bf16 activations: one MMA for
+// the scores, two planes of the weights (2^-17; the second costs 1%).
 //
 // Masked positions are neither loaded nor multiplied: their key and value registers
 // are zero, whatever the cache holds there.
@@ -41,6 +42,7 @@ namespace {
 constexpr int kTile = 16;   // positions per warp step
 constexpr int kWarps = 4;
 constexpr int kThreads = kWarps * 32;
+constexpr int kResident = 3;  // blocks per SM that the registers are held to
 constexpr int kMaxCounters = 16384;  // completion counters, at the start of the scratch
 
 __device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
@@ -60,6 +62,13 @@ __device__ __forceinline__ uint32_t peel(float& lo, float& hi) {
     lo -= __uint_as_float(p << 16);
     hi -= __uint_as_float(p & 0xffff0000u);
     return p;
+}
+// 8 x 8 transpose over the warp: lane 4 n + c gives elements (n, 2 c), (n, 2 c + 1) and
+// gets (2 c, n), (2 c + 1, n).
+__device__ __forceinline__ uint32_t transpose(uint32_t x) {
+    uint32_t y;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
 }
 __device__ __forceinline__ uint4 load_row(const char* p, bool live) {
     uint4 v = make_uint4(0u, 0u, 0u, 0u);
@@ -86,14 +95,18 @@ struct DecodeArgs {
 };
 
 template <int D, typename T>
-__global__ void __launch_bounds__(kThreads, 2) window_decode_kernel(const __grid_constant__ DecodeArgs p) {
+__global__ void __launch_bounds__(kThreads, kResident) window_decode_kernel(const __grid_constant__ DecodeArgs p) {
     constexpr bool F32 = sizeof(T) == 4;
     constexpr int NQ = D / 32;  // 16-byte pieces of a key per lane
     constexpr int NV = D / 64;  // 16-byte pieces of a value row per lane
+    constexpr int PV = F32 ? 3 : 2;  // planes of the weights
     __shared__ __align__(16) float sm_o[kWarps][8][D];
     __shared__ float sm_m[kWarps][8], sm_l[kWarps][8];
     __shared__ bool sm_last;
+    __shared__ uint4 sm_q[NQ][F32 ? 3 : 1][32];
     const WindowArgs& a = p.a;
+    pdl_trigger();
+    pdl_wait();
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, n4 = lane / 4, c4 = lane % 4;
     const int b = blockIdx.x / p.plan.splits, split = blockIdx.x % p.plan.splits;
     const int kvh = blockIdx.y / p.plan.groups, G = a.Hq / a.Hkv;
@@ -110,30 +123,29 @@ __global__ void __launch_bounds__(kThreads, 2) window_decode_kernel(const __grid
     if (split >= active) return;
     const int last = min(tiles, (split + 1) * p.plan.chunk);
 
-    // queries: bf16 planes in the A layout, rows past the group's heads zero
-    uint32_t qa[NQ][2][2], qb[F32 ? NQ : 1][2][2], qc[F32 ? NQ : 1][2][2];
+    // queries: bf16 planes in the B layout (a lane: head n4, elements 32 x + 8 c4 ..), columns past
+    // the group's heads zero; the same for every warp, in shared memory
     {
         const T* q = static_cast<const T*>(a.q) + ((int64_t)b * a.Hq + kvh * G + head0 + n4) * D + 8 * c4;
-#pragma unroll
-        for (int i = 0; i < NQ; ++i) {
+        for (int x = warp; x < NQ; x += kWarps) {
             if constexpr (F32) {
                 float v[8];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[e] = 0.f;
                 if (n4 < heads) {
-                    const float4 x = *reinterpret_cast<const float4*>(q + 32 * i);
-                    const float4 y = *reinterpret_cast<const float4*>(q + 32 * i + 4);
-                    v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w; v[4] = y.x; v[5] = y.y; v[6] = y.z; v[7] = y.w;
+                    const float4 y = *reinterpret_cast<const float4*>(q + 32 * x);
+                    const float4 z = *reinterpret_cast<const float4*>(q + 32 * x + 4);
+                    v[0] = y.x; v[1] = y.y; v[2] = y.z; v[3] = y.w; v[4] = z.x; v[5] = z.y; v[6] = z.z; v[7] = z.w;
                 }
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    qa[i][e / 2][e % 2] = peel(v[2 * e], v[2 * e + 1]);
-                    qb[i][e / 2][e % 2] = peel(v[2 * e], v[2 * e + 1]);
-                    qc[i][e / 2][e % 2] = pack(v[2 * e], v[2 * e + 1]);
+                for (int pl = 0; pl < 3; ++pl) {
+                    uint32_t u[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) u[e] = peel(v[2 * e], v[2 * e + 1]);
+                    sm_q[x][pl][lane] = make_uint4(u[0], u[1], u[2], u[3]);
                 }
             } else {
-                const uint4 x = n4 < heads ? *reinterpret_cast<const uint4*>(q + 32 * i) : make_uint4(0u, 0u, 0u, 0u);
-                qa[i][0][0] = x.x; qa[i][0][1] = x.y; qa[i][1][0] = x.z; qa[i][1][1] = x.w;
+                sm_q[x][0][lane] = n4 < heads ? *reinterpret_cast<const uint4*>(q + 32 * x) : make_uint4(0u, 0u, 0u, 0u);
             }
         }
     }
@@ -149,19 +161,19 @@ __global__ void __launch_bounds__(kThreads, 2) window_decode_kernel(const __grid
     };
     const uint32_t v_off = (uint32_t)(a.Hkv * kPageTokens) * D * 2;
 
-    float o[8 * NV][4];
+    float o[4 * NV][4];  // rows 64 x + 8 n4 + 2 e (+ 1) of O^T, heads 2 c4 and 2 c4 + 1
 #pragma unroll
-    for (int i = 0; i < 8 * NV; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
-    float m = -INFINITY, l = 0.f;
+    for (int i = 0; i < 4 * NV; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
+    float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};  // of heads 2 c4 and 2 c4 + 1
     const float scale = 1.44269504088896f / sqrtf((float)D);  // scores in units of log 2
 
     uint4 k[2][NQ], v[4][NV];
-    auto load_k = [&](int t, const char* at) {
+    auto load_k = [&](int t, const char* at) {  // keys n4 and n4 + 8
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
             const bool live = seen(t * kTile + 8 * j + n4);
 #pragma unroll
-            for (int i = 0; i < NQ; ++i) k[j][i] = load_row(at + ((8 * j + n4) * D + 32 * i + 8 * c4) * 2, live);
+            for (int x = 0; x < NQ; ++x) k[j][x] = load_row(at + ((8 * j + n4) * D + 32 * x + 8 * c4) * 2, live);
         }
     };
     int i = split * p.plan.chunk + warp;
@@ -170,6 +182,7 @@ __global__ void __launch_bounds__(kThreads, 2) window_decode_kernel(const __grid
         at = key_at(tile_at(i));
         load_k(tile_at(i), at);
     }
+    __syncthreads();  // the queries
     for (; i < last; i += kWarps) {
         const int t = tile_at(i);
         const char* at_next = i + kWarps < last ? key_at(tile_at(i + kWarps)) : nullptr;
@@ -180,66 +193,67 @@ __global__ void __launch_bounds__(kThreads, 2) window_decode_kernel(const __grid
 #pragma unroll
             for (int x = 0; x < NV; ++x) v[r][x] = load_row(at + v_off + (row * D + 64 * x + 8 * n4) * 2, live);
         }
-        // ---- scores
-        float s[2][4];
+        // ---- scores, in independent sums (a chain of MMAs waits for each result)
+        float s[4];
+        {
+            constexpr int PL = F32 ? 3 : 1;
+            float z[PL][2][4];
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            s[j][0] = s[j][1] = s[j][2] = s[j][3] = 0.f;
-            if constexpr (F32) {  // the smallest plane first
+            for (int pl = 0; pl < PL; ++pl)
 #pragma unroll
-                for (int x = 0; x < NQ; ++x) {
-                    mma(s[j], qc[x][0][0], 0u, qc[x][0][1], 0u, k[j][x].x, k[j][x].y);
-                    mma(s[j], qc[x][1][0], 0u, qc[x][1][1], 0u, k[j][x].z, k[j][x].w);
+                for (int h = 0; h < 2; ++h) z[pl][h][0] = z[pl][h][1] = z[pl][h][2] = z[pl][h][3] = 0.f;
+#pragma unroll
+            for (int x = 0; x < NQ; ++x)
+#pragma unroll
+                for (int pl = 0; pl < PL; ++pl) {
+                    const uint4 q = sm_q[x][pl][lane];
+                    mma(z[pl][0], k[0][x].x, k[1][x].x, k[0][x].y, k[1][x].y, q.x, q.y);
+                    mma(z[pl][1], k[0][x].z, k[1][x].z, k[0][x].w, k[1][x].w, q.z, q.w);
                 }
-            }
 #pragma unroll
-            for (int x = 0; x < NQ; ++x) {
-                if constexpr (F32) {
-                    mma(s[j], qa[x][0][0], qb[x][0][0], qa[x][0][1], qb[x][0][1], k[j][x].x, k[j][x].y);
-                    mma(s[j], qa[x][1][0], qb[x][1][0], qa[x][1][1], qb[x][1][1], k[j][x].z, k[j][x].w);
-                } else {
-                    mma(s[j], qa[x][0][0], 0u, qa[x][0][1], 0u, k[j][x].x, k[j][x].y);
-                    mma(s[j], qa[x][1][0], 0u, qa[x][1][1], 0u, k[j][x].z, k[j][x].w);
-                }
+            for (int e = 0; e < 4; ++e) {
+                s[e] = z[0][0][e] + z[0][1][e];
+                if constexpr (F32) s[e] += (z[1][0][e] + z[1][1][e]) + (z[2][0][e] + z[2][1][e]);
             }
         }
         if (at_next) load_k(tile_at(i + kWarps), at_next);
-        // ---- softmax: this lane has head n4, positions 8 j + 2 c4 + {0, 1}
-        float w[2][2], mx = -INFINITY;
+        // ---- softmax: this lane has positions n4 (s[0], s[1]) and n4 + 8 (s[2], s[3]), heads 2 c4 + {0, 1}
+        const bool see0 = seen(t * kTile + n4), see1 = seen(t * kTile + 8 + n4);
+        float w[4], mx[2];
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
+        for (int h = 0; h < 2; ++h) {
+            w[h] = see0 ? s[h] * scale : -INFINITY;
+            w[2 + h] = see1 ? s[2 + h] * scale : -INFINITY;
+            mx[h] = fmaxf(w[h], w[2 + h]);
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                w[j][e] = seen(t * kTile + 8 * j + 2 * c4 + e) ? (s[j][e] + s[j][e + 2]) * scale : -INFINITY;
-                mx = fmaxf(mx, w[j][e]);
+            for (int x = 4; x < 32; x *= 2) mx[h] = fmaxf(mx[h], __shfl_xor_sync(0xffffffffu, mx[h], x));
+        }
+        if (__any_sync(0xffffffffu, mx[0] > m[0] || mx[1] > m[1])) {
+            float alpha[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const float m_new = fmaxf(m[h], mx[h]);
+                alpha[h] = m[h] == -INFINITY ? 0.f : exp2f(m[h] - m_new);
+                m[h] = m_new;
+                l[h] *= alpha[h];
             }
-        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
-        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
-        if (__any_sync(0xffffffffu, mx > m)) {
-            const float m_new = fmaxf(m, mx);
-            const float alpha = m == -INFINITY ? 0.f : exp2f(m - m_new);
-            m = m_new;
-            l *= alpha;
 #pragma unroll
-            for (int x = 0; x < 8 * NV; ++x) {
-                o[x][0] *= alpha; o[x][1] *= alpha; o[x][2] *= alpha; o[x][3] *= alpha;
+            for (int x = 0; x < 4 * NV; ++x) {
+                o[x][0] *= alpha[0]; o[x][1] *= alpha[1]; o[x][2] *= alpha[0]; o[x][3] *= alpha[1];
             }
         }
-        const float base = m == -INFINITY ? 0.f : m;  // nothing seen yet: every weight is zero
-        uint32_t p0[2], p1[2], p2[2];
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            w[j][0] = exp2f(w[j][0] - base);
-            w[j][1] = exp2f(w[j][1] - base);
-            l += w[j][0] + w[j][1];
-            p0[j] = peel(w[j][0], w[j][1]);
-            if constexpr (F32) {
-                p1[j] = peel(w[j][0], w[j][1]);
-                p2[j] = pack(w[j][0], w[j][1]);
-            } else {
-                p1[j] = pack(w[j][0], w[j][1]);
-            }
+        for (int h = 0; h < 2; ++h) {
+            const float base = m[h] == -INFINITY ? 0.f : m[h];  // nothing seen yet: every weight is zero
+            w[h] = exp2f(w[h] - base);
+            w[2 + h] = exp2f(w[2 + h] - base);
+            l[h] += w[h] + w[2 + h];
         }
+        uint32_t pb[PV][2];  // planes of P^T in the B layout
+#pragma unroll
+        for (int pl = 0; pl < PV; ++pl)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) pb[pl][j] = transpose(peel(w[2 * j], w[2 * j + 1]));
         // ---- values
 #pragma unroll
         for (int x = 0; x < NV; ++x) {
@@ -248,36 +262,39 @@ __global__ void __launch_bounds__(kThreads, 2) window_decode_kernel(const __grid
             const uint32_t r2[4] = {v[2][x].x, v[2][x].y, v[2][x].z, v[2][x].w};
             const uint32_t r3[4] = {v[3][x].x, v[3][x].y, v[3][x].z, v[3][x].w};
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const uint32_t sel = e & 1 ? 0x7632u : 0x5410u;
-                const uint32_t b0 = __byte_perm(r0[e / 2], r1[e / 2], sel), b1 = __byte_perm(r2[e / 2], r3[e / 2], sel);
-                if constexpr (F32) mma(o[8 * x + e], p2[0], 0u, p2[1], 0u, b0, b1);
-                mma(o[8 * x + e], p0[0], p1[0], p0[1], p1[1], b0, b1);
+            for (int e = 0; e < 4; ++e) {
+                const uint32_t a0 = __byte_perm(r0[e], r1[e], 0x5410u), a1 = __byte_perm(r0[e], r1[e], 0x7632u);
+                const uint32_t a2 = __byte_perm(r2[e], r3[e], 0x5410u), a3 = __byte_perm(r2[e], r3[e], 0x7632u);
+                // smallest plane first; the MMA's sums truncate, so that fp32 rows add a tile's product
+                // to O in fp32
+                float y[4];
+#pragma unroll
+                for (int h = 0; h < 4; ++h) y[h] = F32 ? 0.f : o[4 * x + e][h];
+#pragma unroll
+                for (int pl = PV - 1; pl >= 0; --pl) mma(y, a0, a1, a2, a3, pb[pl][0], pb[pl][1]);
+#pragma unroll
+                for (int h = 0; h < 4; ++h) o[4 * x + e][h] = F32 ? o[4 * x + e][h] + y[h] : y[h];
             }
         }
         at = at_next;
     }
 
-    // ---- join the warps: head n4, elements 64 x + 8 (2 c4 + e) + y
-    l += __shfl_xor_sync(0xffffffffu, l, 1);
-    l += __shfl_xor_sync(0xffffffffu, l, 2);
-    if (c4 == 0) {
-        sm_m[warp][n4] = m;
-        sm_l[warp][n4] = l;
+    // ---- join the warps: heads 2 c4 + h, elements 64 x + 8 n4 .. + 7
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+#pragma unroll
+        for (int x = 4; x < 32; x *= 2) l[h] += __shfl_xor_sync(0xffffffffu, l[h], x);
+        if (n4 == 0) {
+            sm_m[warp][2 * c4 + h] = m[h];
+            sm_l[warp][2 * c4 + h] = l[h];
+        }
+#pragma unroll
+        for (int x = 0; x < NV; ++x)
+#pragma unroll
+            for (int e = 0; e < 4; e += 2)
+                *reinterpret_cast<float4*>(&sm_o[warp][2 * c4 + h][64 * x + 8 * n4 + 2 * e]) = make_float4(
+                    o[4 * x + e][h], o[4 * x + e][2 + h], o[4 * x + e + 1][h], o[4 * x + e + 1][2 + h]);
     }
-#pragma unroll
-    for (int x = 0; x < NV; ++x)
-#pragma unroll
-        for (int e = 0; e < 2; ++e)
-#pragma unroll
-            for (int y = 0; y < 8; y += 4) {
-                float4 r;
-                r.x = o[8 * x + y][e] + o[8 * x + y][e + 2];
-                r.y = o[8 * x + y + 1][e] + o[8 * x + y + 1][e + 2];
-                r.z = o[8 * x + y + 2][e] + o[8 * x + y + 2][e + 2];
-                r.w = o[8 * x + y + 3][e] + o[8 * x + y + 3][e + 2];
-                *reinterpret_cast<float4*>(&sm_o[warp][n4][64 * x + 8 * (2 * c4 + e) + y]) = r;
-            }
     __syncthreads();
     const int64_t unit = (int64_t)b * gridDim.y + blockIdx.y;
     const int units = heads * (D / 4);  // four elements of a head each
@@ -323,25 +340,42 @@ __global__ void __launch_bounds__(kThreads, 2) window_decode_kernel(const __grid
         const int h = u / (D / 4);
         const int64_t first = unit * p.plan.splits * p.plan.heads + h;
         float mt = -INFINITY, lt = 0.f;
-#pragma unroll 8
-        for (int x = 0; x < active; ++x) mt = fmaxf(mt, __ldcg(p.ml + first + (int64_t)x * p.plan.heads).x);
         float4 r = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-        for (int x = 0; x < active; ++x) {
-            const int64_t at = first + (int64_t)x * p.plan.heads;
-            const float2 ml = __ldcg(p.ml + at);
-            const float4 y = __ldcg(reinterpret_cast<const float4*>(p.part + at * D) + u % (D / 4));
-            const float f = ml.x == -INFINITY ? 0.f : exp2f(ml.x - mt);
-            lt = fmaf(f, ml.y, lt);
-            r.x = fmaf(f, y.x, r.x); r.y = fmaf(f, y.y, r.y); r.z = fmaf(f, y.z, r.z); r.w = fmaf(f, y.w, r.w);
+        constexpr int BATCH = 8;  // parts whose loads are in flight together
+        for (int x0 = 0; x0 < active; x0 += BATCH) {
+            float2 ml[BATCH];
+            float4 y[BATCH];
+#pragma unroll
+            for (int x = 0; x < BATCH; ++x) {
+                const int64_t at = first + (int64_t)min(x0 + x, active - 1) * p.plan.heads;
+                ml[x] = __ldcg(p.ml + at);
+                y[x] = __ldcg(reinterpret_cast<const float4*>(p.part + at * D) + u % (D / 4));
+            }
+            float mb = mt;
+#pragma unroll
+            for (int x = 0; x < BATCH; ++x) mb = fmaxf(mb, ml[x].x);
+            const float keep = mt == -INFINITY ? 0.f : exp2f(mt - mb);
+            mt = mb;
+            lt *= keep;
+            r.x *= keep; r.y *= keep; r.z *= keep; r.w *= keep;
+#pragma unroll
+            for (int x = 0; x < BATCH; ++x) {
+                const float f = x0 + x < active && ml[x].x != -INFINITY ? exp2f(ml[x].x - mt) : 0.f;
+                lt = fmaf(f, ml[x].y, lt);
+                r.x = fmaf(f, y[x].x, r.x); r.y = fmaf(f, y[x].y, r.y);
+                r.z = fmaf(f, y[x].z, r.z); r.w = fmaf(f, y[x].w, r.w);
+            }
         }
         put(u, r, lt == 0.f ? 0.f : 1.0f / lt);
     }
 }
 
-// Blocks of `chunk` tiles.  Small problems take the smallest block (a tile per warp),
-// so that they spread over the card; large ones take blocks long enough to hide their
-// first loads and the join, short enough to leave no long tail.
+// Blocks of `chunk` tiles.  With no more (request, group) units than the card holds blocks
+// at a time, each unit is split so that all blocks run at once, down to a tile per warp:
+// whole waves, few joins (4 requests of up to 131072 tokens: 14 parts each, 239 us against
+// 257 us with blocks of 64 tiles; 8 requests of up to 1028: 16 us against 22 us with blocks
+// of 4).  More units run in several waves, where blocks of 64 tiles keep the last one short
+// (64 requests of 4160: 170 us, unsplit 203 us).
 Plan make_plan(int B, int Hq, int Hkv, int window, int sinks, int max_ctx) {
     Plan p{};
     const int G = Hq / Hkv;
@@ -350,10 +384,14 @@ Plan make_plan(int B, int Hq, int Hkv, int window, int sinks, int max_ctx) {
     const int64_t tiles = std::min<int64_t>(((int64_t)max_ctx + kTile - 1) / kTile,
                                             ((int64_t)window + kTile - 1) / kTile + 1 +
                                                 ((int64_t)sinks + kTile - 1) / kTile);
-    const int64_t units = (int64_t)B * Hkv * p.groups;
-    int64_t chunk = (units * tiles / (152 * 16) + kWarps - 1) / kWarps * kWarps;
-    chunk = std::min<int64_t>(std::max<int64_t>(chunk, kWarps), 64);
-    if (units > kMaxCounters) chunk = tiles;
+    const int64_t units = (int64_t)B * Hkv * p.groups, places = 152 * kResident;
+    int64_t chunk = 64;
+    if (units <= places) {
+        const int64_t splits = places / std::max<int64_t>(units, 1);
+        chunk = ((tiles + splits - 1) / splits + kWarps - 1) / kWarps * kWarps;
+    } else if (units > kMaxCounters) {
+        chunk = tiles;
+    }
     p.chunk = (int)std::max<int64_t>(chunk, 1);
     p.splits = (int)std::max<int64_t>((tiles + p.chunk - 1) / p.chunk, 1);
     return p;
@@ -361,9 +399,8 @@ Plan make_plan(int B, int Hq, int Hkv, int window, int sinks, int max_ctx) {
 
 template <int D, typename T>
 cudaError_t launch_t(const DecodeArgs& p, cudaStream_t st) {
-    window_decode_kernel<D, T>
-        <<<dim3((unsigned)p.a.rows * p.plan.splits, p.a.Hkv * p.plan.groups), kThreads, 0, st>>>(p);
-    return cudaGetLastError();
+    return launch_pdl(window_decode_kernel<D, T>,
+                      dim3((unsigned)p.a.rows * p.plan.splits, p.a.Hkv * p.plan.groups), kThreads, 0, st, p);
 }
 
 }  // namespace

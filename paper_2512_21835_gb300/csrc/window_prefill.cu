@@ -371,7 +371,9 @@ __global__ void __launch_bounds__(kThreads, 1) window_prefill_kernel(const __gri
     const int unit = QT == 1 ? blockIdx.x / p.splits : blockIdx.x;  // row tile and kv head (and group)
     const int kvh = unit % units / p.groups, head0 = unit % units % p.groups * p.heads;
     const int G = a.Hq / a.Hkv, heads = min(p.heads, G - head0);
+    pdl_trigger();
     if (warp == 0) {
+        pdl_wait();
         int left = unit / units;  // row tiles from the end
         int row0 = 0, tokens = 0, req = 0, pos0 = 0;
         for (int top = a.n_prompts - 1; top >= 0; top -= 32) {
@@ -440,6 +442,7 @@ __global__ void __launch_bounds__(kThreads, 1) window_prefill_kernel(const __gri
                      : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
+    pdl_wait();
     fence_before();
     __syncthreads();
     fence_after();
@@ -1082,8 +1085,7 @@ cudaError_t launch_t(const PrefillArgs& p, cudaStream_t st) {
     const int64_t tiles = p.a.rows / (QT * p.tok) + p.a.n_prompts;  // at least the sum over prompts
     const int64_t blocks = std::min<int64_t>(tiles, p.a.rows) * p.a.Hkv * p.groups * p.splits;
     if (blocks > 0x7fffffff) return cudaErrorInvalidValue;
-    window_prefill_kernel<D, NP, QT, T><<<(unsigned)blocks, kThreads, C::BYTES, st>>>(p);
-    return cudaGetLastError();
+    return launch_pdl(window_prefill_kernel<D, NP, QT, T>, dim3((unsigned)blocks), kThreads, C::BYTES, st, p);
 }
 
 template <int D>

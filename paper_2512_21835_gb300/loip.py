@@ -399,7 +399,7 @@ def _s(stream):
     the stream object that torch.cuda.current_stream() returns takes 3 us, this 0.2 us.)"""
     if stream is None:
         torch = _torch()
-        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
     return stream
 
 
@@ -537,29 +537,31 @@ F32_ROWS, BF16_ROWS = 0, 1  # `dtype` of the windowed operators' activations
 
 def _dtype(x, like=None):
     """LOIP_F32 / LOIP_BF16 of a tensor; `like`, if given, has to be of the same type."""
-    torch = _torch()
-    if like is not None and like.dtype != x.dtype:
-        raise LoipError(ERR_INVALID, f"input of {x.dtype} with an output of {like.dtype}")
-    if x.dtype == torch.float32:
+    torch, dtype = _torch(), x.dtype
+    if like is not None and like.dtype != dtype:
+        raise LoipError(ERR_INVALID, f"input of {dtype} with an output of {like.dtype}")
+    if dtype == torch.float32:
         return F32_ROWS
-    if x.dtype == torch.bfloat16:
+    if dtype == torch.bfloat16:
         return BF16_ROWS
-    raise LoipError(ERR_INVALID, f"activations are float32 or bfloat16, not {x.dtype}")
+    raise LoipError(ERR_INVALID, f"activations are float32 or bfloat16, not {dtype}")
 
 
 def loip_k_qk_append(qkv, g_q, g_k, Hq, Hkv, d, eps, theta, positions, row_req, q_out, kv_base, page_offsets,
                      max_pages, page_tokens, layer, layer_page_bytes, stream=None):
     """Norm of queries and keys (g_q, g_k or None), rotation (theta 0: none), append.  qkv [T, (Hq + 2 Hkv) * d]
     float32 or bfloat16 with any row stride; page_offsets [requests, max_pages]."""
-    if qkv.stride(-1) != 1 or not q_out.is_contiguous():
+    (T, width), (row_stride, step) = qkv.shape, qkv.stride()
+    if step != 1 or not q_out.is_contiguous():
         raise LoipError(ERR_INVALID, "rows of qkv have to be contiguous, and q_out as a whole")
-    T = qkv.shape[0]
-    if positions.numel() < T or q_out.numel() != T * Hq * d or qkv.shape[1] != (Hq + 2 * Hkv) * d:
+    if positions.numel() < T or q_out.numel() != T * Hq * d or width != (Hq + 2 * Hkv) * d:
         raise LoipError(ERR_INVALID, "qkv, positions and q_out do not fit together")
-    _check(lib().loip_k_qk_append(qkv.data_ptr(), _dtype(qkv, q_out), qkv.stride(0), T, Hq, Hkv, d, _ptr(g_q),
-                                  _ptr(g_k), eps, theta, positions.data_ptr(), _ptr(row_req), page_offsets.shape[0],
-                                  q_out.data_ptr(), _ptr(kv_base), page_offsets.data_ptr(), max_pages, page_tokens,
-                                  layer, layer_page_bytes, _s(stream)))
+    rc = lib().loip_k_qk_append(qkv.data_ptr(), _dtype(qkv, q_out), row_stride, T, Hq, Hkv, d, _ptr(g_q), _ptr(g_k), eps,
+                                theta, positions.data_ptr(), _ptr(row_req), page_offsets.shape[0], q_out.data_ptr(),
+                                kv_base.data_ptr(), page_offsets.data_ptr(), max_pages, page_tokens, layer,
+                                layer_page_bytes, _s(stream))
+    if rc:
+        _check(rc)
 
 
 def loip_k_window_attention_scratch_bytes(B, Hq, Hkv, d, window, sinks, max_ctx) -> int:
@@ -573,9 +575,12 @@ def loip_k_window_attention(q, kv_base, page_offsets, max_pages, ctx_lens, Hq, H
     B = q.shape[0]
     if not (q.is_contiguous() and o.is_contiguous()) or q.numel() != B * Hq * d or o.numel() != q.numel():
         raise LoipError(ERR_INVALID, "q and o are contiguous [B, Hq * d]")
-    _check(lib().loip_k_window_attention(_ptr(q), _dtype(q, o), _ptr(kv_base), _ptr(page_offsets), max_pages,
-                                         _ptr(ctx_lens), B, Hq, Hkv, d, page_tokens, layer, layer_page_bytes, window,
-                                         sinks, max_ctx, _ptr(scratch), scratch.nbytes, _ptr(o), _s(stream)))
+    rc = lib().loip_k_window_attention(q.data_ptr(), _dtype(q, o), kv_base.data_ptr(), page_offsets.data_ptr(),
+                                       max_pages, ctx_lens.data_ptr(), B, Hq, Hkv, d, page_tokens, layer,
+                                       layer_page_bytes, window, sinks, max_ctx, scratch.data_ptr(), scratch.nbytes,
+                                       o.data_ptr(), _s(stream))
+    if rc:
+        _check(rc)
 
 
 def loip_k_window_prefill_scratch_bytes(M, n_prompts, Hq, Hkv, d, window, sinks, max_ctx) -> int:
@@ -589,7 +594,9 @@ def loip_k_window_prefill(q, kv_base, page_offsets, max_pages, row_starts, first
     M = q.shape[0]
     if not (q.is_contiguous() and o.is_contiguous()) or q.numel() != M * Hq * d or o.numel() != q.numel():
         raise LoipError(ERR_INVALID, "q and o are contiguous [M, Hq * d]")
-    _check(lib().loip_k_window_prefill(_ptr(q), _dtype(q, o), _ptr(kv_base), _ptr(page_offsets), max_pages,
-                                       _ptr(row_starts), _ptr(first_pos), row_starts.numel() - 1, M, Hq, Hkv, d,
-                                       page_tokens, layer, layer_page_bytes, window, sinks, max_ctx, _ptr(scratch),
-                                       scratch.nbytes, _ptr(o), _s(stream)))
+    rc = lib().loip_k_window_prefill(q.data_ptr(), _dtype(q, o), kv_base.data_ptr(), page_offsets.data_ptr(), max_pages,
+                                     row_starts.data_ptr(), _ptr(first_pos), row_starts.numel() - 1, M, Hq, Hkv, d,
+                                     page_tokens, layer, layer_page_bytes, window, sinks, max_ctx, scratch.data_ptr(),
+                                     scratch.nbytes, o.data_ptr(), _s(stream))
+    if rc:
+        _check(rc)
