@@ -65,7 +65,7 @@ struct Raw8 {
     uint4 u[sizeof(T) / 2];
     __device__ __forceinline__ void load(const T* p) {
 #pragma unroll
-        for (int i = 0; i < (int)sizeof(T) / 2; ++i) u[i] = __ldg(reinterpret_cast<const uint4*>(p) + i);
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) u[i] = reinterpret_cast<const uint4*>(p)[i];
     }
     __device__ __forceinline__ void values(float (&v)[8]) const {
         if constexpr (sizeof(T) == 4) {

@@ -12,8 +12,10 @@ constexpr int kPageTokens = 64;
 
 // Programmatic dependent launch: a kernel of this family lets its successor in the stream
 // be launched as soon as all its own blocks are, and reads or writes global memory only
-// after pdl_wait, which returns when the predecessor is complete.  What overlaps is the
-// launch and the set-up of a block.
+// after pdl_wait, which returns when the predecessor is complete and its writes are
+// visible.  What overlaps is the launch and the set-up of a block.  The read-only path
+// (ld.global.nc, __ldg) is not used for anything that a predecessor may write: the kernel
+// may have been resident while that was written.
 #ifdef __CUDACC__
 __device__ __forceinline__ void pdl_trigger() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }

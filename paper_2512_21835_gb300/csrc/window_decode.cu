@@ -70,10 +70,11 @@ __device__ __forceinline__ uint32_t transpose(uint32_t x) {
     asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
     return y;
 }
+// (Not the read-only path: the kernel before this one may have written the row, see pdl_wait.)
 __device__ __forceinline__ uint4 load_row(const char* p, bool live) {
     uint4 v = make_uint4(0u, 0u, 0u, 0u);
     if (live)
-        asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
+        asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
                      : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
                      : "l"(p));
     return v;
@@ -156,7 +157,7 @@ __global__ void __launch_bounds__(kThreads, kResident) window_decode_kernel(cons
     auto seen = [&](int j) { return j < ctx && (j >= win0 || j < a.sinks); };
     // the tile's first key of this kv head
     auto key_at = [&](int t) {
-        return layer + __ldg(table + t / (kPageTokens / kTile)) +
+        return layer + table[t / (kPageTokens / kTile)] +
                (uint32_t)((kvh * kPageTokens + (t % (kPageTokens / kTile)) * kTile) * D * 2);
     };
     const uint32_t v_off = (uint32_t)(a.Hkv * kPageTokens) * D * 2;

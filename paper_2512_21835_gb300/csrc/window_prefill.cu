@@ -19,7 +19,9 @@
 //   QT = 1: one row tile, even and odd key tiles; the two partial softmax states are
 //           joined at the end.  For fewer row tiles than the card has places; with
 //           fewer still, a row tile's pages are split over several blocks, which
-//           leave their states in scratch for the last one to join.
+//           leave their states in scratch for a second kernel to join.  (Joined by the
+//           last block to arrive, 16 row tiles in 9 parts each took 22 us: that block
+//           reads 590 KB alone.)
 // S and P have columns of their own (P twice for bf16 rows), so the next tile's S is
 // computed while this one's weights are, and neither waits for P V.  (With P over S, in
 // tiles of 128 keys, the chain softmax - P V - S took 4000 cycles per 128 keys and two
@@ -68,7 +70,6 @@ constexpr int kThreads = 384;
 constexpr int kLoaders = 64;                     // threads of warps 8 and 9
 constexpr int kSms = 152;
 constexpr int kSoftRegs = 208, kOtherRegs = 88;  // 256 x 208 + 128 x 88 = 384 x 168
-constexpr int kMaxUnits = 256;                   // counters and flags at the start of the scratch
 constexpr int KT = kPageTokens;                  // keys per tile
 
 template <int D, int NP, int QT>
@@ -102,7 +103,7 @@ struct Ctl {  // control words behind the ring
     uint64_t p_full[4], pv_done[4];    // per stream and P buffer: for even and odd tiles, no wait is ever two phases behind
     uint64_t o_free, q_full, end;
     uint32_t tmem;
-    int abort, bad, last;
+    int abort, bad;
     int row0, tokens, req, pos0;
 };
 static_assert(sizeof(Ctl) <= 512, "");
@@ -113,9 +114,11 @@ struct PrefillArgs {
     int tok;            // positions per row tile
     int splits;         // blocks per row tile (QT = 1)
     float scale;        // log2(e) / sqrt(d)
-    unsigned *arrived, *flagged;  // [kMaxUnits]: blocks done, whether one met values that are not finite
-    float4* part;       // [row tile and unit][split][d / 4][128 rows], not normalised
-    float2* ml;         // [row tile and unit][split][128 rows]: maximum (log2), sum
+    // in scratch, with splits; a unit is a row tile and kv head (and group)
+    float4* part;       // [unit][split][d / 4][128 rows], not normalised
+    int4* rows;         // [unit]: first row, tokens, request, position of the first
+    float2* ml;         // [unit][split][128 rows]: maximum (log2), sum
+    unsigned* flagged;  // [unit][split]: whether the block met values that are not finite
 };
 
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -519,7 +522,7 @@ __global__ void __launch_bounds__(kThreads, 1) window_prefill_kernel(const __gri
             constexpr int STEP = RPP * D * 2;  // bytes from a pass to the next in the page
             auto load = [&](int t, bool is_v, uint32_t dst) {
                 const int pg = page_at(t), b = pg * KT;
-                const char* src = layer + __ldg(table + pg) + ((int64_t)(is_v ? a.Hkv : 0) + kvh) * (KT * D * 2) +
+                const char* src = layer + table[pg] + ((int64_t)(is_v ? a.Hkv : 0) + kvh) * (KT * D * 2) +
                                   (r0 * D + chunk * 8) * 2;
                 if (b + KT <= pages.last && ((b >= win0 && a.window > 0) || b + KT <= a.sinks)) {  // the whole page
 #pragma unroll
@@ -642,8 +645,8 @@ __global__ void __launch_bounds__(kThreads, 1) window_prefill_kernel(const __gri
                 if constexpr (NP > 1) y[k] = x[k];
                 if (tk < p.tok && tok < tokens) {
                     const uint4* src = reinterpret_cast<const uint4*>(qg + row_at(tok, r - tk * heads) + i % CPR * 8);
-                    x[k] = __ldg(src);
-                    if constexpr (NP > 1) y[k] = __ldg(src + 1);
+                    x[k] = src[0];
+                    if constexpr (NP > 1) y[k] = src[1];
                 }
             }
 #pragma unroll
@@ -978,73 +981,95 @@ __global__ void __launch_bounds__(kThreads, 1) window_prefill_kernel(const __gri
     }
     __syncwarp();
     fence_before();
-    if (QT == 1 && p.splits > 1) __threadfence();
     __syncthreads();
     if (warp == 10) {
         fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
     }
-    if (tokens == 0 || warp >= 8) return;
-    bool bad = false;
+    const bool bad = c->bad && !c->abort;
     if (QT == 1 && p.splits > 1) {
-        // ---- the last block of the row tile to arrive joins the parts, in their order; the
-        // counter wraps to zero with that arrival, the flag is taken back by it
         if (tid == 0) {
-            if (c->bad && !c->abort) atomicOr(p.flagged + unit, 1u);
-            __threadfence();
-            c->last = atomicInc(p.arrived + unit, (unsigned)p.splits - 1u) == (unsigned)p.splits - 1u;
-            __threadfence();
-            if (c->last) c->bad = (int)atomicExch(p.flagged + unit, 0u);
+            p.flagged[unit * p.splits + split] = bad;
+            if (split == 0) p.rows[unit] = make_int4(row0, tokens, req, pos0);
         }
-        asm volatile("bar.sync 1, 256;" ::: "memory");
-        if (!c->last) return;
-        bad = c->bad;
-        const int r = tid % 128, tk = r / heads;
-        if (tk < min(p.tok, tokens)) {
-            const int64_t part = (int64_t)unit * p.splits * 128 + r;
-            float mt = -INFINITY, lt = 0.f;
-            for (int x = 0; x < p.splits; ++x) mt = fmaxf(mt, __ldcg(p.ml + part + x * 128).x);
-            for (int x = 0; x < p.splits; ++x) {
-                const float2 ml = __ldcg(p.ml + part + x * 128);
-                lt += ml.x == -INFINITY ? 0.f : ml.y * ex2(ml.x - mt);
-            }
-            const float inv = lt == 0.f ? 0.f : 1.0f / lt;
-            T* out = static_cast<T*>(a.o) +
-                     ((int64_t)(row0 + tk) * a.Hq + kvh * G + head0 + r - tk * heads) * D;
-            for (int i = tid / 128 * (D / 8); i < (tid / 128 + 1) * (D / 8); i += 2) {  // half of the row per thread
-                float4 y[2] = {make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)};
-#pragma unroll 4
-                for (int x = 0; x < p.splits; ++x) {
-                    const float mx = __ldcg(p.ml + part + x * 128).x;
-                    const float f = mx == -INFINITY ? 0.f : ex2(mx - mt);
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        const float4 v = __ldcg(p.part + ((int64_t)unit * p.splits + x) * 128 * (D / 4) + (i + e) * 128 + r);
-                        y[e].x = fmaf(f, v.x, y[e].x); y[e].y = fmaf(f, v.y, y[e].y);
-                        y[e].z = fmaf(f, v.z, y[e].z); y[e].w = fmaf(f, v.w, y[e].w);
-                    }
-                }
-                if constexpr (NP == 1) {
-                    *reinterpret_cast<uint4*>(out + 4 * i) =
-                        make_uint4(pack(y[0].x * inv, y[0].y * inv), pack(y[0].z * inv, y[0].w * inv),
-                                   pack(y[1].x * inv, y[1].y * inv), pack(y[1].z * inv, y[1].w * inv));
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 2; ++e)
-                        *reinterpret_cast<float4*>(out + 4 * (i + e)) =
-                            make_float4(y[e].x * inv, y[e].y * inv, y[e].z * inv, y[e].w * inv);
-                }
-            }
-        }
-        asm volatile("bar.sync 1, 256;" ::: "memory");
-    } else {
-        bad = c->bad && !c->abort;
-    }
-    if (bad) {
+    } else if (bad && warp < 8) {
         for (int i = warp; i < tokens * heads; i += 8) {
             const int64_t at = ((int64_t)(row0 + i / heads) * a.Hq + kvh * G + head0 + i % heads) * D;
             walk_row<D, T>(a, req, kvh, pos0 + i / heads, static_cast<const T*>(a.q) + at, static_cast<T*>(a.o) + at);
         }
+    }
+}
+
+// The parts of a row tile, in their order: a block per unit and 16 columns, a thread per row
+// and 8 columns.
+template <int D, typename T>
+__global__ void __launch_bounds__(256) window_join_kernel(const __grid_constant__ PrefillArgs p) {
+    const WindowArgs& a = p.a;
+    pdl_trigger();
+    pdl_wait();
+    constexpr int PIECES = D / 16;
+    const int unit = blockIdx.x / PIECES, c4 = blockIdx.x % PIECES * 4 + threadIdx.x / 128 * 2, r = threadIdx.x % 128;
+    const int units = a.Hkv * p.groups;
+    const int kvh = unit % units / p.groups, head0 = unit % units % p.groups * p.heads;
+    const int G = a.Hq / a.Hkv, heads = min(p.heads, G - head0);
+    const int4 rows = __ldcg(p.rows + unit);  // first row, tokens, request, position
+    const int tk = r / heads;
+    bool bad = false;
+    for (int x = 0; x < p.splits; ++x) bad |= __ldcg(p.flagged + unit * p.splits + x) != 0;
+    if (bad) {  // as without splits; the unit's blocks share the rows
+        const int warp = threadIdx.x / 32 + blockIdx.x % PIECES * 8;
+        for (int i = warp; i < rows.y * heads; i += 8 * PIECES) {
+            const int64_t at = ((int64_t)(rows.x + i / heads) * a.Hq + kvh * G + head0 + i % heads) * D;
+            walk_row<D, T>(a, rows.z, kvh, rows.w + i / heads, static_cast<const T*>(a.q) + at,
+                           static_cast<T*>(a.o) + at);
+        }
+        return;
+    }
+    if (tk >= min(p.tok, rows.y)) return;
+    const int64_t first = (int64_t)unit * p.splits;
+    float m = -INFINITY, l = 0.f;
+    float4 y[2] = {make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)};
+    constexpr int BATCH = 8;  // parts whose loads are in flight together
+    for (int x0 = 0; x0 < p.splits; x0 += BATCH) {
+        float2 ml[BATCH];
+        float4 v[BATCH][2];
+#pragma unroll
+        for (int x = 0; x < BATCH; ++x) {
+            const int64_t at = first + min(x0 + x, p.splits - 1);
+            ml[x] = __ldcg(p.ml + at * 128 + r);
+            v[x][0] = __ldcg(p.part + (at * (D / 4) + c4) * 128 + r);
+            v[x][1] = __ldcg(p.part + (at * (D / 4) + c4 + 1) * 128 + r);
+        }
+        float top = m;
+#pragma unroll
+        for (int x = 0; x < BATCH; ++x) top = fmaxf(top, ml[x].x);
+        const float keep = m == -INFINITY ? 0.f : ex2(m - top);
+        m = top;
+        l *= keep;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            y[e].x *= keep; y[e].y *= keep; y[e].z *= keep; y[e].w *= keep;
+        }
+#pragma unroll
+        for (int x = 0; x < BATCH; ++x) {
+            const float f = x0 + x < p.splits && ml[x].x != -INFINITY ? ex2(ml[x].x - m) : 0.f;
+            l = fmaf(f, ml[x].y, l);
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                y[e].x = fmaf(f, v[x][e].x, y[e].x); y[e].y = fmaf(f, v[x][e].y, y[e].y);
+                y[e].z = fmaf(f, v[x][e].z, y[e].z); y[e].w = fmaf(f, v[x][e].w, y[e].w);
+            }
+        }
+    }
+    const float inv = l == 0.f ? 0.f : 1.0f / l;
+    T* out = static_cast<T*>(a.o) + ((int64_t)(rows.x + tk) * a.Hq + kvh * G + head0 + r - tk * heads) * D + 4 * c4;
+    if constexpr (sizeof(T) == 2) {
+        *reinterpret_cast<uint4*>(out) = make_uint4(pack(y[0].x * inv, y[0].y * inv), pack(y[0].z * inv, y[0].w * inv),
+                                                    pack(y[1].x * inv, y[1].y * inv), pack(y[1].z * inv, y[1].w * inv));
+    } else {
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+            reinterpret_cast<float4*>(out)[e] = make_float4(y[e].x * inv, y[e].y * inv, y[e].z * inv, y[e].w * inv);
     }
 }
 
@@ -1085,7 +1110,9 @@ cudaError_t launch_t(const PrefillArgs& p, cudaStream_t st) {
     const int64_t tiles = p.a.rows / (QT * p.tok) + p.a.n_prompts;  // at least the sum over prompts
     const int64_t blocks = std::min<int64_t>(tiles, p.a.rows) * p.a.Hkv * p.groups * p.splits;
     if (blocks > 0x7fffffff) return cudaErrorInvalidValue;
-    return launch_pdl(window_prefill_kernel<D, NP, QT, T>, dim3((unsigned)blocks), kThreads, C::BYTES, st, p);
+    e = launch_pdl(window_prefill_kernel<D, NP, QT, T>, dim3((unsigned)blocks), kThreads, C::BYTES, st, p);
+    if (e != cudaSuccess || p.splits == 1) return e;
+    return launch_pdl(window_join_kernel<D, T>, dim3((unsigned)(blocks / p.splits) * (D / 16)), 256, 0, st, p);
 }
 
 template <int D>
@@ -1098,12 +1125,11 @@ cudaError_t launch_d(const PrefillArgs& p, bool f32, int64_t tiles, cudaStream_t
 }  // namespace
 
 uint64_t window_prefill_scratch(int M, int n_prompts, int Hq, int Hkv, int d, int window, int sinks, int max_ctx) {
-    uint64_t n = 2 * kMaxUnits * sizeof(unsigned);
-    if (M > 0) {
-        const Plan p = make_plan(M, n_prompts, Hq, Hkv, window, sinks, max_ctx);
-        if (p.splits > 1) n += (uint64_t)p.tiles * p.splits * 128 * (d + 2) * sizeof(float);
-    }
-    return n;
+    if (M == 0) return 16;
+    const Plan p = make_plan(M, n_prompts, Hq, Hkv, window, sinks, max_ctx);
+    if (p.splits == 1) return 16;
+    const uint64_t n = p.tiles * (16 + (uint64_t)p.splits * (128 * (d + 2) * sizeof(float) + sizeof(unsigned)));
+    return (n + 15) / 16 * 16;
 }
 
 cudaError_t launch_window_prefill(const WindowArgs& a, bool f32, cudaStream_t st) {
@@ -1117,10 +1143,10 @@ cudaError_t launch_window_prefill(const WindowArgs& a, bool f32, cudaStream_t st
     p.tok = plan.tok;
     p.splits = plan.splits;
     p.scale = (float)(1.4426950408889634 / sqrt((double)a.d));
-    p.arrived = static_cast<unsigned*>(a.scratch);
-    p.flagged = p.arrived + kMaxUnits;
-    p.part = reinterpret_cast<float4*>(p.flagged + kMaxUnits);
-    p.ml = reinterpret_cast<float2*>(p.part + plan.tiles * plan.splits * 128 * (a.d / 4));
+    p.part = static_cast<float4*>(a.scratch);
+    p.rows = reinterpret_cast<int4*>(p.part + plan.tiles * plan.splits * 128 * (a.d / 4));
+    p.ml = reinterpret_cast<float2*>(p.rows + plan.tiles);
+    p.flagged = reinterpret_cast<unsigned*>(p.ml + plan.tiles * plan.splits * 128);
     return a.d == 128 ? launch_d<128>(p, f32, plan.tiles, st) : launch_d<64>(p, f32, plan.tiles, st);
 }
 
