@@ -10,6 +10,12 @@ namespace loip {
 
 constexpr int kPageTokens = 64;
 
+// A scratch starts with the completion counters of the single-token attention, zero between
+// calls.  Every operator leaves them alone or at zero and puts its partial states behind
+// them, so that one scratch serves calls of any shape and of both kinds.
+constexpr int kMaxCounters = 16384;
+constexpr uint64_t kCounterBytes = kMaxCounters * sizeof(unsigned);
+
 // Programmatic dependent launch: a kernel of this family lets its successor in the stream
 // be launched as soon as all its own blocks are, and reads or writes global memory only
 // after pdl_wait, which returns when the predecessor is complete and its writes are
@@ -51,8 +57,8 @@ struct WindowArgs {
     void* scratch;
 };
 
-// Attention of single tokens (window_decode.cu).  The scratch starts with completion
-// counters that a call leaves at zero; its size follows from the sizes alone.
+// Attention of single tokens (window_decode.cu).  The scratch's size follows from the sizes
+// alone.
 uint64_t window_decode_scratch(int B, int Hq, int Hkv, int d, int window, int sinks, int max_ctx);
 cudaError_t launch_window_decode(const WindowArgs& a, bool f32, cudaStream_t st);
 

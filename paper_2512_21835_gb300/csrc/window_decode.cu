@@ -43,7 +43,6 @@ constexpr int kTile = 16;   // positions per warp step
 constexpr int kWarps = 4;
 constexpr int kThreads = kWarps * 32;
 constexpr int kResident = 3;  // blocks per SM that the registers are held to
-constexpr int kMaxCounters = 16384;  // completion counters, at the start of the scratch
 
 __device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
                                     uint32_t b1) {
@@ -408,7 +407,7 @@ cudaError_t launch_t(const DecodeArgs& p, cudaStream_t st) {
 
 uint64_t window_decode_scratch(int B, int Hq, int Hkv, int d, int window, int sinks, int max_ctx) {
     const Plan p = make_plan(B, Hq, Hkv, window, sinks, max_ctx);
-    uint64_t n = kMaxCounters * sizeof(unsigned);
+    uint64_t n = kCounterBytes;
     if (p.splits > 1) n += (uint64_t)B * Hkv * p.groups * p.splits * p.heads * (d + 2) * sizeof(float);
     return (n + 15) / 16 * 16;
 }

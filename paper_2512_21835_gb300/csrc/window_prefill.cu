@@ -1128,7 +1128,7 @@ uint64_t window_prefill_scratch(int M, int n_prompts, int Hq, int Hkv, int d, in
     if (M == 0) return 16;
     const Plan p = make_plan(M, n_prompts, Hq, Hkv, window, sinks, max_ctx);
     if (p.splits == 1) return 16;
-    const uint64_t n = p.tiles * (16 + (uint64_t)p.splits * (128 * (d + 2) * sizeof(float) + sizeof(unsigned)));
+    const uint64_t n = kCounterBytes + p.tiles * (16 + (uint64_t)p.splits * (128 * (d + 2) * sizeof(float) + sizeof(unsigned)));
     return (n + 15) / 16 * 16;
 }
 
@@ -1143,7 +1143,7 @@ cudaError_t launch_window_prefill(const WindowArgs& a, bool f32, cudaStream_t st
     p.tok = plan.tok;
     p.splits = plan.splits;
     p.scale = (float)(1.4426950408889634 / sqrt((double)a.d));
-    p.part = static_cast<float4*>(a.scratch);
+    p.part = reinterpret_cast<float4*>(static_cast<char*>(a.scratch) + kCounterBytes);
     p.rows = reinterpret_cast<int4*>(p.part + plan.tiles * plan.splits * 128 * (a.d / 4));
     p.ml = reinterpret_cast<float2*>(p.rows + plan.tiles);
     p.flagged = reinterpret_cast<unsigned*>(p.ml + plan.tiles * plan.splits * 128);

@@ -416,6 +416,23 @@ def test_prefill_equals_decode(torch, L):
         assert np.all(np.abs(a[r] - b[r]).reshape(Hq, d) <= 2 * t32)
 
 
+def test_one_scratch_for_both_attentions(torch, L):
+    """Prompts whose row tiles are split leave the scratch usable for single tokens, and the reverse."""
+    ctx, Hq, Hkv, d = (900, 640), 8, 2, 64
+    c, _ = _decode_cache(ctx, 1024, Hkv, d, 1 << 30, 0, 181)
+    q = dev_f32(np.random.default_rng(8).standard_normal((2, Hq * d)))
+    runs = [(1, n - 1) for n in ctx]
+    need = max(L.loip_k_window_attention_scratch_bytes(2, Hq, Hkv, d, 1 << 30, 0, 1024),
+               L.loip_k_window_prefill_scratch_bytes(2, 2, Hq, Hkv, d, 1 << 30, 0, 1024))
+    scratch = torch.zeros(need, dtype=torch.uint8, device="cuda")
+    a0 = b0 = None
+    for _ in range(4):
+        a = _decode(torch, L, c, q, ctx, Hq, 1 << 30, 0, 1024, scratch=scratch).cpu().numpy()
+        b = _prefill(torch, L, c, q, runs, Hq, 1 << 30, 0, 1024, scratch=scratch).cpu().numpy()
+        a0, b0 = (a, b) if a0 is None else (a0, b0)
+        assert np.array_equal(a, a0) and np.array_equal(b, b0) and np.all(np.isfinite(a)) and np.all(np.isfinite(b))
+
+
 def test_prefill_same_scratch_and_graph(torch, L):
     runs, Hq, Hkv, d = [(20, 600), (7, 3)], 4, 2, 64
     c, _ = _prefill_cache(runs, 640, Hkv, d, 1 << 30, 0, 151)
