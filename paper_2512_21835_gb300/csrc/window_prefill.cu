@@ -82,7 +82,8 @@ struct Cfg {
     static constexpr int TILE = SLABS * KV_SLAB;       // one tile of keys or of values
     static constexpr int SLOT = 2 * TILE;              // the keys of one tile, the values of an earlier one
     static constexpr int ROOM = 227 * 1024 - 1024 - 512 - Q_BYTES;
-    static constexpr int SLOTS = ROOM / SLOT < 12 ? ROOM / SLOT : 12;
+    static constexpr int MOST = ROOM / SLOT < 12 ? ROOM / SLOT : 12;
+    static constexpr int SLOTS = QT == 2 ? MOST : MOST / 2 * 2;  // (a stream's own slots: every second one)
     static constexpr int AHEAD = 3 - QT;                 // slot i: keys of tile i, values of tile i - AHEAD
     static constexpr int CTL = Q_BYTES + SLOTS * SLOT;
     static constexpr int BYTES = CTL + 512 + 1024;     // + alignment of the window
@@ -572,51 +573,64 @@ __global__ void __launch_bounds__(kThreads, 1) window_prefill_kernel(const __gri
             auto mine = [&](int t) { return t >= 0 && t < n && (QT == 1 ? (t & 1) == w : takes(t)); };
             const uint64_t q_desc = sdesc(q_smem + (QT == 2 ? w * NP * C::Q_PLANE : 0), 16), k_desc = sdesc(ring, 16),
                            v_desc = sdesc(ring + C::TILE, C::KV_SLAB);
-            uint32_t slot = 0, phase = 0;     // a cursor in the ring, and the phase of its round
+            constexpr int STRIDE = QT == 2 ? 1 : 2;  // a slot's keys and values are of both streams, or of one
+            uint32_t slot = QT == 2 ? 0 : w, phase = 0;  // a cursor in the ring, and the phase of its round
             uint32_t free = 1;                // of S (before the first tile: complete)
             uint32_t done = 0;                // products P V
+            int used = -1;                    // slot to be released (QT = 2)
+            const int steps = n + C::AHEAD;
             wait(bar_q, 0, 2);
+            if (QT == 2 || w < steps) wait(bar_full + 8 * slot, phase, 3);
+            // From P of a tile to S of the next but one the stream waits for this warp, so with two row
+            // tiles the next slot is waited for before P, and the last one released after S (467 -> 454
+            // us for 8192 rows behind 4096).  With one row tile a stream has two slots, and there the
+            // release has to come first (4 x 512 fp32 rows: 109 us, 121 the other way).
 #pragma unroll 1
-            for (int i = 0; i < n + C::AHEAD; ++i) {
-                if (QT == 2 || (i & 1) == w) {  // (a slot's keys and values are of one stream, or of both)
-                    wait(bar_full + 8 * slot, phase, 3);
-                    fence_loaded();
-                    if (mine(i)) {  // S = Q K^T, once the softmax has read the last one
-                        wait(bar_s_free + 8 * w, free, 4);
-                        free ^= 1;
-                        fence_after();
-                        const uint64_t k = k_desc + slot * (C::SLOT / 16);
+            for (int i = QT == 2 ? 0 : w; i < steps; i += STRIDE) {
+                const uint32_t k_at = slot * (C::SLOT / 16);
+                fence_loaded();
+                if (mine(i)) {  // S = Q K^T, once the softmax has read the last one
+                    wait(bar_s_free + 8 * w, free, 4);
+                    free ^= 1;
+                    fence_after();
+                    const uint64_t k = k_desc + k_at;
 #pragma unroll
-                        for (int pl = NP - 1; pl >= 0; --pl)
+                    for (int pl = NP - 1; pl >= 0; --pl)
 #pragma unroll
-                            for (int x = 0; x < D / 64; ++x)
-                                mma_ss4(tmem + C::s_col(w), q_desc + (pl * C::Q_PLANE + x * C::Q_SLAB) / 16,
-                                        k + x * C::KV_SLAB / 16, idesc(KT, false), pl != NP - 1 || x != 0);
-                        commit(bar_s + 8 * w);
-                    }
-                    if (mine(i - C::AHEAD)) {  // O += P V
-                        const uint32_t buf = done & 1;
-                        wait(bar_p + 16 * w + 8 * buf, done / 2 & 1, 5);
-                        // O is one for both streams: the other one's last tile has been drained.  (This
-                        // stream's own last one has, as its P is here, so the phase is the right one.)
-                        if (NP > 1) wait(bar_o_free, (i - C::AHEAD + 1) & 1, 9);
-                        fence_after();
-                        const uint64_t v = v_desc + slot * (C::SLOT / 16);
-#pragma unroll
-                        for (int pl = NP - 1; pl >= 0; --pl)
-#pragma unroll
-                            for (int x = 0; x < 2; ++x)  // O is kept (bf16), or drained after every tile
-                                mma_ts2(tmem + C::o_col(w), tmem + C::p_col(w, buf, pl) + 16 * x,
-                                        v + x * (32 * 128 / 16), idesc(D, true),
-                                        pl != NP - 1 || x != 0 || (NP == 1 && done) ? 1u : 0u);
-                        commit(bar_pv + 16 * w + 8 * buf);
-                        ++done;
-                    }
-                    commit(bar_empty + 8 * slot);
+                        for (int x = 0; x < D / 64; ++x)
+                            mma_ss4(tmem + C::s_col(w), q_desc + (pl * C::Q_PLANE + x * C::Q_SLAB) / 16,
+                                    k + x * C::KV_SLAB / 16, idesc(KT, false), pl != NP - 1 || x != 0);
+                    commit(bar_s + 8 * w);
                 }
-                if (++slot == C::SLOTS) {
-                    slot = 0;
+                if (QT == 2 && used >= 0) commit(bar_empty + 8 * used);
+                used = slot;
+                slot += STRIDE;
+                if (slot >= C::SLOTS) {
+                    slot -= C::SLOTS;
                     phase ^= 1;
+                }
+                if (QT == 2 && i + STRIDE < steps) wait(bar_full + 8 * slot, phase, 3);
+                if (mine(i - C::AHEAD)) {  // O += P V
+                    const uint32_t buf = done & 1;
+                    wait(bar_p + 16 * w + 8 * buf, done / 2 & 1, 5);
+                    // O is one for both streams: the other one's last tile has been drained.  (This
+                    // stream's own last one has, as its P is here, so the phase is the right one.)
+                    if (NP > 1) wait(bar_o_free, (i - C::AHEAD + 1) & 1, 9);
+                    fence_after();
+                    const uint64_t v = v_desc + k_at;
+#pragma unroll
+                    for (int pl = NP - 1; pl >= 0; --pl)
+#pragma unroll
+                        for (int x = 0; x < 2; ++x)  // O is kept (bf16), or drained after every tile
+                            mma_ts2(tmem + C::o_col(w), tmem + C::p_col(w, buf, pl) + 16 * x,
+                                    v + x * (32 * 128 / 16), idesc(D, true),
+                                    pl != NP - 1 || x != 0 || (NP == 1 && done) ? 1u : 0u);
+                    commit(bar_pv + 16 * w + 8 * buf);
+                    ++done;
+                }
+                if (QT == 1) {
+                    commit(bar_empty + 8 * used);
+                    if (i + STRIDE < steps) wait(bar_full + 8 * slot, phase, 3);
                 }
             }
             // nothing may be in flight when the tensor memory is released
