@@ -106,7 +106,7 @@ __device__ __forceinline__ void store8(__nv_bfloat16* p, const float (&v)[8]) {
 template <int D, typename T>
 __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 8 : 6) qk_append_kernel(const __grid_constant__ AppendArgs p) {
     constexpr int LANES = D / 16;
-    __shared__ __align__(16) float2 turn[D / 2];  // cos, sin
+    __shared__ float4 turn[4][LANES];  // cos, sin of elements 8l + 2k and 8l + 2k + 1 at [k][l]: no bank conflicts
     pdl_trigger();
     pdl_wait();
     const int t = blockIdx.x, l = threadIdx.x % LANES, head = blockIdx.y * p.heads + threadIdx.x / LANES;
@@ -132,7 +132,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 8 : 6) qk_append_kernel(
         const int32_t turns = (int32_t)((uint64_t)pos * p.rope.turn[threadIdx.x] >> 32);
         float s, c;
         sincospif((float)turns * 0x1p-31f, &s, &c);
-        turn[threadIdx.x] = make_float2(c, s);
+        reinterpret_cast<float2*>(&turn[threadIdx.x % 8 / 2][threadIdx.x / 8])[threadIdx.x % 2] = make_float2(c, s);
     }
     __syncthreads();
     float a[8], b[8];
@@ -162,11 +162,13 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 8 : 6) qk_append_kernel(
     if (!live) return;
     if (!is_v) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float2 cs = turn[8 * l + i];
-            const float x = a[i], y = b[i];
+        for (int i = 0; i < 8; i += 2) {
+            const float4 cs = turn[i / 2][l];
+            const float x = a[i], y = b[i], z = a[i + 1], w = b[i + 1];
             a[i] = x * cs.x - y * cs.y;
             b[i] = y * cs.x + x * cs.y;
+            a[i + 1] = z * cs.z - w * cs.w;
+            b[i + 1] = w * cs.z + z * cs.w;
         }
     }
     if (is_q) {

@@ -370,12 +370,12 @@ __global__ void __launch_bounds__(kThreads, kResident) window_decode_kernel(cons
     }
 }
 
-// Blocks of `chunk` tiles.  With no more (request, group) units than the card holds blocks
-// at a time, each unit is split so that all blocks run at once, down to a tile per warp:
-// whole waves, few joins (4 requests of up to 131072 tokens: 14 parts each, 239 us against
-// 257 us with blocks of 64 tiles; 8 requests of up to 1028: 16 us against 22 us with blocks
-// of 4).  More units run in several waves, where blocks of 64 tiles keep the last one short
-// (64 requests of 4160: 170 us, unsplit 203 us).
+// Blocks of `chunk` tiles.  Where the (request, group) units, each split alike, fill four
+// fifths of the places that the card has for blocks, or more, all blocks run at once: whole
+// waves, few joins, down to a tile per warp (4 requests of up to 131072 tokens: 14 parts
+// each, 253 us against 257 us with blocks of 64 tiles; 8 requests of up to 1028: 12.8 us
+// against 22 us with blocks of 4).  Otherwise blocks of 64 tiles run in several waves, the
+// last of them short (64 requests of 4160: 172 us, unsplit 203 us).
 Plan make_plan(int B, int Hq, int Hkv, int window, int sinks, int max_ctx) {
     Plan p{};
     const int G = Hq / Hkv;
@@ -386,8 +386,8 @@ Plan make_plan(int B, int Hq, int Hkv, int window, int sinks, int max_ctx) {
                                                 ((int64_t)sinks + kTile - 1) / kTile);
     const int64_t units = (int64_t)B * Hkv * p.groups, places = 152 * kResident;
     int64_t chunk = 64;
-    if (units <= places) {
-        const int64_t splits = places / std::max<int64_t>(units, 1);
+    const int64_t splits = places / std::max<int64_t>(units, 1);
+    if (5 * units * splits >= 4 * places) {
         chunk = ((tiles + splits - 1) / splits + kWarps - 1) / kWarps * kWarps;
     } else if (units > kMaxCounters) {
         chunk = tiles;
