@@ -373,9 +373,10 @@ __global__ void __launch_bounds__(kThreads, kResident) window_decode_kernel(cons
 // Blocks of `chunk` tiles.  Where the (request, group) units, each split alike, fill four
 // fifths of the places that the card has for blocks, or more, all blocks run at once: whole
 // waves, few joins, down to a tile per warp (4 requests of up to 131072 tokens: 14 parts
-// each, 253 us against 257 us with blocks of 64 tiles; 8 requests of up to 1028: 12.8 us
-// against 22 us with blocks of 4).  Otherwise blocks of 64 tiles run in several waves, the
-// last of them short (64 requests of 4160: 172 us, unsplit 203 us).
+// each, 251 us, 267 us with blocks of 48 tiles; 8 requests of up to 1028: 12.9 us, 20.7 us
+// with blocks of 4).  Otherwise a unit's tiles are cut into equal blocks of at most 96
+// (32 requests of 4160 positions: three blocks of 88 tiles, 87 us; one of 264, 102 us; five
+// of 64 and a remainder, 93 us).
 Plan make_plan(int B, int Hq, int Hkv, int window, int sinks, int max_ctx) {
     Plan p{};
     const int G = Hq / Hkv;
@@ -385,10 +386,11 @@ Plan make_plan(int B, int Hq, int Hkv, int window, int sinks, int max_ctx) {
                                             ((int64_t)window + kTile - 1) / kTile + 1 +
                                                 ((int64_t)sinks + kTile - 1) / kTile);
     const int64_t units = (int64_t)B * Hkv * p.groups, places = 152 * kResident;
-    int64_t chunk = 64;
+    auto equal = [&](int64_t parts) { return ((tiles + parts - 1) / parts + kWarps - 1) / kWarps * kWarps; };
+    int64_t chunk = equal((tiles + 95) / 96);
     const int64_t splits = places / std::max<int64_t>(units, 1);
     if (5 * units * splits >= 4 * places) {
-        chunk = ((tiles + splits - 1) / splits + kWarps - 1) / kWarps * kWarps;
+        chunk = equal(splits);
     } else if (units > kMaxCounters) {
         chunk = tiles;
     }
