@@ -88,7 +88,7 @@ struct Cfg {
     static constexpr int CTL = Q_BYTES + SLOTS * SLOT;
     static constexpr int BYTES = CTL + 512 + 1024;     // + alignment of the window
     static_assert(SLOTS >= 3, "the loader may signal a slot after it has filled the next");
-    static_assert(QT == 2 || SLOTS * SLOT >= 128 * D * 4 + 2048, "the join goes through the ring");
+    static_assert(QT == 2 || SLOTS * SLOT >= 128 * (D + 8) * 4 + 2048, "the join goes through the ring");
     // Tensor memory.  bf16: per stream S, two P buffers and O.  fp32: one O, drained after
     // every tile, then per stream S and the planes of P.
     __host__ __device__ static constexpr uint32_t s_col(int w) { return NP == 1 ? 256 * w : 128 + 160 * w; }
@@ -646,6 +646,8 @@ __global__ void __launch_bounds__(kThreads, 1) window_prefill_kernel(const __gri
         auto row_at = [&](int tok, int head) {  // element offset of a row of q and o
             return ((int64_t)(row0 + tok) * a.Hq + kvh * G + head0 + head) * D;
         };
+        const uint32_t per_head = 65536u / heads + 1;  // row / heads for rows below 128, without a division
+        auto tok_of = [&](int row) { return (int)(row * per_head >> 16); };
         // ---- queries -> shared memory, bf16 planes, swizzled; all of a thread's loads in flight
         constexpr int CPR = D / 8, EACH = QT * 128 * CPR / 256, MOST = NP == 1 ? 16 : 8, BATCH = EACH < MOST ? EACH : MOST;
         static_assert(EACH % BATCH == 0, "");
@@ -654,7 +656,7 @@ __global__ void __launch_bounds__(kThreads, 1) window_prefill_kernel(const __gri
 #pragma unroll
             for (int k = 0; k < BATCH; ++k) {
                 const int i = i0 + 256 * k, r = i / CPR % 128, tile = i / CPR / 128;
-                const int tk = r / heads, tok = tile * p.tok + tk;
+                const int tk = tok_of(r), tok = tile * p.tok + tk;
                 x[k] = make_uint4(0u, 0u, 0u, 0u);
                 if constexpr (NP > 1) y[k] = x[k];
                 if (tk < p.tok && tok < tokens) {
@@ -688,7 +690,7 @@ __global__ void __launch_bounds__(kThreads, 1) window_prefill_kernel(const __gri
 
         const int w = warp / 4, r = tid % 128;
         const int base_tok = QT == 2 ? w * p.tok : 0, mine = stream_tokens(w);
-        const int tk = r / heads;
+        const int tk = tok_of(r);
         const bool live = tk < min(p.tok, mine);
         const int pos = live ? pos0 + base_tok + tk : -1;
         const int first = pos0 + base_tok, final = first + mine - 1;  // positions of the stream's rows
@@ -917,9 +919,10 @@ __global__ void __launch_bounds__(kThreads, 1) window_prefill_kernel(const __gri
             }
         };
         auto leave = [&](int thread, int threads) {
-            const int n_rows = min(p.tok, mine) * heads;
-            for (int i = thread; i < n_rows * OPR; i += threads) {
-                const int row = i / OPR, ch = i % OPR, t_row = row / heads;
+            const int pieces = min(p.tok, mine) * heads * OPR;
+#pragma unroll 4
+            for (int i = thread; i < pieces; i += threads) {
+                const int row = i / OPR, ch = i % OPR, t_row = tok_of(row);
                 reinterpret_cast<uint4*>(og + row_at(base_tok + t_row, row - t_row * heads))[ch] =
                     *reinterpret_cast<const uint4*>(stage_at(row, ch));
             }
@@ -942,16 +945,19 @@ __global__ void __launch_bounds__(kThreads, 1) window_prefill_kernel(const __gri
         } else {
             // ---- join the streams through the ring, which nothing uses any more once both streams'
             // last products are complete: each gives the other half of its columns
-            float* join = reinterpret_cast<float*>(sm + C::Q_BYTES);   // [2][D / 2][128]
-            float2* join_ml = reinterpret_cast<float2*>(join + D * 128);  // [2][128]
+            constexpr int PITCH = D / 2 + 4;  // floats: rows 16 bytes apart in the banks
+            float* join = reinterpret_cast<float*>(sm + C::Q_BYTES);  // [2][128][D / 2]
+            float2* join_ml = reinterpret_cast<float2*>(join + 256 * PITCH);  // [2][128]
             auto give = [&](auto which) {
                 constexpr int half = decltype(which)::value;
 #pragma unroll
                 for (int i = 0; i < D / 2; i += 32) {
                     uint32_t y[32];
                     o_part(half * (D / 2) + i, y);
+                    float4* to = reinterpret_cast<float4*>(join + (half * 128 + r) * PITCH + i);
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) join[(half * (D / 2) + i + e) * 128 + r] = asf(y[e]);
+                    for (int e = 0; e < 32; e += 4)
+                        to[e / 4] = make_float4(asf(y[e]), asf(y[e + 1]), asf(y[e + 2]), asf(y[e + 3]));
                 }
             };
             const int64_t part = ((int64_t)unit * p.splits + split) * 128;
@@ -961,9 +967,16 @@ __global__ void __launch_bounds__(kThreads, 1) window_prefill_kernel(const __gri
                 for (int i = half * (D / 2); i < (half + 1) * (D / 2); i += 32) {
                     uint32_t y[32];
                     o_part(i, y);
+                    const float4* from =
+                        reinterpret_cast<const float4*>(join + (half * 128 + r) * PITCH + i - half * (D / 2));
 #pragma unroll
-                    for (int e = 0; e < 32; ++e)
-                        y[e] = __float_as_uint(asf(y[e]) * keep + join[(i + e) * 128 + r] * take);
+                    for (int e = 0; e < 32; e += 4) {
+                        const float4 v = from[e / 4];
+                        y[e] = __float_as_uint(asf(y[e]) * keep + v.x * take);
+                        y[e + 1] = __float_as_uint(asf(y[e + 1]) * keep + v.y * take);
+                        y[e + 2] = __float_as_uint(asf(y[e + 2]) * keep + v.z * take);
+                        y[e + 3] = __float_as_uint(asf(y[e + 3]) * keep + v.w * take);
+                    }
                     if (p.splits > 1) {
 #pragma unroll
                         for (int e = 0; e < 32; e += 4)

@@ -152,6 +152,50 @@ def run_attn_tc(iters):
           f"(x80 layers: {80 * t * 1e3:.1f} ms)  status {L.loip_k_attention_tc_status()}")
 
 
+def run_window(iters):
+    """The windowed-serving operators: append, one-token attention and prompt attention behind a window."""
+    P = 64
+
+    def cache(R, ctx, Hkv, d):
+        pages, lpb = -(-ctx // P), 2 * Hkv * P * d * 2
+        kv = torch.randn(R * pages * lpb // 2, device="cuda").bfloat16()
+        return kv, (torch.randperm(R * pages, device="cuda") * lpb).view(R, pages), pages, lpb
+
+    def ints(v):
+        return torch.tensor(list(v), dtype=torch.int32, device="cuda")
+
+    Hq, Hkv, d = 64, 8, 128
+    for T, dt in ((1, torch.float32), (2048, torch.bfloat16), (8192, torch.float32)):
+        kv, pt, pages, lpb = cache(1, T, Hkv, d)
+        x = torch.randn(T, (Hq + 2 * Hkv) * d, device="cuda").to(dt)
+        q, pos, req = torch.empty(T, Hq * d, dtype=dt, device="cuda"), ints(range(T)), ints([0] * T)
+        t = _time(lambda i: L.loip_k_qk_append(x, None, None, Hq, Hkv, d, 0.0, 5e5, pos, req, q, kv, pt, pages, P, 0,
+                                               lpb), iters)
+        by = x.numel() * x.element_size() + q.numel() * q.element_size() + 4 * T * Hkv * d
+        print(f"append {T} {dt} rows: {t * 1e6:9.1f} us  {by / t / 1e9:8.1f} GB/s")
+    for B, ctx, window, dt in ((1, 1088, 1088, torch.float32), (8, 4352, 1024, torch.float32),
+                               (64, 8192, 4096, torch.bfloat16)):
+        kv, pt, pages, lpb = cache(B, ctx, Hkv, d)
+        q, n = torch.randn(B, Hq * d, device="cuda").to(dt), ints([ctx] * B)
+        o, args = torch.empty_like(q), (Hq, Hkv, d, P, 0, lpb, window, 4, ctx)
+        sc = torch.zeros(L.loip_k_window_attention_scratch_bytes(B, Hq, Hkv, d, window, 4, ctx), dtype=torch.uint8,
+                         device="cuda")
+        t = _time(lambda i: L.loip_k_window_attention(q, kv, pt, pages, n, *args, sc, o), iters)
+        by = B * min(ctx, window + 4) * 4 * Hkv * d
+        print(f"window attention {B} x {ctx}, window {window}, {dt}: {t * 1e6:9.1f} us  {by / t / 1e9:8.1f} GB/s")
+    for n, rows, window, dt in ((4, 512, 512, torch.float32), (1, 8192, 4096, torch.bfloat16)):
+        kv, pt, pages, lpb = cache(n, rows, Hkv, d)
+        q, o = torch.randn(n * rows, Hq * d, device="cuda").to(dt), torch.empty(n * rows, Hq * d, dtype=dt, device="cuda")
+        starts = ints(range(0, n * rows + 1, rows))
+        args = (Hq, Hkv, d, P, 0, lpb, window, 0, rows)
+        sc = torch.zeros(L.loip_k_window_prefill_scratch_bytes(n * rows, n, Hq, Hkv, d, window, 0, rows),
+                         dtype=torch.uint8, device="cuda")
+        t = _time(lambda i: L.loip_k_window_prefill(q, kv, pt, pages, starts, None, *args, sc, o), iters)
+        fl = 4 * n * Hq * d * sum(min(p + 1, window) for p in range(rows))
+        print(f"window prefill {n} x {rows}, window {window}, {dt}: {t * 1e6:9.1f} us  {fl / t / 1e12:7.1f} TFLOP/s  "
+              f"status {L.loip_k_attention_tc_status()}")
+
+
 def main():
     ap = argparse.ArgumentParser()
     ap.add_argument("--only", default="")
@@ -169,6 +213,8 @@ def main():
         run_pack(max(3, min(a.iters, 10)))
     if a.only in ("", "attn_tc"):
         run_attn_tc(max(3, min(a.iters, 10)))
+    if a.only in ("", "window"):
+        run_window(max(3, min(a.iters, 10)))
 
 
 if __name__ == "__main__":
