@@ -99,10 +99,10 @@ __device__ __forceinline__ void store8(__nv_bfloat16* p, const float (&v)[8]) {
 // A block takes a group of heads of one token; D / 16 lanes per head, each holding the
 // elements 8l .. 8l + 7 of the head and their partners D / 2 further on.  Bound by memory:
 // short blocks with all their loads issued at once, the gains' among them, and as many of
-// them per SM as the registers can be held to (8191 fp32 tokens of 120 heads of 128: 119.6
-// us, 7.0 TB/s; 1999 bf16 tokens of 80 heads, with norms: 18.3 us, 4.5 TB/s, where six or
-// four blocks per SM take 20.7 and 19.7 us, two tokens per block 19.9 us, and one wave of
-// blocks that walk over the tokens with the next one's loads in flight 28.7 us).
+// them per SM as the registers can be held to.  8191 fp32 tokens of 120 heads of 128: 121
+// us, 6.9 TB/s; 1999 bf16 tokens of 80 heads, with norms: 15.1 us, 5.4 TB/s (each before
+// the bank conflicts went: eight blocks per SM 18.3, six 20.7, two tokens per block 19.9,
+// one wave of blocks that walk over the tokens with the next one's loads in flight 28.7).
 template <int D, typename T>
 __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 8 : 6) qk_append_kernel(const __grid_constant__ AppendArgs p) {
     constexpr int LANES = D / 16;

@@ -24,6 +24,11 @@
 // fp32 (the MMA's own sums truncate: 4e-6 over 150 tiles).  bf16 activations: one MMA for
 // the scores, two planes of the weights (2^-17; the second costs 1%).
 //
+// Measured (GB300): 64 requests behind a 4096-token window, 64 heads of 128: 175 us, 6.0
+// TB/s; 4 requests of up to 131072 tokens, 32 heads: 253 us, 6.2 TB/s (bound by memory); 8
+// fp32 requests of up to 1028: 12.9 us, one request of 1088: 8.0 us (a chain of latencies:
+// length, page table, keys, join).
+//
 // Masked positions are neither loaded nor multiplied: their key and value registers
 // are zero, whatever the cache holds there.
 #include <cuda_bf16.h>
