@@ -398,21 +398,22 @@ def _s(stream):
     """The given stream, or the current one of the current device.  (Its raw handle: building
     the stream object that torch.cuda.current_stream() returns takes 3 us, this 0.2 us.)"""
     if stream is None:
-        torch = _torch()
-        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+        if not _of_torch:
+            _torch()
+        return _of_torch[0](_of_torch[1]())
     return stream
 
 
-_torch_module = None
+_of_torch = []  # current raw stream of a device, current device, types of rows
 
 
 def _torch():
-    """torch, imported at the first call that needs it."""
-    global _torch_module
-    if _torch_module is None:
-        import torch
-        _torch_module = torch
-    return _torch_module
+    """torch, imported at the first call that needs it; fills _of_torch."""
+    import torch
+    if not _of_torch:
+        _of_torch.extend([torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice,
+                          {torch.float32: F32_ROWS, torch.bfloat16: BF16_ROWS}])
+    return torch
 
 
 def loip_k_generate(out, first: int, seed: int, tensor_id: int, kind: int, stream=None):
@@ -535,16 +536,17 @@ def loip_k_lm_head(x, g_final, lm_head, eps, z, logits, tokens, scratch, stream=
 F32_ROWS, BF16_ROWS = 0, 1  # `dtype` of the windowed operators' activations
 
 
-def _dtype(x, like=None):
-    """LOIP_F32 / LOIP_BF16 of a tensor; `like`, if given, has to be of the same type."""
-    torch, dtype = _torch(), x.dtype
-    if like is not None and like.dtype != dtype:
+def _dtype(x, like):
+    """LOIP_F32 / LOIP_BF16 of a tensor; `like` has to be of the same type."""
+    if not _of_torch:
+        _torch()
+    dtype = x.dtype
+    rows = _of_torch[2].get(dtype)
+    if rows is None:
+        raise LoipError(ERR_INVALID, f"activations are float32 or bfloat16, not {dtype}")
+    if like.dtype != dtype:
         raise LoipError(ERR_INVALID, f"input of {dtype} with an output of {like.dtype}")
-    if dtype == torch.float32:
-        return F32_ROWS
-    if dtype == torch.bfloat16:
-        return BF16_ROWS
-    raise LoipError(ERR_INVALID, f"activations are float32 or bfloat16, not {dtype}")
+    return rows
 
 
 def loip_k_qk_append(qkv, g_q, g_k, Hq, Hkv, d, eps, theta, positions, row_req, q_out, kv_base, page_offsets,
