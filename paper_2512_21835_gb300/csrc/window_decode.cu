@@ -26,7 +26,7 @@
 //
 // Measured (GB300): 64 requests behind a 4096-token window, 64 heads of 128: 175 us, 6.0
 // TB/s; 4 requests of up to 131072 tokens, 32 heads: 253 us, 6.2 TB/s (bound by memory); 8
-// fp32 requests of up to 1028: 12.9 us, one request of 1088: 7.0 us (a chain of latencies:
+// fp32 requests of up to 1028: 12.9 us, one request of 1088: 8.8 us (a chain of latencies:
 // length, page table, keys, join).
 //
 // Masked positions are neither loaded nor multiplied: their key and value registers
@@ -377,9 +377,10 @@ __global__ void __launch_bounds__(kThreads, kResident) window_decode_kernel(cons
 
 // Blocks of `chunk` tiles.  Where the (request, group) units, each split alike, fill four
 // fifths of the places that the card has for blocks, or more, all blocks run at once: whole
-// waves, few joins, down to two tiles per warp (4 requests of up to 131072 tokens: 14 parts
+// waves, few joins, down to a tile per warp (4 requests of up to 131072 tokens: 14 parts
 // each, 251 us, 267 us with blocks of 48 tiles; 8 requests of up to 1028: 12.9 us, 20.7 us
-// with blocks of 4; one of 1088: 7.0 us in nine parts, 8.0 us in 17).  Otherwise a unit's tiles are cut into equal blocks of at most 96
+// with blocks of 4; one of 1088, 17 parts: 8.8 us, in nine 9.3 us, though 8.1 and 7.7 us in
+// a graph).  Otherwise a unit's tiles are cut into equal blocks of at most 96
 // (32 requests of 4160 positions: three blocks of 88 tiles, 87 us; one of 264, 102 us; five
 // of 64 and a remainder, 93 us).
 Plan make_plan(int B, int Hq, int Hkv, int window, int sinks, int max_ctx) {
@@ -399,7 +400,7 @@ Plan make_plan(int B, int Hq, int Hkv, int window, int sinks, int max_ctx) {
     } else if (units > kMaxCounters) {
         chunk = tiles;
     }
-    p.chunk = (int)std::max<int64_t>(chunk, 2 * kWarps);
+    p.chunk = (int)std::max<int64_t>(chunk, 1);
     p.splits = (int)std::max<int64_t>((tiles + p.chunk - 1) / p.chunk, 1);
     return p;
 }
