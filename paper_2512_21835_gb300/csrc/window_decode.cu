@@ -26,7 +26,7 @@
 //
 // Measured (GB300): 64 requests behind a 4096-token window, 64 heads of 128: 175 us, 6.0
 // TB/s; 4 requests of up to 131072 tokens, 32 heads: 253 us, 6.2 TB/s (bound by memory); 8
-// fp32 requests of up to 1028: 12.9 us, one request of 1088: 8.8 us (a chain of latencies:
+// fp32 requests of up to 1028: 12.9 us, one request of 1088: 7.7 us (a chain of latencies:
 // length, page table, keys, join).
 //
 // Masked positions are neither loaded nor multiplied: their key and value registers

@@ -556,11 +556,13 @@ def loip_k_qk_append(qkv, g_q, g_k, Hq, Hkv, d, eps, theta, positions, row_req, 
     (T, width), (row_stride, step) = qkv.shape, qkv.stride()
     if step != 1 or not q_out.is_contiguous():
         raise LoipError(ERR_INVALID, "rows of qkv have to be contiguous, and q_out as a whole")
-    if positions.numel() < T or q_out.numel() != T * Hq * d or width != (Hq + 2 * Hkv) * d:
-        raise LoipError(ERR_INVALID, "qkv, positions and q_out do not fit together")
+    n_req = page_offsets.shape[0]
+    if (positions.numel() < T or q_out.numel() != T * Hq * d or width != (Hq + 2 * Hkv) * d
+            or page_offsets.numel() < n_req * max_pages or (row_req is not None and row_req.numel() < T)):
+        raise LoipError(ERR_INVALID, "qkv, positions, row_req, q_out and the page table do not fit together")
     rc = lib().loip_k_qk_append(qkv.data_ptr(), _dtype(qkv, q_out), row_stride, T, Hq, Hkv, d, _ptr(g_q), _ptr(g_k), eps,
-                                theta, positions.data_ptr(), _ptr(row_req), page_offsets.shape[0], q_out.data_ptr(),
-                                kv_base.data_ptr(), page_offsets.data_ptr(), max_pages, page_tokens, layer,
+                                theta, positions.data_ptr(), _ptr(row_req), n_req, q_out.data_ptr(),
+                                _ptr(kv_base), page_offsets.data_ptr(), max_pages, page_tokens, layer,
                                 layer_page_bytes, _s(stream))
     if rc:
         _check(rc)
@@ -577,7 +579,9 @@ def loip_k_window_attention(q, kv_base, page_offsets, max_pages, ctx_lens, Hq, H
     B = q.shape[0]
     if not (q.is_contiguous() and o.is_contiguous()) or q.numel() != B * Hq * d or o.numel() != q.numel():
         raise LoipError(ERR_INVALID, "q and o are contiguous [B, Hq * d]")
-    rc = lib().loip_k_window_attention(q.data_ptr(), _dtype(q, o), kv_base.data_ptr(), page_offsets.data_ptr(),
+    if ctx_lens.numel() < B or page_offsets.numel() < B * max_pages:
+        raise LoipError(ERR_INVALID, "a length and max_pages page-table entries for each request")
+    rc = lib().loip_k_window_attention(q.data_ptr(), _dtype(q, o), _ptr(kv_base), page_offsets.data_ptr(),
                                        max_pages, ctx_lens.data_ptr(), B, Hq, Hkv, d, page_tokens, layer,
                                        layer_page_bytes, window, sinks, max_ctx, scratch.data_ptr(), scratch.nbytes,
                                        o.data_ptr(), _s(stream))
@@ -596,8 +600,11 @@ def loip_k_window_prefill(q, kv_base, page_offsets, max_pages, row_starts, first
     M = q.shape[0]
     if not (q.is_contiguous() and o.is_contiguous()) or q.numel() != M * Hq * d or o.numel() != q.numel():
         raise LoipError(ERR_INVALID, "q and o are contiguous [M, Hq * d]")
-    rc = lib().loip_k_window_prefill(q.data_ptr(), _dtype(q, o), kv_base.data_ptr(), page_offsets.data_ptr(), max_pages,
-                                     row_starts.data_ptr(), _ptr(first_pos), row_starts.numel() - 1, M, Hq, Hkv, d,
+    n = row_starts.numel() - 1
+    if page_offsets.numel() < n * max_pages or (first_pos is not None and first_pos.numel() < n):
+        raise LoipError(ERR_INVALID, "a first position and max_pages page-table entries for each prompt")
+    rc = lib().loip_k_window_prefill(q.data_ptr(), _dtype(q, o), _ptr(kv_base), page_offsets.data_ptr(), max_pages,
+                                     row_starts.data_ptr(), _ptr(first_pos), n, M, Hq, Hkv, d,
                                      page_tokens, layer, layer_page_bytes, window, sinks, max_ctx, scratch.data_ptr(),
                                      scratch.nbytes, o.data_ptr(), _s(stream))
     if rc:

@@ -472,6 +472,15 @@ def test_refusals_of_the_binding(torch, L):
         with pytest.raises(L.LoipError) as e:
             decode(**bad)
         assert e.value.code == L.ERR_INVALID
+    for call in (lambda: L.loip_k_window_attention(q, kv, table, 1, _ints(torch, []), Hq, Hkv, d, P, 0,
+                                                   c.layer_page_bytes, 4, 0, 64, scratch, torch.empty_like(q)),
+                 lambda: L.loip_k_window_prefill(q, kv, table, 2, _ints(torch, [0, 1]), None, Hq, Hkv, d, P, 0,
+                                                 c.layer_page_bytes, 4, 0, 64, scratch, torch.empty_like(q)),
+                 lambda: L.loip_k_qk_append(torch.zeros(1, 8 * d, device="cuda"), None, None, Hq, Hkv, d, 0.0, 0.0,
+                                            _ints(torch, [0]), _ints(torch, []), q, kv, table, 1, P, 0,
+                                            c.layer_page_bytes)):
+        with pytest.raises(L.LoipError):  # arrays shorter than the rows
+            call()
     with pytest.raises(L.LoipError, match="both gains"):
         L.loip_k_qk_append(torch.zeros(1, 8 * d, device="cuda"), dev_bits(np.zeros(d, np.uint16)), None, Hq, Hkv, d,
                            0.0, 0.0, _ints(torch, [0]), None, q, kv, table, 1, P, 0, c.layer_page_bytes)
