@@ -39,6 +39,25 @@ cudaError_t launch_pdl(void (*kernel)(Args), dim3 grid, unsigned threads, size_t
     c.numAttrs = 1;
     return cudaLaunchKernelEx(&c, kernel, args);
 }
+
+// Two fp32 numbers as a pair of bf16, to the nearest.
+__device__ __forceinline__ uint32_t pack(float lo, float hi) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+// An fp32 number is the exact sum of three bf16 planes.  Each of the first two is the largest
+// below what is left (in size), cut off and not rounded: so something of the number's own sign
+// is always left, no plane of a number is zero (down to 2^-100 or so), and the product with
+// an infinity is that infinity, as it would be in one piece.  (Rounded planes gave inf - inf,
+// planes of zero 0 x inf.)  v (1 - 2^-24) is the fp32 number below v.
+//
+// The pair's next plane: v becomes v - plane, exactly.
+__device__ __forceinline__ uint32_t peel(float& lo, float& hi) {
+    const uint32_t a = __float_as_uint(lo * 0x1.fffffep-1f), b = __float_as_uint(hi * 0x1.fffffep-1f);
+    lo -= __uint_as_float(a & 0xffff0000u);
+    hi -= __uint_as_float(b & 0xffff0000u);
+    return __byte_perm(a, b, 0x7632u);
+}
 #endif
 
 // Attention of query rows over the paged cache behind a window with sinks: the

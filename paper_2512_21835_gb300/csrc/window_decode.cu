@@ -22,7 +22,7 @@
 // Precision.  An fp32 query is the exact sum of three bf16 planes, and so are the
 // weights of fp32 activations: three MMAs per product, a tile's product added to O in
 // fp32 (the MMA's own sums truncate: 4e-6 over 150 tiles).  bf16 activations: one MMA for
-// the scores, two planes of the weights (2^-17; the second costs 1%).
+// the scores, two planes of the weights (2^-16; the second costs 1%).
 //
 // Measured (GB300): 64 requests behind a 4096-token window, 64 heads of 128: 175 us, 6.0
 // TB/s; 4 requests of up to 131072 tokens, 32 heads: 253 us, 6.2 TB/s (bound by memory); 8
@@ -55,17 +55,6 @@ __device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uin
         "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-}
-__device__ __forceinline__ uint32_t pack(float lo, float hi) {
-    const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
-    return *reinterpret_cast<const uint32_t*>(&h);
-}
-// The pair's next plane: v becomes v - bf16(v), exactly.
-__device__ __forceinline__ uint32_t peel(float& lo, float& hi) {
-    const uint32_t p = pack(lo, hi);
-    lo -= __uint_as_float(p << 16);
-    hi -= __uint_as_float(p & 0xffff0000u);
-    return p;
 }
 // 8 x 8 transpose over the warp: lane 4 n + c gives elements (n, 2 c), (n, 2 c + 1) and
 // gets (2 c, n), (2 c + 1, n).
@@ -146,7 +135,8 @@ __global__ void __launch_bounds__(kThreads, kResident) window_decode_kernel(cons
                 for (int pl = 0; pl < 3; ++pl) {
                     uint32_t u[4];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) u[e] = peel(v[2 * e], v[2 * e + 1]);
+                    for (int e = 0; e < 4; ++e)
+                        u[e] = pl < 2 ? peel(v[2 * e], v[2 * e + 1]) : pack(v[2 * e], v[2 * e + 1]);
                     sm_q[x][pl][lane] = make_uint4(u[0], u[1], u[2], u[3]);
                 }
             } else {
@@ -254,11 +244,12 @@ __global__ void __launch_bounds__(kThreads, kResident) window_decode_kernel(cons
             w[2 + h] = exp2f(w[2 + h] - base);
             l[h] += w[h] + w[2 + h];
         }
-        uint32_t pb[PV][2];  // planes of P^T in the B layout
+        uint32_t pb[PV][2];  // planes of P^T in the B layout; the last one is rounded (exact if it is the third)
 #pragma unroll
         for (int pl = 0; pl < PV; ++pl)
 #pragma unroll
-            for (int j = 0; j < 2; ++j) pb[pl][j] = transpose(peel(w[2 * j], w[2 * j + 1]));
+            for (int j = 0; j < 2; ++j)
+                pb[pl][j] = transpose(pl < PV - 1 ? peel(w[2 * j], w[2 * j + 1]) : pack(w[2 * j], w[2 * j + 1]));
         // ---- values
 #pragma unroll
         for (int x = 0; x < NV; ++x) {

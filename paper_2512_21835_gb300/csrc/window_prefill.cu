@@ -287,17 +287,6 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b) {
         : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
     return r;
 }
-__device__ __forceinline__ uint32_t pack(float lo, float hi) {
-    const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
-    return *reinterpret_cast<const uint32_t*>(&h);
-}
-// The pair's next plane: v becomes v - bf16(v), exactly.
-__device__ __forceinline__ uint32_t peel(float& lo, float& hi) {
-    const uint32_t p = pack(lo, hi);
-    lo -= asf(p << 16);
-    hi -= asf(p & 0xffff0000u);
-    return p;
-}
 __device__ __forceinline__ uint64_t low_bits(int n) { return n <= 0 ? 0ull : n >= 64 ? ~0ull : (1ull << n) - 1; }
 
 __device__ __forceinline__ float row_load(const float* p) { return *p; }
@@ -685,7 +674,8 @@ __global__ void __launch_bounds__(kThreads, 1) window_prefill_kernel(const __gri
                     for (int pl = 0; pl < NP; ++pl) {
                         uint32_t u[4];
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) u[e] = peel(v[2 * e], v[2 * e + 1]);
+                        for (int e = 0; e < 4; ++e)
+                            u[e] = pl < 2 ? peel(v[2 * e], v[2 * e + 1]) : pack(v[2 * e], v[2 * e + 1]);
                         *reinterpret_cast<uint4*>(dst + pl * C::Q_PLANE) = make_uint4(u[0], u[1], u[2], u[3]);
                     }
                 }
