@@ -589,10 +589,11 @@ int loip_k_qk_append(const void* qkv, int32_t dtype, int64_t row_stride, int32_t
 /* Attention of one new token of each of B requests: request b holds ctx_lens[b]
  * cached positions (dev int32, the new token's included) and its query sees the
  * last `window` of them and the first `sinks` (window >= the context: all of
- * them).  A request that sees nothing (no context, or window and sinks zero)
- * gets zeros.  ctx_lens[b] <= max_ctx <= max_pages * 64 (a larger one is read
- * as max_ctx), max_ctx <= 2^30.  o [B, Hq * d].  `scratch` (dev, 16-byte aligned, scratch_bytes
- * >= loip_k_window_attention_scratch_bytes(...)) holds partial softmax states
+ * them).  A request that sees nothing (no context, or window and sinks zero), or
+ * nothing but scores of -inf, gets zeros.  ctx_lens[b] <= max_ctx <= max_pages * 64
+ * (a larger one is read as max_ctx), max_ctx <= 2^30.  o [B, Hq * d].  `scratch`
+ * (dev, 16-byte aligned, scratch_bytes >=
+ * loip_k_window_attention_scratch_bytes(...)) holds partial softmax states
  * and completion counters: zero-filled once by the caller, left usable by every
  * call.  One scratch, as large as the largest call needs, serves calls of any
  * shape and loip_k_window_prefill too; calls that may overlap on the GPU need a
@@ -610,9 +611,9 @@ uint64_t loip_k_window_attention_scratch_bytes(int32_t B, int32_t Hq, int32_t Hk
  * [n_prompts + 1], from 0 to M, not decreasing) at positions first_pos[i], ...
  * (dev int32 [n_prompts], NULL = 0) of request i, whose keys and values up to
  * the last row are in the cache.  The row at position p sees the cached
- * positions j <= p with j > p - window or j < sinks; a row that sees nothing
- * gets zeros.  No position reaches max_ctx (<= max_pages * 64 and 2^30; keys
- * past it are not read).  o [M, Hq * d].  Scratch as for loip_k_window_attention. */
+ * positions j <= p with j > p - window or j < sinks; a row that sees nothing, or
+ * nothing but scores of -inf, gets zeros.  No position reaches max_ctx
+ * (<= max_pages * 64 and 2^30; keys past it are not read).  o [M, Hq * d].  Scratch as for loip_k_window_attention. */
 int loip_k_window_prefill(const void* q, int32_t dtype, const void* kv_base, const int64_t* page_offsets,
                           int32_t max_pages, const int32_t* row_starts, const int32_t* first_pos, int32_t n_prompts,
                           int32_t M, int32_t Hq, int32_t Hkv, int32_t d, int32_t page_tokens, int32_t layer,

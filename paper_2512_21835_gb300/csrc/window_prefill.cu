@@ -323,7 +323,8 @@ __device__ __forceinline__ void walk_row(const WindowArgs& a, int req, int kvh, 
 #pragma unroll
         for (int x = 16; x; x /= 2) s += __shfl_xor_sync(0xffffffffu, s, x);
         s *= scale;
-        const float m_new = fmaxf(m, s), alpha = m == -INFINITY ? 0.f : expf(m - m_new), w = expf(s - m_new);
+        const float m_new = fmaxf(m, s), alpha = m == -INFINITY ? 0.f : expf(m - m_new);
+        const float w = expf(s - (m_new == -INFINITY ? 0.f : m_new));  // a score of -inf: weight zero, the first one too
         l = l * alpha + w;
 #pragma unroll
         for (int i = 0; i < D / 32; ++i) o[i] = fmaf(w, __bfloat162float(v[i * 32 + lane]), o[i] * alpha);

@@ -128,3 +128,35 @@ def test_prefill_infinite_keys(torch, L, d, dtype):
     qd, q64 = _rows(torch, _signs(np.random.default_rng(3), 159, Hq, d), dtype)
     got = _host(_prefill(torch, L, c, qd, runs, Hq, ALL, 0, 509))
     _check_keys(got, c, [(r, f + t) for r, (n, f) in enumerate(runs) for t in range(n)], Hq, d, dtype, q64, 7)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_prefill_infinite_first_key_of_a_row_walked_alone(torch, L, dtype):
+    """The first position seen has a score of -inf, in a tile whose rows are computed one by one
+    (a value that is not finite, in a page that some of its rows see in part)."""
+    runs, Hq, Hkv, d = [(40, 0)], 4, 2, 64
+    c, _ = _prefill_cache(runs, 40, Hkv, d, ALL, 0, 501)
+    _spoil(c, 0, 0, 0, 0, INF)
+    _spoil(c, 0, 30, 1, 5, INF)
+    qd, q64 = _rows(torch, _signs(np.random.default_rng(4), 40, Hq, d), dtype)
+    got = _host(_prefill(torch, L, c, qd, runs, Hq, ALL, 0, 40))
+    _check_keys(got[1:], c, [(0, t) for t in range(1, 40)], Hq, d, dtype, q64[1:], 0)
+
+
+@pytest.mark.parametrize("walked", [False, True])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_nothing_but_scores_of_minus_infinity(torch, L, dtype, walked):
+    """Every position that the row sees has weight zero: the row is zero, as one that sees nothing."""
+    Hq, Hkv, d = 4, 2, 64
+    c = Cache(1, 1, Hkv, d, 7)
+    c.fill_request(0, range(20), 8)
+    for j in range(3):
+        _spoil(c, 0, j, 0, 0, INF)
+    if walked:
+        _spoil(c, 0, 10, 1, 5, INF)
+    q = -np.abs(np.random.default_rng(5).standard_normal((20, Hq, d))) - 0.1
+    q[:, :, 1:] *= 0.1
+    qd, _ = _rows(torch, q.reshape(20, Hq * d).astype(np.float32), dtype)
+    o = _host(_prefill(torch, L, c, qd, [(20, 0)], Hq, ALL, 0, 20))
+    assert np.all(o[:3] == 0) and np.all(np.isfinite(o[3:10])) and np.any(o[3:10] != 0)
+    assert np.all(_host(_decode(torch, L, c, qd[:1], [3], Hq, ALL, 0, 20)) == 0)
