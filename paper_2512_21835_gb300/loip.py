@@ -404,7 +404,7 @@ def _s(stream):
     return stream
 
 
-_of_torch = []  # current raw stream of a device, current device, types of rows
+_of_torch = []  # current raw stream of a device, current device, types of rows, int32, int64, types of bf16 and its bits
 
 
 def _torch():
@@ -412,7 +412,8 @@ def _torch():
     import torch
     if not _of_torch:
         _of_torch.extend([torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice,
-                          {torch.float32: F32_ROWS, torch.bfloat16: BF16_ROWS}])
+                          {torch.float32: F32_ROWS, torch.bfloat16: BF16_ROWS}, torch.int32, torch.int64,
+                          (torch.bfloat16, torch.int16, torch.uint16)])
     return torch
 
 
@@ -546,7 +547,53 @@ def _dtype(x, like):
         raise LoipError(ERR_INVALID, f"activations are float32 or bfloat16, not {dtype}")
     if like.dtype != dtype:
         raise LoipError(ERR_INVALID, f"input of {dtype} with an output of {like.dtype}")
+    if not (x.is_cuda and like.is_cuda):
+        raise LoipError(ERR_INVALID, "activations are CUDA tensors")
     return rows
+
+
+def _refuse(why):
+    raise LoipError(ERR_INVALID, why)
+
+
+def _ints(x, n, name):
+    """Address of a device array of n int32 numbers or more.  (Another type or stride would be read as it lies.)"""
+    if x.dtype is not _of_torch[3] or not x.is_cuda or not x.is_contiguous() or x.numel() < n:
+        _refuse(f"{name} is a contiguous int32 CUDA tensor of {n} elements, not {x.dtype} {tuple(x.shape)} on {x.device}")
+    return x.data_ptr()
+
+
+def _pages(x, rows, max_pages):
+    """Address of a page table: rows of max_pages byte offsets, one behind the other."""
+    if (x.dtype is not _of_torch[4] or not x.is_cuda or not x.is_contiguous() or x.numel() < rows * max_pages
+            or (rows > 1 and x.dim() > 1 and x.shape[-1] != max_pages)):
+        _refuse(f"the page table is a contiguous int64 CUDA tensor [{rows}, {max_pages}], not {x.dtype} "
+                f"{tuple(x.shape)} on {x.device}")
+    return x.data_ptr()
+
+
+def _gain(x, d):
+    """Address of a gain of d bf16 numbers (or their bits); None and addresses as they are."""
+    if x is None or isinstance(x, int):
+        return x
+    if x.dtype not in _of_torch[5] or not x.is_cuda or not x.is_contiguous() or x.numel() != d:
+        _refuse(f"a gain is a contiguous CUDA tensor of {d} bfloat16 (or their bits), not {x.dtype} {tuple(x.shape)}")
+    return x.data_ptr()
+
+
+def _cache(x):
+    """Address of the cache: a contiguous tensor that the device can reach, or the address itself."""
+    if x is None or isinstance(x, int):
+        return x
+    if isinstance(x, np.ndarray) or not x.is_contiguous() or not (x.is_cuda or x.is_pinned()):
+        _refuse("the cache is a contiguous CUDA (or pinned) tensor, or an address")
+    return x.data_ptr()
+
+
+def _scratch(x):
+    if not x.is_cuda or not x.is_contiguous():
+        _refuse("the scratch is a contiguous CUDA tensor")
+    return x.data_ptr()
 
 
 def loip_k_qk_append(qkv, g_q, g_k, Hq, Hkv, d, eps, theta, positions, row_req, q_out, kv_base, page_offsets,
@@ -554,15 +601,16 @@ def loip_k_qk_append(qkv, g_q, g_k, Hq, Hkv, d, eps, theta, positions, row_req, 
     """Norm of queries and keys (g_q, g_k or None), rotation (theta 0: none), append.  qkv [T, (Hq + 2 Hkv) * d]
     float32 or bfloat16 with any row stride; page_offsets [requests, max_pages]."""
     (T, width), (row_stride, step) = qkv.shape, qkv.stride()
+    dtype = _dtype(qkv, q_out)
     if step != 1 or not q_out.is_contiguous():
-        raise LoipError(ERR_INVALID, "rows of qkv have to be contiguous, and q_out as a whole")
+        _refuse("rows of qkv have to be contiguous, and q_out as a whole")
     n_req = page_offsets.shape[0]
-    if (positions.numel() < T or q_out.numel() != T * Hq * d or width != (Hq + 2 * Hkv) * d
-            or page_offsets.numel() < n_req * max_pages or (row_req is not None and row_req.numel() < T)):
-        raise LoipError(ERR_INVALID, "qkv, positions, row_req, q_out and the page table do not fit together")
-    rc = lib().loip_k_qk_append(qkv.data_ptr(), _dtype(qkv, q_out), row_stride, T, Hq, Hkv, d, _ptr(g_q), _ptr(g_k), eps,
-                                theta, positions.data_ptr(), _ptr(row_req), n_req, q_out.data_ptr(),
-                                _ptr(kv_base), page_offsets.data_ptr(), max_pages, page_tokens, layer,
+    if q_out.numel() != T * Hq * d or width != (Hq + 2 * Hkv) * d:
+        _refuse("qkv and q_out do not fit together")
+    rc = lib().loip_k_qk_append(qkv.data_ptr(), dtype, row_stride, T, Hq, Hkv, d, _gain(g_q, d), _gain(g_k, d), eps,
+                                theta, _ints(positions, T, "positions"),
+                                None if row_req is None else _ints(row_req, T, "row_req"), n_req, q_out.data_ptr(),
+                                _cache(kv_base), _pages(page_offsets, n_req, max_pages), max_pages, page_tokens, layer,
                                 layer_page_bytes, _s(stream))
     if rc:
         _check(rc)
@@ -576,14 +624,12 @@ def loip_k_window_attention(q, kv_base, page_offsets, max_pages, ctx_lens, Hq, H
                             layer_page_bytes, window, sinks, max_ctx, scratch, o, stream=None):
     """Attention of one new token per request behind a window with sinks.  scratch: a uint8 tensor of
     loip_k_window_attention_scratch_bytes(...), zero-filled once."""
-    B = q.shape[0]
+    B, dtype = q.shape[0], _dtype(q, o)
     if not (q.is_contiguous() and o.is_contiguous()) or q.numel() != B * Hq * d or o.numel() != q.numel():
-        raise LoipError(ERR_INVALID, "q and o are contiguous [B, Hq * d]")
-    if ctx_lens.numel() < B or page_offsets.numel() < B * max_pages:
-        raise LoipError(ERR_INVALID, "a length and max_pages page-table entries for each request")
-    rc = lib().loip_k_window_attention(q.data_ptr(), _dtype(q, o), _ptr(kv_base), page_offsets.data_ptr(),
-                                       max_pages, ctx_lens.data_ptr(), B, Hq, Hkv, d, page_tokens, layer,
-                                       layer_page_bytes, window, sinks, max_ctx, scratch.data_ptr(), scratch.nbytes,
+        _refuse("q and o are contiguous [B, Hq * d]")
+    rc = lib().loip_k_window_attention(q.data_ptr(), dtype, _cache(kv_base), _pages(page_offsets, B, max_pages),
+                                       max_pages, _ints(ctx_lens, B, "ctx_lens"), B, Hq, Hkv, d, page_tokens, layer,
+                                       layer_page_bytes, window, sinks, max_ctx, _scratch(scratch), scratch.nbytes,
                                        o.data_ptr(), _s(stream))
     if rc:
         _check(rc)
@@ -597,15 +643,14 @@ def loip_k_window_prefill(q, kv_base, page_offsets, max_pages, row_starts, first
                           layer_page_bytes, window, sinks, max_ctx, scratch, o, stream=None):
     """The same attention for the rows of prompts: row_starts (device int32 [prompts + 1]), first_pos (device int32
     [prompts] or None = 0)."""
-    M = q.shape[0]
+    M, dtype = q.shape[0], _dtype(q, o)
     if not (q.is_contiguous() and o.is_contiguous()) or q.numel() != M * Hq * d or o.numel() != q.numel():
-        raise LoipError(ERR_INVALID, "q and o are contiguous [M, Hq * d]")
+        _refuse("q and o are contiguous [M, Hq * d]")
     n = row_starts.numel() - 1
-    if page_offsets.numel() < n * max_pages or (first_pos is not None and first_pos.numel() < n):
-        raise LoipError(ERR_INVALID, "a first position and max_pages page-table entries for each prompt")
-    rc = lib().loip_k_window_prefill(q.data_ptr(), _dtype(q, o), _ptr(kv_base), page_offsets.data_ptr(), max_pages,
-                                     row_starts.data_ptr(), _ptr(first_pos), n, M, Hq, Hkv, d,
-                                     page_tokens, layer, layer_page_bytes, window, sinks, max_ctx, scratch.data_ptr(),
+    rc = lib().loip_k_window_prefill(q.data_ptr(), dtype, _cache(kv_base), _pages(page_offsets, n, max_pages), max_pages,
+                                     _ints(row_starts, 1, "row_starts"),
+                                     None if first_pos is None else _ints(first_pos, n, "first_pos"), n, M, Hq, Hkv, d,
+                                     page_tokens, layer, layer_page_bytes, window, sinks, max_ctx, _scratch(scratch),
                                      scratch.nbytes, o.data_ptr(), _s(stream))
     if rc:
         _check(rc)
