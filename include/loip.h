@@ -595,9 +595,11 @@ int loip_k_qk_append(const void* qkv, int32_t dtype, int64_t row_stride, int32_t
  * (dev, 16-byte aligned, scratch_bytes >=
  * loip_k_window_attention_scratch_bytes(...)) holds partial softmax states
  * and completion counters: zero-filled once by the caller, left usable by every
- * call.  One scratch, as large as the largest call needs, serves calls of any
- * shape and loip_k_window_prefill too; calls that may overlap on the GPU need a
- * scratch each. */
+ * call.  For given heads the size does not fall as B, window, sinks or max_ctx grow
+ * (nor loip_k_window_prefill's as M or n_prompts grow): a scratch for the largest
+ * batch and context serves the smaller ones.  One scratch, as large as the largest
+ * call needs, serves calls of any shape and loip_k_window_prefill too; calls that
+ * may overlap on the GPU need a scratch each. */
 int loip_k_window_attention(const void* q, int32_t dtype, const void* kv_base, const int64_t* page_offsets,
                             int32_t max_pages, const int32_t* ctx_lens, int32_t B, int32_t Hq, int32_t Hkv, int32_t d,
                             int32_t page_tokens, int32_t layer, uint64_t layer_page_bytes, int32_t window,

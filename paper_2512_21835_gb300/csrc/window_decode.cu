@@ -366,6 +366,14 @@ __global__ void __launch_bounds__(kThreads, kResident) window_decode_kernel(cons
     }
 }
 
+constexpr int kPlaces = 152 * kResident;
+constexpr int kMostTiles = 96;  // per block, without whole waves
+
+int64_t visible_tiles(int window, int sinks, int max_ctx) {
+    return std::min<int64_t>(((int64_t)max_ctx + kTile - 1) / kTile, ((int64_t)window + kTile - 1) / kTile + 1 +
+                                                                         ((int64_t)sinks + kTile - 1) / kTile);
+}
+
 // Blocks of `chunk` tiles.  Where the (request, group) units, each split alike, fill four
 // fifths of the places that the card has for blocks, or more, all blocks run at once: whole
 // waves, few joins, down to a tile per warp (4 requests of up to 131072 tokens: 14 parts
@@ -379,14 +387,11 @@ Plan make_plan(int B, int Hq, int Hkv, int window, int sinks, int max_ctx) {
     const int G = Hq / Hkv;
     p.groups = (G + 7) / 8;
     p.heads = (G + p.groups - 1) / p.groups;
-    const int64_t tiles = std::min<int64_t>(((int64_t)max_ctx + kTile - 1) / kTile,
-                                            ((int64_t)window + kTile - 1) / kTile + 1 +
-                                                ((int64_t)sinks + kTile - 1) / kTile);
-    const int64_t units = (int64_t)B * Hkv * p.groups, places = 152 * kResident;
+    const int64_t tiles = visible_tiles(window, sinks, max_ctx), units = (int64_t)B * Hkv * p.groups;
     auto equal = [&](int64_t parts) { return ((tiles + parts - 1) / parts + kWarps - 1) / kWarps * kWarps; };
-    int64_t chunk = equal((tiles + 95) / 96);
-    const int64_t splits = places / std::max<int64_t>(units, 1);
-    if (5 * units * splits >= 4 * places) {
+    int64_t chunk = equal((tiles + kMostTiles - 1) / kMostTiles);
+    const int64_t splits = kPlaces / std::max<int64_t>(units, 1);
+    if (5 * units * splits >= 4 * kPlaces) {
         chunk = equal(splits);
     } else if (units > kMaxCounters) {
         chunk = tiles;
@@ -404,10 +409,17 @@ cudaError_t launch_t(const DecodeArgs& p, cudaStream_t st) {
 
 }  // namespace
 
+// Enough for every smaller call too: parts of the plans of up to B requests and of this visible
+// length or less.  Blocks in one wave are at most the card's places, and a warp has a tile at
+// least; otherwise parts are equal, and as many as blocks of kMostTiles.
 uint64_t window_decode_scratch(int B, int Hq, int Hkv, int d, int window, int sinks, int max_ctx) {
     const Plan p = make_plan(B, Hq, Hkv, window, sinks, max_ctx);
-    uint64_t n = kCounterBytes;
-    if (p.splits > 1) n += (uint64_t)B * Hkv * p.groups * p.splits * p.heads * (d + 2) * sizeof(float);
+    const int64_t tiles = visible_tiles(window, sinks, max_ctx), units = (int64_t)B * Hkv * p.groups;
+    int64_t parts = 0;
+    if (tiles > kWarps) parts = std::min<int64_t>(kPlaces, units * ((tiles + kWarps - 1) / kWarps));
+    if (tiles > kMostTiles)
+        parts = std::max(parts, std::min<int64_t>(units, kMaxCounters) * ((tiles + kMostTiles - 1) / kMostTiles));
+    const uint64_t n = kCounterBytes + (uint64_t)parts * p.heads * (d + 2) * sizeof(float);
     return (n + 15) / 16 * 16;
 }
 

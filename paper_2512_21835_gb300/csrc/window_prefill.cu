@@ -1103,6 +1103,12 @@ struct Plan {
     int64_t tiles;  // of one row tile per block, over all prompts and units
 };
 
+// Pages that a row tile of `tok` positions sees, at most.
+int64_t visible_pages(int tok, int window, int sinks, int max_ctx) {
+    return std::min<int64_t>(((int64_t)max_ctx + KT - 1) / KT,
+                             ((int64_t)window + tok + KT - 1) / KT + 1 + ((int64_t)sinks + KT - 1) / KT);
+}
+
 // A row tile is split when there are fewer row tiles than SMs, into parts of two pages
 // (one per stream) or more.
 Plan make_plan(int M, int n_prompts, int Hq, int Hkv, int window, int sinks, int max_ctx) {
@@ -1112,8 +1118,7 @@ Plan make_plan(int M, int n_prompts, int Hq, int Hkv, int window, int sinks, int
     p.heads = (G + p.groups - 1) / p.groups;
     p.tok = 128 / p.heads;
     p.tiles = std::min<int64_t>((int64_t)M / p.tok + n_prompts, M) * Hkv * p.groups;
-    const int64_t pages = std::min<int64_t>(((int64_t)max_ctx + KT - 1) / KT,
-                                            ((int64_t)window + p.tok + KT - 1) / KT + 1 + ((int64_t)sinks + KT - 1) / KT);
+    const int64_t pages = visible_pages(p.tok, window, sinks, max_ctx);
     p.splits = p.tiles < kSms ? (int)std::max<int64_t>(1, std::min<int64_t>(kSms / std::max<int64_t>(p.tiles, 1), pages / 2)) : 1;
     return p;
 }
@@ -1148,11 +1153,15 @@ cudaError_t launch_d(const PrefillArgs& p, bool f32, int64_t tiles, cudaStream_t
 
 }  // namespace
 
+// Enough for every smaller call too: a call's row tiles are split into kSms parts at most, of two
+// pages or more.
 uint64_t window_prefill_scratch(int M, int n_prompts, int Hq, int Hkv, int d, int window, int sinks, int max_ctx) {
     if (M == 0) return 16;
     const Plan p = make_plan(M, n_prompts, Hq, Hkv, window, sinks, max_ctx);
-    if (p.splits == 1) return 16;
-    const uint64_t n = kCounterBytes + p.tiles * (16 + (uint64_t)p.splits * (128 * (d + 2) * sizeof(float) + sizeof(unsigned)));
+    const int64_t most = visible_pages(p.tok, window, sinks, max_ctx) / 2;  // parts of a row tile
+    if (most < 2) return 16;
+    const uint64_t parts = std::min<int64_t>(kSms, p.tiles * most), tiles = std::min<int64_t>(kSms, p.tiles);
+    const uint64_t n = kCounterBytes + tiles * 16 + parts * (128 * (d + 2) * sizeof(float) + sizeof(unsigned));
     return (n + 15) / 16 * 16;
 }
 

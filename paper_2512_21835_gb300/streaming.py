@@ -97,7 +97,7 @@ class WindowedDecoder:
         self.kv = torch.empty(n_pages * page_bytes, dtype=torch.uint8, device="cuda")
         heads = (m["n_heads"], m["n_kv_heads"], d, window, sinks, max_ctx)
         need = max(loip.loip_k_window_attention_scratch_bytes(batch, *heads),
-                   max(loip.loip_k_window_prefill_scratch_bytes(r, batch, *heads) for r in range(1, chunk + 1)))
+                   loip.loip_k_window_prefill_scratch_bytes(chunk, 1, *heads))
         self.scratch = torch.zeros(need, dtype=torch.uint8, device="cuda")
         self.pos = [0] * batch
 
