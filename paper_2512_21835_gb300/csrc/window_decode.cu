@@ -367,7 +367,9 @@ __global__ void __launch_bounds__(kThreads, kResident) window_decode_kernel(cons
 }
 
 constexpr int kPlaces = 152 * kResident;
-constexpr int kMostTiles = 96;  // per block, without whole waves
+constexpr int kMostTiles = 96;    // per block, without whole waves
+constexpr int kWaveTiles = 384;   // per block with them, unless
+constexpr int kWaveBlocks = 76;   // a request alone has that many blocks
 
 int64_t visible_tiles(int window, int sinks, int max_ctx) {
     return std::min<int64_t>(((int64_t)max_ctx + kTile - 1) / kTile, ((int64_t)window + kTile - 1) / kTile + 1 +
@@ -379,9 +381,15 @@ int64_t visible_tiles(int window, int sinks, int max_ctx) {
 // waves, few joins, down to a tile per warp (4 requests of up to 131072 tokens: 14 parts
 // each, 251 us, 267 us with blocks of 48 tiles; 8 requests of up to 1028: 12.9 us, 20.7 us
 // with blocks of 4; one of 1088, 17 parts: 8.8 us, in nine 9.3 us, though 8.1 and 7.7 us in
-// a graph).  Otherwise a unit's tiles are cut into equal blocks of at most 96
-// (32 requests of 4160 positions: three blocks of 88 tiles, 87 us; one of 264, 102 us; five
-// of 64 and a remainder, 93 us).
+// a graph).  But the lengths are on the device, and what is one wave of equal requests is a
+// few blocks at work when one is long and the others are short.  So a wave's blocks have at
+// most 384 tiles, or a request alone has blocks for half of the SMs (48 requests, one of
+// 131072 tokens among 1000: 139 us, 2150 us unsplit; 8: 102 and 371 us; the price: 8 of 65536
+// each 333 us, 312 in one wave, 57 of 16384 565 and 546 us; 48 of 4160 stay one wave, 123 us,
+// 135 us with blocks of 88).
+// Otherwise a unit's tiles are cut into equal blocks of at most 96 (32 requests of 4160
+// positions: three blocks of 88 tiles, 87 us; one of 264, 102 us; five of 64 and a remainder,
+// 93 us).
 Plan make_plan(int B, int Hq, int Hkv, int window, int sinks, int max_ctx) {
     Plan p{};
     const int G = Hq / Hkv;
@@ -391,9 +399,10 @@ Plan make_plan(int B, int Hq, int Hkv, int window, int sinks, int max_ctx) {
     auto equal = [&](int64_t parts) { return ((tiles + parts - 1) / parts + kWarps - 1) / kWarps * kWarps; };
     int64_t chunk = equal((tiles + kMostTiles - 1) / kMostTiles);
     const int64_t splits = kPlaces / std::max<int64_t>(units, 1);
-    if (5 * units * splits >= 4 * kPlaces) {
+    if (5 * units * splits >= 4 * kPlaces &&
+        (equal(splits) <= kWaveTiles || splits * Hkv * p.groups >= kWaveBlocks)) {
         chunk = equal(splits);
-    } else if (units > kMaxCounters) {
+    } else if (units > kMaxCounters) {  // no counter for each: unsplit, and far more units than places
         chunk = tiles;
     }
     p.chunk = (int)std::max<int64_t>(chunk, 1);
