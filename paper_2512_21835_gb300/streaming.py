@@ -28,7 +28,7 @@ class PagePool:
     """Pages of a cache shared by several requests, and their page table (host side)."""
 
     def __init__(self, n_pages: int, requests: int, max_ctx: int, page_bytes: int):
-        self.page_bytes = page_bytes
+        self.page_bytes, self.max_ctx = page_bytes, max_ctx
         self.max_pages = -(-max_ctx // PAGE)
         self.free = list(range(n_pages - 1, -1, -1))
         self.table = np.zeros((requests, self.max_pages), dtype=np.int64)  # byte offsets; 0 where no page is held
@@ -36,7 +36,10 @@ class PagePool:
         self.most = 0
 
     def extend(self, request: int, first: int, last: int) -> None:
-        """Pages for the positions first .. last of a request."""
+        """Pages for the positions first .. last of a request.  (The last page may have room past max_ctx, but
+        the attention reads no key there.)"""
+        if last >= self.max_ctx:
+            raise ValueError(f"position {last} of request {request}: the context is {self.max_ctx} tokens")
         for i in range(first // PAGE, last // PAGE + 1):
             if i in self.held[request]:
                 continue
@@ -173,9 +176,17 @@ class WindowedDecoder:
                          scratch)
         return z, logits, tokens
 
+    def _room(self, more):
+        """Refuses tokens past the context before anything is enqueued for any of them."""
+        for r, n in more:
+            if self.pos[r] + n > self.max_ctx:
+                raise ValueError(f"request {r} holds {self.pos[r]} tokens: no room for {n} more in a context of "
+                                 f"{self.max_ctx}")
+
     def prefill(self, request: int, prompt):
         """Takes a prompt in chunks; returns (hidden, logits, token) after its last token."""
         prompt = [int(t) for t in prompt]
+        self._room([(request, len(prompt))])
         for lo in range(0, len(prompt), self.chunk):
             part = prompt[lo:lo + self.chunk]
             first = self.pos[request]
@@ -187,6 +198,7 @@ class WindowedDecoder:
 
     def step(self, tokens):
         """One token of every request; returns (hidden, logits, next tokens)."""
+        self._room([(r, 1) for r in range(len(self.pos))])
         rows = []
         for r, p in enumerate(self.pos):
             self.pool.extend(r, p, p)

@@ -1,0 +1,54 @@
+"""What windowed generation refuses (host only: the passes over the layers are stand-ins)."""
+import pytest
+
+from paper_2512_21835_gb300.streaming import PAGE, PagePool, WindowedDecoder
+
+
+class Decoder(WindowedDecoder):
+    """Bookkeeping alone: a pass records its rows."""
+
+    def __init__(self, batch, max_ctx, chunk=256, window=100, sinks=4, vocab=50):
+        self.m = dict(vocab=vocab)
+        self.window, self.sinks, self.max_ctx, self.chunk = window, sinks, max_ctx, chunk
+        self.pool = PagePool(1000, batch, max_ctx, 4096)
+        self.pos, self.passes = [0] * batch, []
+
+    def _rows(self, tokens, rows, single):
+        self.passes.append((list(tokens), rows))
+        return [None] * len(rows)
+
+    def _head(self, x):
+        return x
+
+
+@pytest.mark.parametrize("max_ctx", [1000, 1024, 65, 1])
+def test_no_position_reaches_the_end_of_the_context(max_ctx):
+    """The last page may have room past max_ctx; positions there would be appended and never read."""
+    d = Decoder(2, max_ctx)
+    d.prefill(0, [1] * max_ctx)
+    with pytest.raises(ValueError):
+        d.prefill(0, [1])
+    if max_ctx > 1:
+        d.prefill(1, [1] * (max_ctx - 1))
+        with pytest.raises(ValueError):
+            d.prefill(1, [1, 1])
+    n = len(d.passes)
+    with pytest.raises(ValueError):
+        d.step([1, 1])
+    assert len(d.passes) == n and d.pos == [max_ctx, max(max_ctx - 1, 0)]
+    assert max(p for _, rows in d.passes for _, p in rows) == max_ctx - 1
+
+
+def test_a_prompt_too_long_takes_no_pass():
+    d = Decoder(1, 1000, chunk=64)
+    with pytest.raises(ValueError):
+        d.prefill(0, [1] * 1001)
+    assert not d.passes and d.pos == [0] and not d.pool.held[0]
+
+
+def test_the_pool_refuses_positions_past_the_context():
+    pool = PagePool(100, 1, 1000, 4096)
+    pool.extend(0, 0, 999)
+    with pytest.raises(ValueError):
+        pool.extend(0, 1000, 1000)
+    assert len(pool.held[0]) == -(-1000 // PAGE)
