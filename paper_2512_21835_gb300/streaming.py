@@ -176,17 +176,26 @@ class WindowedDecoder:
                          scratch)
         return z, logits, tokens
 
-    def _room(self, more):
-        """Refuses tokens past the context before anything is enqueued for any of them."""
+    def _take(self, tokens, more):
+        """The tokens as whole numbers.  Refuses, before anything is enqueued for any of them, tokens that the
+        vocabulary or the context has no place for; more: (request, how many of the tokens)."""
+        tokens = [int(t) for t in tokens]
         for r, n in more:
+            if not 0 <= r < len(self.pos):
+                raise ValueError(f"request {r} of {len(self.pos)}")
             if self.pos[r] + n > self.max_ctx:
                 raise ValueError(f"request {r} holds {self.pos[r]} tokens: no room for {n} more in a context of "
                                  f"{self.max_ctx}")
+        if not tokens or len(tokens) != sum(n for _, n in more):
+            raise ValueError(f"{len(tokens)} tokens for {sum(n for _, n in more)} rows")
+        if min(tokens) < 0 or max(tokens) >= self.m["vocab"]:
+            raise ValueError(f"tokens {min(tokens)} to {max(tokens)} of a vocabulary of {self.m['vocab']}")
+        return tokens
 
     def prefill(self, request: int, prompt):
         """Takes a prompt in chunks; returns (hidden, logits, token) after its last token."""
-        prompt = [int(t) for t in prompt]
-        self._room([(request, len(prompt))])
+        prompt = list(prompt)
+        prompt = self._take(prompt, [(request, len(prompt))])
         for lo in range(0, len(prompt), self.chunk):
             part = prompt[lo:lo + self.chunk]
             first = self.pos[request]
@@ -198,7 +207,7 @@ class WindowedDecoder:
 
     def step(self, tokens):
         """One token of every request; returns (hidden, logits, next tokens)."""
-        self._room([(r, 1) for r in range(len(self.pos))])
+        tokens = self._take(tokens, [(r, 1) for r in range(len(self.pos))])
         rows = []
         for r, p in enumerate(self.pos):
             self.pool.extend(r, p, p)

@@ -52,3 +52,24 @@ def test_the_pool_refuses_positions_past_the_context():
     with pytest.raises(ValueError):
         pool.extend(0, 1000, 1000)
     assert len(pool.held[0]) == -(-1000 // PAGE)
+
+
+@pytest.mark.parametrize("tokens", [[], [1], [1, 1, 1], [1, 50], [-1, 1]])
+def test_steps_take_a_token_of_the_vocabulary_for_each_request(tokens):
+    """More tokens than rows, or a token outside the table, would be read and written out of range."""
+    d = Decoder(2, 1000)
+    d.prefill(0, [1, 2])
+    n = len(d.passes)
+    with pytest.raises(ValueError):
+        d.step(tokens)
+    assert len(d.passes) == n and d.pos == [2, 0]
+    d.step([0, 49])
+    assert d.pos == [3, 1]
+
+
+@pytest.mark.parametrize("request_, prompt", [(0, []), (0, [50]), (0, [3, -1]), (2, [1]), (-1, [1])])
+def test_prompts_are_of_the_vocabulary_and_of_a_request(request_, prompt):
+    d = Decoder(2, 1000)
+    with pytest.raises(ValueError):
+        d.prefill(request_, prompt)
+    assert not d.passes and d.pos == [0, 0]
