@@ -60,6 +60,11 @@ class PagePool:
         return len(gone)
 
 
+def pages_of_a_request(window: int, sinks: int, max_ctx: int, chunk: int) -> int:
+    """Pages that the window, the sinks and a chunk can touch, and no more than the context has."""
+    return min(-(-sinks // PAGE) + (window + chunk) // PAGE + 2, -(-max_ctx // PAGE))
+
+
 class WindowedDecoder:
     """Greedy decoding of a resident model behind a sliding window with sinks."""
 
@@ -94,8 +99,8 @@ class WindowedDecoder:
         # a page holds every layer's keys and values of 64 tokens
         self.layer_page_bytes = 2 * m["n_kv_heads"] * PAGE * d * 2
         page_bytes = m["n_layers"] * self.layer_page_bytes
-        if n_pages is None:  # what the window, the sinks and a chunk can touch
-            n_pages = batch * (-(-sinks // PAGE) + (window + chunk) // PAGE + 2)
+        if n_pages is None:
+            n_pages = batch * pages_of_a_request(window, sinks, max_ctx, chunk)
         self.pool = PagePool(n_pages, batch, max_ctx, page_bytes)
         self.kv = torch.empty(n_pages * page_bytes, dtype=torch.uint8, device="cuda")
         heads = (m["n_heads"], m["n_kv_heads"], d, window, sinks, max_ctx)

@@ -1,7 +1,7 @@
 """What windowed generation refuses (host only: the passes over the layers are stand-ins)."""
 import pytest
 
-from paper_2512_21835_gb300.streaming import PAGE, PagePool, WindowedDecoder
+from paper_2512_21835_gb300.streaming import PAGE, PagePool, WindowedDecoder, pages_of_a_request
 
 
 class Decoder(WindowedDecoder):
@@ -73,3 +73,19 @@ def test_prompts_are_of_the_vocabulary_and_of_a_request(request_, prompt):
     with pytest.raises(ValueError):
         d.prefill(request_, prompt)
     assert not d.passes and d.pos == [0, 0]
+
+
+@pytest.mark.parametrize("window,sinks,max_ctx,chunk", [(1 << 20, 0, 1000, 256), (1 << 30, 1 << 30, 128, 64), (100, 4, 420, 70),
+                                                        (64, 0, 3000, 1), (130, 70, 5000, 256), (1, 0, 64, 1), (0, 0, 65, 32)])
+def test_pages_of_a_request(window, sinks, max_ctx, chunk):
+    """Enough for a whole context taken in chunks, then token by token; never more than the context has."""
+    n = pages_of_a_request(window, sinks, max_ctx, chunk)
+    assert 1 <= n <= -(-max_ctx // PAGE)
+    for prompt in {0, max_ctx // 3, max_ctx}:
+        d = Decoder(1, max_ctx, chunk, window, sinks)
+        d.pool = PagePool(n, 1, max_ctx, 4096)
+        if prompt:
+            d.prefill(0, [1] * prompt)
+        for _ in range(max_ctx - prompt):
+            d.step([1])
+        assert d.pool.most <= n
