@@ -476,7 +476,9 @@ int loip_k_prefill_attention(const float* q, const void* kv_base, const int64_t*
                              void* tiles, uint16_t* o2, void* stream);
 
 /* 0 if no tensor-core attention launch (this one and loip_k_window_prefill) has
- * recorded a failure (a bounded wait that ran out); otherwise the first failure code.  -1 if unreadable. */
+ * recorded a failure (a bounded wait that ran out; loip_k_window_prefill then
+ * leaves the rows concerned as they were); otherwise the first failure code.
+ * -1 if unreadable.  Reading waits for the device. */
 int loip_k_attention_tc_status(void);
 
 /* x += wo o  (output projection with the residual add); o fp32 [B, Hq*d].  As in

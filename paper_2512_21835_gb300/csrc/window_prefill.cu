@@ -65,6 +65,7 @@
 
 #include "internal.h"
 #include "window.h"
+#include "window_parts.h"
 
 namespace loip {
 
@@ -125,7 +126,7 @@ struct PrefillArgs {
     float4* part;       // [unit][split][d / 4][128 rows], not normalised
     int4* rows;         // [unit]: first row, tokens, request, position of the first
     float2* ml;         // [unit][split][128 rows]: maximum (log2), sum
-    unsigned* flagged;  // [unit][split]: whether the block met values that are not finite
+    unsigned* ended;    // [unit][split]: PartEnd
 };
 
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -155,8 +156,10 @@ __device__ __forceinline__ bool bar_try(uint32_t b, uint32_t parity) {
 }
 // A thread's waits.  One that runs out (2 s), or the flag of another thread's that did,
 // ends all further ones: the thread goes on to its end with whatever it finds, within
-// its own buffers, and nothing it makes is stored.  (No way out in between: a warp stays
-// together, and the code of a wait is one instruction and a branch.)
+// its own buffers.  (No way out in between: a warp stays together, and the code of a wait is
+// one instruction and a branch.)  From then on the block stores no row of o (`stopped`, asked
+// behind a barrier that the waiting threads have passed), and for a split row tile the kernel
+// that joins the parts stores none either (`ended`): those rows stay as they were.
 struct Waiter {
     Ctl* c;
     bool dead;
@@ -476,6 +479,7 @@ __global__ void __launch_bounds__(kThreads, 1) window_prefill_kernel(const __gri
     };
 
     Waiter wait{c, false};
+    auto stopped = [&] { return *(volatile int*)&c->abort != 0; };
     if (warp >= 8) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
         if (warp < 10) {
@@ -938,7 +942,7 @@ __global__ void __launch_bounds__(kThreads, 1) window_prefill_kernel(const __gri
                 asm volatile("bar.sync 1, 128;" ::: "memory");
             else
                 asm volatile("bar.sync 2, 128;" ::: "memory");
-            if (!wait.dead) leave(r, 128);
+            if (!stopped()) leave(r, 128);
         } else {
             // ---- join the streams through the ring, which nothing uses any more once both streams'
             // last products are complete: each gives the other half of its columns
@@ -997,7 +1001,7 @@ __global__ void __launch_bounds__(kThreads, 1) window_prefill_kernel(const __gri
             else finish(std::integral_constant<int, 1>{}, keep, take, inv);
             if (p.splits == 1) {
                 asm volatile("bar.sync 1, 256;" ::: "memory");
-                if (!wait.dead) leave(tid, 256);
+                if (!stopped()) leave(tid, 256);
             }
         }
     } else {
@@ -1010,13 +1014,13 @@ __global__ void __launch_bounds__(kThreads, 1) window_prefill_kernel(const __gri
         fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
     }
-    const bool bad = c->bad && !c->abort;
+    const unsigned end = part_end(stopped(), c->bad != 0);
     if (QT == 1 && p.splits > 1) {
         if (tid == 0) {
-            p.flagged[unit * p.splits + split] = bad;
+            p.ended[unit * p.splits + split] = end;
             if (split == 0) p.rows[unit] = make_int4(row0, tokens, req, pos0);
         }
-    } else if (bad && warp < 8) {
+    } else if (end == kPartNotFinite && warp < 8) {
         for (int i = warp; i < tokens * heads; i += 8) {
             const int64_t at = ((int64_t)(row0 + i / heads) * a.Hq + kvh * G + head0 + i % heads) * D;
             walk_row<D, T>(a, req, kvh, pos0 + i / heads, static_cast<const T*>(a.q) + at, static_cast<T*>(a.o) + at);
@@ -1038,9 +1042,10 @@ __global__ void __launch_bounds__(256) window_join_kernel(const __grid_constant_
     const int G = a.Hq / a.Hkv, heads = min(p.heads, G - head0);
     const int4 rows = __ldcg(p.rows + unit);  // first row, tokens, request, position
     const int tk = r / heads;
-    bool bad = false;
-    for (int x = 0; x < p.splits; ++x) bad |= __ldcg(p.flagged + unit * p.splits + x) != 0;
-    if (bad) {  // as without splits; the unit's blocks share the rows
+    unsigned end = kPartGood;
+    for (int x = 0; x < p.splits; ++x) end = worse(end, __ldcg(p.ended + unit * p.splits + x));
+    if (end == kPartStopped) return;
+    if (end == kPartNotFinite) {  // as without splits; the unit's blocks share the rows
         const int warp = threadIdx.x / 32 + blockIdx.x % PIECES * 8;
         for (int i = warp; i < rows.y * heads; i += 8 * PIECES) {
             const int64_t at = ((int64_t)(rows.x + i / heads) * a.Hq + kvh * G + head0 + i % heads) * D;
@@ -1179,7 +1184,7 @@ cudaError_t launch_window_prefill(const WindowArgs& a, bool f32, cudaStream_t st
     p.part = reinterpret_cast<float4*>(static_cast<char*>(a.scratch) + kCounterBytes);
     p.rows = reinterpret_cast<int4*>(p.part + plan.tiles * plan.splits * 128 * (a.d / 4));
     p.ml = reinterpret_cast<float2*>(p.rows + plan.tiles);
-    p.flagged = reinterpret_cast<unsigned*>(p.ml + plan.tiles * plan.splits * 128);
+    p.ended = reinterpret_cast<unsigned*>(p.ml + plan.tiles * plan.splits * 128);
     return a.d == 128 ? launch_d<128>(p, f32, plan.tiles, st) : launch_d<64>(p, f32, plan.tiles, st);
 }
 
