@@ -208,7 +208,11 @@ class WindowedDecoder:
             x = self._rows(part, [(request, first + i) for i in range(len(part))], single=False)
             self.pos[request] += len(part)
             self.pool.retire(request, self.pos[request], self.window, self.sinks)
-        return self._head(x[-1:])
+        out = self._head(x[-1:])
+        code = self.L.loip_k_attention_tc_status()
+        if code:
+            raise RuntimeError(f"the prompt attention gave up on a wait (code {code}): its rows are not complete")
+        return out
 
     def step(self, tokens):
         """One token of every request; returns (hidden, logits, next tokens)."""

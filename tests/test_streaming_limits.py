@@ -1,4 +1,6 @@
 """What windowed generation refuses (host only: the passes over the layers are stand-ins)."""
+from types import SimpleNamespace
+
 import pytest
 
 from paper_2512_21835_gb300.streaming import PAGE, PagePool, WindowedDecoder, pages_of_a_request
@@ -12,6 +14,7 @@ class Decoder(WindowedDecoder):
         self.window, self.sinks, self.max_ctx, self.chunk = window, sinks, max_ctx, chunk
         self.pool = PagePool(1000, batch, max_ctx, 4096)
         self.pos, self.passes = [0] * batch, []
+        self.L = SimpleNamespace(loip_k_attention_tc_status=lambda: 0)
 
     def _rows(self, tokens, rows, single):
         self.passes.append((list(tokens), rows))
@@ -89,3 +92,11 @@ def test_pages_of_a_request(window, sinks, max_ctx, chunk):
         for _ in range(max_ctx - prompt):
             d.step([1])
         assert d.pool.most <= n
+
+
+@pytest.mark.parametrize("code", [6, -1])
+def test_a_prompt_whose_attention_gave_up_is_an_error(code):
+    d = Decoder(1, 1000)
+    d.L.loip_k_attention_tc_status = lambda: code
+    with pytest.raises(RuntimeError, match="gave up"):
+        d.prefill(0, [1] * 40)
