@@ -562,12 +562,17 @@ uint64_t loip_k_lm_head_scratch_bytes(int32_t B, int32_t V);
  * Cache layout and page table as for loip_k_attention (page_tokens = 64; page
  * offsets, kv_base and layer_page_bytes multiples of 16).  `dtype` is the type
  * of the activations (queries in, outputs out): LOIP_F32 or LOIP_BF16; sums,
- * softmax states and norms are fp32, an fp32 query is not rounded on its way to
- * the tensor cores, and each output is rounded once.  d = 64 or 128; any
- * Hq / Hkv.  Zero rows are allowed and launch nothing.  Every call is async on
- * `stream`, allocates nothing and can be captured in a CUDA graph; a refusal
- * (LOIP_ERR_INVALID, message in loip_last_error(NULL)) comes before anything
- * is enqueued.
+ * softmax states and norms are fp32, and each output is rounded once.  With fp32
+ * rows neither queries nor softmax weights are rounded on their way to the tensor
+ * cores; with bf16 rows the weights are: to 2^-16 for single tokens, to bf16 (2^-9)
+ * for prompts, whose outputs are off by 0.0021 of their size (root mean square)
+ * instead of the 0.0017 of their own rounding (a caller who wants more passes
+ * fp32 rows).  An infinity that a row sees answers as by the definition, its
+ * weights being fp32 numbers (one below their range is zero, and 0 x inf NaN).
+ * d = 64 or 128; any Hq / Hkv.  Zero rows are allowed and launch nothing.  Every
+ * call is async on `stream`, allocates nothing and can be captured in a CUDA graph;
+ * a refusal (LOIP_ERR_INVALID, message in loip_last_error(NULL)) comes before
+ * anything is enqueued.
  * ------------------------------------------------------------------------- */
 enum { LOIP_F32 = 0, LOIP_BF16 = 1 };
 

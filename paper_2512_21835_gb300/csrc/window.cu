@@ -22,10 +22,11 @@ namespace {
 // (y_i, y_{i + d/2}) turns by position * theta^(-2i/d).
 //
 // The angle is kept in turns, as a 64-bit fixed-point fraction: turn_i =
-// theta^(-2i/d) / (2 pi) rounded to 2^-64, and position * turn_i modulo 2^64 is
-// the fraction of a turn itself -- one integer product, exact up to position *
-// 2^-65, where a floating-point angle would have to be reduced modulo 2 pi.  Its
-// top 32 bits, as a signed number, are an angle in [-pi, pi) for sincospif.
+// theta^(-2i/d) / (2 pi), and position * turn_i modulo 2^64 is the fraction of a
+// turn itself -- one integer product, with nothing to be reduced modulo 2 pi.
+// turn_i is made in fp64 and is off by less than 2^-54 of a turn, the angle by less
+// than position * 2^-54.  Its top 32 bits, as a signed number, are an angle in
+// [-pi, pi) for sincospif.
 // ---------------------------------------------------------------------------
 struct RopeTurns {
     uint64_t turn[64];
@@ -99,8 +100,9 @@ __device__ __forceinline__ void store8(__nv_bfloat16* p, const float (&v)[8]) {
 // A block takes a group of heads of one token; D / 16 lanes per head, each holding the
 // elements 8l .. 8l + 7 of the head and their partners D / 2 further on.  Bound by memory:
 // short blocks with all their loads issued at once, the gains' among them, and as many of
-// them per SM as the registers can be held to.  8191 fp32 tokens of 120 heads of 128: 121
-// us, 6.9 TB/s; 1999 bf16 tokens of 80 heads, with norms: 15.1 us, 5.4 TB/s (each before
+// them per SM as the registers can be held to (bf16: 32, which costs 16 bytes of spills, 2.5
+// stores and half a load per warp).  8191 fp32 tokens of 120 heads of 128: 121 us, 6.9 TB/s;
+// 1999 bf16 tokens of 80 heads, with norms: 15.2 us, 5.4 TB/s (each before
 // the bank conflicts went: eight blocks per SM 18.3, six 20.7, two tokens per block 19.9,
 // one wave of blocks that walk over the tokens with the next one's loads in flight 28.7).
 template <int D, typename T>

@@ -1,4 +1,5 @@
-// window.h -- what the windowed-serving operators share (window.cu, window_tc.cu).
+// window.h -- what the windowed-serving operators share (window.cu, window_decode.cu,
+// window_prefill.cu).
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>

@@ -24,10 +24,11 @@
 // fp32 (the MMA's own sums truncate: 4e-6 over 150 tiles).  bf16 activations: one MMA for
 // the scores, two planes of the weights (2^-16; the second costs 1%).
 //
-// Measured (GB300): 64 requests behind a 4096-token window, 64 heads of 128: 175 us, 6.0
-// TB/s; 4 requests of up to 131072 tokens, 32 heads: 253 us, 6.2 TB/s (bound by memory); 8
-// fp32 requests of up to 1028: 12.9 us, one request of 1088: 7.7 us (a chain of latencies:
-// length, page table, keys, join).
+// Measured (GB300, in a graph): 64 requests behind a 4096-token window, 64 heads of 128: 175
+// us, 6.0 TB/s (fp32 183, 5.7 TB/s; heads of 64 95, 5.5 TB/s); 4 requests of up to 131072
+// tokens, 32 heads: 251 us, 6.2 TB/s (fp32 276), bound by memory; 8 fp32 requests of up to
+// 1028: 13.1 us, one request of 1088: 7.6 us (a chain of latencies: length, page table, keys,
+// join).
 //
 // Masked positions are neither loaded nor multiplied: their key and value registers
 // are zero, whatever the cache holds there.
@@ -380,8 +381,8 @@ int64_t visible_tiles(int window, int sinks, int max_ctx) {
 // fifths of the places that the card has for blocks, or more, all blocks run at once: whole
 // waves, few joins, down to a tile per warp (4 requests of up to 131072 tokens: 14 parts
 // each, 251 us, 267 us with blocks of 48 tiles; 8 requests of up to 1028: 12.9 us, 20.7 us
-// with blocks of 4; one of 1088, 17 parts: 8.8 us, in nine 9.3 us, though 8.1 and 7.7 us in
-// a graph).  But the lengths are on the device, and what is one wave of equal requests is a
+// with blocks of 4; one of 1088 in 17 parts: 6.7 us a call and 7.6 in a graph, in nine parts
+// 6.7 and 6.9).  But the lengths are on the device, and what is one wave of equal requests is a
 // few blocks at work when one is long and the others are short.  So a wave's blocks have at
 // most 384 tiles, or a request alone has blocks for half of the SMs (48 requests, one of
 // 131072 tokens among 1000: 139 us, 2150 us unsplit; 8: 102 and 371 us; the price: 8 of 65536

@@ -31,12 +31,16 @@
 // Measured (GB300): 8192 bf16 rows of 32 heads of 128 behind a 4096-token window 444 us,
 // 1240 TFLOP/s, tensor pipe active 54%; bound by the chain from P of a tile to S of the
 // next but one (waits, issue and answer, 1700 cycles per tile of which the tensor core
-// works 1280).  4 x 512 fp32 rows of 64 heads 106 us: half of a block's time is its
-// queries, its join and its outputs.
+// works 1280).  4 x 512 fp32 rows of 64 heads 111 us: half of a block's time is its
+// queries, its join and its outputs.  8192 fp32 rows 1330 us.  The registers (168) do not
+// hold everything: in the tile loop a softmax warp reloads two or three spilled words a tile
+// and stores none.
 //
-// Precision.  bf16 rows: one MMA per product, weights rounded to bf16, O stays in
-// tensor memory; it is rescaled only when a row's maximum has grown by 2^8 (weights
-// are relative to an older maximum until then, exact in the end).  fp32 rows (NP = 3):
+// Precision.  bf16 rows: one MMA per product, weights rounded to bf16 (2^-9: the outputs are
+// off by 0.0021 of their size, of which their own rounding is 0.0017; a second plane would
+// double the MMAs of P V), O stays in tensor memory; it is rescaled only when a row's
+// maximum has grown by 2^8 (weights are relative to an older maximum until then, exact in
+// the end).  fp32 rows (NP = 3):
 // queries and weights are exact sums of three bf16 planes, three MMAs per product,
 // smallest plane first; the tensor core's sums truncate, so O of one key tile is
 // drained and added in fp32 registers.
