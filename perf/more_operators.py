@@ -6,11 +6,12 @@ elements.  A block has an exponent byte E and 32 code bytes, sign and 7-bit magn
   value = +-m 2^(E - 133),  m = rint(|x| 2^(133 - E)),
   E the smallest (and 8 at least) for which no magnitude of the block exceeds 127
 
-so that an element is off by half a step at most, and every value is a bf16 number.  E = 255
-stands for NaN in the whole block (it held something that is not finite).  Pages of 64 tokens are found through a
-page table; a layer's part of a page is [kv head][4 granules], a granule (16 tokens, 33 d bytes)
-is the codes of the keys [16][d], those of the values [16][d], the exponents of the keys
-[16][d / 32] and those of the values.  The 16-byte piece c of token t's codes lies at
+so that an element is off by half a step at most, and every value is a bf16 number.  E is at most
+253: a block that holds something that is not finite, or 127.5 2^120 (1.7e38) or more, is stored
+with E = 255, which stands for NaN in all its elements (as 254 would).  Pages of 64 tokens are
+found through a page table; a layer's part of a page is [kv head][4 granules], a granule (16
+tokens, 33 d bytes) is the codes of the keys [16][d], those of the values [16][d], the exponents
+of the keys [16][d / 32] and those of the values.  The 16-byte piece c of token t's codes lies at
 c ^ (t d / 128 % (d / 16)) in its row.
 
   store    norm of queries and keys for each head (optional), position rotation, the new keys
@@ -189,7 +190,7 @@ def _encode(x):
     _, e = torch.frexp(torch.where(most.isfinite(), most, 1.0))  # most = f 2^e with f in [1/2, 1)
     E = e + 126
     E = (E + (torch.ldexp(most, 133 - E) >= 127.5)).clamp(min=8)
-    bad = ~most.isfinite() | (E > 254)
+    bad = ~most.isfinite() | (E > 253)
     E = torch.where(bad, 255, E)
     m = torch.where(bad, 0.0, torch.ldexp(torch.where(bad, 0.0, b), 133 - E).round())
     codes = m.abs().to(torch.uint8) | ((m < 0).to(torch.uint8) << 7)
@@ -201,7 +202,7 @@ def _decode(codes, exps):
     m = (codes & 127).float()
     m = torch.where(codes > 127, -m, m)
     step = ((exps.int().clamp(min=7) - 6) << 23).view(torch.float32)  # the fp32 number 2^(E - 133)
-    step = torch.where(exps == 255, math.nan, step)
+    step = torch.where(exps >= 254, math.nan, step)
     return (m.unflatten(-1, (-1, BLOCK)) * step[..., None]).flatten(-2)
 
 
@@ -432,7 +433,7 @@ def _exact_rows(s, pages, pos, head, is_v):
     dev = pos.device
     bytes_ = s["kv"].view(-1)
     value = torch.tensor([c if c < 128 else 128 - c for c in range(256)], dtype=torch.float64, device=dev)
-    step = torch.tensor([2.0 ** (E - 133) for E in range(255)] + [math.nan], dtype=torch.float64, device=dev)
+    step = torch.tensor([2.0 ** (E - 133) for E in range(254)] + 2 * [math.nan], dtype=torch.float64, device=dev)
     start = ((pages * Hkv + head) * 4 + pos % 64 // 16) * (33 * d)
     t, i = (pos % 16)[:, None], torch.arange(d, device=dev)[None, :]
     code = start[:, None] + is_v * 16 * d + t * d + ((i // 16) ^ (t * d // 128 % (d // 16))) * 16 + i % 16
