@@ -631,6 +631,63 @@ int loip_k_window_prefill(const void* q, int32_t dtype, const void* kv_base, con
 uint64_t loip_k_window_prefill_scratch_bytes(int32_t M, int32_t n_prompts, int32_t Hq, int32_t Hkv, int32_t d,
                                              int32_t window, int32_t sinks, int32_t max_ctx);
 
+/* ---------------------------------------------------------------------------
+ * The same serving over a cache of 8 bits per element and an exponent per 32:
+ * 33 d bytes for 16 tokens' keys and values of a kv head, 33/64 of the bf16
+ * cache, with everything else as above (types, streams, graphs, refusals).
+ *
+ * A row (a token's key or value of one kv head) is d / 32 blocks of 32 elements.
+ * A block has an exponent byte E and 32 code bytes, a sign (the top bit) and a
+ * 7-bit magnitude m:  value = +-m 2^(E - 133),  m = rint(|x| 2^(133 - E)), E the
+ * smallest (and 8 at least) for which no m exceeds 127.  So an element is off by
+ * half a step at most, 1/127 of its block's largest one, and every value is a
+ * bf16 number.  E is 253 at most: a block with an element that is not finite, or
+ * of 127.5 2^120 (1.7e38) or more, is stored with E = 255, which like 254 stands
+ * for NaN in the whole block.
+ *
+ * A layer's part of a page (layer_page_bytes, Hkv * 132 * d at least) is
+ * [Hkv][4 granules]; a granule, 16 tokens, is the codes of the keys [16][d], the
+ * codes of the values [16][d], the exponents of the keys [16][d / 32] and those of
+ * the values.  The 16-byte piece c of token t's codes lies at
+ * c ^ (t d / 128 % (d / 16)) of its row.
+ * ------------------------------------------------------------------------- */
+
+/* loip_k_qk_append into the 8-bit cache: keys after norm and rotation, values as
+ * they come, each rounded once. */
+int loip_k_qk_append_q8(const void* qkv, int32_t dtype, int64_t row_stride, int32_t T, int32_t Hq, int32_t Hkv,
+                        int32_t d, const uint16_t* g_q, const uint16_t* g_k, float eps, float theta,
+                        const int32_t* positions, const int32_t* row_req, int32_t n_req, void* q_out, void* kv_base,
+                        const int64_t* page_offsets, int32_t max_pages, int32_t page_tokens, int32_t layer,
+                        uint64_t layer_page_bytes, void* stream);
+
+/* What the 8-bit cache holds, as numbers of type `dtype` (exact in both): row t of
+ * out ([T, 2 * Hkv * d], dense: key heads, value heads) is position positions[t] of
+ * request row_req[t] (of request t when row_req is NULL).  Rows of padding, as for
+ * the append, are zero. */
+int loip_k_cache_read_q8(const void* kv_base, const int64_t* page_offsets, int32_t max_pages,
+                         const int32_t* positions, const int32_t* row_req, int32_t n_req, int32_t T, int32_t Hkv,
+                         int32_t d, int32_t page_tokens, int32_t layer, uint64_t layer_page_bytes, void* out,
+                         int32_t dtype, void* stream);
+
+/* loip_k_window_attention and loip_k_window_prefill over the 8-bit cache.  A NaN that
+ * a row sees makes NaN of what it meets: a key's block the row's whole head, a
+ * value's block the 32 elements.  The scratch rules are the same, and one scratch
+ * serves the calls on both kinds of cache. */
+int loip_k_window_attention_q8(const void* q, int32_t dtype, const void* kv_base, const int64_t* page_offsets,
+                               int32_t max_pages, const int32_t* ctx_lens, int32_t B, int32_t Hq, int32_t Hkv,
+                               int32_t d, int32_t page_tokens, int32_t layer, uint64_t layer_page_bytes,
+                               int32_t window, int32_t sinks, int32_t max_ctx, void* scratch,
+                               uint64_t scratch_bytes, void* o, void* stream);
+uint64_t loip_k_window_attention_q8_scratch_bytes(int32_t B, int32_t Hq, int32_t Hkv, int32_t d, int32_t window,
+                                                  int32_t sinks, int32_t max_ctx);
+int loip_k_window_prefill_q8(const void* q, int32_t dtype, const void* kv_base, const int64_t* page_offsets,
+                             int32_t max_pages, const int32_t* row_starts, const int32_t* first_pos,
+                             int32_t n_prompts, int32_t M, int32_t Hq, int32_t Hkv, int32_t d, int32_t page_tokens,
+                             int32_t layer, uint64_t layer_page_bytes, int32_t window, int32_t sinks,
+                             int32_t max_ctx, void* scratch, uint64_t scratch_bytes, void* o, void* stream);
+uint64_t loip_k_window_prefill_q8_scratch_bytes(int32_t M, int32_t n_prompts, int32_t Hq, int32_t Hkv, int32_t d,
+                                                int32_t window, int32_t sinks, int32_t max_ctx);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,15 +1,18 @@
-// window.cu -- windowed serving over the paged cache: the append of new tokens
-// (norm of queries and keys for each head, position rotation, keys and values
-// into their pages) and the attention behind a sliding window with sinks.
+// window.cu -- windowed serving over the paged cache, in bf16 or in 8 bits: the append of
+// new tokens (norm of queries and keys for each head, position rotation, keys and values
+// into their pages), rows of the 8-bit cache read back, and the entries of the attention
+// behind a sliding window with sinks.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <math.h>
 #include <stdint.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "../../include/loip.h"
 #include "internal.h"
+#include "q8.h"
 #include "window.h"
 
 namespace loip {
@@ -105,7 +108,9 @@ __device__ __forceinline__ void store8(__nv_bfloat16* p, const float (&v)[8]) {
 // 1999 bf16 tokens of 80 heads, with norms: 15.2 us, 5.4 TB/s (each before
 // the bank conflicts went: eight blocks per SM 18.3, six 20.7, two tokens per block 19.9,
 // one wave of blocks that walk over the tokens with the next one's loads in flight 28.7).
-template <int D, typename T>
+//
+// Q8: keys and values go to the 8-bit cache (q8.h).  Four lanes hold the 32 elements of a block.
+template <int D, typename T, bool Q8>
 __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 8 : 6) qk_append_kernel(const __grid_constant__ AppendArgs p) {
     constexpr int LANES = D / 16;
     __shared__ float4 turn[4][LANES];  // cos, sin of elements 8l + 2k and 8l + 2k + 1 at [k][l]: no bank conflicts
@@ -162,7 +167,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 8 : 6) qk_append_kernel(
         }
     }
     if (!live) return;
-    if (!is_v) {
+    if (!is_v && p.rope.turn[0]) {  // (theta 0: no rotation, and no 0 x inf)
 #pragma unroll
         for (int i = 0; i < 8; i += 2) {
             const float4 cs = turn[i / 2][l];
@@ -181,7 +186,35 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 8 : 6) qk_append_kernel(
         }
         store8(o, a);
         store8(o + D / 2, b);
-    } else if (!padding) {
+    } else if (padding) {
+        return;
+    } else if constexpr (Q8) {
+        const unsigned four = 15u << (threadIdx.x % 32 / 4 * 4);
+        auto most_of = [&](const float (&v)[8]) {  // as bits, so that a NaN is the largest
+            uint32_t most = 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) most = max(most, __float_as_uint(v[i]) & 0x7fffffffu);
+            most = max(most, __shfl_xor_sync(four, most, 1));
+            return max(most, __shfl_xor_sync(four, most, 2));
+        };
+        using G = q8::Granule<D>;
+        const int token = pos % q8::kGranule, c = l / 2;
+        char* o = p.kv.base + page + (uint64_t)p.kv.layer * p.kv.layer_page_bytes +
+                  q8::granule_at<D>(head - p.Hq - (is_v ? p.Hkv : 0), pos);
+        auto put = [&](const float (&v)[8], int half) {
+            const uint32_t E = q8::exponent_of(most_of(v));
+            uint2 u = make_uint2(0u, 0u);
+            if (E != 255u) {
+                const float inv = q8::inverse_step(E);
+                u.x = q8::codes_of(v[0], v[1], v[2], v[3], inv);
+                u.y = q8::codes_of(v[4], v[5], v[6], v[7], inv);
+            }
+            *reinterpret_cast<uint2*>(o + G::piece(is_v, token, half * (D / 32) + c) + l % 2 * 8) = u;
+            if (l % 4 == 0) o[G::exponents(is_v, token) + half * (D / 64) + l / 4] = (char)E;
+        };
+        put(a, 0);
+        put(b, 1);
+    } else {
         // keys, then values, of the layer: [Hkv][64][D] each
         __nv_bfloat16* o =
             reinterpret_cast<__nv_bfloat16*>(p.kv.base + page + (uint64_t)p.kv.layer * p.kv.layer_page_bytes) +
@@ -192,19 +225,67 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 8 : 6) qk_append_kernel(
 }
 
 // Heads in equal groups of at most a block's 256 threads.
-template <int D, typename T>
+template <int D, typename T, bool Q8>
 cudaError_t launch_append(AppendArgs& a, cudaStream_t st) {
     constexpr int LANES = D / 16, MOST = 256 / LANES;
     const int heads = a.Hq + 2 * a.Hkv, groups = (heads + MOST - 1) / MOST;
     a.heads = (heads + groups - 1) / groups;
     const unsigned threads = std::max((a.heads * LANES + 31) / 32 * 32, D / 2);
-    return launch_pdl(qk_append_kernel<D, T>, dim3(a.rows, groups), threads, 0, st, a);
+    return launch_pdl(qk_append_kernel<D, T, Q8>, dim3(a.rows, groups), threads, 0, st, a);
+}
+
+// ---------------------------------------------------------------------------
+// Rows of the 8-bit cache as numbers.
+// ---------------------------------------------------------------------------
+struct ReadArgs {
+    const int32_t *positions, *row_req;
+    int rows, n_req, Hkv;
+    KvView kv;
+    void* out;  // [rows][keys, values][Hkv][d]
+};
+
+// A thread takes a piece (16 elements) of a row.
+template <int D, typename T>
+__global__ void __launch_bounds__(256) cache_read_kernel(const __grid_constant__ ReadArgs p) {
+    using G = q8::Granule<D>;
+    pdl_trigger();
+    pdl_wait();
+    const int per_row = 2 * p.Hkv * G::PIECES;
+    const int i = blockIdx.y * 256 + threadIdx.x, t = blockIdx.x;
+    if (i >= per_row) return;
+    const int is_v = i >= per_row / 2, head = i / G::PIECES - is_v * p.Hkv, c = i % G::PIECES;
+    const int pos = p.positions[t], req = p.row_req ? p.row_req[t] : t;
+    float v[16];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) v[e] = 0.f;
+    if (pos >= 0 && pos / kPageTokens < p.kv.max_pages && req >= 0 && req < p.n_req) {
+        const char* g = p.kv.base + p.kv.page_offsets[(int64_t)req * p.kv.max_pages + pos / kPageTokens] +
+                        (uint64_t)p.kv.layer * p.kv.layer_page_bytes + q8::granule_at<D>(head, pos);
+        const uint4 u = *reinterpret_cast<const uint4*>(g + G::piece(is_v, pos % q8::kGranule, c));
+        const float step = q8::step_of((uint8_t)g[G::exponents(is_v, pos % q8::kGranule) + c / 2]);
+        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+        for (int e = 0; e < 16; ++e) v[e] = q8::value_of(w[e / 4] >> (8 * (e % 4)) & 255u, step);
+    }
+    T* o = static_cast<T*>(p.out) + ((int64_t)t * per_row + i) * 16;
+#pragma unroll
+    for (int e = 0; e < 16; e += 8) {
+        float y[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) y[k] = v[e + k];
+        store8(o + e, y);
+    }
+}
+
+template <int D, typename T>
+cudaError_t launch_read(const ReadArgs& a, cudaStream_t st) {
+    return launch_pdl(cache_read_kernel<D, T>, dim3(a.rows, (2 * a.Hkv * (D / 16) + 255) / 256), 256, 0, st, a);
 }
 
 bool aligned(const void* p, uintptr_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
 
 // What every call on the cache has in common; null if it is in order.
-const char* cache_refusal(int dtype, int rows, int Hq, int Hkv, int d, const void* kv_base, const int64_t* page_offsets,
+const char* cache_refusal(bool q8, int dtype, int rows, int Hq, int Hkv, int d, const void* kv_base, const int64_t* page_offsets,
                           int max_pages, int page_tokens, int layer, uint64_t layer_page_bytes) {
     if (dtype != LOIP_F32 && dtype != LOIP_BF16) return "dtype is LOIP_F32 or LOIP_BF16";
     if (rows < 0) return "a negative number of rows";
@@ -215,6 +296,7 @@ const char* cache_refusal(int dtype, int rows, int Hq, int Hkv, int d, const voi
     if (max_pages < 1 || layer < 0) return "no pages, or a negative layer";
     if (!kv_base || !aligned(kv_base, 16) || layer_page_bytes % 16) return "the cache is 16-byte aligned";
     if (!page_offsets || !aligned(page_offsets, 8)) return "the page table is an 8-byte aligned device array";
+    if (q8 && layer_page_bytes < q8::layer_bytes(Hkv, d)) return "a layer's part of a page is Hkv * 132 * d bytes";
     return nullptr;
 }
 
@@ -234,12 +316,13 @@ const char* window_refusal(const void* q, const void* o, int max_pages, int wind
 
 using namespace loip;
 
-extern "C" int loip_k_qk_append(const void* qkv, int32_t dtype, int64_t row_stride, int32_t T, int32_t Hq, int32_t Hkv,
-                                int32_t d, const uint16_t* g_q, const uint16_t* g_k, float eps, float theta,
-                                const int32_t* positions, const int32_t* row_req, int32_t n_req, void* q_out,
-                                void* kv_base, const int64_t* page_offsets, int32_t max_pages, int32_t page_tokens,
-                                int32_t layer, uint64_t layer_page_bytes, void* stream) {
-    if (const char* why = cache_refusal(dtype, T, Hq, Hkv, d, kv_base, page_offsets, max_pages, page_tokens, layer,
+namespace {
+
+int append(bool q8, const void* qkv, int32_t dtype, int64_t row_stride, int32_t T, int32_t Hq, int32_t Hkv, int32_t d,
+           const uint16_t* g_q, const uint16_t* g_k, float eps, float theta, const int32_t* positions,
+           const int32_t* row_req, int32_t n_req, void* q_out, void* kv_base, const int64_t* page_offsets,
+           int32_t max_pages, int32_t page_tokens, int32_t layer, uint64_t layer_page_bytes, void* stream) {
+    if (const char* why = cache_refusal(q8, dtype, T, Hq, Hkv, d, kv_base, page_offsets, max_pages, page_tokens, layer,
                                         layer_page_bytes))
         return kernel_refused(why);
     if (T == 0) return LOIP_OK;
@@ -269,31 +352,29 @@ extern "C" int loip_k_qk_append(const void* qkv, int32_t dtype, int64_t row_stri
     a.kv = KvView{(char*)kv_base, page_offsets, max_pages, page_tokens, layer, layer_page_bytes};
     a.rope = rope_turns(theta, d);
     cudaStream_t st = (cudaStream_t)stream;
-    if (d == 128)
-        return kernel_status(dtype == LOIP_F32 ? launch_append<128, float>(a, st)
-                                               : launch_append<128, __nv_bfloat16>(a, st));
-    return kernel_status(dtype == LOIP_F32 ? launch_append<64, float>(a, st)
-                                           : launch_append<64, __nv_bfloat16>(a, st));
+    auto go = [&](auto head, auto q8_cache) {
+        constexpr int D = decltype(head)::value;
+        constexpr bool Q8 = decltype(q8_cache)::value;
+        return kernel_status(dtype == LOIP_F32 ? launch_append<D, float, Q8>(a, st)
+                                               : launch_append<D, __nv_bfloat16, Q8>(a, st));
+    };
+    using D64 = std::integral_constant<int, 64>;
+    using D128 = std::integral_constant<int, 128>;
+    if (q8) return d == 128 ? go(D128{}, std::true_type{}) : go(D64{}, std::true_type{});
+    return d == 128 ? go(D128{}, std::false_type{}) : go(D64{}, std::false_type{});
 }
 
-extern "C" uint64_t loip_k_window_attention_scratch_bytes(int32_t B, int32_t Hq, int32_t Hkv, int32_t d,
-                                                          int32_t window, int32_t sinks, int32_t max_ctx) {
-    if (B < 0 || Hq < 1 || Hkv < 1 || Hq % Hkv || (d != 64 && d != 128) || window < 0 || sinks < 0 || max_ctx < 1)
-        return 0;
-    return window_decode_scratch(B, Hq, Hkv, d, window, sinks, max_ctx);
-}
-
-extern "C" int loip_k_window_attention(const void* q, int32_t dtype, const void* kv_base, const int64_t* page_offsets,
-                                       int32_t max_pages, const int32_t* ctx_lens, int32_t B, int32_t Hq, int32_t Hkv,
-                                       int32_t d, int32_t page_tokens, int32_t layer, uint64_t layer_page_bytes,
-                                       int32_t window, int32_t sinks, int32_t max_ctx, void* scratch,
-                                       uint64_t scratch_bytes, void* o, void* stream) {
-    if (const char* why = cache_refusal(dtype, B, Hq, Hkv, d, kv_base, page_offsets, max_pages, page_tokens, layer,
+int attention(bool q8, const void* q, int32_t dtype, const void* kv_base, const int64_t* page_offsets,
+              int32_t max_pages, const int32_t* ctx_lens, int32_t B, int32_t Hq, int32_t Hkv, int32_t d,
+              int32_t page_tokens, int32_t layer, uint64_t layer_page_bytes, int32_t window, int32_t sinks,
+              int32_t max_ctx, void* scratch, uint64_t scratch_bytes, void* o, void* stream) {
+    if (const char* why = cache_refusal(q8, dtype, B, Hq, Hkv, d, kv_base, page_offsets, max_pages, page_tokens, layer,
                                         layer_page_bytes))
         return kernel_refused(why);
     if (B == 0) return LOIP_OK;
-    if (const char* why = window_refusal(q, o, max_pages, window, sinks, max_ctx, scratch, scratch_bytes,
-                                         loip_k_window_attention_scratch_bytes(B, Hq, Hkv, d, window, sinks, max_ctx)))
+    const uint64_t need = q8 ? loip_k_window_attention_q8_scratch_bytes(B, Hq, Hkv, d, window, sinks, max_ctx)
+                             : loip_k_window_attention_scratch_bytes(B, Hq, Hkv, d, window, sinks, max_ctx);
+    if (const char* why = window_refusal(q, o, max_pages, window, sinks, max_ctx, scratch, scratch_bytes, need))
         return kernel_refused(why);
     if (!ctx_lens || !aligned(ctx_lens, 4)) return kernel_refused("ctx_lens is a device int32 array");
     WindowArgs a{};
@@ -309,31 +390,21 @@ extern "C" int loip_k_window_attention(const void* q, int32_t dtype, const void*
     a.sinks = sinks;
     a.max_ctx = max_ctx;
     a.scratch = scratch;
-    return kernel_status(launch_window_decode(a, dtype == LOIP_F32, (cudaStream_t)stream));
+    return kernel_status((q8 ? launch_window_decode_q8 : launch_window_decode)(a, dtype == LOIP_F32, (cudaStream_t)stream));
 }
 
-extern "C" uint64_t loip_k_window_prefill_scratch_bytes(int32_t M, int32_t n_prompts, int32_t Hq, int32_t Hkv,
-                                                        int32_t d, int32_t window, int32_t sinks, int32_t max_ctx) {
-    if (M < 0 || n_prompts < 0 || Hq < 1 || Hkv < 1 || Hq % Hkv || (d != 64 && d != 128) || window < 0 || sinks < 0 ||
-        max_ctx < 1)
-        return 0;
-    return window_prefill_scratch(M, n_prompts, Hq, Hkv, d, window, sinks, max_ctx);
-}
-
-extern "C" int loip_k_window_prefill(const void* q, int32_t dtype, const void* kv_base, const int64_t* page_offsets,
-                                     int32_t max_pages, const int32_t* row_starts, const int32_t* first_pos,
-                                     int32_t n_prompts, int32_t M, int32_t Hq, int32_t Hkv, int32_t d,
-                                     int32_t page_tokens, int32_t layer, uint64_t layer_page_bytes, int32_t window,
-                                     int32_t sinks, int32_t max_ctx, void* scratch, uint64_t scratch_bytes, void* o,
-                                     void* stream) {
-    if (const char* why = cache_refusal(dtype, M, Hq, Hkv, d, kv_base, page_offsets, max_pages, page_tokens, layer,
+int prefill(bool q8, const void* q, int32_t dtype, const void* kv_base, const int64_t* page_offsets, int32_t max_pages,
+            const int32_t* row_starts, const int32_t* first_pos, int32_t n_prompts, int32_t M, int32_t Hq, int32_t Hkv,
+            int32_t d, int32_t page_tokens, int32_t layer, uint64_t layer_page_bytes, int32_t window, int32_t sinks,
+            int32_t max_ctx, void* scratch, uint64_t scratch_bytes, void* o, void* stream) {
+    if (const char* why = cache_refusal(q8, dtype, M, Hq, Hkv, d, kv_base, page_offsets, max_pages, page_tokens, layer,
                                         layer_page_bytes))
         return kernel_refused(why);
     if (M == 0) return LOIP_OK;
     if (n_prompts < 1) return kernel_refused("rows without a prompt");
-    if (const char* why = window_refusal(q, o, max_pages, window, sinks, max_ctx, scratch, scratch_bytes,
-                                         loip_k_window_prefill_scratch_bytes(M, n_prompts, Hq, Hkv, d, window, sinks,
-                                                                             max_ctx)))
+    const uint64_t need = q8 ? loip_k_window_prefill_q8_scratch_bytes(M, n_prompts, Hq, Hkv, d, window, sinks, max_ctx)
+                             : loip_k_window_prefill_scratch_bytes(M, n_prompts, Hq, Hkv, d, window, sinks, max_ctx);
+    if (const char* why = window_refusal(q, o, max_pages, window, sinks, max_ctx, scratch, scratch_bytes, need))
         return kernel_refused(why);
     if (!row_starts || !aligned(row_starts, 4) || !aligned(first_pos, 4))
         return kernel_refused("row_starts (and first_pos) are device int32 arrays");
@@ -352,5 +423,111 @@ extern "C" int loip_k_window_prefill(const void* q, int32_t dtype, const void* k
     a.sinks = sinks;
     a.max_ctx = max_ctx;
     a.scratch = scratch;
-    return kernel_status(launch_window_prefill(a, dtype == LOIP_F32, (cudaStream_t)stream));
+    return kernel_status((q8 ? launch_window_prefill_q8 : launch_window_prefill)(a, dtype == LOIP_F32, (cudaStream_t)stream));
+}
+
+bool scratch_sizes(int rows, int Hq, int Hkv, int d, int window, int sinks, int max_ctx) {
+    return rows >= 0 && Hq >= 1 && Hkv >= 1 && Hq % Hkv == 0 && (d == 64 || d == 128) && window >= 0 && sinks >= 0 &&
+           max_ctx >= 1;
+}
+
+}  // namespace
+
+extern "C" int loip_k_qk_append(const void* qkv, int32_t dtype, int64_t row_stride, int32_t T, int32_t Hq, int32_t Hkv,
+                                int32_t d, const uint16_t* g_q, const uint16_t* g_k, float eps, float theta,
+                                const int32_t* positions, const int32_t* row_req, int32_t n_req, void* q_out,
+                                void* kv_base, const int64_t* page_offsets, int32_t max_pages, int32_t page_tokens,
+                                int32_t layer, uint64_t layer_page_bytes, void* stream) {
+    return append(false, qkv, dtype, row_stride, T, Hq, Hkv, d, g_q, g_k, eps, theta, positions, row_req, n_req, q_out,
+                  kv_base, page_offsets, max_pages, page_tokens, layer, layer_page_bytes, stream);
+}
+
+extern "C" uint64_t loip_k_window_attention_scratch_bytes(int32_t B, int32_t Hq, int32_t Hkv, int32_t d,
+                                                          int32_t window, int32_t sinks, int32_t max_ctx) {
+    if (!scratch_sizes(B, Hq, Hkv, d, window, sinks, max_ctx)) return 0;
+    return window_decode_scratch(B, Hq, Hkv, d, window, sinks, max_ctx);
+}
+
+extern "C" int loip_k_window_attention(const void* q, int32_t dtype, const void* kv_base, const int64_t* page_offsets,
+                                       int32_t max_pages, const int32_t* ctx_lens, int32_t B, int32_t Hq, int32_t Hkv,
+                                       int32_t d, int32_t page_tokens, int32_t layer, uint64_t layer_page_bytes,
+                                       int32_t window, int32_t sinks, int32_t max_ctx, void* scratch,
+                                       uint64_t scratch_bytes, void* o, void* stream) {
+    return attention(false, q, dtype, kv_base, page_offsets, max_pages, ctx_lens, B, Hq, Hkv, d, page_tokens, layer,
+                     layer_page_bytes, window, sinks, max_ctx, scratch, scratch_bytes, o, stream);
+}
+
+extern "C" uint64_t loip_k_window_prefill_scratch_bytes(int32_t M, int32_t n_prompts, int32_t Hq, int32_t Hkv,
+                                                        int32_t d, int32_t window, int32_t sinks, int32_t max_ctx) {
+    if (!scratch_sizes(M, Hq, Hkv, d, window, sinks, max_ctx) || n_prompts < 0) return 0;
+    return window_prefill_scratch(M, n_prompts, Hq, Hkv, d, window, sinks, max_ctx);
+}
+
+extern "C" int loip_k_window_prefill(const void* q, int32_t dtype, const void* kv_base, const int64_t* page_offsets,
+                                     int32_t max_pages, const int32_t* row_starts, const int32_t* first_pos,
+                                     int32_t n_prompts, int32_t M, int32_t Hq, int32_t Hkv, int32_t d,
+                                     int32_t page_tokens, int32_t layer, uint64_t layer_page_bytes, int32_t window,
+                                     int32_t sinks, int32_t max_ctx, void* scratch, uint64_t scratch_bytes, void* o,
+                                     void* stream) {
+    return prefill(false, q, dtype, kv_base, page_offsets, max_pages, row_starts, first_pos, n_prompts, M, Hq, Hkv, d,
+                   page_tokens, layer, layer_page_bytes, window, sinks, max_ctx, scratch, scratch_bytes, o, stream);
+}
+
+extern "C" int loip_k_qk_append_q8(const void* qkv, int32_t dtype, int64_t row_stride, int32_t T, int32_t Hq, int32_t Hkv,
+                                   int32_t d, const uint16_t* g_q, const uint16_t* g_k, float eps, float theta,
+                                   const int32_t* positions, const int32_t* row_req, int32_t n_req, void* q_out,
+                                   void* kv_base, const int64_t* page_offsets, int32_t max_pages, int32_t page_tokens,
+                                   int32_t layer, uint64_t layer_page_bytes, void* stream) {
+    return append(true, qkv, dtype, row_stride, T, Hq, Hkv, d, g_q, g_k, eps, theta, positions, row_req, n_req, q_out,
+                  kv_base, page_offsets, max_pages, page_tokens, layer, layer_page_bytes, stream);
+}
+
+extern "C" uint64_t loip_k_window_attention_q8_scratch_bytes(int32_t B, int32_t Hq, int32_t Hkv, int32_t d,
+                                                             int32_t window, int32_t sinks, int32_t max_ctx) {
+    if (!scratch_sizes(B, Hq, Hkv, d, window, sinks, max_ctx)) return 0;
+    return window_decode_q8_scratch(B, Hq, Hkv, d, window, sinks, max_ctx);
+}
+
+extern "C" int loip_k_window_attention_q8(const void* q, int32_t dtype, const void* kv_base, const int64_t* page_offsets,
+                                          int32_t max_pages, const int32_t* ctx_lens, int32_t B, int32_t Hq, int32_t Hkv,
+                                          int32_t d, int32_t page_tokens, int32_t layer, uint64_t layer_page_bytes,
+                                          int32_t window, int32_t sinks, int32_t max_ctx, void* scratch,
+                                          uint64_t scratch_bytes, void* o, void* stream) {
+    return attention(true, q, dtype, kv_base, page_offsets, max_pages, ctx_lens, B, Hq, Hkv, d, page_tokens, layer,
+                     layer_page_bytes, window, sinks, max_ctx, scratch, scratch_bytes, o, stream);
+}
+
+extern "C" uint64_t loip_k_window_prefill_q8_scratch_bytes(int32_t M, int32_t n_prompts, int32_t Hq, int32_t Hkv,
+                                                           int32_t d, int32_t window, int32_t sinks, int32_t max_ctx) {
+    if (!scratch_sizes(M, Hq, Hkv, d, window, sinks, max_ctx) || n_prompts < 0) return 0;
+    return window_prefill_q8_scratch(M, n_prompts, Hq, Hkv, d, window, sinks, max_ctx);
+}
+
+extern "C" int loip_k_window_prefill_q8(const void* q, int32_t dtype, const void* kv_base, const int64_t* page_offsets,
+                                        int32_t max_pages, const int32_t* row_starts, const int32_t* first_pos,
+                                        int32_t n_prompts, int32_t M, int32_t Hq, int32_t Hkv, int32_t d,
+                                        int32_t page_tokens, int32_t layer, uint64_t layer_page_bytes, int32_t window,
+                                        int32_t sinks, int32_t max_ctx, void* scratch, uint64_t scratch_bytes, void* o,
+                                        void* stream) {
+    return prefill(true, q, dtype, kv_base, page_offsets, max_pages, row_starts, first_pos, n_prompts, M, Hq, Hkv, d,
+                   page_tokens, layer, layer_page_bytes, window, sinks, max_ctx, scratch, scratch_bytes, o, stream);
+}
+
+extern "C" int loip_k_cache_read_q8(const void* kv_base, const int64_t* page_offsets, int32_t max_pages,
+                                    const int32_t* positions, const int32_t* row_req, int32_t n_req, int32_t T,
+                                    int32_t Hkv, int32_t d, int32_t page_tokens, int32_t layer,
+                                    uint64_t layer_page_bytes, void* out, int32_t dtype, void* stream) {
+    if (const char* why = cache_refusal(true, dtype, T, Hkv, Hkv, d, kv_base, page_offsets, max_pages, page_tokens,
+                                        layer, layer_page_bytes))
+        return kernel_refused(why);
+    if (T == 0) return LOIP_OK;
+    if (!out || !aligned(out, 16)) return kernel_refused("the rows that are read are 16-byte aligned");
+    if (!positions || !aligned(positions, 4) || !aligned(row_req, 4) || n_req < 1)
+        return kernel_refused("positions (and requests) are device int32 arrays, the page table has a row");
+    const ReadArgs a{positions, row_req, T, n_req, Hkv,
+                     KvView{(char*)kv_base, page_offsets, max_pages, page_tokens, layer, layer_page_bytes}, out};
+    cudaStream_t st = (cudaStream_t)stream;
+    if (d == 128)
+        return kernel_status(dtype == LOIP_F32 ? launch_read<128, float>(a, st) : launch_read<128, __nv_bfloat16>(a, st));
+    return kernel_status(dtype == LOIP_F32 ? launch_read<64, float>(a, st) : launch_read<64, __nv_bfloat16>(a, st));
 }

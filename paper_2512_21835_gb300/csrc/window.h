@@ -1,5 +1,5 @@
-// window.h -- what the windowed-serving operators share (window.cu, window_decode.cu,
-// window_prefill.cu).
+// window.h -- what the windowed-serving operators share (window.cu, window_decode*.cu,
+// window_prefill*.cu).
 #pragma once
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
@@ -85,6 +85,11 @@ cudaError_t launch_window_decode(const WindowArgs& a, bool f32, cudaStream_t st)
 // Attention of prompt rows (window_prefill.cu).
 uint64_t window_prefill_scratch(int M, int n_prompts, int Hq, int Hkv, int d, int window, int sinks, int max_ctx);
 cudaError_t launch_window_prefill(const WindowArgs& a, bool f32, cudaStream_t st);
+// The same over the 8-bit cache (window_q8.cu).
+uint64_t window_decode_q8_scratch(int B, int Hq, int Hkv, int d, int window, int sinks, int max_ctx);
+cudaError_t launch_window_decode_q8(const WindowArgs& a, bool f32, cudaStream_t st);
+uint64_t window_prefill_q8_scratch(int M, int n_prompts, int Hq, int Hkv, int d, int window, int sinks, int max_ctx);
+cudaError_t launch_window_prefill_q8(const WindowArgs& a, bool f32, cudaStream_t st);
 cudaError_t window_prefill_error(int* code);  // first failure code of any launch (0 = none)
 
 }  // namespace loip

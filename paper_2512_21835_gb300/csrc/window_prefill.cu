@@ -70,6 +70,7 @@
 #include "internal.h"
 #include "window.h"
 #include "window_parts.h"
+#include "window_walk.h"
 
 namespace loip {
 
@@ -295,52 +296,6 @@ __device__ __forceinline__ float2 add2(float2 a, float2 b) {
     return r;
 }
 __device__ __forceinline__ uint64_t low_bits(int n) { return n <= 0 ? 0ull : n >= 64 ? ~0ull : (1ull << n) - 1; }
-
-__device__ __forceinline__ float row_load(const float* p) { return *p; }
-__device__ __forceinline__ float row_load(const __nv_bfloat16* p) { return __bfloat162float(*p); }
-__device__ __forceinline__ void row_store(float* p, float v) { *p = v; }
-__device__ __forceinline__ void row_store(__nv_bfloat16* p, float v) { *p = __float2bfloat16_rn(v); }
-
-// One row by one warp, position by position: what is not seen is not touched.
-template <int D, typename T>
-__device__ __forceinline__ void walk_row(const WindowArgs& a, int req, int kvh, int pos, const T* q, T* out) {
-    const int lane = threadIdx.x % 32;
-    const char* layer = a.kv.base + (uint64_t)a.kv.layer * a.kv.layer_page_bytes;
-    float qv[D / 32], o[D / 32], m = -INFINITY, l = 0.f;
-#pragma unroll
-    for (int i = 0; i < D / 32; ++i) {
-        qv[i] = row_load(q + i * 32 + lane);
-        o[i] = 0.f;
-    }
-    const float scale = 1.0f / sqrtf((float)D);
-    const int last = min(pos, a.max_ctx - 1);
-    for (int j = 0; j <= last; ++j) {
-        if (j >= a.sinks && j <= pos - a.window) {  // to the window's first position
-            j = pos - a.window;
-            continue;
-        }
-        const __nv_bfloat16* k =
-            reinterpret_cast<const __nv_bfloat16*>(
-                layer + a.kv.page_offsets[(int64_t)req * a.kv.max_pages + j / kPageTokens]) +
-            ((int64_t)kvh * kPageTokens + j % kPageTokens) * D;
-        const __nv_bfloat16* v = k + (int64_t)a.Hkv * kPageTokens * D;
-        float s = 0.f;
-#pragma unroll
-        for (int i = 0; i < D / 32; ++i) s = fmaf(qv[i], __bfloat162float(k[i * 32 + lane]), s);
-#pragma unroll
-        for (int x = 16; x; x /= 2) s += __shfl_xor_sync(0xffffffffu, s, x);
-        s *= scale;
-        const float m_new = fmaxf(m, s), alpha = m == -INFINITY ? 0.f : expf(m - m_new);
-        const float w = expf(s - (m_new == -INFINITY ? 0.f : m_new));  // a score of -inf: weight zero, the first one too
-        l = l * alpha + w;
-#pragma unroll
-        for (int i = 0; i < D / 32; ++i) o[i] = fmaf(w, __bfloat162float(v[i * 32 + lane]), o[i] * alpha);
-        m = m_new;
-    }
-    const float inv = l == 0.f ? 0.f : 1.0f / l;
-#pragma unroll
-    for (int i = 0; i < D / 32; ++i) row_store(out + i * 32 + lane, o[i] * inv);
-}
 
 // The pages that rows at positions p0 .. p1 see: [0, sink) and [win, end), a list of n.
 struct Pages {
@@ -1027,7 +982,7 @@ __global__ void __launch_bounds__(kThreads, 1) window_prefill_kernel(const __gri
     } else if (end == kPartNotFinite && warp < 8) {
         for (int i = warp; i < tokens * heads; i += 8) {
             const int64_t at = ((int64_t)(row0 + i / heads) * a.Hq + kvh * G + head0 + i % heads) * D;
-            walk_row<D, T>(a, req, kvh, pos0 + i / heads, static_cast<const T*>(a.q) + at, static_cast<T*>(a.o) + at);
+            walk_row<D, false, T>(a, req, kvh, pos0 + i / heads, static_cast<const T*>(a.q) + at, static_cast<T*>(a.o) + at);
         }
     }
 }
@@ -1053,7 +1008,7 @@ __global__ void __launch_bounds__(256) window_join_kernel(const __grid_constant_
         const int warp = threadIdx.x / 32 + blockIdx.x % PIECES * 8;
         for (int i = warp; i < rows.y * heads; i += 8 * PIECES) {
             const int64_t at = ((int64_t)(rows.x + i / heads) * a.Hq + kvh * G + head0 + i % heads) * D;
-            walk_row<D, T>(a, rows.z, kvh, rows.w + i / heads, static_cast<const T*>(a.q) + at,
+            walk_row<D, false, T>(a, rows.z, kvh, rows.w + i / heads, static_cast<const T*>(a.q) + at,
                            static_cast<T*>(a.o) + at);
         }
         return;
