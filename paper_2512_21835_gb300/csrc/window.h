@@ -5,6 +5,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "internal.h"
 
 namespace loip {
@@ -39,6 +41,18 @@ cudaError_t launch_pdl(void (*kernel)(Args), dim3 grid, unsigned threads, size_t
     c.attrs = at;
     c.numAttrs = 1;
     return cudaLaunchKernelEx(&c, kernel, args);
+}
+
+// Lets a kernel have `bytes` of dynamic shared memory, once per device and kernel.
+template <typename Args>
+cudaError_t raise_smem_limit(void (*kernel)(Args), int bytes, std::atomic<uint64_t>& ready) {
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    if (dev < 64 && (ready.load() >> dev & 1)) return cudaSuccess;
+    e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e == cudaSuccess && dev < 64) ready.fetch_or(1ull << dev);
+    return e;
 }
 
 // Two fp32 numbers as a pair of bf16, to the nearest.

@@ -40,6 +40,7 @@
 #include <algorithm>
 
 #include "internal.h"
+#include "q8.h"
 #include "window.h"
 
 namespace loip {
@@ -89,216 +90,110 @@ struct DecodeArgs {
     float* part;    // [request][group][split][heads][d], not normalised
 };
 
+// The tiles that a request's token sees: those of the sinks, then those of the window (which may
+// touch), as a list without a gap.
+struct Tiles {
+    int ctx, win0, sinks;  // cached positions, first position of the window
+    int sink_tiles, win_tile, n;
+    __device__ __forceinline__ Tiles(const WindowArgs& a, int b) {
+        ctx = max(0, min(a.ctx_lens[b], a.max_ctx));
+        win0 = a.window >= ctx ? 0 : ctx - a.window;
+        sinks = a.sinks;
+        const int end = (ctx + kTile - 1) / kTile;
+        sink_tiles = min((int)(((int64_t)a.sinks + kTile - 1) / kTile), end);
+        win_tile = a.window == 0 ? end : max(win0 / kTile, sink_tiles);
+        n = sink_tiles + max(0, end - win_tile);
+    }
+    __device__ __forceinline__ int at(int i) const { return i < sink_tiles ? i : i - sink_tiles + win_tile; }
+    __device__ __forceinline__ bool seen(int j) const { return j < ctx && (j >= win0 || j < sinks); }
+};
+
+// The running softmax over a tile: a lane has the scores of positions n4 (s[0], s[1]) and n4 + 8
+// (s[2], s[3]) and heads 2 c4 + {0, 1}; O is rescaled where a maximum has grown.  pb: the planes of
+// P^T in the MMA's B layout; the last one is rounded (exact if it is the third).
+template <int PV, int NO>
+__device__ __forceinline__ void soften(const float (&s)[4], bool see0, bool see1, float scale, float (&m)[2], float (&l)[2],
+                                       float (&o)[NO][4], uint32_t (&pb)[PV][2]) {
+    float w[4], mx[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        w[h] = see0 ? s[h] * scale : -INFINITY;
+        w[2 + h] = see1 ? s[2 + h] * scale : -INFINITY;
+        mx[h] = fmaxf(w[h], w[2 + h]);
+#pragma unroll
+        for (int x = 4; x < 32; x *= 2) mx[h] = fmaxf(mx[h], __shfl_xor_sync(0xffffffffu, mx[h], x));
+    }
+    if (__any_sync(0xffffffffu, mx[0] > m[0] || mx[1] > m[1])) {
+        float alpha[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const float m_new = fmaxf(m[h], mx[h]);
+            alpha[h] = m[h] == -INFINITY ? 0.f : exp2f(m[h] - m_new);
+            m[h] = m_new;
+            l[h] *= alpha[h];
+        }
+#pragma unroll
+        for (int x = 0; x < NO; ++x) {
+            o[x][0] *= alpha[0]; o[x][1] *= alpha[1]; o[x][2] *= alpha[0]; o[x][3] *= alpha[1];
+        }
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const float base = m[h] == -INFINITY ? 0.f : m[h];  // nothing seen yet: every weight is zero
+        w[h] = exp2f(w[h] - base);
+        w[2 + h] = exp2f(w[2 + h] - base);
+        l[h] += w[h] + w[2 + h];
+    }
+#pragma unroll
+    for (int pl = 0; pl < PV; ++pl)
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+            pb[pl][j] = transpose(pl < PV - 1 ? peel(w[2 * j], w[2 * j + 1]) : pack(w[2 * j], w[2 * j + 1]));
+}
+
+// O^T += V^T P^T of a tile, 16 of its rows; smallest plane first.  The MMA's sums truncate, so that
+// fp32 rows add a tile's product to O in fp32.
+template <bool F32, int PV>
+__device__ __forceinline__ void add_values(float (&o)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
+                                           const uint32_t (&pb)[PV][2]) {
+    float y[4];
+#pragma unroll
+    for (int h = 0; h < 4; ++h) y[h] = F32 ? 0.f : o[h];
+#pragma unroll
+    for (int pl = PV - 1; pl >= 0; --pl) mma(y, a0, a1, a2, a3, pb[pl][0], pb[pl][1]);
+#pragma unroll
+    for (int h = 0; h < 4; ++h) o[h] = F32 ? o[h] + y[h] : y[h];
+}
+
+// What the warps of a block share at the end: maxima, sums, and where their O lie ([8][D], a
+// warp's `pitch` floats behind the last one's).
+struct Shared {
+    float m[kWarps][8], l[kWarps][8];
+    bool last;
+};
+
+// The end of a block: sums of its warps, and of the blocks of a unit in the last one to arrive.
+// head: the first of the group's `heads` query heads.
 template <int D, typename T>
-__global__ void __launch_bounds__(kThreads, kResident) window_decode_kernel(const __grid_constant__ DecodeArgs p) {
-    constexpr bool F32 = sizeof(T) == 4;
-    constexpr int NQ = D / 32;  // 16-byte pieces of a key per lane
-    constexpr int NV = D / 64;  // 16-byte pieces of a value row per lane
-    constexpr int PV = F32 ? 3 : 2;  // planes of the weights
-    __shared__ __align__(16) float sm_o[kWarps][8][D];
-    __shared__ float sm_m[kWarps][8], sm_l[kWarps][8];
-    __shared__ bool sm_last;
-    __shared__ uint4 sm_q[NQ][F32 ? 3 : 1][32];
-    const WindowArgs& a = p.a;
-    pdl_trigger();
-    pdl_wait();
+__device__ __forceinline__ void join(const DecodeArgs& p, Shared& sh, const float* sm_o, int pitch, const float (&m)[2],
+                                     float (&l)[2], int b, int head, int heads, int split, int active) {
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, n4 = lane / 4, c4 = lane % 4;
-    const int b = blockIdx.x / p.plan.splits, split = blockIdx.x % p.plan.splits;
-    const int kvh = blockIdx.y / p.plan.groups, G = a.Hq / a.Hkv;
-    const int head0 = (blockIdx.y % p.plan.groups) * p.plan.heads;          // of the kv head's G
-    const int heads = min(p.plan.heads, G - head0);
-    const int ctx = max(0, min(a.ctx_lens[b], a.max_ctx));
-    // visible tiles: those of the sinks, then those of the window (which may touch)
-    const int win0 = a.window >= ctx ? 0 : ctx - a.window;                  // first position of the window
-    const int tiles_end = (ctx + kTile - 1) / kTile;
-    const int sink_tiles = min((int)(((int64_t)a.sinks + kTile - 1) / kTile), tiles_end);
-    const int win_tile = a.window == 0 ? tiles_end : max(win0 / kTile, sink_tiles);
-    const int tiles = sink_tiles + max(0, tiles_end - win_tile);
-    const int active = max(1, (tiles + p.plan.chunk - 1) / p.plan.chunk);   // blocks with work
-    if (split >= active) return;
-    const int last = min(tiles, (split + 1) * p.plan.chunk);
-
-    // queries: bf16 planes in the B layout (a lane: head n4, elements 32 x + 8 c4 ..), columns past
-    // the group's heads zero; the same for every warp, in shared memory
-    {
-        const T* q = static_cast<const T*>(a.q) + ((int64_t)b * a.Hq + kvh * G + head0 + n4) * D + 8 * c4;
-        for (int x = warp; x < NQ; x += kWarps) {
-            if constexpr (F32) {
-                float v[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = 0.f;
-                if (n4 < heads) {
-                    const float4 y = *reinterpret_cast<const float4*>(q + 32 * x);
-                    const float4 z = *reinterpret_cast<const float4*>(q + 32 * x + 4);
-                    v[0] = y.x; v[1] = y.y; v[2] = y.z; v[3] = y.w; v[4] = z.x; v[5] = z.y; v[6] = z.z; v[7] = z.w;
-                }
-#pragma unroll
-                for (int pl = 0; pl < 3; ++pl) {
-                    uint32_t u[4];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        u[e] = pl < 2 ? peel(v[2 * e], v[2 * e + 1]) : pack(v[2 * e], v[2 * e + 1]);
-                    sm_q[x][pl][lane] = make_uint4(u[0], u[1], u[2], u[3]);
-                }
-            } else {
-                sm_q[x][0][lane] = n4 < heads ? *reinterpret_cast<const uint4*>(q + 32 * x) : make_uint4(0u, 0u, 0u, 0u);
-            }
-        }
-    }
-
-    const char* layer = a.kv.base + (uint64_t)a.kv.layer * a.kv.layer_page_bytes;
-    const int64_t* table = a.kv.page_offsets + (int64_t)b * a.kv.max_pages;
-    auto tile_at = [&](int i) { return i < sink_tiles ? i : i - sink_tiles + win_tile; };
-    auto seen = [&](int j) { return j < ctx && (j >= win0 || j < a.sinks); };
-    // the tile's first key of this kv head
-    auto key_at = [&](int t) {
-        return layer + table[t / (kPageTokens / kTile)] +
-               (uint32_t)((kvh * kPageTokens + (t % (kPageTokens / kTile)) * kTile) * D * 2);
-    };
-    const uint32_t v_off = (uint32_t)(a.Hkv * kPageTokens) * D * 2;
-
-    float o[4 * NV][4];  // rows 64 x + 8 n4 + 2 e (+ 1) of O^T, heads 2 c4 and 2 c4 + 1
-#pragma unroll
-    for (int i = 0; i < 4 * NV; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
-    float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};  // of heads 2 c4 and 2 c4 + 1
-    const float scale = 1.44269504088896f / sqrtf((float)D);  // scores in units of log 2
-
-    uint4 k[2][NQ], v[4][NV];
-    auto load_k = [&](int t, const char* at) {  // keys n4 and n4 + 8
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const bool live = seen(t * kTile + 8 * j + n4);
-#pragma unroll
-            for (int x = 0; x < NQ; ++x) k[j][x] = load_row(at + ((8 * j + n4) * D + 32 * x + 8 * c4) * 2, live);
-        }
-    };
-    int i = split * p.plan.chunk + warp;
-    const char* at = nullptr;
-    if (i < last) {
-        at = key_at(tile_at(i));
-        load_k(tile_at(i), at);
-    }
-    __syncthreads();  // the queries
-    for (; i < last; i += kWarps) {
-        const int t = tile_at(i);
-        const char* at_next = i + kWarps < last ? key_at(tile_at(i + kWarps)) : nullptr;
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {  // value rows 2 c4, 2 c4 + 1, 2 c4 + 8, 2 c4 + 9
-            const int row = 2 * c4 + (r & 1) + 8 * (r >> 1);
-            const bool live = seen(t * kTile + row);
-#pragma unroll
-            for (int x = 0; x < NV; ++x) v[r][x] = load_row(at + v_off + (row * D + 64 * x + 8 * n4) * 2, live);
-        }
-        // ---- scores, in independent sums (a chain of MMAs waits for each result)
-        float s[4];
-        {
-            constexpr int PL = F32 ? 3 : 1;
-            float z[PL][2][4];
-#pragma unroll
-            for (int pl = 0; pl < PL; ++pl)
-#pragma unroll
-                for (int h = 0; h < 2; ++h) z[pl][h][0] = z[pl][h][1] = z[pl][h][2] = z[pl][h][3] = 0.f;
-#pragma unroll
-            for (int x = 0; x < NQ; ++x)
-#pragma unroll
-                for (int pl = 0; pl < PL; ++pl) {
-                    const uint4 q = sm_q[x][pl][lane];
-                    mma(z[pl][0], k[0][x].x, k[1][x].x, k[0][x].y, k[1][x].y, q.x, q.y);
-                    mma(z[pl][1], k[0][x].z, k[1][x].z, k[0][x].w, k[1][x].w, q.z, q.w);
-                }
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                s[e] = z[0][0][e] + z[0][1][e];
-                if constexpr (F32) s[e] += (z[1][0][e] + z[1][1][e]) + (z[2][0][e] + z[2][1][e]);
-            }
-        }
-        if (at_next) load_k(tile_at(i + kWarps), at_next);
-        // ---- softmax: this lane has positions n4 (s[0], s[1]) and n4 + 8 (s[2], s[3]), heads 2 c4 + {0, 1}
-        const bool see0 = seen(t * kTile + n4), see1 = seen(t * kTile + 8 + n4);
-        float w[4], mx[2];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            w[h] = see0 ? s[h] * scale : -INFINITY;
-            w[2 + h] = see1 ? s[2 + h] * scale : -INFINITY;
-            mx[h] = fmaxf(w[h], w[2 + h]);
-#pragma unroll
-            for (int x = 4; x < 32; x *= 2) mx[h] = fmaxf(mx[h], __shfl_xor_sync(0xffffffffu, mx[h], x));
-        }
-        if (__any_sync(0xffffffffu, mx[0] > m[0] || mx[1] > m[1])) {
-            float alpha[2];
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const float m_new = fmaxf(m[h], mx[h]);
-                alpha[h] = m[h] == -INFINITY ? 0.f : exp2f(m[h] - m_new);
-                m[h] = m_new;
-                l[h] *= alpha[h];
-            }
-#pragma unroll
-            for (int x = 0; x < 4 * NV; ++x) {
-                o[x][0] *= alpha[0]; o[x][1] *= alpha[1]; o[x][2] *= alpha[0]; o[x][3] *= alpha[1];
-            }
-        }
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const float base = m[h] == -INFINITY ? 0.f : m[h];  // nothing seen yet: every weight is zero
-            w[h] = exp2f(w[h] - base);
-            w[2 + h] = exp2f(w[2 + h] - base);
-            l[h] += w[h] + w[2 + h];
-        }
-        uint32_t pb[PV][2];  // planes of P^T in the B layout; the last one is rounded (exact if it is the third)
-#pragma unroll
-        for (int pl = 0; pl < PV; ++pl)
-#pragma unroll
-            for (int j = 0; j < 2; ++j)
-                pb[pl][j] = transpose(pl < PV - 1 ? peel(w[2 * j], w[2 * j + 1]) : pack(w[2 * j], w[2 * j + 1]));
-        // ---- values
-#pragma unroll
-        for (int x = 0; x < NV; ++x) {
-            const uint32_t r0[4] = {v[0][x].x, v[0][x].y, v[0][x].z, v[0][x].w};
-            const uint32_t r1[4] = {v[1][x].x, v[1][x].y, v[1][x].z, v[1][x].w};
-            const uint32_t r2[4] = {v[2][x].x, v[2][x].y, v[2][x].z, v[2][x].w};
-            const uint32_t r3[4] = {v[3][x].x, v[3][x].y, v[3][x].z, v[3][x].w};
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const uint32_t a0 = __byte_perm(r0[e], r1[e], 0x5410u), a1 = __byte_perm(r0[e], r1[e], 0x7632u);
-                const uint32_t a2 = __byte_perm(r2[e], r3[e], 0x5410u), a3 = __byte_perm(r2[e], r3[e], 0x7632u);
-                // smallest plane first; the MMA's sums truncate, so that fp32 rows add a tile's product
-                // to O in fp32
-                float y[4];
-#pragma unroll
-                for (int h = 0; h < 4; ++h) y[h] = F32 ? 0.f : o[4 * x + e][h];
-#pragma unroll
-                for (int pl = PV - 1; pl >= 0; --pl) mma(y, a0, a1, a2, a3, pb[pl][0], pb[pl][1]);
-#pragma unroll
-                for (int h = 0; h < 4; ++h) o[4 * x + e][h] = F32 ? o[4 * x + e][h] + y[h] : y[h];
-            }
-        }
-        at = at_next;
-    }
-
-    // ---- join the warps: heads 2 c4 + h, elements 64 x + 8 n4 .. + 7
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
 #pragma unroll
         for (int x = 4; x < 32; x *= 2) l[h] += __shfl_xor_sync(0xffffffffu, l[h], x);
         if (n4 == 0) {
-            sm_m[warp][2 * c4 + h] = m[h];
-            sm_l[warp][2 * c4 + h] = l[h];
+            sh.m[warp][2 * c4 + h] = m[h];
+            sh.l[warp][2 * c4 + h] = l[h];
         }
-#pragma unroll
-        for (int x = 0; x < NV; ++x)
-#pragma unroll
-            for (int e = 0; e < 4; e += 2)
-                *reinterpret_cast<float4*>(&sm_o[warp][2 * c4 + h][64 * x + 8 * n4 + 2 * e]) = make_float4(
-                    o[4 * x + e][h], o[4 * x + e][2 + h], o[4 * x + e + 1][h], o[4 * x + e + 1][2 + h]);
     }
     __syncthreads();
     const int64_t unit = (int64_t)b * gridDim.y + blockIdx.y;
     const int units = heads * (D / 4);  // four elements of a head each
-    T* out = static_cast<T*>(a.o) + ((int64_t)b * a.Hq + kvh * G + head0) * D;
+    T* out = static_cast<T*>(p.a.o) + ((int64_t)b * p.a.Hq + head) * D;
     auto put = [&](int u, float4 r, float inv) {
         r.x *= inv; r.y *= inv; r.z *= inv; r.w *= inv;
-        if constexpr (F32)
+        if constexpr (sizeof(T) == 4)
             reinterpret_cast<float4*>(out)[u] = r;
         else
             reinterpret_cast<uint2*>(out)[u] = make_uint2(pack(r.x, r.y), pack(r.z, r.w));
@@ -307,13 +202,13 @@ __global__ void __launch_bounds__(kThreads, kResident) window_decode_kernel(cons
         const int h = u / (D / 4);
         float mt = -INFINITY, lt = 0.f;
 #pragma unroll
-        for (int x = 0; x < kWarps; ++x) mt = fmaxf(mt, sm_m[x][h]);
+        for (int x = 0; x < kWarps; ++x) mt = fmaxf(mt, sh.m[x][h]);
         float4 r = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
         for (int x = 0; x < kWarps; ++x) {
-            const float f = sm_m[x][h] == -INFINITY ? 0.f : exp2f(sm_m[x][h] - mt);
-            const float4 y = *reinterpret_cast<const float4*>(&sm_o[x][h][4 * (u % (D / 4))]);
-            lt = fmaf(f, sm_l[x][h], lt);
+            const float f = sh.m[x][h] == -INFINITY ? 0.f : exp2f(sh.m[x][h] - mt);
+            const float4 y = *reinterpret_cast<const float4*>(sm_o + x * pitch + h * D + 4 * (u % (D / 4)));
+            lt = fmaf(f, sh.l[x][h], lt);
             r.x = fmaf(f, y.x, r.x); r.y = fmaf(f, y.y, r.y); r.z = fmaf(f, y.z, r.z); r.w = fmaf(f, y.w, r.w);
         }
         if (active == 1) {
@@ -329,9 +224,9 @@ __global__ void __launch_bounds__(kThreads, kResident) window_decode_kernel(cons
     // counter wraps to zero with that arrival
     __threadfence();
     __syncthreads();
-    if (threadIdx.x == 0) sm_last = atomicInc(p.counters + unit, (unsigned)active - 1u) == (unsigned)active - 1u;
+    if (threadIdx.x == 0) sh.last = atomicInc(p.counters + unit, (unsigned)active - 1u) == (unsigned)active - 1u;
     __syncthreads();
-    if (!sm_last) return;
+    if (!sh.last) return;
     __threadfence();
     for (int u = threadIdx.x; u < units; u += kThreads) {
         const int h = u / (D / 4);
@@ -365,6 +260,343 @@ __global__ void __launch_bounds__(kThreads, kResident) window_decode_kernel(cons
         }
         put(u, r, lt == 0.f ? 0.f : 1.0f / lt);
     }
+}
+
+// Queries into shared memory, the same for every warp: bf16 planes in the MMA's B layout, of which a
+// lane holds eight elements of head n4 in piece x, `step` elements from one piece to the next.
+// Columns past the group's heads are zero.
+template <int NQ, int PL, typename T>
+__device__ __forceinline__ void load_queries(uint4 (&sm_q)[NQ][PL][32], const T* q, int step, bool live) {
+    const int lane = threadIdx.x % 32;
+    for (int x = threadIdx.x / 32; x < NQ; x += kWarps) {
+        if constexpr (PL == 3) {
+            float v[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = 0.f;
+            if (live) {
+                const float4 y = *reinterpret_cast<const float4*>(q + step * x);
+                const float4 z = *reinterpret_cast<const float4*>(q + step * x + 4);
+                v[0] = y.x; v[1] = y.y; v[2] = y.z; v[3] = y.w; v[4] = z.x; v[5] = z.y; v[6] = z.z; v[7] = z.w;
+            }
+#pragma unroll
+            for (int pl = 0; pl < 3; ++pl) {
+                uint32_t u[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    u[e] = pl < 2 ? peel(v[2 * e], v[2 * e + 1]) : pack(v[2 * e], v[2 * e + 1]);
+                sm_q[x][pl][lane] = make_uint4(u[0], u[1], u[2], u[3]);
+            }
+        } else {
+            sm_q[x][0][lane] = live ? *reinterpret_cast<const uint4*>(q + step * x) : make_uint4(0u, 0u, 0u, 0u);
+        }
+    }
+}
+
+template <int D, typename T>
+__global__ void __launch_bounds__(kThreads, kResident) window_decode_kernel(const __grid_constant__ DecodeArgs p) {
+    constexpr bool F32 = sizeof(T) == 4;
+    constexpr int NQ = D / 32;  // 16-byte pieces of a key per lane
+    constexpr int NV = D / 64;  // 16-byte pieces of a value row per lane
+    constexpr int PV = F32 ? 3 : 2;  // planes of the weights
+    __shared__ __align__(16) float sm_o[kWarps][8][D];
+    __shared__ Shared sh;
+    __shared__ uint4 sm_q[NQ][F32 ? 3 : 1][32];
+    const WindowArgs& a = p.a;
+    pdl_trigger();
+    pdl_wait();
+    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, n4 = lane / 4, c4 = lane % 4;
+    const int b = blockIdx.x / p.plan.splits, split = blockIdx.x % p.plan.splits;
+    const int kvh = blockIdx.y / p.plan.groups, G = a.Hq / a.Hkv;
+    const int head0 = (blockIdx.y % p.plan.groups) * p.plan.heads;          // of the kv head's G
+    const int heads = min(p.plan.heads, G - head0);
+    const Tiles seen(a, b);
+    const int active = max(1, (seen.n + p.plan.chunk - 1) / p.plan.chunk);  // blocks with work
+    if (split >= active) return;
+    const int last = min(seen.n, (split + 1) * p.plan.chunk);
+
+    load_queries(sm_q, static_cast<const T*>(a.q) + ((int64_t)b * a.Hq + kvh * G + head0 + n4) * D + 8 * c4, 32, n4 < heads);
+
+    const char* layer = a.kv.base + (uint64_t)a.kv.layer * a.kv.layer_page_bytes;
+    const int64_t* table = a.kv.page_offsets + (int64_t)b * a.kv.max_pages;
+    // the tile's first key of this kv head
+    auto key_at = [&](int t) {
+        return layer + table[t / (kPageTokens / kTile)] +
+               (uint32_t)((kvh * kPageTokens + (t % (kPageTokens / kTile)) * kTile) * D * 2);
+    };
+    const uint32_t v_off = (uint32_t)(a.Hkv * kPageTokens) * D * 2;
+
+    float o[4 * NV][4];  // rows 64 x + 8 n4 + 2 e (+ 1) of O^T, heads 2 c4 and 2 c4 + 1
+#pragma unroll
+    for (int i = 0; i < 4 * NV; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
+    float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};  // of heads 2 c4 and 2 c4 + 1
+    const float scale = 1.44269504088896f / sqrtf((float)D);  // scores in units of log 2
+
+    uint4 k[2][NQ], v[4][NV];
+    auto load_k = [&](int t, const char* at) {  // keys n4 and n4 + 8
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const bool live = seen.seen(t * kTile + 8 * j + n4);
+#pragma unroll
+            for (int x = 0; x < NQ; ++x) k[j][x] = load_row(at + ((8 * j + n4) * D + 32 * x + 8 * c4) * 2, live);
+        }
+    };
+    int i = split * p.plan.chunk + warp;
+    const char* at = nullptr;
+    if (i < last) {
+        at = key_at(seen.at(i));
+        load_k(seen.at(i), at);
+    }
+    __syncthreads();  // the queries
+    for (; i < last; i += kWarps) {
+        const int t = seen.at(i);
+        const char* at_next = i + kWarps < last ? key_at(seen.at(i + kWarps)) : nullptr;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {  // value rows 2 c4, 2 c4 + 1, 2 c4 + 8, 2 c4 + 9
+            const int row = 2 * c4 + (r & 1) + 8 * (r >> 1);
+            const bool live = seen.seen(t * kTile + row);
+#pragma unroll
+            for (int x = 0; x < NV; ++x) v[r][x] = load_row(at + v_off + (row * D + 64 * x + 8 * n4) * 2, live);
+        }
+        // ---- scores, in independent sums (a chain of MMAs waits for each result)
+        float s[4];
+        {
+            constexpr int PL = F32 ? 3 : 1;
+            float z[PL][2][4];
+#pragma unroll
+            for (int pl = 0; pl < PL; ++pl)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) z[pl][h][0] = z[pl][h][1] = z[pl][h][2] = z[pl][h][3] = 0.f;
+#pragma unroll
+            for (int x = 0; x < NQ; ++x)
+#pragma unroll
+                for (int pl = 0; pl < PL; ++pl) {
+                    const uint4 q = sm_q[x][pl][lane];
+                    mma(z[pl][0], k[0][x].x, k[1][x].x, k[0][x].y, k[1][x].y, q.x, q.y);
+                    mma(z[pl][1], k[0][x].z, k[1][x].z, k[0][x].w, k[1][x].w, q.z, q.w);
+                }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                s[e] = z[0][0][e] + z[0][1][e];
+                if constexpr (F32) s[e] += (z[1][0][e] + z[1][1][e]) + (z[2][0][e] + z[2][1][e]);
+            }
+        }
+        if (at_next) load_k(seen.at(i + kWarps), at_next);
+        // ---- softmax
+        uint32_t pb[PV][2];
+        soften(s, seen.seen(t * kTile + n4), seen.seen(t * kTile + 8 + n4), scale, m, l, o, pb);
+        // ---- values
+#pragma unroll
+        for (int x = 0; x < NV; ++x) {
+            const uint32_t r0[4] = {v[0][x].x, v[0][x].y, v[0][x].z, v[0][x].w};
+            const uint32_t r1[4] = {v[1][x].x, v[1][x].y, v[1][x].z, v[1][x].w};
+            const uint32_t r2[4] = {v[2][x].x, v[2][x].y, v[2][x].z, v[2][x].w};
+            const uint32_t r3[4] = {v[3][x].x, v[3][x].y, v[3][x].z, v[3][x].w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const uint32_t a0 = __byte_perm(r0[e], r1[e], 0x5410u), a1 = __byte_perm(r0[e], r1[e], 0x7632u);
+                const uint32_t a2 = __byte_perm(r2[e], r3[e], 0x5410u), a3 = __byte_perm(r2[e], r3[e], 0x7632u);
+                add_values<F32>(o[4 * x + e], a0, a1, a2, a3, pb);
+            }
+        }
+        at = at_next;
+    }
+
+    // ---- join the warps: heads 2 c4 + h, elements 64 x + 8 n4 .. + 7
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+#pragma unroll
+        for (int x = 0; x < NV; ++x)
+#pragma unroll
+            for (int e = 0; e < 4; e += 2)
+                *reinterpret_cast<float4*>(&sm_o[warp][2 * c4 + h][64 * x + 8 * n4 + 2 * e]) = make_float4(
+                    o[4 * x + e][h], o[4 * x + e][2 + h], o[4 * x + e + 1][h], o[4 * x + e + 1][2 + h]);
+    }
+    join<D, T>(p, sh, &sm_o[0][0][0], 8 * D, m, l, b, kvh * G + head0, heads, split, active);
+}
+
+// ---------------------------------------------------------------------------
+// The 8-bit cache.
+//
+// 33 d bytes a tile instead of 64 d, so that the conversion to bf16 is what the memory's rate
+// has to hide: two instructions an element (q8.h), 256 a tile of d = 128, some 400 in all,
+// where memory leaves a scheduler 730 issue slots a tile.  A tile is one contiguous granule:
+// a warp copies its own tiles, kStages - 1 ahead, whole (the positions of a granule that are
+// not seen lie in a page of the request all the same), and reads the MMAs' fragments from
+// shared memory, 16 bytes a lane without bank conflicts:
+//   S^T = K Q^T     lane (n4, c4) has, of keys n4 and n4 + 8, the d / 4 elements from d / 4 c4,
+//                   which are of one block; four codes are a lane's A registers of one MMA
+//   O^T += V^T P^T  the d / 8 elements from d / 8 n4 of values 2 c4 + {0, 1, 8, 9}; adjacent
+//                   tokens are paired by the byte permute that spreads the codes
+// Positions that are not seen have steps of zero, so that whatever the cache holds there is zero.
+// ---------------------------------------------------------------------------
+constexpr int kStages = 4;
+
+__device__ __forceinline__ void copy16(uint32_t to, const char* from) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+}
+
+template <int D, typename T>
+__global__ void __launch_bounds__(kThreads, kResident) window_decode_q8_kernel(const __grid_constant__ DecodeArgs p) {
+    using Gr = q8::Granule<D>;
+    constexpr bool F32 = sizeof(T) == 4;
+    constexpr int NK = D / 64;       // 16-byte pieces of a key per lane
+    constexpr int NW = D / 32;       // words of four codes of a value row per lane
+    constexpr int PL = F32 ? 3 : 1;  // planes of the queries
+    constexpr int PV = F32 ? 3 : 2;  // planes of the weights
+    extern __shared__ __align__(16) uint8_t ring[];  // [warp][stage][granule]; at the end [warp][8][D] floats
+    static_assert(8 * D * sizeof(float) <= kStages * Gr::BYTES, "the join goes through a warp's own part");
+    __shared__ Shared sh;
+    __shared__ uint4 sm_q[D / 32][PL][32];
+    const WindowArgs& a = p.a;
+    pdl_trigger();
+    pdl_wait();
+    const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, n4 = lane / 4, c4 = lane % 4;
+    const int b = blockIdx.x / p.plan.splits, split = blockIdx.x % p.plan.splits;
+    const int kvh = blockIdx.y / p.plan.groups, G = a.Hq / a.Hkv;
+    const int head0 = (blockIdx.y % p.plan.groups) * p.plan.heads;          // of the kv head's G
+    const int heads = min(p.plan.heads, G - head0);
+    const Tiles seen(a, b);
+    const int active = max(1, (seen.n + p.plan.chunk - 1) / p.plan.chunk);  // blocks with work
+    if (split >= active) return;
+    const int last = min(seen.n, (split + 1) * p.plan.chunk);
+
+    const char* layer = a.kv.base + (uint64_t)a.kv.layer * a.kv.layer_page_bytes + (int64_t)kvh * 4 * Gr::BYTES;
+    const int64_t* table = a.kv.page_offsets + (int64_t)b * a.kv.max_pages;
+    auto granule = [&](int i) {  // of the list's tile i
+        const int t = seen.at(i);
+        return layer + table[t / 4] + t % 4 * Gr::BYTES + lane * 16;
+    };
+    uint8_t* const mine = ring + warp * kStages * Gr::BYTES;
+    const uint32_t to = (uint32_t)__cvta_generic_to_shared(mine) + lane * 16;
+    auto copy = [&](const char* from, int stage) {
+        constexpr int PIECES = Gr::BYTES / 16;
+#pragma unroll
+        for (int x = 0; x < PIECES; x += 32)
+            if (x + 32 <= PIECES || lane < PIECES - x) copy16(to + stage * Gr::BYTES + x * 16, from + x * 16);
+    };
+    int i = split * p.plan.chunk + warp;
+    {
+        const char* at[kStages - 1];
+#pragma unroll
+        for (int x = 0; x < kStages - 1; ++x) at[x] = i + x * kWarps < last ? granule(i + x * kWarps) : nullptr;
+#pragma unroll
+        for (int x = 0; x < kStages - 1; ++x) {
+            if (at[x]) copy(at[x], x);
+            asm volatile("cp.async.commit_group;" ::: "memory");
+        }
+    }
+    load_queries(sm_q, static_cast<const T*>(a.q) + ((int64_t)b * a.Hq + kvh * G + head0 + n4) * D + D / 4 * c4, 8, n4 < heads);
+    const char* next = i + (kStages - 1) * kWarps < last ? granule(i + (kStages - 1) * kWarps) : nullptr;
+
+    float o[D / 16][4];  // rows d / 8 n4 + 2 e (+ 1) of O^T, heads 2 c4 and 2 c4 + 1
+#pragma unroll
+    for (int e = 0; e < D / 16; ++e) o[e][0] = o[e][1] = o[e][2] = o[e][3] = 0.f;
+    float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};  // of heads 2 c4 and 2 c4 + 1
+    const float scale = 1.44269504088896f / sqrtf((float)D);  // scores in units of log 2
+    __syncthreads();  // the queries
+    for (int stage = 0; i < last; i += kWarps, stage = stage + 1 == kStages ? 0 : stage + 1) {
+        asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 2) : "memory");
+        __syncwarp();  // every lane's part of the tile is here, and the tile before is read
+        if (next) copy(next, stage == 0 ? kStages - 1 : stage - 1);
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        const int ahead = i + kStages * kWarps;
+        next = ahead < last ? granule(ahead) : nullptr;
+        const uint8_t* g = mine + stage * Gr::BYTES;
+        const int j0 = seen.at(i) * kTile;
+        const bool all = seen.seen(j0) && seen.seen(j0 + kTile - 1) && (j0 >= seen.win0 || j0 + kTile <= seen.sinks);
+        // ---- scores, in independent sums (a chain of MMAs waits for each result)
+        const bool see0 = all || seen.seen(j0 + n4), see1 = all || seen.seen(j0 + 8 + n4);
+        float s[4];
+        {
+            q8::Step2 st[2];
+            uint32_t k[2][4 * NK];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const uint32_t E = g[Gr::exponents(0, 8 * j + n4) + c4 * (D / 64) / 2];
+                st[j] = q8::step2(E, E);
+                if (!(j ? see1 : see0)) st[j] = q8::Step2{0u, 0u};
+#pragma unroll
+                for (int x = 0; x < NK; ++x) {
+                    const uint4 u = *reinterpret_cast<const uint4*>(g + Gr::piece(0, 8 * j + n4, NK * c4 + x));
+                    k[j][4 * x] = u.x; k[j][4 * x + 1] = u.y; k[j][4 * x + 2] = u.z; k[j][4 * x + 3] = u.w;
+                }
+            }
+            float z[PL][2][4];
+#pragma unroll
+            for (int pl = 0; pl < PL; ++pl)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) z[pl][h][0] = z[pl][h][1] = z[pl][h][2] = z[pl][h][3] = 0.f;
+#pragma unroll
+            for (int x = 0; x < 4 * NK; ++x) {
+                uint32_t A[2][2];
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    A[j][0] = q8::pair_of(__byte_perm(k[j][x], 0u, 0x1100u), st[j]);
+                    A[j][1] = q8::pair_of(__byte_perm(k[j][x], 0u, 0x3322u), st[j]);
+                }
+#pragma unroll
+                for (int pl = 0; pl < PL; ++pl) {
+                    const uint4 q = sm_q[x / 2][pl][lane];
+                    mma(z[pl][x % 2], A[0][0], A[1][0], A[0][1], A[1][1], x % 2 ? q.z : q.x, x % 2 ? q.w : q.y);
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                s[e] = z[0][0][e] + z[0][1][e];
+                if constexpr (F32) s[e] += (z[1][0][e] + z[1][1][e]) + (z[2][0][e] + z[2][1][e]);
+            }
+        }
+        uint32_t pb[PV][2];
+        soften(s, see0, see1, scale, m, l, o, pb);
+        // ---- values: rows 2 c4, 2 c4 + 1, 2 c4 + 8, 2 c4 + 9
+        q8::Step2 st[2];
+        uint32_t v[4][NW];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            uint32_t E[2];
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+                const int row = 2 * c4 + r + 8 * j;
+                E[r] = g[Gr::exponents(1, row) + n4 / 2 * (D / 64) / 2];
+                const uint8_t* at = g + Gr::piece(1, row, D == 128 ? n4 : n4 / 2);
+                if constexpr (D == 128) {
+                    const uint4 u = *reinterpret_cast<const uint4*>(at);
+                    v[2 * j + r][0] = u.x; v[2 * j + r][1] = u.y; v[2 * j + r][2] = u.z; v[2 * j + r][3] = u.w;
+                } else {
+                    const uint2 u = *reinterpret_cast<const uint2*>(at + n4 % 2 * 8);
+                    v[2 * j + r][0] = u.x; v[2 * j + r][1] = u.y;
+                }
+            }
+            st[j] = q8::step2(E[0], E[1]);
+            if (!all) {
+                const uint32_t keep = (seen.seen(j0 + 2 * c4 + 8 * j) ? 0xffffu : 0u) |
+                                      (seen.seen(j0 + 2 * c4 + 1 + 8 * j) ? 0xffff0000u : 0u);
+                st[j].step &= keep;
+                st[j].minus128 &= keep;
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < D / 16; ++e) {
+            uint32_t A[2][2];
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int r = 0; r < 2; ++r)
+                    A[j][r] = q8::pair_of(__byte_perm(v[2 * j][e / 2], v[2 * j + 1][e / 2], 0x4400u + 0x1111u * (e % 2 * 2 + r)), st[j]);
+            add_values<F32>(o[e], A[0][0], A[0][1], A[1][0], A[1][1], pb);
+        }
+    }
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    __syncwarp();
+    float* sm_o = reinterpret_cast<float*>(mine);
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int e = 0; e < D / 16; e += 2)
+            *reinterpret_cast<float4*>(sm_o + (2 * c4 + h) * D + D / 8 * n4 + 2 * e) =
+                make_float4(o[e][h], o[e][2 + h], o[e + 1][h], o[e + 1][2 + h]);
+    join<D, T>(p, sh, reinterpret_cast<const float*>(ring), kStages * Gr::BYTES / 4, m, l, b, kvh * G + head0, heads, split,
+               active);
 }
 
 constexpr int kPlaces = 152 * kResident;
@@ -412,9 +644,26 @@ Plan make_plan(int B, int Hq, int Hkv, int window, int sinks, int max_ctx) {
 }
 
 template <int D, typename T>
-cudaError_t launch_t(const DecodeArgs& p, cudaStream_t st) {
-    return launch_pdl(window_decode_kernel<D, T>,
-                      dim3((unsigned)p.a.rows * p.plan.splits, p.a.Hkv * p.plan.groups), kThreads, 0, st, p);
+cudaError_t launch_t(const DecodeArgs& p, bool q8, cudaStream_t st) {
+    const dim3 grid((unsigned)p.a.rows * p.plan.splits, p.a.Hkv * p.plan.groups);
+    if (!q8) return launch_pdl(window_decode_kernel<D, T>, grid, kThreads, 0, st, p);
+    constexpr int BYTES = kWarps * kStages * q8::Granule<D>::BYTES;
+    static std::atomic<uint64_t> ready{0};
+    const cudaError_t e = raise_smem_limit(window_decode_q8_kernel<D, T>, BYTES, ready);
+    return e != cudaSuccess ? e : launch_pdl(window_decode_q8_kernel<D, T>, grid, kThreads, BYTES, st, p);
+}
+
+cudaError_t launch_any(const WindowArgs& a, bool f32, bool q8, cudaStream_t st) {
+    DecodeArgs p{};
+    p.a = a;
+    p.plan = make_plan(a.rows, a.Hq, a.Hkv, a.window, a.sinks, a.max_ctx);
+    if ((int64_t)a.rows * p.plan.splits > 0x7fffffff) return cudaErrorInvalidValue;
+    const int64_t parts = (int64_t)a.rows * a.Hkv * p.plan.groups * p.plan.splits * p.plan.heads;
+    p.counters = static_cast<unsigned*>(a.scratch);
+    p.part = reinterpret_cast<float*>(p.counters + kMaxCounters);
+    p.ml = reinterpret_cast<float2*>(p.part + parts * a.d);
+    if (a.d == 128) return f32 ? launch_t<128, float>(p, q8, st) : launch_t<128, __nv_bfloat16>(p, q8, st);
+    return f32 ? launch_t<64, float>(p, q8, st) : launch_t<64, __nv_bfloat16>(p, q8, st);
 }
 
 }  // namespace
@@ -433,17 +682,11 @@ uint64_t window_decode_scratch(int B, int Hq, int Hkv, int d, int window, int si
     return (n + 15) / 16 * 16;
 }
 
-cudaError_t launch_window_decode(const WindowArgs& a, bool f32, cudaStream_t st) {
-    DecodeArgs p{};
-    p.a = a;
-    p.plan = make_plan(a.rows, a.Hq, a.Hkv, a.window, a.sinks, a.max_ctx);
-    if ((int64_t)a.rows * p.plan.splits > 0x7fffffff) return cudaErrorInvalidValue;
-    const int64_t parts = (int64_t)a.rows * a.Hkv * p.plan.groups * p.plan.splits * p.plan.heads;
-    p.counters = static_cast<unsigned*>(a.scratch);
-    p.part = reinterpret_cast<float*>(p.counters + kMaxCounters);
-    p.ml = reinterpret_cast<float2*>(p.part + parts * a.d);
-    if (a.d == 128) return f32 ? launch_t<128, float>(p, st) : launch_t<128, __nv_bfloat16>(p, st);
-    return f32 ? launch_t<64, float>(p, st) : launch_t<64, __nv_bfloat16>(p, st);
+cudaError_t launch_window_decode(const WindowArgs& a, bool f32, cudaStream_t st) { return launch_any(a, f32, false, st); }
+
+uint64_t window_decode_q8_scratch(int B, int Hq, int Hkv, int d, int window, int sinks, int max_ctx) {
+    return window_decode_scratch(B, Hq, Hkv, d, window, sinks, max_ctx);
 }
+cudaError_t launch_window_decode_q8(const WindowArgs& a, bool f32, cudaStream_t st) { return launch_any(a, f32, true, st); }
 
 }  // namespace loip

@@ -1091,15 +1091,8 @@ template <int D, int NP, int QT, typename T>
 cudaError_t launch_t(const PrefillArgs& p, cudaStream_t st) {
     using C = Cfg<D, NP, QT>;
     static std::atomic<uint64_t> ready{0};  // devices whose limit has been raised, one bit each
-    int dev = 0;
-    cudaError_t e = cudaGetDevice(&dev);
+    cudaError_t e = raise_smem_limit(window_prefill_kernel<D, NP, QT, T>, C::BYTES, ready);
     if (e != cudaSuccess) return e;
-    if (dev >= 64 || !(ready.load() >> dev & 1)) {
-        e = cudaFuncSetAttribute(window_prefill_kernel<D, NP, QT, T>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                 C::BYTES);
-        if (e != cudaSuccess) return e;
-        if (dev < 64) ready.fetch_or(1ull << dev);
-    }
     const int64_t tiles = p.a.rows / (QT * p.tok) + p.a.n_prompts;  // at least the sum over prompts
     const int64_t blocks = std::min<int64_t>(tiles, p.a.rows) * p.a.Hkv * p.groups * p.splits;
     if (blocks > 0x7fffffff) return cudaErrorInvalidValue;

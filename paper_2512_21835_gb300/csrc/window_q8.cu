@@ -48,10 +48,6 @@ cudaError_t launch(WindowArgs a, bool f32, cudaStream_t st) {
 
 }  // namespace
 
-uint64_t window_decode_q8_scratch(int B, int Hq, int Hkv, int d, int window, int sinks, int max_ctx) {
-    return window_decode_scratch(B, Hq, Hkv, d, window, sinks, max_ctx);
-}
-cudaError_t launch_window_decode_q8(const WindowArgs& a, bool f32, cudaStream_t st) { return launch(a, f32, st); }
 uint64_t window_prefill_q8_scratch(int M, int n_prompts, int Hq, int Hkv, int d, int window, int sinks, int max_ctx) {
     return window_prefill_scratch(M, n_prompts, Hq, Hkv, d, window, sinks, max_ctx);
 }
