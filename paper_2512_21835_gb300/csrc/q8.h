@@ -75,23 +75,23 @@ __device__ __forceinline__ float value_of(uint32_t code, float step) {
     return (code & 128u ? -m : m) * step;
 }
 
-// Codes to pairs of bf16, exactly and in four instructions.  0x4300 | m is the bf16 number 128 + m,
-// so with the sign at its place x = +-(128 + m), and x step -+ 128 step is +-m step, rounded once
-// and exact.  Of a pair of blocks (or of one, twice): the step and the bits of -128 step.
-// (128 step = 2^(E - 126) is why exponents end at 253.)
-struct Step2 {
-    uint32_t step, minus128;
-};
-__device__ __forceinline__ Step2 step2(uint32_t Elo, uint32_t Ehi) {
-    auto one = [](uint32_t E) { return E > kMostExponent ? 0x7fc0u : (max(E, 7u) - 6u) << 7; };
-    const uint32_t s = one(Elo) | one(Ehi) << 16;
-    return Step2{s, (s + 0x03800380u) | 0x80008000u};  // (of a NaN: any bits)
+// Codes to pairs of bf16, exactly, in four instructions of which two are the integer pipe's (which
+// takes one every second cycle, and is what bounds the conversion).  Sign and magnitude of a code,
+// put where a bf16 number has its sign and its mantissa, are the subnormal number +-m 2^-133.  Times
+// 2^127 that is +-m 2^-6, times 2^(E - 127) the value: two products by powers of two, both exact.
+//
+// The second factor for a pair of blocks (or for one, twice).
+__device__ __forceinline__ uint32_t scale2(uint32_t Elo, uint32_t Ehi) {
+    const uint32_t e = __vmaxu2(Elo | Ehi << 16, 0x00070007u);
+    const uint32_t nan = (e + 0x00020002u & 0x01000100u) >> 2;  // 0x40 where it is 254 or 255
+    return e * 128u | nan * 511u;                               // 0x40 x 511 = 0x7fc0
 }
 // (code byte, the same again) twice -> the pair of values
-__device__ __forceinline__ uint32_t pair_of(uint32_t twice, Step2 s) {
-    const uint32_t x = (twice & 0x807f807fu) | 0x43004300u, y = (twice & 0x80008000u) ^ s.minus128;
+__device__ __forceinline__ uint32_t pair_of(uint32_t twice, uint32_t scale) {
     uint32_t r;
-    asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(x), "r"(s.step), "r"(y));
+    asm("{\n .reg .b32 x;\n and.b32 x, %1, 0x807f807f;\n mul.rn.bf16x2 x, x, %3;\n mul.rn.bf16x2 %0, x, %2;\n}\n"
+        : "=r"(r)
+        : "r"(twice), "r"(scale), "r"(0x7f007f00u));
     return r;
 }
 #endif

@@ -172,11 +172,13 @@ struct Shared {
     bool last;
 };
 
-// The end of a block: sums of its warps, and of the blocks of a unit in the last one to arrive.
-// head: the first of the group's `heads` query heads.
-template <int D, typename T>
+// The end of a unit, or of a part of it: sums of the block's warps, and of the unit's `active` blocks
+// in the last one to arrive.  head: the first of the group's `heads` query heads; slot: where this
+// block's part goes; slot_of(x): where the unit's part x is.
+template <int D, typename T, typename SlotOf>
 __device__ __forceinline__ void join(const DecodeArgs& p, Shared& sh, const float* sm_o, int pitch, const float (&m)[2],
-                                     float (&l)[2], int b, int head, int heads, int split, int active) {
+                                     float (&l)[2], int b, int head, int heads, int active, unsigned* counter, int64_t slot,
+                                     SlotOf&& slot_of) {
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, n4 = lane / 4, c4 = lane % 4;
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
@@ -188,7 +190,6 @@ __device__ __forceinline__ void join(const DecodeArgs& p, Shared& sh, const floa
         }
     }
     __syncthreads();
-    const int64_t unit = (int64_t)b * gridDim.y + blockIdx.y;
     const int units = heads * (D / 4);  // four elements of a head each
     T* out = static_cast<T*>(p.a.o) + ((int64_t)b * p.a.Hq + head) * D;
     auto put = [&](int u, float4 r, float inv) {
@@ -214,7 +215,7 @@ __device__ __forceinline__ void join(const DecodeArgs& p, Shared& sh, const floa
         if (active == 1) {
             put(u, r, lt == 0.f ? 0.f : 1.0f / lt);
         } else {
-            const int64_t at = (unit * p.plan.splits + split) * p.plan.heads + h;
+            const int64_t at = slot * p.plan.heads + h;
             __stcg(reinterpret_cast<float4*>(p.part + at * D) + u % (D / 4), r);
             if (u % (D / 4) == 0) __stcg(p.ml + at, make_float2(mt, lt));
         }
@@ -224,13 +225,12 @@ __device__ __forceinline__ void join(const DecodeArgs& p, Shared& sh, const floa
     // counter wraps to zero with that arrival
     __threadfence();
     __syncthreads();
-    if (threadIdx.x == 0) sh.last = atomicInc(p.counters + unit, (unsigned)active - 1u) == (unsigned)active - 1u;
+    if (threadIdx.x == 0) sh.last = atomicInc(counter, (unsigned)active - 1u) == (unsigned)active - 1u;
     __syncthreads();
     if (!sh.last) return;
     __threadfence();
     for (int u = threadIdx.x; u < units; u += kThreads) {
         const int h = u / (D / 4);
-        const int64_t first = unit * p.plan.splits * p.plan.heads + h;
         float mt = -INFINITY, lt = 0.f;
         float4 r = make_float4(0.f, 0.f, 0.f, 0.f);
         constexpr int BATCH = 12;  // parts whose loads are in flight together
@@ -239,7 +239,7 @@ __device__ __forceinline__ void join(const DecodeArgs& p, Shared& sh, const floa
             float4 y[BATCH];
 #pragma unroll
             for (int x = 0; x < BATCH; ++x) {
-                const int64_t at = first + (int64_t)min(x0 + x, active - 1) * p.plan.heads;
+                const int64_t at = slot_of(min(x0 + x, active - 1)) * p.plan.heads + h;
                 ml[x] = __ldcg(p.ml + at);
                 y[x] = __ldcg(reinterpret_cast<const float4*>(p.part + at * D) + u % (D / 4));
             }
@@ -411,15 +411,16 @@ __global__ void __launch_bounds__(kThreads, kResident) window_decode_kernel(cons
                 *reinterpret_cast<float4*>(&sm_o[warp][2 * c4 + h][64 * x + 8 * n4 + 2 * e]) = make_float4(
                     o[4 * x + e][h], o[4 * x + e][2 + h], o[4 * x + e + 1][h], o[4 * x + e + 1][2 + h]);
     }
-    join<D, T>(p, sh, &sm_o[0][0][0], 8 * D, m, l, b, kvh * G + head0, heads, split, active);
+    const int64_t unit = (int64_t)b * gridDim.y + blockIdx.y, part0 = unit * p.plan.splits;
+    join<D, T>(p, sh, &sm_o[0][0][0], 8 * D, m, l, b, kvh * G + head0, heads, active, p.counters + unit, part0 + split,
+               [&](int x) { return part0 + x; });
 }
 
 // ---------------------------------------------------------------------------
 // The 8-bit cache.
 //
 // 33 d bytes a tile instead of 64 d, so that the conversion to bf16 is what the memory's rate
-// has to hide: two instructions an element (q8.h), 256 a tile of d = 128, some 400 in all,
-// where memory leaves a scheduler 730 issue slots a tile.  A tile is one contiguous granule:
+// has to hide: two instructions an element (q8.h).  A tile is one contiguous granule:
 // a warp copies its own tiles, kStages - 1 ahead, whole (the positions of a granule that are
 // not seen lie in a page of the request all the same), and reads the MMAs' fragments from
 // shared memory, 16 bytes a lane without bank conflicts:
@@ -427,23 +428,30 @@ __global__ void __launch_bounds__(kThreads, kResident) window_decode_kernel(cons
 //                   which are of one block; four codes are a lane's A registers of one MMA
 //   O^T += V^T P^T  the d / 8 elements from d / 8 n4 of values 2 c4 + {0, 1, 8, 9}; adjacent
 //                   tokens are paired by the byte permute that spreads the codes
-// Positions that are not seen have steps of zero, so that whatever the cache holds there is zero.
+// Positions that are not seen have a scale of zero, so that whatever the cache holds there is zero.
+//
+// Where the work is.  A step is four tiles of a unit (request, kv head and group of heads), one a
+// warp.  The blocks share the steps of all units equally, as one list in their order, whatever
+// the lengths are: each adds them up, finds its share and goes through it unit by unit.  A unit that
+// begins in one block and ends in a later one is joined by the last of its blocks to arrive.
 // ---------------------------------------------------------------------------
-constexpr int kStages = 4;
+constexpr int kStages = 3;
+constexpr int kResident8 = 4;  // blocks per SM
+constexpr int kPlaces8 = 152 * kResident8;
 
 __device__ __forceinline__ void copy16(uint32_t to, const char* from) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
 }
 
 template <int D, typename T>
-__global__ void __launch_bounds__(kThreads, kResident) window_decode_q8_kernel(const __grid_constant__ DecodeArgs p) {
+__global__ void __launch_bounds__(kThreads, kResident8) window_decode_q8_kernel(const __grid_constant__ DecodeArgs p) {
     using Gr = q8::Granule<D>;
     constexpr bool F32 = sizeof(T) == 4;
     constexpr int NK = D / 64;       // 16-byte pieces of a key per lane
     constexpr int NW = D / 32;       // words of four codes of a value row per lane
     constexpr int PL = F32 ? 3 : 1;  // planes of the queries
     constexpr int PV = F32 ? 3 : 2;  // planes of the weights
-    extern __shared__ __align__(16) uint8_t ring[];  // [warp][stage][granule]; at the end [warp][8][D] floats
+    extern __shared__ __align__(16) uint8_t ring[];  // [warp][stage][granule]; at a unit's end [warp][8][D] floats
     static_assert(8 * D * sizeof(float) <= kStages * Gr::BYTES, "the join goes through a warp's own part");
     __shared__ Shared sh;
     __shared__ uint4 sm_q[D / 32][PL][32];
@@ -451,21 +459,45 @@ __global__ void __launch_bounds__(kThreads, kResident) window_decode_q8_kernel(c
     pdl_trigger();
     pdl_wait();
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32, n4 = lane / 4, c4 = lane % 4;
-    const int b = blockIdx.x / p.plan.splits, split = blockIdx.x % p.plan.splits;
-    const int kvh = blockIdx.y / p.plan.groups, G = a.Hq / a.Hkv;
-    const int head0 = (blockIdx.y % p.plan.groups) * p.plan.heads;          // of the kv head's G
-    const int heads = min(p.plan.heads, G - head0);
-    const Tiles seen(a, b);
-    const int active = max(1, (seen.n + p.plan.chunk - 1) / p.plan.chunk);  // blocks with work
-    if (split >= active) return;
-    const int last = min(seen.n, (split + 1) * p.plan.chunk);
-
-    const char* layer = a.kv.base + (uint64_t)a.kv.layer * a.kv.layer_page_bytes + (int64_t)kvh * 4 * Gr::BYTES;
-    const int64_t* table = a.kv.page_offsets + (int64_t)b * a.kv.max_pages;
-    auto granule = [&](int i) {  // of the list's tile i
-        const int t = seen.at(i);
-        return layer + table[t / 4] + t % 4 * Gr::BYTES + lane * 16;
-    };
+    const int units = a.Hkv * p.plan.groups, G = a.Hq / a.Hkv;  // units of a request
+    // ---- this block's share
+    auto steps_of = [&](int b) { return b < a.rows ? max(1, (Tiles(a, b).n + kWarps - 1) / kWarps) : 0; };
+    const int first32 = steps_of(lane);
+    int64_t total = first32;
+    for (int b = 32 + lane; b < a.rows; b += 32) total += steps_of(b);
+#pragma unroll
+    for (int x = 16; x; x /= 2) total += __shfl_xor_sync(0xffffffffu, total, x);
+    total *= units;
+    const int64_t share = (total + gridDim.x - 1) / gridDim.x;
+    int64_t at = share * blockIdx.x;
+    const int64_t end = min(at + share, total);
+    if (at >= end) return;
+    int b = 0, unit, step;  // where the share begins
+    int64_t unit_at;        // first step of that unit in the list
+    {
+        int64_t before = 0;
+        for (;; b += 32) {
+            const int mine = b == 0 ? first32 : steps_of(b + lane);
+            int64_t sum = mine;
+#pragma unroll
+            for (int x = 1; x < 32; x *= 2) {
+                const int64_t y = __shfl_up_sync(0xffffffffu, sum, x);
+                if (lane >= x) sum += y;
+            }
+            const unsigned past = __ballot_sync(0xffffffffu, (before + sum) * units > at);
+            if (past) {  // (at < total: in some round)
+                const int src = __ffs(past) - 1;
+                before += __shfl_sync(0xffffffffu, sum - mine, src);
+                const int steps = __shfl_sync(0xffffffffu, mine, src);
+                b += src;
+                unit = (int)((at - before * units) / steps);
+                unit_at = before * units + (int64_t)unit * steps;
+                step = (int)(at - unit_at);
+                break;
+            }
+            before += __shfl_sync(0xffffffffu, sum, 31);
+        }
+    }
     uint8_t* const mine = ring + warp * kStages * Gr::BYTES;
     const uint32_t to = (uint32_t)__cvta_generic_to_shared(mine) + lane * 16;
     auto copy = [&](const char* from, int stage) {
@@ -474,129 +506,159 @@ __global__ void __launch_bounds__(kThreads, kResident) window_decode_q8_kernel(c
         for (int x = 0; x < PIECES; x += 32)
             if (x + 32 <= PIECES || lane < PIECES - x) copy16(to + stage * Gr::BYTES + x * 16, from + x * 16);
     };
-    int i = split * p.plan.chunk + warp;
-    {
-        const char* at[kStages - 1];
-#pragma unroll
-        for (int x = 0; x < kStages - 1; ++x) at[x] = i + x * kWarps < last ? granule(i + x * kWarps) : nullptr;
-#pragma unroll
-        for (int x = 0; x < kStages - 1; ++x) {
-            if (at[x]) copy(at[x], x);
-            asm volatile("cp.async.commit_group;" ::: "memory");
-        }
-    }
-    load_queries(sm_q, static_cast<const T*>(a.q) + ((int64_t)b * a.Hq + kvh * G + head0 + n4) * D + D / 4 * c4, 8, n4 < heads);
-    const char* next = i + (kStages - 1) * kWarps < last ? granule(i + (kStages - 1) * kWarps) : nullptr;
-
-    float o[D / 16][4];  // rows d / 8 n4 + 2 e (+ 1) of O^T, heads 2 c4 and 2 c4 + 1
-#pragma unroll
-    for (int e = 0; e < D / 16; ++e) o[e][0] = o[e][1] = o[e][2] = o[e][3] = 0.f;
-    float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};  // of heads 2 c4 and 2 c4 + 1
     const float scale = 1.44269504088896f / sqrtf((float)D);  // scores in units of log 2
-    __syncthreads();  // the queries
-    for (int stage = 0; i < last; i += kWarps, stage = stage + 1 == kStages ? 0 : stage + 1) {
-        asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 2) : "memory");
-        __syncwarp();  // every lane's part of the tile is here, and the tile before is read
-        if (next) copy(next, stage == 0 ? kStages - 1 : stage - 1);
-        asm volatile("cp.async.commit_group;" ::: "memory");
-        const int ahead = i + kStages * kWarps;
-        next = ahead < last ? granule(ahead) : nullptr;
-        const uint8_t* g = mine + stage * Gr::BYTES;
-        const int j0 = seen.at(i) * kTile;
-        const bool all = seen.seen(j0) && seen.seen(j0 + kTile - 1) && (j0 >= seen.win0 || j0 + kTile <= seen.sinks);
-        // ---- scores, in independent sums (a chain of MMAs waits for each result)
-        const bool see0 = all || seen.seen(j0 + n4), see1 = all || seen.seen(j0 + 8 + n4);
-        float s[4];
+    const char* layer = a.kv.base + (uint64_t)a.kv.layer * a.kv.layer_page_bytes;
+
+#pragma unroll 1
+    for (;;) {
+        const Tiles seen(a, b);
+        const int steps = max(1, (seen.n + kWarps - 1) / kWarps);
+        const int kvh = unit / p.plan.groups, head0 = unit % p.plan.groups * p.plan.heads;  // of the kv head's G
+        const int heads = min(p.plan.heads, G - head0);
+        const int last = min((int64_t)seen.n, (end - unit_at) * kWarps);  // tiles
+        const char* head = layer + (int64_t)kvh * 4 * Gr::BYTES + lane * 16;
+        const int64_t* table = a.kv.page_offsets + (int64_t)b * a.kv.max_pages;
+        auto granule = [&](int i) {  // of the list's tile i
+            const int t = seen.at(i);
+            return head + table[t / 4] + t % 4 * Gr::BYTES;
+        };
+        int i = step * kWarps + warp;
         {
-            q8::Step2 st[2];
-            uint32_t k[2][4 * NK];
+            const char* from[kStages - 1];
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const uint32_t E = g[Gr::exponents(0, 8 * j + n4) + c4 * (D / 64) / 2];
-                st[j] = q8::step2(E, E);
-                if (!(j ? see1 : see0)) st[j] = q8::Step2{0u, 0u};
+            for (int x = 0; x < kStages - 1; ++x) from[x] = i + x * kWarps < last ? granule(i + x * kWarps) : nullptr;
 #pragma unroll
-                for (int x = 0; x < NK; ++x) {
-                    const uint4 u = *reinterpret_cast<const uint4*>(g + Gr::piece(0, 8 * j + n4, NK * c4 + x));
-                    k[j][4 * x] = u.x; k[j][4 * x + 1] = u.y; k[j][4 * x + 2] = u.z; k[j][4 * x + 3] = u.w;
-                }
+            for (int x = 0; x < kStages - 1; ++x) {
+                if (from[x]) copy(from[x], x);
+                asm volatile("cp.async.commit_group;" ::: "memory");
             }
-            float z[PL][2][4];
+        }
+        load_queries(sm_q, static_cast<const T*>(a.q) + ((int64_t)b * a.Hq + kvh * G + head0 + n4) * D + D / 4 * c4, 8,
+                     n4 < heads);
+        const char* next = i + (kStages - 1) * kWarps < last ? granule(i + (kStages - 1) * kWarps) : nullptr;
+
+        float o[D / 16][4];  // rows d / 8 n4 + 2 e (+ 1) of O^T, heads 2 c4 and 2 c4 + 1
 #pragma unroll
-            for (int pl = 0; pl < PL; ++pl)
-#pragma unroll
-                for (int h = 0; h < 2; ++h) z[pl][h][0] = z[pl][h][1] = z[pl][h][2] = z[pl][h][3] = 0.f;
-#pragma unroll
-            for (int x = 0; x < 4 * NK; ++x) {
-                uint32_t A[2][2];
+        for (int e = 0; e < D / 16; ++e) o[e][0] = o[e][1] = o[e][2] = o[e][3] = 0.f;
+        float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};  // of heads 2 c4 and 2 c4 + 1
+        __syncthreads();  // the queries
+#pragma unroll 1
+        for (int stage = 0; i < last; i += kWarps, stage = stage + 1 == kStages ? 0 : stage + 1) {
+            asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 2) : "memory");
+            __syncwarp();  // every lane's part of the tile is here, and the tile before is read
+            if (next) copy(next, stage == 0 ? kStages - 1 : stage - 1);
+            asm volatile("cp.async.commit_group;" ::: "memory");
+            const int ahead = i + kStages * kWarps;
+            next = ahead < last ? granule(ahead) : nullptr;
+            const uint8_t* g = mine + stage * Gr::BYTES;
+            const int j0 = seen.at(i) * kTile;
+            const bool all = j0 + kTile <= seen.ctx && (j0 >= seen.win0 || j0 + kTile <= seen.sinks);
+            const bool see0 = all || seen.seen(j0 + n4), see1 = all || seen.seen(j0 + 8 + n4);
+            // ---- scores, in independent sums (a chain of MMAs waits for each result)
+            float s[4];
+            {
+                uint32_t sc[2];
+                uint32_t k[2][4 * NK];
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
-                    A[j][0] = q8::pair_of(__byte_perm(k[j][x], 0u, 0x1100u), st[j]);
-                    A[j][1] = q8::pair_of(__byte_perm(k[j][x], 0u, 0x3322u), st[j]);
+                    const uint32_t E = g[Gr::exponents(0, 8 * j + n4) + c4 * (D / 64) / 2];
+                    sc[j] = (j ? see1 : see0) ? q8::scale2(E, E) : 0u;
+#pragma unroll
+                    for (int x = 0; x < NK; ++x) {
+                        const uint4 u = *reinterpret_cast<const uint4*>(g + Gr::piece(0, 8 * j + n4, NK * c4 + x));
+                        k[j][4 * x] = u.x; k[j][4 * x + 1] = u.y; k[j][4 * x + 2] = u.z; k[j][4 * x + 3] = u.w;
+                    }
+                }
+                constexpr int SUMS = F32 ? 1 : 2;
+                float z[PL][SUMS][4];
+#pragma unroll
+                for (int pl = 0; pl < PL; ++pl)
+#pragma unroll
+                    for (int h = 0; h < SUMS; ++h) z[pl][h][0] = z[pl][h][1] = z[pl][h][2] = z[pl][h][3] = 0.f;
+#pragma unroll
+                for (int x = 0; x < 4 * NK; ++x) {
+                    uint32_t A[2][2];
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        A[j][0] = q8::pair_of(__byte_perm(k[j][x], 0u, 0x1100u), sc[j]);
+                        A[j][1] = q8::pair_of(__byte_perm(k[j][x], 0u, 0x3322u), sc[j]);
+                    }
+#pragma unroll
+                    for (int pl = 0; pl < PL; ++pl) {
+                        const uint4 q = sm_q[x / 2][pl][lane];
+                        mma(z[pl][x % SUMS], A[0][0], A[1][0], A[0][1], A[1][1], x % 2 ? q.z : q.x, x % 2 ? q.w : q.y);
+                    }
                 }
 #pragma unroll
-                for (int pl = 0; pl < PL; ++pl) {
-                    const uint4 q = sm_q[x / 2][pl][lane];
-                    mma(z[pl][x % 2], A[0][0], A[1][0], A[0][1], A[1][1], x % 2 ? q.z : q.x, x % 2 ? q.w : q.y);
+                for (int e = 0; e < 4; ++e) {
+                    if constexpr (F32)
+                        s[e] = z[0][0][e] + (z[1][0][e] + z[2][0][e]);
+                    else
+                        s[e] = z[0][0][e] + z[0][1][e];
                 }
             }
+            uint32_t pb[PV][2];
+            soften(s, see0, see1, scale, m, l, o, pb);
+            // ---- values: rows 2 c4, 2 c4 + 1, 2 c4 + 8, 2 c4 + 9
+            uint32_t sc[2];
+            uint32_t v[4][NW];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                s[e] = z[0][0][e] + z[0][1][e];
-                if constexpr (F32) s[e] += (z[1][0][e] + z[1][1][e]) + (z[2][0][e] + z[2][1][e]);
-            }
-        }
-        uint32_t pb[PV][2];
-        soften(s, see0, see1, scale, m, l, o, pb);
-        // ---- values: rows 2 c4, 2 c4 + 1, 2 c4 + 8, 2 c4 + 9
-        q8::Step2 st[2];
-        uint32_t v[4][NW];
+            for (int j = 0; j < 2; ++j) {
+                uint32_t E[2];
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            uint32_t E[2];
-#pragma unroll
-            for (int r = 0; r < 2; ++r) {
-                const int row = 2 * c4 + r + 8 * j;
-                E[r] = g[Gr::exponents(1, row) + n4 / 2 * (D / 64) / 2];
-                const uint8_t* at = g + Gr::piece(1, row, D == 128 ? n4 : n4 / 2);
-                if constexpr (D == 128) {
-                    const uint4 u = *reinterpret_cast<const uint4*>(at);
-                    v[2 * j + r][0] = u.x; v[2 * j + r][1] = u.y; v[2 * j + r][2] = u.z; v[2 * j + r][3] = u.w;
-                } else {
-                    const uint2 u = *reinterpret_cast<const uint2*>(at + n4 % 2 * 8);
-                    v[2 * j + r][0] = u.x; v[2 * j + r][1] = u.y;
+                for (int r = 0; r < 2; ++r) {
+                    const int row = 2 * c4 + r + 8 * j;
+                    E[r] = g[Gr::exponents(1, row) + n4 / 2 * (D / 64) / 2];
+                    const uint8_t* from = g + Gr::piece(1, row, D == 128 ? n4 : n4 / 2);
+                    if constexpr (D == 128) {
+                        const uint4 u = *reinterpret_cast<const uint4*>(from);
+                        v[2 * j + r][0] = u.x; v[2 * j + r][1] = u.y; v[2 * j + r][2] = u.z; v[2 * j + r][3] = u.w;
+                    } else {
+                        const uint2 u = *reinterpret_cast<const uint2*>(from + n4 % 2 * 8);
+                        v[2 * j + r][0] = u.x; v[2 * j + r][1] = u.y;
+                    }
                 }
+                sc[j] = q8::scale2(E[0], E[1]);
+                if (!all)
+                    sc[j] &= (seen.seen(j0 + 2 * c4 + 8 * j) ? 0xffffu : 0u) |
+                             (seen.seen(j0 + 2 * c4 + 1 + 8 * j) ? 0xffff0000u : 0u);
             }
-            st[j] = q8::step2(E[0], E[1]);
-            if (!all) {
-                const uint32_t keep = (seen.seen(j0 + 2 * c4 + 8 * j) ? 0xffffu : 0u) |
-                                      (seen.seen(j0 + 2 * c4 + 1 + 8 * j) ? 0xffff0000u : 0u);
-                st[j].step &= keep;
-                st[j].minus128 &= keep;
+#pragma unroll
+            for (int e = 0; e < D / 16; ++e) {
+                uint32_t A[2][2];
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+#pragma unroll
+                    for (int r = 0; r < 2; ++r)
+                        A[j][r] = q8::pair_of(
+                            __byte_perm(v[2 * j][e / 2], v[2 * j + 1][e / 2], 0x4400u + 0x1111u * (e % 2 * 2 + r)), sc[j]);
+                add_values<F32>(o[e], A[0][0], A[0][1], A[1][0], A[1][1], pb);
             }
         }
+        asm volatile("cp.async.wait_all;" ::: "memory");
+        __syncwarp();
+        float* sm_o = reinterpret_cast<float*>(mine);
 #pragma unroll
-        for (int e = 0; e < D / 16; ++e) {
-            uint32_t A[2][2];
+        for (int h = 0; h < 2; ++h)
 #pragma unroll
-            for (int j = 0; j < 2; ++j)
-#pragma unroll
-                for (int r = 0; r < 2; ++r)
-                    A[j][r] = q8::pair_of(__byte_perm(v[2 * j][e / 2], v[2 * j + 1][e / 2], 0x4400u + 0x1111u * (e % 2 * 2 + r)), st[j]);
-            add_values<F32>(o[e], A[0][0], A[0][1], A[1][0], A[1][1], pb);
+            for (int e = 0; e < D / 16; e += 2)
+                *reinterpret_cast<float4*>(sm_o + (2 * c4 + h) * D + D / 8 * n4 + 2 * e) =
+                    make_float4(o[e][h], o[e][2 + h], o[e + 1][h], o[e + 1][2 + h]);
+        // A block's part of a unit that began in an earlier block is its first, of one that ends in a
+        // later block its second; a unit's counter is that of the block where it begins.
+        const int64_t from = unit_at / share, active = (unit_at + steps - 1) / share - from + 1;
+        join<D, T>(p, sh, reinterpret_cast<const float*>(ring), kStages * Gr::BYTES / 4, m, l, b, kvh * G + head0, heads,
+                   (int)active, p.counters + from, 2 * (int64_t)blockIdx.x + (from == blockIdx.x),
+                   [&](int x) { return 2 * (from + x) + (x == 0); });
+        unit_at += steps;
+        if (unit_at >= end) return;
+        step = 0;
+        if (++unit == units) {
+            unit = 0;
+            ++b;
         }
+        __syncthreads();  // the join has read the ring and the queries are free
     }
-    asm volatile("cp.async.wait_all;" ::: "memory");
-    __syncwarp();
-    float* sm_o = reinterpret_cast<float*>(mine);
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int e = 0; e < D / 16; e += 2)
-            *reinterpret_cast<float4*>(sm_o + (2 * c4 + h) * D + D / 8 * n4 + 2 * e) =
-                make_float4(o[e][h], o[e][2 + h], o[e + 1][h], o[e + 1][2 + h]);
-    join<D, T>(p, sh, reinterpret_cast<const float*>(ring), kStages * Gr::BYTES / 4, m, l, b, kvh * G + head0, heads, split,
-               active);
 }
 
 constexpr int kPlaces = 152 * kResident;
@@ -643,14 +705,20 @@ Plan make_plan(int B, int Hq, int Hkv, int window, int sinks, int max_ctx) {
     return p;
 }
 
+// Steps of a call over the 8-bit cache, at most.
+int64_t most_steps(int B, int Hkv, int groups, int window, int sinks, int max_ctx) {
+    return (int64_t)B * Hkv * groups * ((visible_tiles(window, sinks, max_ctx) + kWarps - 1) / kWarps);
+}
+
 template <int D, typename T>
 cudaError_t launch_t(const DecodeArgs& p, bool q8, cudaStream_t st) {
     const dim3 grid((unsigned)p.a.rows * p.plan.splits, p.a.Hkv * p.plan.groups);
     if (!q8) return launch_pdl(window_decode_kernel<D, T>, grid, kThreads, 0, st, p);
     constexpr int BYTES = kWarps * kStages * q8::Granule<D>::BYTES;
+    const dim3 grid8((unsigned)std::min<int64_t>(kPlaces8, most_steps(p.a.rows, p.a.Hkv, p.plan.groups, p.a.window, p.a.sinks, p.a.max_ctx)));
     static std::atomic<uint64_t> ready{0};
     const cudaError_t e = raise_smem_limit(window_decode_q8_kernel<D, T>, BYTES, ready);
-    return e != cudaSuccess ? e : launch_pdl(window_decode_q8_kernel<D, T>, grid, kThreads, BYTES, st, p);
+    return e != cudaSuccess ? e : launch_pdl(window_decode_q8_kernel<D, T>, grid8, kThreads, BYTES, st, p);
 }
 
 cudaError_t launch_any(const WindowArgs& a, bool f32, bool q8, cudaStream_t st) {
@@ -658,10 +726,11 @@ cudaError_t launch_any(const WindowArgs& a, bool f32, bool q8, cudaStream_t st) 
     p.a = a;
     p.plan = make_plan(a.rows, a.Hq, a.Hkv, a.window, a.sinks, a.max_ctx);
     if ((int64_t)a.rows * p.plan.splits > 0x7fffffff) return cudaErrorInvalidValue;
-    const int64_t parts = (int64_t)a.rows * a.Hkv * p.plan.groups * p.plan.splits * p.plan.heads;
+    const int64_t parts = q8 ? 2 * std::min<int64_t>(kPlaces8, most_steps(a.rows, a.Hkv, p.plan.groups, a.window, a.sinks, a.max_ctx))
+                             : (int64_t)a.rows * a.Hkv * p.plan.groups * p.plan.splits;
     p.counters = static_cast<unsigned*>(a.scratch);
     p.part = reinterpret_cast<float*>(p.counters + kMaxCounters);
-    p.ml = reinterpret_cast<float2*>(p.part + parts * a.d);
+    p.ml = reinterpret_cast<float2*>(p.part + parts * p.plan.heads * a.d);
     if (a.d == 128) return f32 ? launch_t<128, float>(p, q8, st) : launch_t<128, __nv_bfloat16>(p, q8, st);
     return f32 ? launch_t<64, float>(p, q8, st) : launch_t<64, __nv_bfloat16>(p, q8, st);
 }
@@ -684,8 +753,11 @@ uint64_t window_decode_scratch(int B, int Hq, int Hkv, int d, int window, int si
 
 cudaError_t launch_window_decode(const WindowArgs& a, bool f32, cudaStream_t st) { return launch_any(a, f32, false, st); }
 
+// Two parts for each block; more blocks for more or longer requests.
 uint64_t window_decode_q8_scratch(int B, int Hq, int Hkv, int d, int window, int sinks, int max_ctx) {
-    return window_decode_scratch(B, Hq, Hkv, d, window, sinks, max_ctx);
+    const Plan p = make_plan(B, Hq, Hkv, window, sinks, max_ctx);
+    const uint64_t blocks = std::min<int64_t>(kPlaces8, most_steps(B, Hkv, p.groups, window, sinks, max_ctx));
+    return (kCounterBytes + blocks * 2 * p.heads * (d + 2) * sizeof(float) + 15) / 16 * 16;
 }
 cudaError_t launch_window_decode_q8(const WindowArgs& a, bool f32, cudaStream_t st) { return launch_any(a, f32, true, st); }
 
