@@ -82,7 +82,7 @@ __device__ __forceinline__ float value_of(uint32_t code, float step) {
 //
 // The second factor for a pair of blocks (or for one, twice).
 __device__ __forceinline__ uint32_t scale2(uint32_t Elo, uint32_t Ehi) {
-    const uint32_t e = __vmaxu2(Elo | Ehi << 16, 0x00070007u);
+    const uint32_t e = Elo + Ehi * 65536u;
     const uint32_t nan = (e + 0x00020002u & 0x01000100u) >> 2;  // 0x40 where it is 254 or 255
     return e * 128u | nan * 511u;                               // 0x40 x 511 = 0x7fc0
 }

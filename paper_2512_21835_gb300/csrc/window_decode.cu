@@ -110,10 +110,17 @@ struct Tiles {
 
 // The running softmax over a tile: a lane has the scores of positions n4 (s[0], s[1]) and n4 + 8
 // (s[2], s[3]) and heads 2 c4 + {0, 1}; O is rescaled where a maximum has grown.  pb: the planes of
-// P^T in the MMA's B layout; the last one is rounded (exact if it is the third).
-template <int PV, int NO>
+// P^T in the MMA's B layout; the last one is rounded (exact if it is the third).  FAST: weights below
+// 2^-126 are zero.
+__device__ __forceinline__ float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+template <bool FAST, int PV, int NO>
 __device__ __forceinline__ void soften(const float (&s)[4], bool see0, bool see1, float scale, float (&m)[2], float (&l)[2],
                                        float (&o)[NO][4], uint32_t (&pb)[PV][2]) {
+    auto power = [](float x) { return FAST ? ex2(x) : exp2f(x); };
     float w[4], mx[2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
@@ -128,7 +135,7 @@ __device__ __forceinline__ void soften(const float (&s)[4], bool see0, bool see1
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const float m_new = fmaxf(m[h], mx[h]);
-            alpha[h] = m[h] == -INFINITY ? 0.f : exp2f(m[h] - m_new);
+            alpha[h] = m[h] == -INFINITY ? 0.f : power(m[h] - m_new);
             m[h] = m_new;
             l[h] *= alpha[h];
         }
@@ -140,8 +147,8 @@ __device__ __forceinline__ void soften(const float (&s)[4], bool see0, bool see1
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
         const float base = m[h] == -INFINITY ? 0.f : m[h];  // nothing seen yet: every weight is zero
-        w[h] = exp2f(w[h] - base);
-        w[2 + h] = exp2f(w[2 + h] - base);
+        w[h] = power(w[h] - base);
+        w[2 + h] = power(w[2 + h] - base);
         l[h] += w[h] + w[2 + h];
     }
 #pragma unroll
@@ -383,7 +390,7 @@ __global__ void __launch_bounds__(kThreads, kResident) window_decode_kernel(cons
         if (at_next) load_k(seen.at(i + kWarps), at_next);
         // ---- softmax
         uint32_t pb[PV][2];
-        soften(s, seen.seen(t * kTile + n4), seen.seen(t * kTile + 8 + n4), scale, m, l, o, pb);
+        soften<false>(s, seen.seen(t * kTile + n4), seen.seen(t * kTile + 8 + n4), scale, m, l, o, pb);
         // ---- values
 #pragma unroll
         for (int x = 0; x < NV; ++x) {
@@ -557,18 +564,18 @@ __global__ void __launch_bounds__(kThreads, kResident8) window_decode_q8_kernel(
             // ---- scores, in independent sums (a chain of MMAs waits for each result)
             float s[4];
             {
-                uint32_t sc[2];
-                uint32_t k[2][4 * NK];
+                uint32_t k[2][4 * NK], E[2];
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
-                    const uint32_t E = g[Gr::exponents(0, 8 * j + n4) + c4 * (D / 64) / 2];
-                    sc[j] = (j ? see1 : see0) ? q8::scale2(E, E) : 0u;
+                    E[j] = g[Gr::exponents(0, 8 * j + n4) + c4 * (D / 64) / 2];
 #pragma unroll
                     for (int x = 0; x < NK; ++x) {
                         const uint4 u = *reinterpret_cast<const uint4*>(g + Gr::piece(0, 8 * j + n4, NK * c4 + x));
                         k[j][4 * x] = u.x; k[j][4 * x + 1] = u.y; k[j][4 * x + 2] = u.z; k[j][4 * x + 3] = u.w;
                     }
                 }
+                const uint32_t both = q8::scale2(E[0], E[1]);
+                const uint32_t sc[2] = {see0 ? __byte_perm(both, 0u, 0x1010u) : 0u, see1 ? __byte_perm(both, 0u, 0x3232u) : 0u};
                 constexpr int SUMS = F32 ? 1 : 2;
                 float z[PL][SUMS][4];
 #pragma unroll
@@ -598,7 +605,7 @@ __global__ void __launch_bounds__(kThreads, kResident8) window_decode_q8_kernel(
                 }
             }
             uint32_t pb[PV][2];
-            soften(s, see0, see1, scale, m, l, o, pb);
+            soften<true>(s, see0, see1, scale, m, l, o, pb);
             // ---- values: rows 2 c4, 2 c4 + 1, 2 c4 + 8, 2 c4 + 9
             uint32_t sc[2];
             uint32_t v[4][NW];
