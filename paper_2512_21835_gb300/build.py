@@ -11,7 +11,7 @@ CSRC = os.path.join(HERE, "csrc")
 OUT = os.path.join(HERE, "libloip.so")
 BUILD = os.path.join(HERE, "_build")
 SOURCES = ["decode.cu", "prefill.cu", "gemm_tc.cu", "attn_tc.cu", "pack.cu", "runtime.cu", "plan.cpp", "hostpool.cpp", "noalloc.cu",
-           "disktier.cpp", "window.cu", "window_decode.cu", "window_prefill.cu", "window_q8.cu"]
+           "disktier.cpp", "window.cu", "window_decode.cu", "window_prefill.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 
 

@@ -99,7 +99,7 @@ cudaError_t launch_window_decode(const WindowArgs& a, bool f32, cudaStream_t st)
 // Attention of prompt rows (window_prefill.cu).
 uint64_t window_prefill_scratch(int M, int n_prompts, int Hq, int Hkv, int d, int window, int sinks, int max_ctx);
 cudaError_t launch_window_prefill(const WindowArgs& a, bool f32, cudaStream_t st);
-// The same over the 8-bit cache (window_q8.cu).
+// The same over the 8-bit cache (the same files).
 uint64_t window_decode_q8_scratch(int B, int Hq, int Hkv, int d, int window, int sinks, int max_ctx);
 cudaError_t launch_window_decode_q8(const WindowArgs& a, bool f32, cudaStream_t st);
 uint64_t window_prefill_q8_scratch(int M, int n_prompts, int Hq, int Hkv, int d, int window, int sinks, int max_ctx);

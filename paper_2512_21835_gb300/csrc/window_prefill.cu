@@ -68,6 +68,7 @@
 #include <type_traits>
 
 #include "internal.h"
+#include "q8.h"
 #include "window.h"
 #include "window_parts.h"
 #include "window_walk.h"
@@ -78,14 +79,18 @@ __device__ int g_window_error;  // first failure code of any launch (0 = none)
 
 namespace {
 
-constexpr int kThreads = 384;
-constexpr int kLoaders = 64;                     // threads of warps 8 and 9
 constexpr int kSms = 152;
-constexpr int kSoftRegs = 200, kOtherRegs = 104;  // 256 x 200 + 128 x 104 = 384 x 168
 constexpr int KT = kPageTokens;                  // keys per tile
 
-template <int D, int NP, int QT>
+template <int D, int NP, int QT, bool Q8>
 struct Cfg {
+    // Warps 0 to 7 softmax, from 8 on loaders, then one per stream that issues MMAs.  The registers
+    // of the softmax warps, of the loaders' warpgroup and (Q8) of the issuing one:
+    static constexpr int LOADERS = Q8 ? 128 : 64;      // threads
+    static constexpr int MMA_WARP = 8 + LOADERS / 32;
+    static constexpr int THREADS = Q8 ? 512 : 384;
+    static constexpr int SOFT_REGS = 200, LOAD_REGS = Q8 ? 72 : 104, MMA_REGS = Q8 ? 40 : 104;
+    static_assert(2 * SOFT_REGS + (Q8 ? LOAD_REGS + MMA_REGS : LOAD_REGS) <= 65536 / THREADS / 8 * 8 * (THREADS / 128), "");
     static constexpr int SLABS = D / 64;               // 128-byte columns of a row
     static constexpr int Q_SLAB = 128 * 128;
     static constexpr int Q_PLANE = SLABS * Q_SLAB;
@@ -311,9 +316,9 @@ struct Pages {
     __device__ int at(int v) const { return v < sink ? v : v - sink + win; }
 };
 
-template <int D, int NP, int QT, typename T>
-__global__ void __launch_bounds__(kThreads, 1) window_prefill_kernel(const __grid_constant__ PrefillArgs p) {
-    using C = Cfg<D, NP, QT>;
+template <int D, int NP, int QT, bool Q8, typename T>
+__global__ void __launch_bounds__(Q8 ? 512 : 384, 1) window_prefill_kernel(const __grid_constant__ PrefillArgs p) {
+    using C = Cfg<D, NP, QT, Q8>;
     const WindowArgs& a = p.a;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* sm = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
@@ -382,7 +387,7 @@ __global__ void __launch_bounds__(kThreads, 1) window_prefill_kernel(const __gri
             c->abort = 0;
             c->bad = 0;
             for (int i = 0; i < C::SLOTS; ++i) {
-                bar_init(bar_full + 8 * i, kLoaders);
+                bar_init(bar_full + 8 * i, C::LOADERS);
                 bar_init(bar_empty + 8 * i, QT);
             }
             for (int w = 0; w < 2; ++w) {
@@ -398,7 +403,7 @@ __global__ void __launch_bounds__(kThreads, 1) window_prefill_kernel(const __gri
             bar_init(bar_end, 2);
             asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         }
-    } else if (warp == 10) {
+    } else if (warp == C::MMA_WARP) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&c->tmem)),
                      "r"(512u)
                      : "memory");
@@ -440,11 +445,110 @@ __global__ void __launch_bounds__(kThreads, 1) window_prefill_kernel(const __gri
     Waiter wait{c, false};
     auto stopped = [&] { return *(volatile int*)&c->abort != 0; };
     if (warp >= 8) {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegs));
-        if (warp < 10) {
+        if (!Q8 || warp < 12)
+            asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::LOAD_REGS));
+        else
+            asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::MMA_REGS));
+        if (warp < C::MMA_WARP) {
+            if constexpr (Q8) {
+                // ------------------------------------------------------------ loader, 8-bit cache
+                // A thread takes a piece (16 elements) of one token in PASSES groups of tokens, of keys
+                // and of values: from the cache into registers a slot ahead, then as bf16 into its slot.
+                // (Eight lanes have four pieces of two neighbouring tokens: the 16-byte stores meet no
+                // bank conflicts.)
+                using Gr = q8::Granule<D>;
+                const int lt = tid - 256;
+                constexpr int GROUP = C::LOADERS * 16 / D, PASSES = KT / GROUP;  // tokens of a pass
+                static_assert(GROUP % q8::kGranule == 0, "");
+                const int ch = D == 128 ? (lt & 3) | (lt >> 1 & 4) : lt & 3;
+                const int r0 = D == 128 ? lt >> 4 << 1 | (lt >> 2 & 1) : lt >> 2;
+                constexpr int STEP = GROUP / q8::kGranule * Gr::BYTES;  // from a pass to the next in the cache
+                const char* from = a.kv.base + (uint64_t)a.kv.layer * a.kv.layer_page_bytes +
+                                   ((int64_t)kvh * 4 + r0 / 16) * Gr::BYTES;
+                const int codes = Gr::piece(0, r0 % 16, ch), exps = Gr::exponents(0, r0 % 16) + ch / 2;
+                const int64_t* table = a.kv.page_offsets + (int64_t)req * a.kv.max_pages;
+                const int win0 = max(0, pos0 - a.window + 1);  // (window 0: no page of it is in the list)
+                const uint32_t place =
+                    (uint32_t)((ch >> 2) * C::KV_SLAB + r0 * 128 + ((2 * (ch & 3) ^ (r0 & 7)) << 4));
+                uint4 code[2][PASSES];  // of keys, of values
+                uint32_t exp[2][PASSES];
+                auto fetch = [&](int64_t page, auto which) {
+                    constexpr int V = decltype(which)::value;
+                    const char* g = from + page;
+#pragma unroll
+                    for (int k = 0; k < PASSES; ++k) {
+                        code[V][k] = *reinterpret_cast<const uint4*>(g + codes + V * 16 * D + k * STEP);
+                        exp[V][k] = *reinterpret_cast<const uint8_t*>(g + exps + V * (D / 2) + k * STEP);
+                    }
+                };
+                // What no row of the block sees is zero.  A value's NaN that only some rows see is taken out,
+                // and the block's rows are walked one by one.
+                auto put = [&](int t, uint32_t to, auto which) {
+                    constexpr int V = decltype(which)::value;
+                    const int b = page_at(t) * KT;
+                    const bool whole = b + KT <= pages.last && ((b >= win0 && a.window > 0) || b + KT <= a.sinks);
+                    const bool shared = b + KT - 1 <= pos0 && (b > pos1 - a.window || b + KT <= a.sinks);
+#pragma unroll
+                    for (int k = 0; k < PASSES; ++k) {
+                        const int pos = b + r0 + k * GROUP;
+                        uint32_t scale = q8::scale2(exp[V][k], exp[V][k]);
+                        if (!whole && !(pos < pages.last && ((pos >= win0 && a.window > 0) || pos < a.sinks))) {
+                            scale = 0u;
+                        } else if (V && !shared && exp[V][k] > q8::kMostExponent) {
+                            scale = 0u;
+                            *(volatile int*)&c->bad = 1;
+                        }
+                        const uint32_t w[4] = {code[V][k].x, code[V][k].y, code[V][k].z, code[V][k].w};
+                        uint32_t u[8];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            u[2 * e] = q8::pair_of(__byte_perm(w[e], 0u, 0x1100u), scale);
+                            u[2 * e + 1] = q8::pair_of(__byte_perm(w[e], 0u, 0x3322u), scale);
+                        }
+                        const uint32_t dst = to + place + k * GROUP * 128;
+                        asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(dst), "r"(u[0]), "r"(u[1]), "r"(u[2]),
+                                     "r"(u[3])
+                                     : "memory");
+                        asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(dst ^ 16u), "r"(u[4]), "r"(u[5]),
+                                     "r"(u[6]), "r"(u[7])
+                                     : "memory");
+                    }
+                };
+                using Keys = std::integral_constant<int, 0>;
+                using Values = std::integral_constant<int, 1>;
+                auto page_of = [&](int t) { return t < n ? table[page_at(t)] : 0; };
+                constexpr int AT = C::AHEAD + 2;
+                int64_t at[AT];  // page offsets of tiles i + 1 - AHEAD .. i + 2
+                int slot = 0;
+                uint32_t free_phase = 1;  // of the ring's previous round (before the first one: complete)
+                if (n > 0) {
+                    at[AT - 3] = page_of(0);
+                    at[AT - 2] = page_of(1);
+                    fetch(at[AT - 3], Keys{});
+                }
+#pragma unroll 1
+                for (int i = 0; i < n + C::AHEAD && n > 0; ++i) {
+                    const int t = i - C::AHEAD;  // whose values
+                    const uint32_t dst = ring + (uint32_t)slot * C::SLOT;
+                    at[AT - 1] = page_of(i + 2);
+                    wait(bar_empty + 8 * slot, free_phase, 1);
+                    if (i < n) put(i, dst, Keys{});
+                    if (i + 1 < n) fetch(at[AT - 2], Keys{});
+                    if (t >= 0) put(t, dst + C::TILE, Values{});
+                    if (t + 1 >= 0 && t + 1 < n) fetch(at[0], Values{});
+                    fence_loaded();
+                    bar_arrive(bar_full + 8 * slot);
+#pragma unroll
+                    for (int x = 0; x < AT - 1; ++x) at[x] = at[x + 1];
+                    if (++slot == C::SLOTS) {
+                        slot = 0;
+                        free_phase ^= 1;
+                    }
+                }
+            } else {
             // ---------------------------------------------------------------- loader
             const int lt = tid - 256;
-            constexpr int CPR = D / 8, RPP = kLoaders / CPR;  // 16-byte chunks per row, rows per pass
+            constexpr int CPR = D / 8, RPP = C::LOADERS / CPR;  // 16-byte chunks per row, rows per pass
             constexpr int PASSES = KT / RPP;
             const int chunk = lt % CPR, r0 = lt / CPR;
             const char* layer = a.kv.base + (uint64_t)a.kv.layer * a.kv.layer_page_bytes;
@@ -525,9 +629,10 @@ __global__ void __launch_bounds__(kThreads, 1) window_prefill_kernel(const __gri
             }
             asm volatile("cp.async.wait_all;" ::: "memory");
             if (late >= 0) checked(late);
-        } else if (n > 0) {
+            }
+        } else if (n > 0 && warp < C::MMA_WARP + 2) {
             // ---------------------------------------------------------------- MMA issue
-            const int w = warp - 10;  // the stream
+            const int w = warp - C::MMA_WARP;  // the stream
             const Takes takes = takes_of(w);
             auto mine = [&](int t) { return t >= 0 && t < n && (QT == 1 ? (t & 1) == w : takes(t)); };
             const uint64_t q_desc = sdesc(q_smem + (QT == 2 ? w * NP * C::Q_PLANE : 0), 16), k_desc = sdesc(ring, 16),
@@ -599,7 +704,7 @@ __global__ void __launch_bounds__(kThreads, 1) window_prefill_kernel(const __gri
         }
     } else if (tokens > 0) {
         // -------------------------------------------------------------------- softmax
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftRegs));
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(C::SOFT_REGS));
         const T* qg = static_cast<const T*>(a.q);
         T* og = static_cast<T*>(a.o);
         auto row_at = [&](int tok, int head) {  // element offset of a row of q and o
@@ -964,12 +1069,12 @@ __global__ void __launch_bounds__(kThreads, 1) window_prefill_kernel(const __gri
             }
         }
     } else {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftRegs));
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(C::SOFT_REGS));
     }
     __syncwarp();
     fence_before();
     __syncthreads();
-    if (warp == 10) {
+    if (warp == C::MMA_WARP) {
         fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
     }
@@ -982,14 +1087,14 @@ __global__ void __launch_bounds__(kThreads, 1) window_prefill_kernel(const __gri
     } else if (end == kPartNotFinite && warp < 8) {
         for (int i = warp; i < tokens * heads; i += 8) {
             const int64_t at = ((int64_t)(row0 + i / heads) * a.Hq + kvh * G + head0 + i % heads) * D;
-            walk_row<D, false, T>(a, req, kvh, pos0 + i / heads, static_cast<const T*>(a.q) + at, static_cast<T*>(a.o) + at);
+            walk_row<D, Q8, T>(a, req, kvh, pos0 + i / heads, static_cast<const T*>(a.q) + at, static_cast<T*>(a.o) + at);
         }
     }
 }
 
 // The parts of a row tile, in their order: a block per unit and 16 columns, a thread per row
 // and 8 columns.
-template <int D, typename T>
+template <int D, bool Q8, typename T>
 __global__ void __launch_bounds__(256) window_join_kernel(const __grid_constant__ PrefillArgs p) {
     const WindowArgs& a = p.a;
     pdl_trigger();
@@ -1008,7 +1113,7 @@ __global__ void __launch_bounds__(256) window_join_kernel(const __grid_constant_
         const int warp = threadIdx.x / 32 + blockIdx.x % PIECES * 8;
         for (int i = warp; i < rows.y * heads; i += 8 * PIECES) {
             const int64_t at = ((int64_t)(rows.x + i / heads) * a.Hq + kvh * G + head0 + i % heads) * D;
-            walk_row<D, false, T>(a, rows.z, kvh, rows.w + i / heads, static_cast<const T*>(a.q) + at,
+            walk_row<D, Q8, T>(a, rows.z, kvh, rows.w + i / heads, static_cast<const T*>(a.q) + at,
                            static_cast<T*>(a.o) + at);
         }
         return;
@@ -1087,25 +1192,25 @@ Plan make_plan(int M, int n_prompts, int Hq, int Hkv, int window, int sinks, int
     return p;
 }
 
-template <int D, int NP, int QT, typename T>
+template <int D, int NP, int QT, bool Q8, typename T>
 cudaError_t launch_t(const PrefillArgs& p, cudaStream_t st) {
-    using C = Cfg<D, NP, QT>;
+    using C = Cfg<D, NP, QT, Q8>;
     static std::atomic<uint64_t> ready{0};  // devices whose limit has been raised, one bit each
-    cudaError_t e = raise_smem_limit(window_prefill_kernel<D, NP, QT, T>, C::BYTES, ready);
+    cudaError_t e = raise_smem_limit(window_prefill_kernel<D, NP, QT, Q8, T>, C::BYTES, ready);
     if (e != cudaSuccess) return e;
     const int64_t tiles = p.a.rows / (QT * p.tok) + p.a.n_prompts;  // at least the sum over prompts
     const int64_t blocks = std::min<int64_t>(tiles, p.a.rows) * p.a.Hkv * p.groups * p.splits;
     if (blocks > 0x7fffffff) return cudaErrorInvalidValue;
-    e = launch_pdl(window_prefill_kernel<D, NP, QT, T>, dim3((unsigned)blocks), kThreads, C::BYTES, st, p);
+    e = launch_pdl(window_prefill_kernel<D, NP, QT, Q8, T>, dim3((unsigned)blocks), C::THREADS, C::BYTES, st, p);
     if (e != cudaSuccess || p.splits == 1) return e;
-    return launch_pdl(window_join_kernel<D, T>, dim3((unsigned)(blocks / p.splits) * (D / 16)), 256, 0, st, p);
+    return launch_pdl(window_join_kernel<D, Q8, T>, dim3((unsigned)(blocks / p.splits) * (D / 16)), 256, 0, st, p);
 }
 
-template <int D>
+template <int D, bool Q8>
 cudaError_t launch_d(const PrefillArgs& p, bool f32, int64_t tiles, cudaStream_t st) {
-    if (f32) return launch_t<D, 3, 1, float>(p, st);
+    if (f32) return launch_t<D, 3, 1, Q8, float>(p, st);
     // two row tiles per block once that leaves no SM without a block
-    return tiles >= 2 * kSms ? launch_t<D, 1, 2, __nv_bfloat16>(p, st) : launch_t<D, 1, 1, __nv_bfloat16>(p, st);
+    return tiles >= 2 * kSms ? launch_t<D, 1, 2, Q8, __nv_bfloat16>(p, st) : launch_t<D, 1, 1, Q8, __nv_bfloat16>(p, st);
 }
 
 }  // namespace
@@ -1122,7 +1227,10 @@ uint64_t window_prefill_scratch(int M, int n_prompts, int Hq, int Hkv, int d, in
     return (n + 15) / 16 * 16;
 }
 
-cudaError_t launch_window_prefill(const WindowArgs& a, bool f32, cudaStream_t st) {
+namespace {
+
+template <bool Q8>
+cudaError_t launch_any(const WindowArgs& a, bool f32, cudaStream_t st) {
     const Plan plan = make_plan(a.rows, a.n_prompts, a.Hq, a.Hkv, a.window, a.sinks, a.max_ctx);
     PrefillArgs p{};
     p.a = a;
@@ -1137,8 +1245,17 @@ cudaError_t launch_window_prefill(const WindowArgs& a, bool f32, cudaStream_t st
     p.rows = reinterpret_cast<int4*>(p.part + plan.tiles * plan.splits * 128 * (a.d / 4));
     p.ml = reinterpret_cast<float2*>(p.rows + plan.tiles);
     p.ended = reinterpret_cast<unsigned*>(p.ml + plan.tiles * plan.splits * 128);
-    return a.d == 128 ? launch_d<128>(p, f32, plan.tiles, st) : launch_d<64>(p, f32, plan.tiles, st);
+    return a.d == 128 ? launch_d<128, Q8>(p, f32, plan.tiles, st) : launch_d<64, Q8>(p, f32, plan.tiles, st);
 }
+
+}  // namespace
+
+cudaError_t launch_window_prefill(const WindowArgs& a, bool f32, cudaStream_t st) { return launch_any<false>(a, f32, st); }
+
+uint64_t window_prefill_q8_scratch(int M, int n_prompts, int Hq, int Hkv, int d, int window, int sinks, int max_ctx) {
+    return window_prefill_scratch(M, n_prompts, Hq, Hkv, d, window, sinks, max_ctx);
+}
+cudaError_t launch_window_prefill_q8(const WindowArgs& a, bool f32, cudaStream_t st) { return launch_any<true>(a, f32, st); }
 
 cudaError_t window_prefill_error(int* code) { return cudaMemcpyFromSymbol(code, g_window_error, sizeof(int)); }
 
