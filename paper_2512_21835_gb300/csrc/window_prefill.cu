@@ -98,11 +98,18 @@ struct Cfg {
     static constexpr int KV_SLAB = KT * 128;
     static constexpr int TILE = SLABS * KV_SLAB;       // one tile of keys or of values
     static constexpr int SLOT = 2 * TILE;              // the keys of one tile, the values of an earlier one
-    static constexpr int ROOM = 227 * 1024 - 1024 - 512 - Q_BYTES;
-    static constexpr int MOST = ROOM / SLOT < 12 ? ROOM / SLOT : 12;
-    static constexpr int SLOTS = QT == 2 ? MOST : MOST / 2 * 2;  // (a stream's own slots: every second one)
+    static constexpr int PAGE = Q8 ? 4 * q8::Granule<D>::BYTES : 0;  // a page's part of a kv head, as it is cached
+    static constexpr int STAGES = Q8 && NP == 1 ? 3 : 2;             // of those
+    static constexpr int ROOM = 227 * 1024 - 1024 - 512 - Q_BYTES - STAGES * PAGE;
+    static constexpr int LIMIT = Q8 ? 4 : 12;
+    static constexpr int MOST = ROOM / SLOT < LIMIT ? ROOM / SLOT : LIMIT;
+    static constexpr int SLOTS = QT == 2 || Q8 ? MOST : MOST / 2 * 2;
+    // Use i of the ring is of slot i % SLOTS and of barrier i % CYCLE.  With one row tile a stream takes
+    // every second use: CYCLE is even, so that a stream meets every phase of its barriers.
+    static constexpr int CYCLE = QT == 1 && SLOTS % 2 ? 2 * SLOTS : SLOTS;
     static constexpr int AHEAD = 3 - QT;                 // slot i: keys of tile i, values of tile i - AHEAD
-    static constexpr int CTL = Q_BYTES + SLOTS * SLOT;
+    static constexpr int STAGE = Q_BYTES + SLOTS * SLOT;
+    static constexpr int CTL = STAGE + STAGES * PAGE;
     static constexpr int BYTES = CTL + 512 + 1024;     // + alignment of the window
     static_assert(SLOTS >= 3, "the loader may signal a slot after it has filled the next");
     static_assert(QT == 2 || SLOTS * SLOT >= 128 * (D + 8) * 4 + 2048, "the join goes through the ring");
@@ -120,11 +127,25 @@ struct Ctl {  // control words behind the ring
     uint64_t s_full[2], s_free[2];     // per stream
     uint64_t p_full[4], pv_done[4];    // per stream and P buffer: for even and odd tiles, no wait is ever two phases behind
     uint64_t o_free, q_full, end;
+    uint64_t page_full[4], page_free[4];  // of the pages as they are cached
     uint32_t tmem;
     int abort, bad;
     int row0, tokens, req, pos0;
 };
 static_assert(sizeof(Ctl) <= 512, "");
+
+// A use of the ring: its slot, its barriers, and their phase.
+struct Use {
+    uint32_t slot, bar, phase;
+    template <int SLOTS, int CYCLE>
+    __device__ __forceinline__ void next() {
+        if (++slot == SLOTS) slot = 0;
+        if (++bar == CYCLE) {
+            bar = 0;
+            phase ^= 1;
+        }
+    }
+};
 
 struct PrefillArgs {
     WindowArgs a;
@@ -328,7 +349,8 @@ __global__ void __launch_bounds__(Q8 ? 512 : 384, 1) window_prefill_kernel(const
                    bar_s = ctl + offsetof(Ctl, s_full), bar_s_free = ctl + offsetof(Ctl, s_free),
                    bar_p = ctl + offsetof(Ctl, p_full), bar_pv = ctl + offsetof(Ctl, pv_done),
                    bar_o_free = ctl + offsetof(Ctl, o_free), bar_q = ctl + offsetof(Ctl, q_full),
-                   bar_end = ctl + offsetof(Ctl, end);
+                   bar_end = ctl + offsetof(Ctl, end), bar_page = ctl + offsetof(Ctl, page_full),
+                   bar_page_free = ctl + offsetof(Ctl, page_free);
     const int tid = threadIdx.x, warp = tid / 32, lane = tid % 32;
 
     // ---- which rows: splits fastest, then kv heads (and groups of their heads), then
@@ -386,9 +408,13 @@ __global__ void __launch_bounds__(Q8 ? 512 : 384, 1) window_prefill_kernel(const
         if (lane == 0) {
             c->abort = 0;
             c->bad = 0;
-            for (int i = 0; i < C::SLOTS; ++i) {
+            for (int i = 0; i < C::CYCLE; ++i) {
                 bar_init(bar_full + 8 * i, C::LOADERS);
                 bar_init(bar_empty + 8 * i, QT);
+            }
+            for (int i = 0; Q8 && i < C::STAGES; ++i) {
+                bar_init(bar_page + 8 * i, 1);
+                bar_init(bar_page_free + 8 * i, C::LOADERS);
             }
             for (int w = 0; w < 2; ++w) {
                 bar_init(bar_s + 8 * w, 1);
@@ -452,58 +478,47 @@ __global__ void __launch_bounds__(Q8 ? 512 : 384, 1) window_prefill_kernel(const
         if (warp < C::MMA_WARP) {
             if constexpr (Q8) {
                 // ------------------------------------------------------------ loader, 8-bit cache
-                // A thread takes a piece (16 elements) of one token in PASSES groups of tokens, of keys
-                // and of values: from the cache into registers a slot ahead, then as bf16 into its slot.
-                // (Eight lanes have four pieces of two neighbouring tokens: the 16-byte stores meet no
-                // bank conflicts.)
+                // Pages lie in shared memory as they are cached (copied by warp 14).  Of a page a thread
+                // turns a piece (16 elements) of one token in each of PASSES groups into bf16, of its keys
+                // for use t of the ring, then of its values for use t + AHEAD.  (Eight lanes have the
+                // pieces of half a row of one token, and of the other half of its neighbour's: neither
+                // their 16-byte loads nor their stores meet bank conflicts.)
                 using Gr = q8::Granule<D>;
                 const int lt = tid - 256;
                 constexpr int GROUP = C::LOADERS * 16 / D, PASSES = KT / GROUP;  // tokens of a pass
                 static_assert(GROUP % q8::kGranule == 0, "");
-                const int ch = D == 128 ? (lt & 3) | (lt >> 1 & 4) : lt & 3;
+                const int ch = D == 128 ? (lt & 3) | ((lt ^ lt >> 1) & 4) : lt & 3;
                 const int r0 = D == 128 ? lt >> 4 << 1 | (lt >> 2 & 1) : lt >> 2;
-                constexpr int STEP = GROUP / q8::kGranule * Gr::BYTES;  // from a pass to the next in the cache
-                const char* from = a.kv.base + (uint64_t)a.kv.layer * a.kv.layer_page_bytes +
-                                   ((int64_t)kvh * 4 + r0 / 16) * Gr::BYTES;
-                const int codes = Gr::piece(0, r0 % 16, ch), exps = Gr::exponents(0, r0 % 16) + ch / 2;
-                const int64_t* table = a.kv.page_offsets + (int64_t)req * a.kv.max_pages;
+                constexpr int STEP = GROUP / q8::kGranule * Gr::BYTES;  // from a pass to the next in the page
+                const int codes = r0 / 16 * Gr::BYTES + Gr::piece(0, r0 % 16, ch);
+                const int exps = r0 / 16 * Gr::BYTES + Gr::exponents(0, r0 % 16) + ch / 2;
                 const int win0 = max(0, pos0 - a.window + 1);  // (window 0: no page of it is in the list)
                 const uint32_t place =
                     (uint32_t)((ch >> 2) * C::KV_SLAB + r0 * 128 + ((2 * (ch & 3) ^ (r0 & 7)) << 4));
-                uint4 code[2][PASSES];  // of keys, of values
-                uint32_t exp[2][PASSES];
-                auto fetch = [&](int64_t page, auto which) {
-                    constexpr int V = decltype(which)::value;
-                    const char* g = from + page;
-#pragma unroll
-                    for (int k = 0; k < PASSES; ++k) {
-                        code[V][k] = *reinterpret_cast<const uint4*>(g + codes + V * 16 * D + k * STEP);
-                        exp[V][k] = *reinterpret_cast<const uint8_t*>(g + exps + V * (D / 2) + k * STEP);
-                    }
-                };
                 // What no row of the block sees is zero.  A value's NaN that only some rows see is taken out,
                 // and the block's rows are walked one by one.
-                auto put = [&](int t, uint32_t to, auto which) {
+                auto put = [&](int b, const uint8_t* page, uint32_t to, auto which) {
                     constexpr int V = decltype(which)::value;
-                    const int b = page_at(t) * KT;
                     const bool whole = b + KT <= pages.last && ((b >= win0 && a.window > 0) || b + KT <= a.sinks);
                     const bool shared = b + KT - 1 <= pos0 && (b > pos1 - a.window || b + KT <= a.sinks);
 #pragma unroll
                     for (int k = 0; k < PASSES; ++k) {
+                        const uint32_t E = page[exps + V * (D / 2) + k * STEP];
+                        const uint4 w = *reinterpret_cast<const uint4*>(page + codes + V * 16 * D + k * STEP);
                         const int pos = b + r0 + k * GROUP;
-                        uint32_t scale = q8::scale2(exp[V][k], exp[V][k]);
+                        uint32_t scale = q8::scale2(E, E);
                         if (!whole && !(pos < pages.last && ((pos >= win0 && a.window > 0) || pos < a.sinks))) {
                             scale = 0u;
-                        } else if (V && !shared && exp[V][k] > q8::kMostExponent) {
+                        } else if (V && !shared && E > q8::kMostExponent) {
                             scale = 0u;
                             *(volatile int*)&c->bad = 1;
                         }
-                        const uint32_t w[4] = {code[V][k].x, code[V][k].y, code[V][k].z, code[V][k].w};
+                        const uint32_t x[4] = {w.x, w.y, w.z, w.w};
                         uint32_t u[8];
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
-                            u[2 * e] = q8::pair_of(__byte_perm(w[e], 0u, 0x1100u), scale);
-                            u[2 * e + 1] = q8::pair_of(__byte_perm(w[e], 0u, 0x3322u), scale);
+                            u[2 * e] = q8::pair_of(__byte_perm(x[e], 0u, 0x1100u), scale);
+                            u[2 * e + 1] = q8::pair_of(__byte_perm(x[e], 0u, 0x3322u), scale);
                         }
                         const uint32_t dst = to + place + k * GROUP * 128;
                         asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(dst), "r"(u[0]), "r"(u[1]), "r"(u[2]),
@@ -514,35 +529,40 @@ __global__ void __launch_bounds__(Q8 ? 512 : 384, 1) window_prefill_kernel(const
                                      : "memory");
                     }
                 };
-                using Keys = std::integral_constant<int, 0>;
-                using Values = std::integral_constant<int, 1>;
-                auto page_of = [&](int t) { return t < n ? table[page_at(t)] : 0; };
-                constexpr int AT = C::AHEAD + 2;
-                int64_t at[AT];  // page offsets of tiles i + 1 - AHEAD .. i + 2
-                int slot = 0;
-                uint32_t free_phase = 1;  // of the ring's previous round (before the first one: complete)
-                if (n > 0) {
-                    at[AT - 3] = page_of(0);
-                    at[AT - 2] = page_of(1);
-                    fetch(at[AT - 3], Keys{});
-                }
-#pragma unroll 1
-                for (int i = 0; i < n + C::AHEAD && n > 0; ++i) {
-                    const int t = i - C::AHEAD;  // whose values
-                    const uint32_t dst = ring + (uint32_t)slot * C::SLOT;
-                    at[AT - 1] = page_of(i + 2);
-                    wait(bar_empty + 8 * slot, free_phase, 1);
-                    if (i < n) put(i, dst, Keys{});
-                    if (i + 1 < n) fetch(at[AT - 2], Keys{});
-                    if (t >= 0) put(t, dst + C::TILE, Values{});
-                    if (t + 1 >= 0 && t + 1 < n) fetch(at[0], Values{});
-                    fence_loaded();
-                    bar_arrive(bar_full + 8 * slot);
+                int stage = 0;
+                uint32_t stage_phase = 0;
+                Use keys{0, 0, 0}, values{0, 0, 0};  // of the ring, the next ones
+                Use freed{0, 0, 0};                  // the use whose end the next values wait for
 #pragma unroll
-                    for (int x = 0; x < AT - 1; ++x) at[x] = at[x + 1];
-                    if (++slot == C::SLOTS) {
-                        slot = 0;
-                        free_phase ^= 1;
+                for (int x = 0; x < C::AHEAD; ++x) values.template next<C::SLOTS, C::CYCLE>();
+#pragma unroll 1
+                for (int t = 0; t < n; ++t) {
+                    wait(bar_page + 8 * stage, stage_phase, 10);
+                    const uint8_t* page = sm + C::STAGE + stage * C::PAGE;
+                    const int b = page_at(t) * KT;
+                    // (this use of the ring was waited for when the values of an earlier page went into it)
+                    put(b, page, ring + keys.slot * C::SLOT, std::integral_constant<int, 0>{});
+                    fence_loaded();
+                    bar_arrive(bar_full + 8 * keys.bar);
+                    keys.template next<C::SLOTS, C::CYCLE>();
+                    if (t + C::AHEAD >= C::SLOTS) {
+                        wait(bar_empty + 8 * freed.bar, freed.phase, 1);
+                        freed.template next<C::SLOTS, C::CYCLE>();
+                    }
+                    put(b, page, ring + values.slot * C::SLOT + C::TILE, std::integral_constant<int, 1>{});
+                    values.template next<C::SLOTS, C::CYCLE>();
+                    bar_arrive(bar_page_free + 8 * stage);
+                    if (++stage == C::STAGES) {
+                        stage = 0;
+                        stage_phase ^= 1;
+                    }
+                }
+                if (n > 0) {
+                    fence_loaded();
+#pragma unroll
+                    for (int x = 0; x < C::AHEAD; ++x) {  // the last uses have no keys
+                        bar_arrive(bar_full + 8 * keys.bar);
+                        keys.template next<C::SLOTS, C::CYCLE>();
                     }
                 }
             } else {
@@ -638,20 +658,21 @@ __global__ void __launch_bounds__(Q8 ? 512 : 384, 1) window_prefill_kernel(const
             const uint64_t q_desc = sdesc(q_smem + (QT == 2 ? w * NP * C::Q_PLANE : 0), 16), k_desc = sdesc(ring, 16),
                            v_desc = sdesc(ring + C::TILE, C::KV_SLAB);
             constexpr int STRIDE = QT == 2 ? 1 : 2;  // a slot's keys and values are of both streams, or of one
-            uint32_t slot = QT == 2 ? 0 : w, phase = 0;  // a cursor in the ring, and the phase of its round
+            Use use{0, 0, 0};                 // of the ring, the next one
             uint32_t free = 1;                // of S (before the first tile: complete)
             uint32_t done = 0;                // products P V
-            int used = -1;                    // slot to be released (QT = 2)
+            int used = -1;                    // barrier of the one to be released (QT = 2)
+            if (QT == 1 && w == 1) use.template next<C::SLOTS, C::CYCLE>();
             const int steps = n + C::AHEAD;
             wait(bar_q, 0, 2);
-            if (QT == 2 || w < steps) wait(bar_full + 8 * slot, phase, 3);
+            if (QT == 2 || w < steps) wait(bar_full + 8 * use.bar, use.phase, 3);
             // From P of a tile to S of the next but one the stream waits for this warp, so with two row
             // tiles the next slot is waited for before P, and the last one released after S (467 -> 454
             // us for 8192 rows behind 4096).  With one row tile a stream has two slots, and there the
             // release has to come first (4 x 512 fp32 rows: 109 us, 121 the other way).
 #pragma unroll 1
             for (int i = QT == 2 ? 0 : w; i < steps; i += STRIDE) {
-                const uint32_t k_at = slot * (C::SLOT / 16);
+                const uint32_t k_at = use.slot * (C::SLOT / 16);
                 fence_loaded();
                 if (mine(i)) {  // S = Q K^T, once the softmax has read the last one
                     wait(bar_s_free + 8 * w, free, 4);
@@ -667,13 +688,10 @@ __global__ void __launch_bounds__(Q8 ? 512 : 384, 1) window_prefill_kernel(const
                     commit(bar_s + 8 * w);
                 }
                 if (QT == 2 && used >= 0) commit(bar_empty + 8 * used);
-                used = slot;
-                slot += STRIDE;
-                if (slot >= C::SLOTS) {
-                    slot -= C::SLOTS;
-                    phase ^= 1;
-                }
-                if (QT == 2 && i + STRIDE < steps) wait(bar_full + 8 * slot, phase, 3);
+                used = use.bar;
+#pragma unroll
+                for (int x = 0; x < STRIDE; ++x) use.template next<C::SLOTS, C::CYCLE>();
+                if (QT == 2 && i + STRIDE < steps) wait(bar_full + 8 * use.bar, use.phase, 3);
                 if (mine(i - C::AHEAD)) {  // O += P V
                     const uint32_t buf = done & 1;
                     wait(bar_p + 16 * w + 8 * buf, done / 2 & 1, 5);
@@ -694,13 +712,48 @@ __global__ void __launch_bounds__(Q8 ? 512 : 384, 1) window_prefill_kernel(const
                 }
                 if (QT == 1) {
                     commit(bar_empty + 8 * used);
-                    if (i + STRIDE < steps) wait(bar_full + 8 * slot, phase, 3);
+                    if (i + STRIDE < steps) wait(bar_full + 8 * use.bar, use.phase, 3);
                 }
             }
             // nothing may be in flight when the tensor memory is released
             commit(bar_end);
             const uint64_t t0 = now_ns();
             while (!bar_try(bar_end, 0) && now_ns() - t0 < 2000000000ull) {}
+        } else if (Q8 && n > 0 && warp == C::MMA_WARP + 2) {
+            // ---------------------------------------------------------------- pages of the 8-bit cache
+            const char* from = a.kv.base + (uint64_t)a.kv.layer * a.kv.layer_page_bytes + (int64_t)kvh * C::PAGE;
+            const int64_t* table = a.kv.page_offsets + (int64_t)req * a.kv.max_pages;
+            int stage = 0;
+            uint32_t phase = 1;  // of the stage's last round (before the first one: complete)
+            int64_t offset = 0;  // of 32 pages, a lane each
+            int issued = 0;
+#pragma unroll 1
+            for (int t = 0; t < n; ++t) {
+                if (t % 32 == 0 && t + lane < n) offset = table[page_at(t + lane)];
+                const int64_t at = __shfl_sync(0xffffffffu, offset, t % 32);
+                wait(bar_page_free + 8 * stage, phase, 11);
+                __syncwarp();
+                if (lane == 0 && !wait.dead) {
+                    const uint32_t bar = bar_page + 8 * stage;
+                    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "n"(C::PAGE) : "memory");
+                    asm volatile(
+                        "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
+                            q_smem + C::STAGE + stage * C::PAGE),
+                        "l"(from + at), "n"(C::PAGE), "r"(bar)
+                        : "memory");
+                    issued = t + 1;
+                }
+                if (++stage == C::STAGES) {
+                    stage = 0;
+                    phase ^= 1;
+                }
+            }
+            // no copy may be in flight at the block's end
+            if (lane == 0) {
+                const uint64_t t0 = now_ns();
+                for (int t = max(0, issued - C::STAGES); t < issued; ++t)
+                    while (!bar_try(bar_page + 8 * (t % C::STAGES), t / C::STAGES & 1) && now_ns() - t0 < 2000000000ull) {}
+            }
         }
     } else if (tokens > 0) {
         // -------------------------------------------------------------------- softmax
