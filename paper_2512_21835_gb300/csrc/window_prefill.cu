@@ -298,6 +298,10 @@ __device__ __forceinline__ void tmem_stored() { asm volatile("tcgen05.wait::st.s
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, uint32_t n) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
 }
+// (Without a clobber, so that loads of shared memory can pass it: fenced before it is signalled.)
+__device__ __forceinline__ void store16(uint32_t to, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(to), "r"(a), "r"(b), "r"(c), "r"(d));
+}
 __device__ __forceinline__ float ex2(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -497,36 +501,36 @@ __global__ void __launch_bounds__(Q8 ? 512 : 384, 1) window_prefill_kernel(const
                     (uint32_t)((ch >> 2) * C::KV_SLAB + r0 * 128 + ((2 * (ch & 3) ^ (r0 & 7)) << 4));
                 // What no row of the block sees is zero.  A value's NaN that only some rows see is taken out,
                 // and the block's rows are walked one by one.
-                auto put = [&](int b, const uint8_t* page, uint32_t to, auto which) {
+                uint4 code[2][PASSES];  // of keys, of values
+                uint32_t exp[2][PASSES];
+                auto put = [&](int b, uint32_t to, auto which) {
                     constexpr int V = decltype(which)::value;
                     const bool whole = b + KT <= pages.last && ((b >= win0 && a.window > 0) || b + KT <= a.sinks);
                     const bool shared = b + KT - 1 <= pos0 && (b > pos1 - a.window || b + KT <= a.sinks);
+                    uint32_t scale[PASSES];
 #pragma unroll
                     for (int k = 0; k < PASSES; ++k) {
-                        const uint32_t E = page[exps + V * (D / 2) + k * STEP];
-                        const uint4 w = *reinterpret_cast<const uint4*>(page + codes + V * 16 * D + k * STEP);
                         const int pos = b + r0 + k * GROUP;
-                        uint32_t scale = q8::scale2(E, E);
+                        scale[k] = q8::scale2(exp[V][k], exp[V][k]);
                         if (!whole && !(pos < pages.last && ((pos >= win0 && a.window > 0) || pos < a.sinks))) {
-                            scale = 0u;
-                        } else if (V && !shared && E > q8::kMostExponent) {
-                            scale = 0u;
+                            scale[k] = 0u;
+                        } else if (V && !shared && exp[V][k] > q8::kMostExponent) {
+                            scale[k] = 0u;
                             *(volatile int*)&c->bad = 1;
                         }
-                        const uint32_t x[4] = {w.x, w.y, w.z, w.w};
+                    }
+#pragma unroll
+                    for (int k = 0; k < PASSES; ++k) {
+                        const uint32_t x[4] = {code[V][k].x, code[V][k].y, code[V][k].z, code[V][k].w};
                         uint32_t u[8];
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
-                            u[2 * e] = q8::pair_of(__byte_perm(x[e], 0u, 0x1100u), scale);
-                            u[2 * e + 1] = q8::pair_of(__byte_perm(x[e], 0u, 0x3322u), scale);
+                            u[2 * e] = q8::pair_of(__byte_perm(x[e], 0u, 0x1100u), scale[k]);
+                            u[2 * e + 1] = q8::pair_of(__byte_perm(x[e], 0u, 0x3322u), scale[k]);
                         }
                         const uint32_t dst = to + place + k * GROUP * 128;
-                        asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(dst), "r"(u[0]), "r"(u[1]), "r"(u[2]),
-                                     "r"(u[3])
-                                     : "memory");
-                        asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(dst ^ 16u), "r"(u[4]), "r"(u[5]),
-                                     "r"(u[6]), "r"(u[7])
-                                     : "memory");
+                        store16(dst, u[0], u[1], u[2], u[3]);
+                        store16(dst ^ 16u, u[4], u[5], u[6], u[7]);
                     }
                 };
                 int stage = 0;
@@ -539,9 +543,16 @@ __global__ void __launch_bounds__(Q8 ? 512 : 384, 1) window_prefill_kernel(const
                 for (int t = 0; t < n; ++t) {
                     wait(bar_page + 8 * stage, stage_phase, 10);
                     const uint8_t* page = sm + C::STAGE + stage * C::PAGE;
+#pragma unroll
+                    for (int v = 0; v < 2; ++v)
+#pragma unroll
+                        for (int k = 0; k < PASSES; ++k) {
+                            exp[v][k] = page[exps + v * (D / 2) + k * STEP];
+                            code[v][k] = *reinterpret_cast<const uint4*>(page + codes + v * 16 * D + k * STEP);
+                        }
                     const int b = page_at(t) * KT;
                     // (this use of the ring was waited for when the values of an earlier page went into it)
-                    put(b, page, ring + keys.slot * C::SLOT, std::integral_constant<int, 0>{});
+                    put(b, ring + keys.slot * C::SLOT, std::integral_constant<int, 0>{});
                     fence_loaded();
                     bar_arrive(bar_full + 8 * keys.bar);
                     keys.template next<C::SLOTS, C::CYCLE>();
@@ -549,7 +560,7 @@ __global__ void __launch_bounds__(Q8 ? 512 : 384, 1) window_prefill_kernel(const
                         wait(bar_empty + 8 * freed.bar, freed.phase, 1);
                         freed.template next<C::SLOTS, C::CYCLE>();
                     }
-                    put(b, page, ring + values.slot * C::SLOT + C::TILE, std::integral_constant<int, 1>{});
+                    put(b, ring + values.slot * C::SLOT + C::TILE, std::integral_constant<int, 1>{});
                     values.template next<C::SLOTS, C::CYCLE>();
                     bar_arrive(bar_page_free + 8 * stage);
                     if (++stage == C::STAGES) {
