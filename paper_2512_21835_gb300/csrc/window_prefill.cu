@@ -84,13 +84,17 @@ constexpr int KT = kPageTokens;                  // keys per tile
 
 template <int D, int NP, int QT, bool Q8>
 struct Cfg {
-    // Warps 0 to 7 softmax, from 8 on loaders, then one per stream that issues MMAs.  The registers
-    // of the softmax warps, of the loaders' warpgroup and (Q8) of the issuing one:
-    static constexpr int LOADERS = Q8 ? 128 : 64;      // threads
+    // Warps 0 to 7 softmax, from 8 on loaders, then one per stream that issues MMAs (Q8: and one that
+    // copies pages).  The registers of a softmax warp's threads, of a loader's, and of the others
+    // (which without Q8 share the loaders' warpgroup).
+    static constexpr int LOADERS = !Q8 ? 64 : NP == 1 ? 256 : 128;  // threads
     static constexpr int MMA_WARP = 8 + LOADERS / 32;
-    static constexpr int THREADS = Q8 ? 512 : 384;
-    static constexpr int SOFT_REGS = 200, LOAD_REGS = Q8 ? 72 : 104, MMA_REGS = Q8 ? 40 : 104;
-    static_assert(2 * SOFT_REGS + (Q8 ? LOAD_REGS + MMA_REGS : LOAD_REGS) <= 65536 / THREADS / 8 * 8 * (THREADS / 128), "");
+    static constexpr int THREADS = !Q8 ? 384 : 384 + LOADERS;
+    static constexpr int SOFT_REGS = Q8 && NP == 1 ? 160 : 200;
+    static constexpr int LOAD_REGS = !Q8 ? 104 : NP == 1 ? 56 : 72, MMA_REGS = Q8 ? 40 : 104;
+    // (what the launch gives a thread, 65536 / THREADS to the eight below, has to suffice for all)
+    static_assert(256 * SOFT_REGS + (Q8 ? LOADERS * LOAD_REGS + 128 * MMA_REGS : 128 * LOAD_REGS) <=
+                      65536 / THREADS / 8 * 8 * THREADS, "");
     static constexpr int SLABS = D / 64;               // 128-byte columns of a row
     static constexpr int Q_SLAB = 128 * 128;
     static constexpr int Q_PLANE = SLABS * Q_SLAB;
@@ -107,7 +111,10 @@ struct Cfg {
     // Use i of the ring is of slot i % SLOTS and of barrier i % CYCLE.  With one row tile a stream takes
     // every second use: CYCLE is even, so that a stream meets every phase of its barriers.
     static constexpr int CYCLE = QT == 1 && SLOTS % 2 ? 2 * SLOTS : SLOTS;
-    static constexpr int AHEAD = 3 - QT;                 // slot i: keys of tile i, values of tile i - AHEAD
+    // S of the tile after next goes into the columns of P once P V is issued, so that it is there
+    // when the softmax comes to it.
+    static constexpr bool PIPE = Q8 && NP == 1 && QT == 2;
+    static constexpr int AHEAD = PIPE ? 2 : 3 - QT;      // slot i: keys of tile i, values of tile i - AHEAD
     static constexpr int STAGE = Q_BYTES + SLOTS * SLOT;
     static constexpr int CTL = STAGE + STAGES * PAGE;
     static constexpr int BYTES = CTL + 512 + 1024;     // + alignment of the window
@@ -124,7 +131,7 @@ struct Cfg {
 
 struct Ctl {  // control words behind the ring
     uint64_t full[12], empty[12];      // of the ring's slots
-    uint64_t s_full[2], s_free[2];     // per stream
+    uint64_t s_full[4], s_free[2];     // per stream (and S buffer)
     uint64_t p_full[4], pv_done[4];    // per stream and P buffer: for even and odd tiles, no wait is ever two phases behind
     uint64_t o_free, q_full, end;
     uint64_t page_full[4], page_free[4];  // of the pages as they are cached
@@ -284,6 +291,13 @@ __device__ __forceinline__ void tmem_landed(uint32_t (&r)[N]) {
 #pragma unroll
     for (int i = 0; i < N; ++i) asm volatile("" : "+r"(r[i])::"memory");
 }
+__device__ __forceinline__ void tmem_ld16(uint32_t addr, uint32_t (&r)[16]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(addr));
+}
 template <int B, int N>
 __device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t (&r)[N]) {
     asm volatile(
@@ -342,7 +356,7 @@ struct Pages {
 };
 
 template <int D, int NP, int QT, bool Q8, typename T>
-__global__ void __launch_bounds__(Q8 ? 512 : 384, 1) window_prefill_kernel(const __grid_constant__ PrefillArgs p) {
+__global__ void __launch_bounds__(Cfg<D, NP, QT, Q8>::THREADS, 1) window_prefill_kernel(const __grid_constant__ PrefillArgs p) {
     using C = Cfg<D, NP, QT, Q8>;
     const WindowArgs& a = p.a;
     extern __shared__ uint8_t smem_raw[];
@@ -421,10 +435,10 @@ __global__ void __launch_bounds__(Q8 ? 512 : 384, 1) window_prefill_kernel(const
                 bar_init(bar_page_free + 8 * i, C::LOADERS);
             }
             for (int w = 0; w < 2; ++w) {
-                bar_init(bar_s + 8 * w, 1);
                 bar_init(bar_s_free + 8 * w, 128);
             }
             for (int i = 0; i < 4; ++i) {
+                bar_init(bar_s + 8 * i, 1);
                 bar_init(bar_p + 8 * i, 128);
                 bar_init(bar_pv + 8 * i, 1);
             }
@@ -475,14 +489,14 @@ __global__ void __launch_bounds__(Q8 ? 512 : 384, 1) window_prefill_kernel(const
     Waiter wait{c, false};
     auto stopped = [&] { return *(volatile int*)&c->abort != 0; };
     if (warp >= 8) {
-        if (!Q8 || warp < 12)
+        if (!Q8 || warp < C::MMA_WARP)
             asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::LOAD_REGS));
         else
             asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(C::MMA_REGS));
         if (warp < C::MMA_WARP) {
             if constexpr (Q8) {
                 // ------------------------------------------------------------ loader, 8-bit cache
-                // Pages lie in shared memory as they are cached (copied by warp 14).  Of a page a thread
+                // Pages lie in shared memory as they are cached (copied by another warp).  Of a page a thread
                 // turns a piece (16 elements) of one token in each of PASSES groups into bf16, of its keys
                 // for use t of the ring, then of its values for use t + AHEAD.  (Eight lanes have the
                 // pieces of half a row of one token, and of the other half of its neighbour's: neither
@@ -676,6 +690,36 @@ __global__ void __launch_bounds__(Q8 ? 512 : 384, 1) window_prefill_kernel(const
             if (QT == 1 && w == 1) use.template next<C::SLOTS, C::CYCLE>();
             const int steps = n + C::AHEAD;
             wait(bar_q, 0, 2);
+            if constexpr (C::PIPE) {
+                uint32_t made = 0;  // tiles of S
+#pragma unroll 1
+                for (int i = 0; i < steps; ++i) {
+                    const uint32_t k_at = use.slot * (C::SLOT / 16);
+                    wait(bar_full + 8 * use.bar, use.phase, 3);
+                    fence_loaded();
+                    if (mine(i - C::AHEAD)) {  // O += P V
+                        const uint32_t buf = done & 1;
+                        wait(bar_p + 16 * w + 8 * buf, done / 2 & 1, 5);
+                        fence_after();
+#pragma unroll
+                        for (int x = 0; x < 2; ++x)
+                            mma_ts2(tmem + C::o_col(w), tmem + C::s_col(w) + 64 * buf + 16 * x,
+                                    v_desc + k_at + x * (32 * 128 / 16), idesc(D, true), x != 0 || done ? 1u : 0u);
+                        commit(bar_pv + 16 * w + 8 * buf);
+                        ++done;
+                    }
+                    if (mine(i)) {  // S = Q K^T, over the P that the product before this one has read
+                        const uint32_t buf = made++ & 1;
+#pragma unroll
+                        for (int x = 0; x < D / 64; ++x)
+                            mma_ss4(tmem + C::s_col(w) + 64 * buf, q_desc + x * C::Q_SLAB / 16,
+                                    k_desc + k_at + x * C::KV_SLAB / 16, idesc(KT, false), x != 0);
+                        commit(bar_s + 16 * w + 8 * buf);
+                    }
+                    commit(bar_empty + 8 * use.bar);
+                    use.template next<C::SLOTS, C::CYCLE>();
+                }
+            } else {
             if (QT == 2 || w < steps) wait(bar_full + 8 * use.bar, use.phase, 3);
             // From P of a tile to S of the next but one the stream waits for this warp, so with two row
             // tiles the next slot is waited for before P, and the last one released after S (467 -> 454
@@ -725,6 +769,7 @@ __global__ void __launch_bounds__(Q8 ? 512 : 384, 1) window_prefill_kernel(const
                     commit(bar_empty + 8 * used);
                     if (i + STRIDE < steps) wait(bar_full + 8 * use.bar, use.phase, 3);
                 }
+            }
             }
             // nothing may be in flight when the tensor memory is released
             commit(bar_end);
@@ -839,6 +884,94 @@ __global__ void __launch_bounds__(Q8 ? 512 : 384, 1) window_prefill_kernel(const
             for (int i = 0; i < D; ++i) o[i] = 0.f;
         }
         const Takes takes = takes_of(w);
+        // which positions of a key tile this row sees, one bit each; whether it does not see all
+        auto seen_of = [&](int t, uint32_t (&see)[2]) {
+            see[0] = see[1] = 0xffffffffu;
+            if (t >= full0 && t < full1) return false;
+            const int b = page_at(t) * KT;
+            const uint64_t bits = live ? low_bits(min(pos, a.max_ctx - 1) - b + 1) &
+                                             (~low_bits(pos - a.window + 1 - b) | low_bits(a.sinks - b))
+                                       : 0ull;
+            see[0] = (uint32_t)bits;
+            see[1] = (uint32_t)(bits >> 32);
+            return true;
+        };
+        if constexpr (C::PIPE) {
+            auto read = [&](uint32_t k, uint32_t (&s)[KT]) {  // S of the stream's tile k, on its way
+                wait(bar_s + 16 * w + 8 * (k & 1), k >> 1 & 1, 6);
+                __syncwarp();
+                fence_after();
+                tmem_ld32<0>(tmem + lanes + C::s_col(w) + 64 * (k & 1), s);
+                tmem_ld32<32>(tmem + lanes + C::s_col(w) + 64 * (k & 1) + 32, s);
+            };
+            auto tile = [&](int t) {
+                uint32_t s[KT];
+                read(done, s);
+                tmem_landed(s);
+                uint32_t see[2];
+                const bool masked = seen_of(t, see);
+                if (masked) {
+#pragma unroll
+                    for (int i = 0; i < KT; ++i)
+                        if (!(see[i / 32] >> (i % 32) & 1u)) s[i] = 0xff800000u;  // -inf
+                }
+                float x[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                for (int i = 0; i < KT; i += 8)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) x[e] = fmaxf(x[e], fmaxf(asf(s[i + 2 * e]), asf(s[i + 2 * e + 1])));
+                const float mx = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])) * p.scale;
+                // O is rescaled when a row's maximum has outgrown the one in use by 2^8
+                const bool grown = mx > m + 8.f;  // the first time too: m is -inf
+                if (__any_sync(0xffffffffu, grown)) {
+                    const float m_new = grown ? mx : m;
+                    const float alpha = m == -INFINITY ? 0.f : ex2(m - m_new);
+                    m = m_new;
+                    l *= alpha;
+                    if (done) {
+                        pv_wait(done - 1, 8);
+                        __syncwarp();
+                        fence_after();
+#pragma unroll
+                        for (int i = 0; i < D; i += 16) {
+                            uint32_t y[16];
+                            tmem_ld16(tmem + lanes + C::o_col(w) + i, y);
+                            tmem_landed(y);
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) y[e] = __float_as_uint(asf(y[e]) * alpha);
+                            tmem_st16<0>(tmem + lanes + C::o_col(w) + i, y);
+                        }
+                    }
+                }
+                const float base = m == -INFINITY ? 0.f : m;
+                const float2 scale2 = make_float2(p.scale, p.scale), base2 = make_float2(-base, -base);
+                float2 l0 = make_float2(0.f, 0.f), l1 = l0;
+#pragma unroll
+                for (int i = 0; i < KT; i += 32) {
+                    uint32_t pk[16];
+#pragma unroll
+                    for (int e = 0; e < 32; e += 4) {
+                        float2 y = fma2(make_float2(asf(s[i + e]), asf(s[i + e + 1])), scale2, base2);
+                        float2 z = fma2(make_float2(asf(s[i + e + 2]), asf(s[i + e + 3])), scale2, base2);
+                        y.x = ex2(y.x); y.y = ex2(y.y); z.x = ex2(z.x); z.y = ex2(z.y);
+                        l0 = add2(l0, y);
+                        l1 = add2(l1, z);
+                        pk[e / 2] = pack(y.x, y.y);
+                        pk[e / 2 + 1] = pack(z.x, z.y);
+                    }
+                    tmem_st16<0>(tmem + lanes + C::s_col(w) + 64 * (done & 1) + i / 2, pk);
+                }
+                l0 = add2(l0, l1);
+                l += l0.x + l0.y;
+                tmem_stored();
+                fence_before();
+                bar_arrive(bar_p + 16 * w + 8 * (done & 1));
+                ++done;
+            };
+#pragma unroll 1
+            for (int t = 0; t < n; ++t)
+                if (takes(t)) tile(t);
+        } else
         for (int t = QT == 1 ? w : 0; t < n; t += QT == 1 ? 2 : 1) {
             if (QT == 2 && !takes(t)) continue;
             // which positions of the page this row sees, one bit each
