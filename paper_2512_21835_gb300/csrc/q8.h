@@ -75,10 +75,12 @@ __device__ __forceinline__ float value_of(uint32_t code, float step) {
     return (code & 128u ? -m : m) * step;
 }
 
-// Codes to pairs of bf16, exactly, in four instructions of which two are the integer pipe's (which
-// takes one every second cycle, and is what bounds the conversion).  Sign and magnitude of a code,
-// put where a bf16 number has its sign and its mantissa, are the subnormal number +-m 2^-133.  Times
-// 2^127 that is +-m 2^-6, times 2^(E - 127) the value: two products by powers of two, both exact.
+// Codes to pairs of bf16, exactly.  Sign and magnitude of a code, put where a bf16 number has its sign
+// and its mantissa, are the subnormal number +-m 2^-133, and times 2^E that is the value.  (The byte
+// permute and the mask are the integer pipe's, which takes an instruction every second cycle, and
+// bound the conversion.)  2^E is a bf16 number up to E = 127 only, so
+//   pair_of     takes two products by powers of two, 2^127 and 2^(E - 127): four instructions
+//   shifted_of  makes the value times 2^-kShift in one, for the exponents of shift_holds: three
 //
 // The second factor for a pair of blocks (or for one, twice).
 __device__ __forceinline__ uint32_t scale2(uint32_t Elo, uint32_t Ehi) {
@@ -92,6 +94,19 @@ __device__ __forceinline__ uint32_t pair_of(uint32_t twice, uint32_t scale) {
     asm("{\n .reg .b32 x;\n and.b32 x, %1, 0x807f807f;\n mul.rn.bf16x2 x, x, %3;\n mul.rn.bf16x2 %0, x, %2;\n}\n"
         : "=r"(r)
         : "r"(twice), "r"(scale), "r"(0x7f007f00u));
+    return r;
+}
+
+// Values times 2^-64 are normal bf16 numbers for exponents 71 to 191 (elements of 2^-62 to 2^58 in
+// size), and the factor 2^(E - 64) is one too.
+constexpr int kShift = 64;
+__device__ __forceinline__ bool shift_holds(uint32_t E) { return E - 71u <= 191u - 71u; }
+__device__ __forceinline__ uint32_t shifted_scale(uint32_t E) { return (E + (127 - kShift)) * 0x00800080u; }
+__device__ __forceinline__ uint32_t shifted_of(uint32_t twice, uint32_t scale) {
+    uint32_t r;
+    asm("{\n .reg .b32 x;\n and.b32 x, %1, 0x807f807f;\n mul.rn.bf16x2 %0, x, %2;\n}\n"
+        : "=r"(r)
+        : "r"(twice), "r"(scale));
     return r;
 }
 #endif

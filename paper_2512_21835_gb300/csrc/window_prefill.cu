@@ -82,8 +82,12 @@ namespace {
 constexpr int kSms = 152;
 constexpr int KT = kPageTokens;                  // keys per tile
 
+constexpr float kUnit8 = 0x1p64f;                // keys and values of the 8-bit cache are multiplied as their 2^-kShift-fold
+static_assert(q8::kShift == 64, "");
+
 template <int D, int NP, int QT, bool Q8>
 struct Cfg {
+    static constexpr float UNIT = Q8 ? kUnit8 : 1.0f;  // of O as the tensor core has it
     // Warps 0 to 7 softmax, from 8 on loaders, then one per stream that issues MMAs (Q8: and one that
     // copies pages).  The registers of a softmax warp's threads, of a loader's, and of the others
     // (which without Q8 share the loaders' warpgroup).
@@ -159,7 +163,7 @@ struct PrefillArgs {
     int heads, groups;  // query heads per row tile, groups per kv head
     int tok;            // positions per row tile
     int splits;         // blocks per row tile (QT = 1)
-    float scale;        // log2(e) / sqrt(d)
+    float scale;        // log2(e) / sqrt(d), of scores as the tensor core has them (Q8: times 2^-kShift)
     // in scratch, with splits; a unit is a row tile and kv head (and group)
     float4* part;       // [unit][split][d / 4][128 rows], not normalised
     int4* rows;         // [unit]: first row, tokens, request, position of the first
@@ -320,6 +324,11 @@ __device__ __forceinline__ float ex2(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
 }
 __device__ __forceinline__ float asf(uint32_t u) { return __uint_as_float(u); }
 // two fp32 lanes in one instruction
@@ -513,8 +522,14 @@ __global__ void __launch_bounds__(Cfg<D, NP, QT, Q8>::THREADS, 1) window_prefill
                 const int win0 = max(0, pos0 - a.window + 1);  // (window 0: no page of it is in the list)
                 const uint32_t place =
                     (uint32_t)((ch >> 2) * C::KV_SLAB + r0 * 128 + ((2 * (ch & 3) ^ (r0 & 7)) << 4));
-                // What no row of the block sees is zero.  A value's NaN that only some rows see is taken out,
-                // and the block's rows are walked one by one.
+                // What no row of the block sees is zero.  Elements are made times 2^-kShift, which all
+                // but extreme exponents allow.  For the others, blocks of zeros are zero and NaN is NaN
+                // (except in values that only some rows see), and else the block's rows are walked one by one.
+                auto unheld = [&](const uint4& u, uint32_t E, bool some) {
+                    if (E > q8::kMostExponent && !some) return 0x7fc07fc0u;
+                    if (E > q8::kMostExponent || ((u.x | u.y | u.z | u.w) & 0x7f7f7f7fu)) *(volatile int*)&c->bad = 1;
+                    return 0u;
+                };
                 uint4 code[2][PASSES];  // of keys, of values
                 uint32_t exp[2][PASSES];
                 auto put = [&](int b, uint32_t to, auto which) {
@@ -525,12 +540,11 @@ __global__ void __launch_bounds__(Cfg<D, NP, QT, Q8>::THREADS, 1) window_prefill
 #pragma unroll
                     for (int k = 0; k < PASSES; ++k) {
                         const int pos = b + r0 + k * GROUP;
-                        scale[k] = q8::scale2(exp[V][k], exp[V][k]);
+                        scale[k] = q8::shifted_scale(exp[V][k]);
                         if (!whole && !(pos < pages.last && ((pos >= win0 && a.window > 0) || pos < a.sinks))) {
                             scale[k] = 0u;
-                        } else if (V && !shared && exp[V][k] > q8::kMostExponent) {
-                            scale[k] = 0u;
-                            *(volatile int*)&c->bad = 1;
+                        } else if (!q8::shift_holds(exp[V][k])) {
+                            scale[k] = unheld(code[V][k], exp[V][k], V && !shared);
                         }
                     }
 #pragma unroll
@@ -539,8 +553,8 @@ __global__ void __launch_bounds__(Cfg<D, NP, QT, Q8>::THREADS, 1) window_prefill
                         uint32_t u[8];
 #pragma unroll
                         for (int e = 0; e < 4; ++e) {
-                            u[2 * e] = q8::pair_of(__byte_perm(x[e], 0u, 0x1100u), scale[k]);
-                            u[2 * e + 1] = q8::pair_of(__byte_perm(x[e], 0u, 0x3322u), scale[k]);
+                            u[2 * e] = q8::shifted_of(__byte_perm(x[e], 0u, 0x1100u), scale[k]);
+                            u[2 * e + 1] = q8::shifted_of(__byte_perm(x[e], 0u, 0x3322u), scale[k]);
                         }
                         const uint32_t dst = to + place + k * GROUP * 128;
                         store16(dst, u[0], u[1], u[2], u[3]);
@@ -897,16 +911,18 @@ __global__ void __launch_bounds__(Cfg<D, NP, QT, Q8>::THREADS, 1) window_prefill
             return true;
         };
         if constexpr (C::PIPE) {
-            auto read = [&](uint32_t k, uint32_t (&s)[KT]) {  // S of the stream's tile k, on its way
-                wait(bar_s + 16 * w + 8 * (k & 1), k >> 1 & 1, 6);
+            // (S is read only once P of the tile before is on its way: waited for earlier, with its loads
+            // among the exponentials, it held that P up, 1359 -> 1509 us for 8192 rows behind 8192.)
+#pragma unroll 1
+            for (int t = 0; t < n; ++t) {
+                if (!takes(t)) continue;
+                wait(bar_s + 16 * w + 8 * (done & 1), done >> 1 & 1, 6);
                 __syncwarp();
                 fence_after();
-                tmem_ld32<0>(tmem + lanes + C::s_col(w) + 64 * (k & 1), s);
-                tmem_ld32<32>(tmem + lanes + C::s_col(w) + 64 * (k & 1) + 32, s);
-            };
-            auto tile = [&](int t) {
+                const uint32_t s_at = tmem + lanes + C::s_col(w) + 64 * (done & 1);
                 uint32_t s[KT];
-                read(done, s);
+                tmem_ld32<0>(s_at, s);
+                tmem_ld32<32>(s_at + 32, s);
                 tmem_landed(s);
                 uint32_t see[2];
                 const bool masked = seen_of(t, see);
@@ -919,7 +935,7 @@ __global__ void __launch_bounds__(Cfg<D, NP, QT, Q8>::THREADS, 1) window_prefill
 #pragma unroll
                 for (int i = 0; i < KT; i += 8)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) x[e] = fmaxf(x[e], fmaxf(asf(s[i + 2 * e]), asf(s[i + 2 * e + 1])));
+                    for (int e = 0; e < 4; ++e) x[e] = max3(x[e], asf(s[i + 2 * e]), asf(s[i + 2 * e + 1]));
                 const float mx = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])) * p.scale;
                 // O is rescaled when a row's maximum has outgrown the one in use by 2^8
                 const bool grown = mx > m + 8.f;  // the first time too: m is -inf
@@ -959,7 +975,7 @@ __global__ void __launch_bounds__(Cfg<D, NP, QT, Q8>::THREADS, 1) window_prefill
                         pk[e / 2] = pack(y.x, y.y);
                         pk[e / 2 + 1] = pack(z.x, z.y);
                     }
-                    tmem_st16<0>(tmem + lanes + C::s_col(w) + 64 * (done & 1) + i / 2, pk);
+                    tmem_st16<0>(s_at + i / 2, pk);
                 }
                 l0 = add2(l0, l1);
                 l += l0.x + l0.y;
@@ -967,10 +983,7 @@ __global__ void __launch_bounds__(Cfg<D, NP, QT, Q8>::THREADS, 1) window_prefill
                 fence_before();
                 bar_arrive(bar_p + 16 * w + 8 * (done & 1));
                 ++done;
-            };
-#pragma unroll 1
-            for (int t = 0; t < n; ++t)
-                if (takes(t)) tile(t);
+            }
         } else
         for (int t = QT == 1 ? w : 0; t < n; t += QT == 1 ? 2 : 1) {
             if (QT == 2 && !takes(t)) continue;
@@ -1191,7 +1204,7 @@ __global__ void __launch_bounds__(Cfg<D, NP, QT, Q8>::THREADS, 1) window_prefill
         };
         if constexpr (QT == 2) {
             {
-                const float inv = l == 0.f ? 0.f : 1.0f / l;  // a row that sees nothing: zeros
+                const float inv = l == 0.f ? 0.f : C::UNIT / l;  // a row that sees nothing: zeros
 #pragma unroll
                 for (int i = 0; i < D; i += 32) {
                     uint32_t y[32];
@@ -1256,7 +1269,7 @@ __global__ void __launch_bounds__(Cfg<D, NP, QT, Q8>::THREADS, 1) window_prefill
             const float2 his = join_ml[(1 - w) * 128 + r];
             const float mt = fmaxf(m, his.x);
             const float keep = m == -INFINITY ? 0.f : ex2(m - mt), take = his.x == -INFINITY ? 0.f : ex2(his.x - mt);
-            const float lt = l * keep + his.y * take, inv = lt == 0.f ? 0.f : 1.0f / lt;
+            const float lt = l * keep + his.y * take, inv = lt == 0.f ? 0.f : C::UNIT / lt;
             if (p.splits > 1 && w == 0) __stcg(p.ml + part + r, make_float2(mt, lt));
             if (w == 0) finish(std::integral_constant<int, 0>{}, keep, take, inv);
             else finish(std::integral_constant<int, 1>{}, keep, take, inv);
@@ -1351,7 +1364,7 @@ __global__ void __launch_bounds__(256) window_join_kernel(const __grid_constant_
             }
         }
     }
-    const float inv = l == 0.f ? 0.f : 1.0f / l;
+    const float inv = l == 0.f ? 0.f : (Q8 ? kUnit8 : 1.0f) / l;
     T* out = static_cast<T*>(a.o) + ((int64_t)(rows.x + tk) * a.Hq + kvh * G + head0 + r - tk * heads) * D + 4 * c4;
     if constexpr (sizeof(T) == 2) {
         *reinterpret_cast<uint4*>(out) = make_uint4(pack(y[0].x * inv, y[0].y * inv), pack(y[0].z * inv, y[0].w * inv),
@@ -1437,7 +1450,7 @@ cudaError_t launch_any(const WindowArgs& a, bool f32, cudaStream_t st) {
     p.groups = plan.groups;
     p.tok = plan.tok;
     p.splits = plan.splits;
-    p.scale = (float)(1.4426950408889634 / sqrt((double)a.d));
+    p.scale = (float)((Q8 ? ldexp(1.0, q8::kShift) : 1.0) * 1.4426950408889634 / sqrt((double)a.d));
     p.part = reinterpret_cast<float4*>(static_cast<char*>(a.scratch) + kCounterBytes);
     p.rows = reinterpret_cast<int4*>(p.part + plan.tiles * plan.splits * 128 * (a.d / 4));
     p.ml = reinterpret_cast<float2*>(p.rows + plan.tiles);
