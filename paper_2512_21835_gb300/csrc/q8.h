@@ -82,9 +82,8 @@ __device__ __forceinline__ float value_of(uint32_t code, float step) {
 //   pair_of     takes two products by powers of two, 2^127 and 2^(E - 127): four instructions
 //   shifted_of  makes the value times 2^-kShift in one, for the exponents of shift_holds: three
 //
-// The second factor for a pair of blocks (or for one, twice).
-__device__ __forceinline__ uint32_t scale2(uint32_t Elo, uint32_t Ehi) {
-    const uint32_t e = Elo + Ehi * 65536u;
+// The second factor for a pair of blocks with exponents E[0] + 2^16 E[1] (or for one, twice).
+__device__ __forceinline__ uint32_t scale2(uint32_t e) {
     const uint32_t nan = (e + 0x00020002u & 0x01000100u) >> 2;  // 0x40 where it is 254 or 255
     return e * 128u | nan * 511u;                               // 0x40 x 511 = 0x7fc0
 }
@@ -98,10 +97,10 @@ __device__ __forceinline__ uint32_t pair_of(uint32_t twice, uint32_t scale) {
 }
 
 // Values times 2^-64 are normal bf16 numbers for exponents 71 to 191 (elements of 2^-62 to 2^58 in
-// size), and the factor 2^(E - 64) is one too.
+// size), and the factor 2^(E - 64) is one too.  (shifted2 as scale2.)
 constexpr int kShift = 64;
 __device__ __forceinline__ bool shift_holds(uint32_t E) { return E - 71u <= 191u - 71u; }
-__device__ __forceinline__ uint32_t shifted_scale(uint32_t E) { return (E + (127 - kShift)) * 0x00800080u; }
+__device__ __forceinline__ uint32_t shifted2(uint32_t e) { return e * 128u + (127 - kShift) * 0x00800080u; }
 __device__ __forceinline__ uint32_t shifted_of(uint32_t twice, uint32_t scale) {
     uint32_t r;
     asm("{\n .reg .b32 x;\n and.b32 x, %1, 0x807f807f;\n mul.rn.bf16x2 %0, x, %2;\n}\n"

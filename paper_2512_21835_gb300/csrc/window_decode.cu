@@ -38,6 +38,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "internal.h"
 #include "q8.h"
@@ -427,7 +428,7 @@ __global__ void __launch_bounds__(kThreads, kResident) window_decode_kernel(cons
 // The 8-bit cache.
 //
 // 33 d bytes a tile instead of 64 d, so that the conversion to bf16 is what the memory's rate
-// has to hide: two instructions an element (q8.h).  A tile is one contiguous granule:
+// has to hide: three instructions for two elements, four where exponents are extreme (q8.h).  A tile is one contiguous granule:
 // a warp copies its own tiles, kStages - 1 ahead, whole (the positions of a granule that are
 // not seen lie in a page of the request all the same), and reads the MMAs' fragments from
 // shared memory, 16 bytes a lane without bank conflicts:
@@ -443,6 +444,8 @@ __global__ void __launch_bounds__(kThreads, kResident) window_decode_kernel(cons
 // begins in one block and ends in a later one is joined by the last of its blocks to arrive.
 // ---------------------------------------------------------------------------
 constexpr int kStages = 3;
+constexpr float kUnit8 = 0x1p64f;  // of elements as shifted_of makes them
+static_assert(q8::kShift == 64, "");
 constexpr int kResident8 = 4;  // blocks per SM
 constexpr int kPlaces8 = 152 * kResident8;
 
@@ -548,6 +551,7 @@ __global__ void __launch_bounds__(kThreads, kResident8) window_decode_q8_kernel(
 #pragma unroll
         for (int e = 0; e < D / 16; ++e) o[e][0] = o[e][1] = o[e][2] = o[e][3] = 0.f;
         float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};  // of heads 2 c4 and 2 c4 + 1
+        bool exact = false;  // O in units of its own, and not of kUnit8
         __syncthreads();  // the queries
 #pragma unroll 1
         for (int stage = 0; i < last; i += kWarps, stage = stage + 1 == kStages ? 0 : stage + 1) {
@@ -561,96 +565,131 @@ __global__ void __launch_bounds__(kThreads, kResident8) window_decode_q8_kernel(
             const int j0 = seen.at(i) * kTile;
             const bool all = j0 + kTile <= seen.ctx && (j0 >= seen.win0 || j0 + kTile <= seen.sinks);
             const bool see0 = all || seen.seen(j0 + n4), see1 = all || seen.seen(j0 + 8 + n4);
-            // ---- scores, in independent sums (a chain of MMAs waits for each result)
-            float s[4];
+            // exponents: of keys n4 and n4 + 8, of values 2 c4 and 2 c4 + 1, and eight further on
+            uint32_t ek, ev[2];
             {
-                uint32_t k[2][4 * NK], E[2];
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    E[j] = g[Gr::exponents(0, 8 * j + n4) + c4 * (D / 64) / 2];
-#pragma unroll
-                    for (int x = 0; x < NK; ++x) {
-                        const uint4 u = *reinterpret_cast<const uint4*>(g + Gr::piece(0, 8 * j + n4, NK * c4 + x));
-                        k[j][4 * x] = u.x; k[j][4 * x + 1] = u.y; k[j][4 * x + 2] = u.z; k[j][4 * x + 3] = u.w;
-                    }
-                }
-                const uint32_t both = q8::scale2(E[0], E[1]);
-                const uint32_t sc[2] = {see0 ? __byte_perm(both, 0u, 0x1010u) : 0u, see1 ? __byte_perm(both, 0u, 0x3232u) : 0u};
-                constexpr int SUMS = F32 ? 1 : 2;
-                float z[PL][SUMS][4];
-#pragma unroll
-                for (int pl = 0; pl < PL; ++pl)
-#pragma unroll
-                    for (int h = 0; h < SUMS; ++h) z[pl][h][0] = z[pl][h][1] = z[pl][h][2] = z[pl][h][3] = 0.f;
-#pragma unroll
-                for (int x = 0; x < 4 * NK; ++x) {
-                    uint32_t A[2][2];
-#pragma unroll
-                    for (int j = 0; j < 2; ++j) {
-                        A[j][0] = q8::pair_of(__byte_perm(k[j][x], 0u, 0x1100u), sc[j]);
-                        A[j][1] = q8::pair_of(__byte_perm(k[j][x], 0u, 0x3322u), sc[j]);
-                    }
-#pragma unroll
-                    for (int pl = 0; pl < PL; ++pl) {
-                        const uint4 q = sm_q[x / 2][pl][lane];
-                        mma(z[pl][x % SUMS], A[0][0], A[1][0], A[0][1], A[1][1], x % 2 ? q.z : q.x, x % 2 ? q.w : q.y);
-                    }
-                }
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    if constexpr (F32)
-                        s[e] = z[0][0][e] + (z[1][0][e] + z[2][0][e]);
-                    else
-                        s[e] = z[0][0][e] + z[0][1][e];
-                }
-            }
-            uint32_t pb[PV][2];
-            soften<true>(s, see0, see1, scale, m, l, o, pb);
-            // ---- values: rows 2 c4, 2 c4 + 1, 2 c4 + 8, 2 c4 + 9
-            uint32_t sc[2];
-            uint32_t v[4][NW];
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                uint32_t E[2];
+                uint32_t E[3][2];
 #pragma unroll
                 for (int r = 0; r < 2; ++r) {
-                    const int row = 2 * c4 + r + 8 * j;
-                    E[r] = g[Gr::exponents(1, row) + n4 / 2 * (D / 64) / 2];
-                    const uint8_t* from = g + Gr::piece(1, row, D == 128 ? n4 : n4 / 2);
-                    if constexpr (D == 128) {
-                        const uint4 u = *reinterpret_cast<const uint4*>(from);
-                        v[2 * j + r][0] = u.x; v[2 * j + r][1] = u.y; v[2 * j + r][2] = u.z; v[2 * j + r][3] = u.w;
-                    } else {
-                        const uint2 u = *reinterpret_cast<const uint2*>(from + n4 % 2 * 8);
-                        v[2 * j + r][0] = u.x; v[2 * j + r][1] = u.y;
+                    E[0][r] = g[Gr::exponents(0, 8 * r + n4) + c4 * (D / 64) / 2];
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) E[1 + j][r] = g[Gr::exponents(1, 2 * c4 + r + 8 * j) + n4 / 2 * (D / 64) / 2];
+                }
+                ek = E[0][0] + E[0][1] * 65536u;
+                ev[0] = E[1][0] + E[1][1] * 65536u;
+                ev[1] = E[2][0] + E[2][1] * 65536u;
+            }
+            uint32_t keep[2] = {~0u, ~0u};  // the values that are seen
+            if (!all) {
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    keep[j] = (seen.seen(j0 + 2 * c4 + 8 * j) ? 0xffffu : 0u) |
+                              (seen.seen(j0 + 2 * c4 + 1 + 8 * j) ? 0xffff0000u : 0u);
+                    ev[j] = (ev[j] & keep[j]) | (0x00800080u & ~keep[j]);
+                }
+                const uint32_t mask = (see0 ? 0xffffu : 0u) | (see1 ? 0xffff0000u : 0u);
+                ek = (ek & mask) | (0x00800080u & ~mask);
+            }
+            // An exponent of 96 to 159 is one whose shift is a test of bits.  A tile with another one takes O to
+            // its own units, and from then on elements are made by two products.
+            if (!exact && __any_sync(0xffffffffu, ((ek - 0x00600060u) | (ev[0] - 0x00600060u) | (ev[1] - 0x00600060u)) & 0xffc0ffc0u)) {
+                exact = true;
+#pragma unroll
+                for (int e = 0; e < D / 16; ++e)
+#pragma unroll
+                    for (int h = 0; h < 4; ++h) o[e][h] *= kUnit8;
+            }
+            auto tile = [&](auto exactly) {
+                constexpr bool EXACT = decltype(exactly)::value;
+                auto pair = [](uint32_t twice, uint32_t sc) { return EXACT ? q8::pair_of(twice, sc) : q8::shifted_of(twice, sc); };
+                // ---- scores, in independent sums (a chain of MMAs waits for each result)
+                float s[4];
+                {
+                    uint32_t k[2][4 * NK];
+#pragma unroll
+                    for (int j = 0; j < 2; ++j)
+#pragma unroll
+                        for (int x = 0; x < NK; ++x) {
+                            const uint4 u = *reinterpret_cast<const uint4*>(g + Gr::piece(0, 8 * j + n4, NK * c4 + x));
+                            k[j][4 * x] = u.x; k[j][4 * x + 1] = u.y; k[j][4 * x + 2] = u.z; k[j][4 * x + 3] = u.w;
+                        }
+                    const uint32_t both = EXACT ? q8::scale2(ek) : q8::shifted2(ek);
+                    const uint32_t sc[2] = {see0 ? __byte_perm(both, 0u, 0x1010u) : 0u, see1 ? __byte_perm(both, 0u, 0x3232u) : 0u};
+                    constexpr int SUMS = F32 ? 1 : 2;
+                    float z[PL][SUMS][4];
+#pragma unroll
+                    for (int pl = 0; pl < PL; ++pl)
+#pragma unroll
+                        for (int h = 0; h < SUMS; ++h) z[pl][h][0] = z[pl][h][1] = z[pl][h][2] = z[pl][h][3] = 0.f;
+#pragma unroll
+                    for (int x = 0; x < 4 * NK; ++x) {
+                        uint32_t A[2][2];
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) {
+                            A[j][0] = pair(__byte_perm(k[j][x], 0u, 0x1100u), sc[j]);
+                            A[j][1] = pair(__byte_perm(k[j][x], 0u, 0x3322u), sc[j]);
+                        }
+#pragma unroll
+                        for (int pl = 0; pl < PL; ++pl) {
+                            const uint4 q = sm_q[x / 2][pl][lane];
+                            mma(z[pl][x % SUMS], A[0][0], A[1][0], A[0][1], A[1][1], x % 2 ? q.z : q.x, x % 2 ? q.w : q.y);
+                        }
+                    }
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        if constexpr (F32)
+                            s[e] = z[0][0][e] + (z[1][0][e] + z[2][0][e]);
+                        else
+                            s[e] = z[0][0][e] + z[0][1][e];
                     }
                 }
-                sc[j] = q8::scale2(E[0], E[1]);
-                if (!all)
-                    sc[j] &= (seen.seen(j0 + 2 * c4 + 8 * j) ? 0xffffu : 0u) |
-                             (seen.seen(j0 + 2 * c4 + 1 + 8 * j) ? 0xffff0000u : 0u);
-            }
+                uint32_t pb[PV][2];
+                soften<true>(s, see0, see1, EXACT ? scale : scale * kUnit8, m, l, o, pb);
+                // ---- values: rows 2 c4, 2 c4 + 1, 2 c4 + 8, 2 c4 + 9
+                uint32_t sc[2];
+                uint32_t v[4][NW];
 #pragma unroll
-            for (int e = 0; e < D / 16; ++e) {
-                uint32_t A[2][2];
+                for (int j = 0; j < 2; ++j) {
 #pragma unroll
-                for (int j = 0; j < 2; ++j)
+                    for (int r = 0; r < 2; ++r) {
+                        const uint8_t* from = g + Gr::piece(1, 2 * c4 + r + 8 * j, D == 128 ? n4 : n4 / 2);
+                        if constexpr (D == 128) {
+                            const uint4 u = *reinterpret_cast<const uint4*>(from);
+                            v[2 * j + r][0] = u.x; v[2 * j + r][1] = u.y; v[2 * j + r][2] = u.z; v[2 * j + r][3] = u.w;
+                        } else {
+                            const uint2 u = *reinterpret_cast<const uint2*>(from + n4 % 2 * 8);
+                            v[2 * j + r][0] = u.x; v[2 * j + r][1] = u.y;
+                        }
+                    }
+                    sc[j] = (EXACT ? q8::scale2(ev[j]) : q8::shifted2(ev[j])) & keep[j];
+                }
 #pragma unroll
-                    for (int r = 0; r < 2; ++r)
-                        A[j][r] = q8::pair_of(
-                            __byte_perm(v[2 * j][e / 2], v[2 * j + 1][e / 2], 0x4400u + 0x1111u * (e % 2 * 2 + r)), sc[j]);
-                add_values<F32>(o[e], A[0][0], A[0][1], A[1][0], A[1][1], pb);
-            }
+                for (int e = 0; e < D / 16; ++e) {
+                    uint32_t A[2][2];
+#pragma unroll
+                    for (int j = 0; j < 2; ++j)
+#pragma unroll
+                        for (int r = 0; r < 2; ++r)
+                            A[j][r] = pair(
+                                __byte_perm(v[2 * j][e / 2], v[2 * j + 1][e / 2], 0x4400u + 0x1111u * (e % 2 * 2 + r)), sc[j]);
+                    add_values<F32>(o[e], A[0][0], A[0][1], A[1][0], A[1][1], pb);
+                }
+            };
+            if (exact)
+                tile(std::true_type{});
+            else
+                tile(std::false_type{});
         }
         asm volatile("cp.async.wait_all;" ::: "memory");
         __syncwarp();
         float* sm_o = reinterpret_cast<float*>(mine);
+        const float unit_o = exact ? 1.f : kUnit8;
 #pragma unroll
         for (int h = 0; h < 2; ++h)
 #pragma unroll
             for (int e = 0; e < D / 16; e += 2)
                 *reinterpret_cast<float4*>(sm_o + (2 * c4 + h) * D + D / 8 * n4 + 2 * e) =
-                    make_float4(o[e][h], o[e][2 + h], o[e + 1][h], o[e + 1][2 + h]);
+                    make_float4(o[e][h] * unit_o, o[e][2 + h] * unit_o, o[e + 1][h] * unit_o, o[e + 1][2 + h] * unit_o);
         // A block's part of a unit that began in an earlier block is its first, of one that ends in a
         // later block its second; a unit's counter is that of the block where it begins.
         const int64_t from = unit_at / share, active = (unit_at + steps - 1) / share - from + 1;

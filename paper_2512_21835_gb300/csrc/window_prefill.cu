@@ -540,7 +540,7 @@ __global__ void __launch_bounds__(Cfg<D, NP, QT, Q8>::THREADS, 1) window_prefill
 #pragma unroll
                     for (int k = 0; k < PASSES; ++k) {
                         const int pos = b + r0 + k * GROUP;
-                        scale[k] = q8::shifted_scale(exp[V][k]);
+                        scale[k] = q8::shifted2(exp[V][k] * 0x00010001u);
                         if (!whole && !(pos < pages.last && ((pos >= win0 && a.window > 0) || pos < a.sinks))) {
                             scale[k] = 0u;
                         } else if (!q8::shift_holds(exp[V][k])) {
