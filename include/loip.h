@@ -661,9 +661,9 @@ int loip_k_qk_append_q8(const void* qkv, int32_t dtype, int64_t row_stride, int3
                         uint64_t layer_page_bytes, void* stream);
 
 /* What the 8-bit cache holds, as numbers of type `dtype` (exact in both): row t of
- * out ([T, 2 * Hkv * d], dense: key heads, value heads) is position positions[t] of
- * request row_req[t] (of request t when row_req is NULL).  Rows of padding, as for
- * the append, are zero. */
+ * out ([T, 2 * Hkv * d], dense and 32-byte aligned: key heads, value heads) is
+ * position positions[t] of request row_req[t] (of request t when row_req is NULL).
+ * Rows of padding, as for the append, are zero. */
 int loip_k_cache_read_q8(const void* kv_base, const int64_t* page_offsets, int32_t max_pages,
                          const int32_t* positions, const int32_t* row_req, int32_t n_req, int32_t T, int32_t Hkv,
                          int32_t d, int32_t page_tokens, int32_t layer, uint64_t layer_page_bytes, void* out,

@@ -28,8 +28,9 @@ constexpr uint64_t kCounterBytes = kMaxCounters * sizeof(unsigned);
 #ifdef __CUDACC__
 __device__ __forceinline__ void pdl_trigger() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
-template <typename Args>
-cudaError_t launch_pdl(void (*kernel)(Args), dim3 grid, unsigned threads, size_t smem, cudaStream_t st, const Args& args) {
+template <typename... Args, typename... Given>
+cudaError_t launch_pdl(void (*kernel)(Args...), dim3 grid, unsigned threads, size_t smem, cudaStream_t st,
+                       const Given&... args) {
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[0].val.programmaticStreamSerializationAllowed = 1;
@@ -40,7 +41,7 @@ cudaError_t launch_pdl(void (*kernel)(Args), dim3 grid, unsigned threads, size_t
     c.stream = st;
     c.attrs = at;
     c.numAttrs = 1;
-    return cudaLaunchKernelEx(&c, kernel, args);
+    return cudaLaunchKernelEx(&c, kernel, args...);
 }
 
 // Lets a kernel have `bytes` of dynamic shared memory, once per device and kernel.

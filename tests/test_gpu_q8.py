@@ -173,6 +173,23 @@ def test_append_identity_rows_and_no_rows(torch, L):
     assert np.all(np.isnan(read([1], [0])))  # not written
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("Hkv,d,T", [(40, 64, 5003), (40, 128, 2501)])
+def test_read_of_many_rows(torch, L, Hkv, d, T, dtype):
+    """Enough rows that a thread takes four: any order, padding among them, the last group not full."""
+    c = Cache8(1, 10, Hkv, d, 13, layers=2, layer=1)
+    c.fill_request(0, range(600), 14)  # the last 40 positions are not written
+    pos = np.random.default_rng(15).integers(0, 640, T).astype(np.int32)
+    pos[[3, T - 2]] = -1, 640
+    out = torch.full((T, 2 * Hkv * d), 7.0, dtype=torch.float32 if dtype == "f32" else torch.bfloat16, device="cuda")
+    L.loip_k_cache_read_q8(_dev(torch, c.bytes), _dev(torch, c.table), 10, _ints(torch, pos), _ints(torch, [0] * T), Hkv,
+                           d, P, c.layer, c.layer_page_bytes, out)
+    k, v = c.gather(0, np.arange(640))
+    want = np.concatenate([k, v], 1).reshape(640, -1)[pos.clip(0, 639)]
+    want[[3, T - 2]] = 0
+    assert np.array_equal(_host(out), want, equal_nan=True)
+
+
 # ---------------------------------------------------------------------------
 # attention of single tokens
 # ---------------------------------------------------------------------------

@@ -69,7 +69,7 @@ ROWS_BAD = [dict(T=-1), dict(pos=None), dict(pos=A + 2), dict(req=A + 1), dict(n
     dict(x=None), dict(x=A + 4), dict(q=None), dict(q=A + 8), dict(stride=511), dict(stride=508), dict(stride=514),
     dict(dtype=1, stride=516), dict(gq=A), dict(gk=A), dict(gq=A + 2, gk=A), dict(theta=0.5), dict(theta=-1.0),
     dict(theta=float("nan")), dict(theta=float("inf")), dict(eps=-1.0), dict(eps=float("nan"))]]
-    + [(read, b) for b in CACHE_BAD + ROWS_BAD + [dict(o=None), dict(o=A + 8)]]
+    + [(read, b) for b in CACHE_BAD + ROWS_BAD + [dict(o=None), dict(o=A + 8), dict(o=A + 16)]]
     + [(decode, b) for b in CACHE_BAD + HEADS_BAD + WINDOW_BAD + [dict(B=-1), dict(ctx=None), dict(ctx=A + 2)]]
     + [(prefill, b) for b in CACHE_BAD + HEADS_BAD + WINDOW_BAD + [
         dict(M=-1), dict(n=0), dict(n=-1), dict(starts=None), dict(starts=A + 2), dict(first=A + 1)]])
