@@ -1254,7 +1254,7 @@ __global__ void __launch_bounds__(Cfg<D, NP, QT, Q8>::THREADS, 1) window_prefill
                     }
                     if (p.splits > 1) {
 #pragma unroll
-                        for (int e = 0; e < 32; e += 4)
+                        for (int e = 0; e < 32 && (!Q8 || live); e += 4)  // (of the other rows nothing is read)
                             __stcg(p.part + part * (D / 4) + (i + e) / 4 * 128 + r,
                                    make_float4(asf(y[e]), asf(y[e + 1]), asf(y[e + 2]), asf(y[e + 3])));
                     } else {
@@ -1303,21 +1303,30 @@ __global__ void __launch_bounds__(Cfg<D, NP, QT, Q8>::THREADS, 1) window_prefill
 }
 
 // The parts of a row tile, in their order: a block per unit and 16 columns, a thread per row
-// and 8 columns.
+// and 8 columns.  Q8: 8 and 4, ten parts' loads in flight, and the ends asked for by a lane each (nine
+// parts of 47 rows: 4.5 -> 2.3 us).
+template <bool Q8>
+constexpr int kJoinVectors = Q8 ? 1 : 2;  // of four columns, a thread's
+
 template <int D, bool Q8, typename T>
 __global__ void __launch_bounds__(256) window_join_kernel(const __grid_constant__ PrefillArgs p) {
     const WindowArgs& a = p.a;
     pdl_trigger();
     pdl_wait();
-    constexpr int PIECES = D / 16;
-    const int unit = blockIdx.x / PIECES, c4 = blockIdx.x % PIECES * 4 + threadIdx.x / 128 * 2, r = threadIdx.x % 128;
+    constexpr int N = kJoinVectors<Q8>, PIECES = D / (8 * N);
+    const int unit = blockIdx.x / PIECES, c4 = (blockIdx.x % PIECES * 2 + threadIdx.x / 128) * N, r = threadIdx.x % 128;
     const int units = a.Hkv * p.groups;
     const int kvh = unit % units / p.groups, head0 = unit % units % p.groups * p.heads;
     const int G = a.Hq / a.Hkv, heads = min(p.heads, G - head0);
     const int4 rows = __ldcg(p.rows + unit);  // first row, tokens, request, position
     const int tk = r / heads;
     unsigned end = kPartGood;
-    for (int x = 0; x < p.splits; ++x) end = worse(end, __ldcg(p.ended + unit * p.splits + x));
+    if constexpr (Q8) {
+        for (int x = threadIdx.x % 32; x < p.splits; x += 32) end = worse(end, __ldcg(p.ended + unit * p.splits + x));
+        end = __reduce_max_sync(0xffffffffu, end);
+    } else {
+        for (int x = 0; x < p.splits; ++x) end = worse(end, __ldcg(p.ended + unit * p.splits + x));
+    }
     if (end == kPartStopped) return;
     if (end == kPartNotFinite) {  // as without splits; the unit's blocks share the rows
         const int warp = threadIdx.x / 32 + blockIdx.x % PIECES * 8;
@@ -1331,17 +1340,19 @@ __global__ void __launch_bounds__(256) window_join_kernel(const __grid_constant_
     if (tk >= min(p.tok, rows.y)) return;
     const int64_t first = (int64_t)unit * p.splits;
     float m = -INFINITY, l = 0.f;
-    float4 y[2] = {make_float4(0.f, 0.f, 0.f, 0.f), make_float4(0.f, 0.f, 0.f, 0.f)};
-    constexpr int BATCH = 8;  // parts whose loads are in flight together
+    float4 y[N];
+#pragma unroll
+    for (int e = 0; e < N; ++e) y[e] = make_float4(0.f, 0.f, 0.f, 0.f);
+    constexpr int BATCH = Q8 ? 10 : 8;  // parts whose loads are in flight together
     for (int x0 = 0; x0 < p.splits; x0 += BATCH) {
         float2 ml[BATCH];
-        float4 v[BATCH][2];
+        float4 v[BATCH][N];
 #pragma unroll
         for (int x = 0; x < BATCH; ++x) {
             const int64_t at = first + min(x0 + x, p.splits - 1);
             ml[x] = __ldcg(p.ml + at * 128 + r);
-            v[x][0] = __ldcg(p.part + (at * (D / 4) + c4) * 128 + r);
-            v[x][1] = __ldcg(p.part + (at * (D / 4) + c4 + 1) * 128 + r);
+#pragma unroll
+            for (int e = 0; e < N; ++e) v[x][e] = __ldcg(p.part + (at * (D / 4) + c4 + e) * 128 + r);
         }
         float top = m;
 #pragma unroll
@@ -1350,7 +1361,7 @@ __global__ void __launch_bounds__(256) window_join_kernel(const __grid_constant_
         m = top;
         l *= keep;
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
+        for (int e = 0; e < N; ++e) {
             y[e].x *= keep; y[e].y *= keep; y[e].z *= keep; y[e].w *= keep;
         }
 #pragma unroll
@@ -1358,7 +1369,7 @@ __global__ void __launch_bounds__(256) window_join_kernel(const __grid_constant_
             const float f = x0 + x < p.splits && ml[x].x != -INFINITY ? ex2(ml[x].x - m) : 0.f;
             l = fmaf(f, ml[x].y, l);
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
+            for (int e = 0; e < N; ++e) {
                 y[e].x = fmaf(f, v[x][e].x, y[e].x); y[e].y = fmaf(f, v[x][e].y, y[e].y);
                 y[e].z = fmaf(f, v[x][e].z, y[e].z); y[e].w = fmaf(f, v[x][e].w, y[e].w);
             }
@@ -1366,12 +1377,14 @@ __global__ void __launch_bounds__(256) window_join_kernel(const __grid_constant_
     }
     const float inv = l == 0.f ? 0.f : (Q8 ? kUnit8 : 1.0f) / l;
     T* out = static_cast<T*>(a.o) + ((int64_t)(rows.x + tk) * a.Hq + kvh * G + head0 + r - tk * heads) * D + 4 * c4;
-    if constexpr (sizeof(T) == 2) {
+    if constexpr (sizeof(T) == 2 && N == 1) {
+        *reinterpret_cast<uint2*>(out) = make_uint2(pack(y[0].x * inv, y[0].y * inv), pack(y[0].z * inv, y[0].w * inv));
+    } else if constexpr (sizeof(T) == 2) {
         *reinterpret_cast<uint4*>(out) = make_uint4(pack(y[0].x * inv, y[0].y * inv), pack(y[0].z * inv, y[0].w * inv),
                                                     pack(y[1].x * inv, y[1].y * inv), pack(y[1].z * inv, y[1].w * inv));
     } else {
 #pragma unroll
-        for (int e = 0; e < 2; ++e)
+        for (int e = 0; e < N; ++e)
             reinterpret_cast<float4*>(out)[e] = make_float4(y[e].x * inv, y[e].y * inv, y[e].z * inv, y[e].w * inv);
     }
 }
@@ -1388,9 +1401,13 @@ int64_t visible_pages(int tok, int window, int sinks, int max_ctx) {
                              ((int64_t)window + tok + KT - 1) / KT + 1 + ((int64_t)sinks + KT - 1) / KT);
 }
 
-// A row tile is split when there are fewer row tiles than SMs, into parts of two pages
-// (one per stream) or more.
-Plan make_plan(int M, int n_prompts, int Hq, int Hkv, int window, int sinks, int max_ctx) {
+// Parts of a row tile, at most: of two pages (one per stream) or more; over the 8-bit cache one may
+// have a single page, as a third one costs the whole call 3 us (47 rows behind 1041: 17 pages in
+// eight parts 20.9 us, in nine 17.3 with the joining kernel as it is).
+int64_t most_parts(bool q8, int64_t pages) { return (pages + q8) / 2; }
+
+// A row tile is split when there are fewer row tiles than SMs.
+Plan make_plan(bool q8, int M, int n_prompts, int Hq, int Hkv, int window, int sinks, int max_ctx) {
     Plan p{};
     const int G = Hq / Hkv;
     p.groups = (G + 127) / 128;
@@ -1398,7 +1415,7 @@ Plan make_plan(int M, int n_prompts, int Hq, int Hkv, int window, int sinks, int
     p.tok = 128 / p.heads;
     p.tiles = std::min<int64_t>((int64_t)M / p.tok + n_prompts, M) * Hkv * p.groups;
     const int64_t pages = visible_pages(p.tok, window, sinks, max_ctx);
-    p.splits = p.tiles < kSms ? (int)std::max<int64_t>(1, std::min<int64_t>(kSms / std::max<int64_t>(p.tiles, 1), pages / 2)) : 1;
+    p.splits = p.tiles < kSms ? (int)std::max<int64_t>(1, std::min<int64_t>(kSms / std::max<int64_t>(p.tiles, 1), most_parts(q8, pages))) : 1;
     return p;
 }
 
@@ -1413,7 +1430,7 @@ cudaError_t launch_t(const PrefillArgs& p, cudaStream_t st) {
     if (blocks > 0x7fffffff) return cudaErrorInvalidValue;
     e = launch_pdl(window_prefill_kernel<D, NP, QT, Q8, T>, dim3((unsigned)blocks), C::THREADS, C::BYTES, st, p);
     if (e != cudaSuccess || p.splits == 1) return e;
-    return launch_pdl(window_join_kernel<D, Q8, T>, dim3((unsigned)(blocks / p.splits) * (D / 16)), 256, 0, st, p);
+    return launch_pdl(window_join_kernel<D, Q8, T>, dim3((unsigned)(blocks / p.splits) * (D / (8 * kJoinVectors<Q8>))), 256, 0, st, p);
 }
 
 template <int D, bool Q8>
@@ -1427,21 +1444,27 @@ cudaError_t launch_d(const PrefillArgs& p, bool f32, int64_t tiles, cudaStream_t
 
 // Enough for every smaller call too: a call's row tiles are split into kSms parts at most, of two
 // pages or more.
-uint64_t window_prefill_scratch(int M, int n_prompts, int Hq, int Hkv, int d, int window, int sinks, int max_ctx) {
+static uint64_t scratch_of(bool q8, int M, int n_prompts, int Hq, int Hkv, int d, int window, int sinks, int max_ctx) {
     if (M == 0) return 16;
-    const Plan p = make_plan(M, n_prompts, Hq, Hkv, window, sinks, max_ctx);
-    const int64_t most = visible_pages(p.tok, window, sinks, max_ctx) / 2;  // parts of a row tile
+    const Plan p = make_plan(q8, M, n_prompts, Hq, Hkv, window, sinks, max_ctx);
+    const int64_t most = most_parts(q8, visible_pages(p.tok, window, sinks, max_ctx));  // parts of a row tile
     if (most < 2) return 16;
     const uint64_t parts = std::min<int64_t>(kSms, p.tiles * most), tiles = std::min<int64_t>(kSms, p.tiles);
     const uint64_t n = kCounterBytes + tiles * 16 + parts * (128 * (d + 2) * sizeof(float) + sizeof(unsigned));
     return (n + 15) / 16 * 16;
+}
+uint64_t window_prefill_scratch(int M, int n_prompts, int Hq, int Hkv, int d, int window, int sinks, int max_ctx) {
+    return scratch_of(false, M, n_prompts, Hq, Hkv, d, window, sinks, max_ctx);
+}
+uint64_t window_prefill_q8_scratch(int M, int n_prompts, int Hq, int Hkv, int d, int window, int sinks, int max_ctx) {
+    return scratch_of(true, M, n_prompts, Hq, Hkv, d, window, sinks, max_ctx);
 }
 
 namespace {
 
 template <bool Q8>
 cudaError_t launch_any(const WindowArgs& a, bool f32, cudaStream_t st) {
-    const Plan plan = make_plan(a.rows, a.n_prompts, a.Hq, a.Hkv, a.window, a.sinks, a.max_ctx);
+    const Plan plan = make_plan(Q8, a.rows, a.n_prompts, a.Hq, a.Hkv, a.window, a.sinks, a.max_ctx);
     PrefillArgs p{};
     p.a = a;
     p.a.window = std::min(a.window, 1 << 30);  // positions are below max_ctx <= 2^30
@@ -1462,9 +1485,6 @@ cudaError_t launch_any(const WindowArgs& a, bool f32, cudaStream_t st) {
 
 cudaError_t launch_window_prefill(const WindowArgs& a, bool f32, cudaStream_t st) { return launch_any<false>(a, f32, st); }
 
-uint64_t window_prefill_q8_scratch(int M, int n_prompts, int Hq, int Hkv, int d, int window, int sinks, int max_ctx) {
-    return window_prefill_scratch(M, n_prompts, Hq, Hkv, d, window, sinks, max_ctx);
-}
 cudaError_t launch_window_prefill_q8(const WindowArgs& a, bool f32, cudaStream_t st) { return launch_any<true>(a, f32, st); }
 
 cudaError_t window_prefill_error(int* code) { return cudaMemcpyFromSymbol(code, g_window_error, sizeof(int)); }
