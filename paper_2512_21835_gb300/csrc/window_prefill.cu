@@ -85,9 +85,14 @@ constexpr int KT = kPageTokens;                  // keys per tile
 constexpr float kUnit8 = 0x1p64f;                // keys and values of the 8-bit cache are multiplied as their 2^-kShift-fold
 static_assert(q8::kShift == 64, "");
 
-template <int D, int NP, int QT, bool Q8>
+// Where the tiles of keys and values come from: the bf16 cache; the 8-bit cache, through loaders that turn
+// codes into bf16; images of its pages that a kernel before this one has made (window_image_kernel).
+enum Source { kBf16, kCodes, kImages };
+
+template <int D, int NP, int QT, Source SRC>
 struct Cfg {
-    static constexpr float UNIT = Q8 ? kUnit8 : 1.0f;  // of O as the tensor core has it
+    static constexpr bool Q8 = SRC == kCodes, IMG = SRC == kImages, EIGHT = SRC != kBf16;
+    static constexpr float UNIT = EIGHT ? kUnit8 : 1.0f;  // of O as the tensor core has it
     // Warps 0 to 7 softmax, from 8 on loaders, then one per stream that issues MMAs (Q8: and one that
     // copies pages).  The registers of a softmax warp's threads, of a loader's, and of the others
     // (which without Q8 share the loaders' warpgroup).
@@ -109,15 +114,15 @@ struct Cfg {
     static constexpr int PAGE = Q8 ? 4 * q8::Granule<D>::BYTES : 0;  // a page's part of a kv head, as it is cached
     static constexpr int STAGES = Q8 && NP == 1 ? 3 : 2;             // of those
     static constexpr int ROOM = 227 * 1024 - 1024 - 512 - Q_BYTES - STAGES * PAGE;
-    static constexpr int LIMIT = Q8 ? 4 : 12;
+    static constexpr int LIMIT = EIGHT ? 5 : 12;
     static constexpr int MOST = ROOM / SLOT < LIMIT ? ROOM / SLOT : LIMIT;
-    static constexpr int SLOTS = QT == 2 || Q8 ? MOST : MOST / 2 * 2;
+    static constexpr int SLOTS = QT == 2 || EIGHT ? MOST : MOST / 2 * 2;
     // Use i of the ring is of slot i % SLOTS and of barrier i % CYCLE.  With one row tile a stream takes
     // every second use: CYCLE is even, so that a stream meets every phase of its barriers.
     static constexpr int CYCLE = QT == 1 && SLOTS % 2 ? 2 * SLOTS : SLOTS;
     // S of the tile after next goes into the columns of P once P V is issued, so that it is there
     // when the softmax comes to it.
-    static constexpr bool PIPE = Q8 && NP == 1 && QT == 2;
+    static constexpr bool PIPE = EIGHT && NP == 1 && QT == 2;
     static constexpr int AHEAD = PIPE ? 2 : 3 - QT;      // slot i: keys of tile i, values of tile i - AHEAD
     static constexpr int STAGE = Q_BYTES + SLOTS * SLOT;
     static constexpr int CTL = STAGE + STAGES * PAGE;
@@ -142,6 +147,7 @@ struct Ctl {  // control words behind the ring
     uint32_t tmem;
     int abort, bad;
     int row0, tokens, req, pos0;
+    int prompt0, prompt1;  // positions of the prompt's rows
 };
 static_assert(sizeof(Ctl) <= 512, "");
 
@@ -169,6 +175,10 @@ struct PrefillArgs {
     int4* rows;         // [unit]: first row, tokens, request, position of the first
     float2* ml;         // [unit][split][128 rows]: maximum (log2), sum
     unsigned* ended;    // [unit][split]: PartEnd
+    // in scratch, with images; a prompt's pages in the order of its list
+    uint8_t* images;    // [prompt][image_pages][kv head][keys, values]: tiles as they lie in shared memory
+    unsigned* flags;    // [prompt][image_pages][kv head]: whether rows that see the page are walked
+    int image_pages;
 };
 
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -316,6 +326,12 @@ __device__ __forceinline__ void tmem_stored() { asm volatile("tcgen05.wait::st.s
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, uint32_t n) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
 }
+// Whole pieces of 16 bytes; the barrier counts them.
+__device__ __forceinline__ void copy_bulk(uint32_t to, const void* from, uint32_t bytes, uint32_t bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(to),
+                 "l"(from), "r"(bytes), "r"(bar)
+                 : "memory");
+}
 // (Without a clobber, so that loads of shared memory can pass it: fenced before it is signalled.)
 __device__ __forceinline__ void store16(uint32_t to, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
     asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(to), "r"(a), "r"(b), "r"(c), "r"(d));
@@ -364,9 +380,10 @@ struct Pages {
     __device__ int at(int v) const { return v < sink ? v : v - sink + win; }
 };
 
-template <int D, int NP, int QT, bool Q8, typename T>
-__global__ void __launch_bounds__(Cfg<D, NP, QT, Q8>::THREADS, 1) window_prefill_kernel(const __grid_constant__ PrefillArgs p) {
-    using C = Cfg<D, NP, QT, Q8>;
+template <int D, int NP, int QT, Source SRC, typename T>
+__global__ void __launch_bounds__(Cfg<D, NP, QT, SRC>::THREADS, 1) window_prefill_kernel(const __grid_constant__ PrefillArgs p) {
+    using C = Cfg<D, NP, QT, SRC>;
+    constexpr bool Q8 = C::Q8;
     const WindowArgs& a = p.a;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* sm = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
@@ -391,7 +408,7 @@ __global__ void __launch_bounds__(Cfg<D, NP, QT, Q8>::THREADS, 1) window_prefill
     if (warp == 0) {
         pdl_wait();
         int left = unit / units;  // row tiles from the end
-        int row0 = 0, tokens = 0, req = 0, pos0 = 0;
+        int row0 = 0, tokens = 0, req = 0, pos0 = 0, prompt0 = 0, prompt1 = 0;
         for (int top = a.n_prompts - 1; top >= 0; top -= 32) {
             const int i = top - lane;
             int lo = 0, hi = 0, at = 0;
@@ -415,12 +432,16 @@ __global__ void __launch_bounds__(Cfg<D, NP, QT, Q8>::THREADS, 1) window_prefill
                     row0 = lo + first;
                     tokens = min(QT * p.tok, hi - lo - first);
                     req = i;
-                    pos0 = min(max(at, -(1 << 30)), 1 << 30) + first;
+                    prompt0 = min(max(at, -(1 << 30)), 1 << 30);
+                    prompt1 = prompt0 + hi - lo - 1;
+                    pos0 = prompt0 + first;
                 }
                 row0 = __shfl_sync(0xffffffffu, row0, src);
                 tokens = __shfl_sync(0xffffffffu, tokens, src);
                 req = __shfl_sync(0xffffffffu, req, src);
                 pos0 = __shfl_sync(0xffffffffu, pos0, src);
+                prompt0 = __shfl_sync(0xffffffffu, prompt0, src);
+                prompt1 = __shfl_sync(0xffffffffu, prompt1, src);
                 break;
             }
             left -= __shfl_sync(0xffffffffu, sum, 31);
@@ -430,13 +451,15 @@ __global__ void __launch_bounds__(Cfg<D, NP, QT, Q8>::THREADS, 1) window_prefill
             c->tokens = tokens;
             c->req = req;
             c->pos0 = pos0;
+            c->prompt0 = prompt0;
+            c->prompt1 = prompt1;
         }
     } else if (warp == 8) {
         if (lane == 0) {
             c->abort = 0;
             c->bad = 0;
             for (int i = 0; i < C::CYCLE; ++i) {
-                bar_init(bar_full + 8 * i, C::LOADERS);
+                bar_init(bar_full + 8 * i, C::IMG ? 1 : C::LOADERS);
                 bar_init(bar_empty + 8 * i, QT);
             }
             for (int i = 0; Q8 && i < C::STAGES; ++i) {
@@ -602,6 +625,42 @@ __global__ void __launch_bounds__(Cfg<D, NP, QT, Q8>::THREADS, 1) window_prefill
                     for (int x = 0; x < C::AHEAD; ++x) {  // the last uses have no keys
                         bar_arrive(bar_full + 8 * keys.bar);
                         keys.template next<C::SLOTS, C::CYCLE>();
+                    }
+                }
+            } else if constexpr (C::IMG) {
+                if (warp == 8 && n > 0) {
+                    // -------------------------------------------------------- loader, images
+                    const Pages all(a, c->prompt0, c->prompt1);
+                    auto image = [&](int t) {  // of tile t, counted in kv heads of pages
+                        const int j = page_at(t);
+                        return ((int64_t)req * p.image_pages + (j < all.sink ? j : j - all.win + all.sink)) * a.Hkv + kvh;
+                    };
+                    for (int t = lane; t < n; t += 32)
+                        if (p.flags[image(t)]) *(volatile int*)&c->bad = 1;
+                    Use use{0, 0, 0}, freed{0, 0, 0};
+                    int issued = 0;
+#pragma unroll 1
+                    for (int i = 0; i < n + C::AHEAD; ++i) {
+                        if (i >= C::SLOTS) {
+                            wait(bar_empty + 8 * freed.bar, freed.phase, 1);
+                            freed.template next<C::SLOTS, C::CYCLE>();
+                        }
+                        __syncwarp();
+                        if (lane == 0 && !wait.dead) {
+                            const int t = i - C::AHEAD;  // whose values
+                            const uint32_t bar = bar_full + 8 * use.bar, dst = ring + use.slot * C::SLOT;
+                            const uint32_t bytes = ((i < n) + (t >= 0)) * C::TILE;
+                            asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+                            if (i < n) copy_bulk(dst, p.images + image(i) * (2 * C::TILE), C::TILE, bar);
+                            if (t >= 0) copy_bulk(dst + C::TILE, p.images + image(t) * (2 * C::TILE) + C::TILE, C::TILE, bar);
+                            issued = i + 1;
+                        }
+                        use.template next<C::SLOTS, C::CYCLE>();
+                    }
+                    if (lane == 0) {  // no copy may be in flight at the block's end
+                        const uint64_t t0 = now_ns();
+                        for (int i = max(0, issued - C::SLOTS); i < issued; ++i)
+                            while (!bar_try(bar_full + 8 * (i % C::CYCLE), i / C::CYCLE & 1) && now_ns() - t0 < 2000000000ull) {}
                     }
                 }
             } else {
@@ -806,11 +865,7 @@ __global__ void __launch_bounds__(Cfg<D, NP, QT, Q8>::THREADS, 1) window_prefill
                 if (lane == 0 && !wait.dead) {
                     const uint32_t bar = bar_page + 8 * stage;
                     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "n"(C::PAGE) : "memory");
-                    asm volatile(
-                        "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
-                            q_smem + C::STAGE + stage * C::PAGE),
-                        "l"(from + at), "n"(C::PAGE), "r"(bar)
-                        : "memory");
+                    copy_bulk(q_smem + C::STAGE + stage * C::PAGE, from + at, C::PAGE, bar);
                     issued = t + 1;
                 }
                 if (++stage == C::STAGES) {
@@ -1254,7 +1309,7 @@ __global__ void __launch_bounds__(Cfg<D, NP, QT, Q8>::THREADS, 1) window_prefill
                     }
                     if (p.splits > 1) {
 #pragma unroll
-                        for (int e = 0; e < 32 && (!Q8 || live); e += 4)  // (of the other rows nothing is read)
+                        for (int e = 0; e < 32 && (!C::EIGHT || live); e += 4)  // (of the other rows nothing is read)
                             __stcg(p.part + part * (D / 4) + (i + e) / 4 * 128 + r,
                                    make_float4(asf(y[e]), asf(y[e + 1]), asf(y[e + 2]), asf(y[e + 3])));
                     } else {
@@ -1297,9 +1352,74 @@ __global__ void __launch_bounds__(Cfg<D, NP, QT, Q8>::THREADS, 1) window_prefill
     } else if (end == kPartNotFinite && warp < 8) {
         for (int i = warp; i < tokens * heads; i += 8) {
             const int64_t at = ((int64_t)(row0 + i / heads) * a.Hq + kvh * G + head0 + i % heads) * D;
-            walk_row<D, Q8, T>(a, req, kvh, pos0 + i / heads, static_cast<const T*>(a.q) + at, static_cast<T*>(a.o) + at);
+            walk_row<D, C::EIGHT, T>(a, req, kvh, pos0 + i / heads, static_cast<const T*>(a.q) + at, static_cast<T*>(a.o) + at);
         }
     }
+}
+
+// Images of the pages that some row of a prompt sees, a block per page and kv head: codes to bf16 times
+// 2^-kShift, as the tiles lie in shared memory, so that a plain copy fetches them.  Worth it where many row
+// tiles meet a page (images_of): the loaders' conversions cost a row tile more than its products do.
+// What no row of the prompt sees is zero.  Values of NaN, and extreme exponents, flag the page.
+template <int D>
+__global__ void __launch_bounds__(256) window_image_kernel(const __grid_constant__ PrefillArgs p) {
+    using Gr = q8::Granule<D>;
+    using C = Cfg<D, 1, 2, kImages>;
+    const WindowArgs& a = p.a;
+    pdl_trigger();
+    pdl_wait();
+    const int req = blockIdx.x / p.image_pages, slot = blockIdx.x % p.image_pages, kvh = blockIdx.y;
+    const int lo = min(max(a.row_starts[req], 0), a.rows), hi = min(max(a.row_starts[req + 1], lo), a.rows);
+    if (hi == lo) return;
+    const int p0 = min(max(a.first_pos ? a.first_pos[req] : 0, -(1 << 30)), 1 << 30);
+    const Pages pages(a, p0, p0 + hi - lo - 1);
+    if (slot >= pages.n) return;
+    const int j = pages.at(slot), win0 = max(0, p0 - a.window + 1);
+    const char* page = a.kv.base + a.kv.page_offsets[(int64_t)req * a.kv.max_pages + j] +
+                       (uint64_t)a.kv.layer * a.kv.layer_page_bytes + (int64_t)kvh * 4 * Gr::BYTES;
+    const int64_t at = ((int64_t)req * p.image_pages + slot) * a.Hkv + kvh;
+    constexpr int GROUP = 256 * 16 / D, PASSES = KT / GROUP;  // tokens of a pass
+    const int ch = threadIdx.x % (D / 16), r0 = threadIdx.x / (D / 16);
+    uint4 code[2][PASSES];
+    uint32_t exp[2][PASSES];
+#pragma unroll
+    for (int v = 0; v < 2; ++v)
+#pragma unroll
+        for (int k = 0; k < PASSES; ++k) {
+            const int r = r0 + k * GROUP;
+            const char* g = page + r / 16 * Gr::BYTES;
+            code[v][k] = *reinterpret_cast<const uint4*>(g + Gr::piece(v, r % 16, ch));
+            exp[v][k] = *reinterpret_cast<const uint8_t*>(g + Gr::exponents(v, r % 16) + ch / 2);
+        }
+    bool flag = false;
+#pragma unroll
+    for (int v = 0; v < 2; ++v)
+#pragma unroll
+        for (int k = 0; k < PASSES; ++k) {
+            const int r = r0 + k * GROUP, pos = j * KT + r;
+            const uint32_t x[4] = {code[v][k].x, code[v][k].y, code[v][k].z, code[v][k].w}, E = exp[v][k];
+            uint32_t scale = q8::shifted2(E * 0x00010001u);
+            if (!(pos < pages.last && ((pos >= win0 && a.window > 0) || pos < a.sinks))) {
+                scale = 0u;
+            } else if (!q8::shift_holds(E)) {
+                const bool nan = E > q8::kMostExponent;
+                scale = nan && !v ? 0x7fc07fc0u : 0u;
+                flag |= nan ? v : ((x[0] | x[1] | x[2] | x[3]) & 0x7f7f7f7fu) != 0u;
+            }
+            uint32_t u[8];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {  // (the two halves change places in odd rows)
+                u[2 * e] = q8::shifted_of(__byte_perm(x[e ^ (r & 1) * 2], 0u, 0x1100u), scale);
+                u[2 * e + 1] = q8::shifted_of(__byte_perm(x[e ^ (r & 1) * 2], 0u, 0x3322u), scale);
+            }
+            uint8_t* out = p.images + at * (2 * C::TILE) + v * C::TILE + (ch >> 2) * C::KV_SLAB + r * 128 +
+                           (((2 * (ch & 3) ^ (r & 7)) & 6) << 4);
+            asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(out), "r"(u[0]), "r"(u[1]), "r"(u[2]),
+                         "r"(u[3]), "r"(u[4]), "r"(u[5]), "r"(u[6]), "r"(u[7])
+                         : "memory");
+        }
+    const int any = __syncthreads_or(flag);
+    if (threadIdx.x == 0) p.flags[at] = any != 0;
 }
 
 // The parts of a row tile, in their order: a block per unit and 16 columns, a thread per row
@@ -1419,25 +1539,57 @@ Plan make_plan(bool q8, int M, int n_prompts, int Hq, int Hkv, int window, int s
     return p;
 }
 
-template <int D, int NP, int QT, bool Q8, typename T>
+bool two_tiles(int64_t tiles) { return tiles >= 2 * kSms; }
+
+// Images of the pages that the prompts see: how many each has room for, and bytes of all (with their
+// flags), or 0 where the loaders of the row tiles do better: where a page meets few row tiles
+// (`rows` of a prompt at most), or the images take more than kMostImages.
+constexpr int64_t kImageReuse = 8;
+constexpr int64_t kMostImages = 1ll << 30;
+struct Images {
+    int pages;
+    int64_t tiles, bytes;
+};
+Images images_of(int M, int n_prompts, int heads, int Hkv, int d, int window, int sinks, int max_ctx) {
+    Images m{};
+    const int64_t pages = visible_pages(M, window, sinks, max_ctx);
+    m.pages = (int)pages;
+    m.tiles = n_prompts * pages * Hkv;
+    m.bytes = m.tiles * (2 * KT * (int64_t)d * 2 + (int64_t)sizeof(unsigned));
+    return m;
+}
+// Row tiles that meet a page, about, when a prompt has `rows` rows.
+int64_t image_reuse(int64_t rows, int heads, int window) { return std::min<int64_t>(rows, (int64_t)window + KT) * heads / 128; }
+
+template <int D, int NP, int QT, Source SRC, typename T>
 cudaError_t launch_t(const PrefillArgs& p, cudaStream_t st) {
-    using C = Cfg<D, NP, QT, Q8>;
+    using C = Cfg<D, NP, QT, SRC>;
+    constexpr bool Q8 = C::EIGHT;
     static std::atomic<uint64_t> ready{0};  // devices whose limit has been raised, one bit each
-    cudaError_t e = raise_smem_limit(window_prefill_kernel<D, NP, QT, Q8, T>, C::BYTES, ready);
+    cudaError_t e = raise_smem_limit(window_prefill_kernel<D, NP, QT, SRC, T>, C::BYTES, ready);
     if (e != cudaSuccess) return e;
     const int64_t tiles = p.a.rows / (QT * p.tok) + p.a.n_prompts;  // at least the sum over prompts
     const int64_t blocks = std::min<int64_t>(tiles, p.a.rows) * p.a.Hkv * p.groups * p.splits;
     if (blocks > 0x7fffffff) return cudaErrorInvalidValue;
-    e = launch_pdl(window_prefill_kernel<D, NP, QT, Q8, T>, dim3((unsigned)blocks), C::THREADS, C::BYTES, st, p);
+    e = launch_pdl(window_prefill_kernel<D, NP, QT, SRC, T>, dim3((unsigned)blocks), C::THREADS, C::BYTES, st, p);
     if (e != cudaSuccess || p.splits == 1) return e;
     return launch_pdl(window_join_kernel<D, Q8, T>, dim3((unsigned)(blocks / p.splits) * (D / (8 * kJoinVectors<Q8>))), 256, 0, st, p);
 }
 
-template <int D, bool Q8>
+template <int D, Source SRC>
 cudaError_t launch_d(const PrefillArgs& p, bool f32, int64_t tiles, cudaStream_t st) {
-    if (f32) return launch_t<D, 3, 1, Q8, float>(p, st);
+    if constexpr (SRC != kBf16) {
+        // (bf16 rows with one row tile per block have no form for images: few row tiles, images_of)
+        if (p.images) {
+            const cudaError_t e = launch_pdl(window_image_kernel<D>, dim3((unsigned)(p.a.n_prompts * (int64_t)p.image_pages), p.a.Hkv),
+                                             256, 0, st, p);
+            if (e != cudaSuccess) return e;
+            return f32 ? launch_t<D, 3, 1, kImages, float>(p, st) : launch_t<D, 1, 2, kImages, __nv_bfloat16>(p, st);
+        }
+    }
+    if (f32) return launch_t<D, 3, 1, SRC, float>(p, st);
     // two row tiles per block once that leaves no SM without a block
-    return tiles >= 2 * kSms ? launch_t<D, 1, 2, Q8, __nv_bfloat16>(p, st) : launch_t<D, 1, 1, Q8, __nv_bfloat16>(p, st);
+    return two_tiles(tiles) ? launch_t<D, 1, 2, SRC, __nv_bfloat16>(p, st) : launch_t<D, 1, 1, SRC, __nv_bfloat16>(p, st);
 }
 
 }  // namespace
@@ -1448,10 +1600,14 @@ static uint64_t scratch_of(bool q8, int M, int n_prompts, int Hq, int Hkv, int d
     if (M == 0) return 16;
     const Plan p = make_plan(q8, M, n_prompts, Hq, Hkv, window, sinks, max_ctx);
     const int64_t most = most_parts(q8, visible_pages(p.tok, window, sinks, max_ctx));  // parts of a row tile
-    if (most < 2) return 16;
+    // (a smaller call may have all its rows in one prompt)
+    const uint64_t images = q8 && image_reuse(M, p.heads, window) >= kImageReuse
+                                ? (std::min(images_of(M, n_prompts, p.heads, Hkv, d, window, sinks, max_ctx).bytes, kMostImages) + 31) / 16 * 16
+                                : 0;
+    if (most < 2) return images ? kCounterBytes + images : 16;
     const uint64_t parts = std::min<int64_t>(kSms, p.tiles * most), tiles = std::min<int64_t>(kSms, p.tiles);
     const uint64_t n = kCounterBytes + tiles * 16 + parts * (128 * (d + 2) * sizeof(float) + sizeof(unsigned));
-    return (n + 15) / 16 * 16;
+    return (n + 15) / 16 * 16 + images;
 }
 uint64_t window_prefill_scratch(int M, int n_prompts, int Hq, int Hkv, int d, int window, int sinks, int max_ctx) {
     return scratch_of(false, M, n_prompts, Hq, Hkv, d, window, sinks, max_ctx);
@@ -1462,9 +1618,9 @@ uint64_t window_prefill_q8_scratch(int M, int n_prompts, int Hq, int Hkv, int d,
 
 namespace {
 
-template <bool Q8>
+template <Source SRC>
 cudaError_t launch_any(const WindowArgs& a, bool f32, cudaStream_t st) {
-    const Plan plan = make_plan(Q8, a.rows, a.n_prompts, a.Hq, a.Hkv, a.window, a.sinks, a.max_ctx);
+    const Plan plan = make_plan(SRC != kBf16, a.rows, a.n_prompts, a.Hq, a.Hkv, a.window, a.sinks, a.max_ctx);
     PrefillArgs p{};
     p.a = a;
     p.a.window = std::min(a.window, 1 << 30);  // positions are below max_ctx <= 2^30
@@ -1473,19 +1629,31 @@ cudaError_t launch_any(const WindowArgs& a, bool f32, cudaStream_t st) {
     p.groups = plan.groups;
     p.tok = plan.tok;
     p.splits = plan.splits;
-    p.scale = (float)((Q8 ? ldexp(1.0, q8::kShift) : 1.0) * 1.4426950408889634 / sqrt((double)a.d));
+    p.scale = (float)((SRC != kBf16 ? ldexp(1.0, q8::kShift) : 1.0) * 1.4426950408889634 / sqrt((double)a.d));
     p.part = reinterpret_cast<float4*>(static_cast<char*>(a.scratch) + kCounterBytes);
     p.rows = reinterpret_cast<int4*>(p.part + plan.tiles * plan.splits * 128 * (a.d / 4));
     p.ml = reinterpret_cast<float2*>(p.rows + plan.tiles);
     p.ended = reinterpret_cast<unsigned*>(p.ml + plan.tiles * plan.splits * 128);
-    return a.d == 128 ? launch_d<128, Q8>(p, f32, plan.tiles, st) : launch_d<64, Q8>(p, f32, plan.tiles, st);
+    if (SRC != kBf16 && (f32 || two_tiles(plan.tiles)) &&
+        image_reuse(a.rows / a.n_prompts, plan.heads, a.window) >= kImageReuse) {
+        const Images m = images_of(a.rows, a.n_prompts, plan.heads, a.Hkv, a.d, a.window, a.sinks, a.max_ctx);
+        if (m.bytes <= kMostImages && a.n_prompts * (int64_t)m.pages <= 0x7fffffff) {
+            // (of the scratch's end, which the parts do not reach)
+            char* behind = reinterpret_cast<char*>(p.ended + plan.tiles * plan.splits);
+            if (plan.splits == 1) behind = static_cast<char*>(a.scratch) + kCounterBytes;
+            p.images = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(behind) + 31) / 32 * 32);
+            p.flags = reinterpret_cast<unsigned*>(p.images + m.tiles * (2 * KT * (int64_t)a.d * 2));
+            p.image_pages = m.pages;
+        }
+    }
+    return a.d == 128 ? launch_d<128, SRC>(p, f32, plan.tiles, st) : launch_d<64, SRC>(p, f32, plan.tiles, st);
 }
 
 }  // namespace
 
-cudaError_t launch_window_prefill(const WindowArgs& a, bool f32, cudaStream_t st) { return launch_any<false>(a, f32, st); }
+cudaError_t launch_window_prefill(const WindowArgs& a, bool f32, cudaStream_t st) { return launch_any<kBf16>(a, f32, st); }
 
-cudaError_t launch_window_prefill_q8(const WindowArgs& a, bool f32, cudaStream_t st) { return launch_any<true>(a, f32, st); }
+cudaError_t launch_window_prefill_q8(const WindowArgs& a, bool f32, cudaStream_t st) { return launch_any<kCodes>(a, f32, st); }
 
 cudaError_t window_prefill_error(int* code) { return cudaMemcpyFromSymbol(code, g_window_error, sizeof(int)); }
 

@@ -479,6 +479,52 @@ def test_prefill_two_tiles_and_values_that_later_rows_alone_see(torch, L):
     assert np.array_equal(np.isnan(got), nan)
 
 
+# enough row tiles per page that images of the pages are made first
+IMAGE_RUNS = [(400, 70), (330, 3)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("Hq,Hkv,d", [(64, 4, 64), (64, 4, 128)])
+@pytest.mark.parametrize("window,sinks", [(ALL, 0), (100, 70), (65, 3)])
+def test_prefill_many_tiles_of_a_page(torch, L, Hq, Hkv, d, window, sinks, dtype):
+    _check_prefill(torch, L, IMAGE_RUNS, Hq, Hkv, d, window, sinks, dtype, 191, max_ctx=600)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("E", [254, 255, 40, 200])
+def test_prefill_many_tiles_of_a_page_and_extreme_exponents(torch, L, E, dtype):
+    """NaN that some rows see, and blocks whose exponents images (and loaders) have no form for."""
+    def edit(c):
+        for which, j in ((1, 133), (0, 260)):
+            c.bytes[c.slot(0, j, which)[1][:, 1]] = E if which else min(E, 120)
+
+    got = _check_prefill(torch, L, IMAGE_RUNS[:1] + [(2, 5)], 64, 4, 64, 100, 1, dtype, 201, edit=edit)
+    nan = np.zeros(got.shape, dtype=bool)
+    if E >= 254:
+        nan[133 - 70:233 - 70, :, 32:] = True
+    assert np.array_equal(np.isnan(got), nan)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("runs", [[(150, 30)], [(520, 30)]])
+def test_prefill_exponents_at_the_borders(torch, L, runs, dtype):
+    """Blocks on both sides of the exponents that one product serves, in keys and in values, zeros too."""
+    Hkv, d, n = 4, 128, 600
+    c = Cache8(1, 10, Hkv, d, 211)
+    rng = np.random.default_rng(212)
+    k = rng.standard_normal((n, Hkv, d // 32, 32)) * 2.0 ** rng.integers(-70, 1, (n, Hkv, d // 32, 1))
+    v = rng.standard_normal((n, Hkv, d // 32, 32)) * 2.0 ** rng.choice([-70, -58, -57, -56, 0, 1, 57, 60], (n, Hkv, d // 32, 1))
+    v[::7, :, 1] = 0
+    c.put(0, np.arange(n), k.reshape(n, Hkv, d), v.reshape(n, Hkv, d))
+    (rows, first), = runs
+    q = rng.standard_normal((rows, 64, d)).astype(np.float32)
+    qd, q64 = _rows(torch, q.reshape(rows, -1), dtype)
+    got = _host(_prefill(torch, L, c, qd, runs, 64, ALL, 2, 600)).reshape(rows, 64, d)
+    for t in range(0, rows, 13):
+        want, t32, tbf = W.attend(c, 0, first + t, q64[t].reshape(64, d), ALL, 2)
+        assert np.all(np.abs(got[t] - want) <= (t32 if dtype == "f32" else tbf)), t
+
+
 def test_prefill_rows_behind_the_last_prompt(torch, L):
     """Rows past row_starts[-1] keep what they hold."""
     c, _ = _prefill_cache([(20, 0)], 64, 2, 64, ALL, 0, 181)
