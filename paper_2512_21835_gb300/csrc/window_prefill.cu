@@ -206,6 +206,16 @@ __device__ __forceinline__ bool bar_try(uint32_t b, uint32_t parity) {
         : "memory");
     return ok != 0;
 }
+// The same, without a wait.
+__device__ __forceinline__ bool bar_test(uint32_t b, uint32_t parity) {
+    uint32_t ok;
+    asm volatile(
+        "{\n .reg .pred p;\n mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}\n"
+        : "=r"(ok)
+        : "r"(b), "r"(parity)
+        : "memory");
+    return ok != 0;
+}
 // A thread's waits.  One that runs out (2 s), or the flag of another thread's that did,
 // ends all further ones: the thread goes on to its end with whatever it finds, within
 // its own buffers.  (No way out in between: a warp stays together, and the code of a wait is
@@ -764,15 +774,18 @@ __global__ void __launch_bounds__(Cfg<D, NP, QT, SRC>::THREADS, 1) window_prefil
             const int steps = n + C::AHEAD;
             wait(bar_q, 0, 2);
             if constexpr (C::PIPE) {
+                // (An answer of a barrier takes 150 cycles, and the queue of the tensor core is two MMAs deep: the
+                // next step's barriers are asked for between the MMAs of this one.)
                 uint32_t made = 0;  // tiles of S
+                bool full = false, p_full = false;
 #pragma unroll 1
                 for (int i = 0; i < steps; ++i) {
                     const uint32_t k_at = use.slot * (C::SLOT / 16);
-                    wait(bar_full + 8 * use.bar, use.phase, 3);
+                    if (!full) wait(bar_full + 8 * use.bar, use.phase, 3);
                     fence_loaded();
                     if (mine(i - C::AHEAD)) {  // O += P V
                         const uint32_t buf = done & 1;
-                        wait(bar_p + 16 * w + 8 * buf, done / 2 & 1, 5);
+                        if (!p_full) wait(bar_p + 16 * w + 8 * buf, done / 2 & 1, 5);
                         fence_after();
 #pragma unroll
                         for (int x = 0; x < 2; ++x)
@@ -781,16 +794,22 @@ __global__ void __launch_bounds__(Cfg<D, NP, QT, SRC>::THREADS, 1) window_prefil
                         commit(bar_pv + 16 * w + 8 * buf);
                         ++done;
                     }
+                    const uint32_t empty = bar_empty + 8 * use.bar;
+                    use.template next<C::SLOTS, C::CYCLE>();
+                    full = i + 1 < steps && bar_test(bar_full + 8 * use.bar, use.phase);
                     if (mine(i)) {  // S = Q K^T, over the P that the product before this one has read
                         const uint32_t buf = made++ & 1;
 #pragma unroll
-                        for (int x = 0; x < D / 64; ++x)
+                        for (int x = 0; x < D / 64; ++x) {
+                            if (x == D / 64 - 1) p_full = bar_test(bar_p + 16 * w + 8 * (done & 1), done / 2 & 1);
                             mma_ss4(tmem + C::s_col(w) + 64 * buf, q_desc + x * C::Q_SLAB / 16,
                                     k_desc + k_at + x * C::KV_SLAB / 16, idesc(KT, false), x != 0);
+                        }
                         commit(bar_s + 16 * w + 8 * buf);
+                    } else {
+                        p_full = false;
                     }
-                    commit(bar_empty + 8 * use.bar);
-                    use.template next<C::SLOTS, C::CYCLE>();
+                    commit(empty);
                 }
             } else {
             if (QT == 2 || w < steps) wait(bar_full + 8 * use.bar, use.phase, 3);
