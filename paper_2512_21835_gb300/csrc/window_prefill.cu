@@ -1377,8 +1377,8 @@ __global__ void __launch_bounds__(Cfg<D, NP, QT, SRC>::THREADS, 1) window_prefil
 }
 
 // Images of the pages that some row of a prompt sees, a block per page and kv head: codes to bf16 times
-// 2^-kShift, as the tiles lie in shared memory, so that a plain copy fetches them.  Worth it where many row
-// tiles meet a page (images_of): the loaders' conversions cost a row tile more than its products do.
+// 2^-kShift, as the tiles lie in shared memory, so that a plain copy fetches them (made where enough row
+// tiles meet a page, least_reuse).
 // What no row of the prompt sees is zero.  Values of NaN, and extreme exponents, flag the page.
 template <int D>
 __global__ void __launch_bounds__(256) window_image_kernel(const __grid_constant__ PrefillArgs p) {
@@ -1560,11 +1560,15 @@ Plan make_plan(bool q8, int M, int n_prompts, int Hq, int Hkv, int window, int s
 
 bool two_tiles(int64_t tiles) { return tiles >= 2 * kSms; }
 
-// Images of the pages that the prompts see: how many each has room for, and bytes of all (with their
-// flags), or 0 where the loaders of the row tiles do better: where a page meets few row tiles
-// (`rows` of a prompt at most), or the images take more than kMostImages.
-constexpr int64_t kImageReuse = 8;
+// Images of the pages that the prompts see: room for each prompt's pages, and bytes of all with their
+// flags.  They are made where a page meets enough row tiles, and take kMostImages at most (else the
+// row tiles' loaders convert).  With images and without, us, by the row tiles that meet a page:
+//   fp32 rows                 1.5: 20.5 17.3   2: 35 41   4: 50 70   8: 68 108   16: 106 197
+//   bf16, one tile a block    2.5: 44.7 44.7   4: 29 32   8: 38 46   16: 46 68
+//   bf16, two                 5.6: 178 160     8: 59 56   12: 73 72  20: 127 135  32: 83 134  256: 1050 1364
 constexpr int64_t kMostImages = 1ll << 30;
+constexpr int64_t kLeastReuse = 2;
+int64_t least_reuse(bool f32, int64_t tiles) { return f32 ? kLeastReuse : two_tiles(tiles) ? 12 : 4; }
 struct Images {
     int pages;
     int64_t tiles, bytes;
@@ -1598,12 +1602,13 @@ cudaError_t launch_t(const PrefillArgs& p, cudaStream_t st) {
 template <int D, Source SRC>
 cudaError_t launch_d(const PrefillArgs& p, bool f32, int64_t tiles, cudaStream_t st) {
     if constexpr (SRC != kBf16) {
-        // (bf16 rows with one row tile per block have no form for images: few row tiles, images_of)
         if (p.images) {
             const cudaError_t e = launch_pdl(window_image_kernel<D>, dim3((unsigned)(p.a.n_prompts * (int64_t)p.image_pages), p.a.Hkv),
                                              256, 0, st, p);
             if (e != cudaSuccess) return e;
-            return f32 ? launch_t<D, 3, 1, kImages, float>(p, st) : launch_t<D, 1, 2, kImages, __nv_bfloat16>(p, st);
+            return f32                ? launch_t<D, 3, 1, kImages, float>(p, st)
+                   : two_tiles(tiles) ? launch_t<D, 1, 2, kImages, __nv_bfloat16>(p, st)
+                                      : launch_t<D, 1, 1, kImages, __nv_bfloat16>(p, st);
         }
     }
     if (f32) return launch_t<D, 3, 1, SRC, float>(p, st);
@@ -1620,7 +1625,7 @@ static uint64_t scratch_of(bool q8, int M, int n_prompts, int Hq, int Hkv, int d
     const Plan p = make_plan(q8, M, n_prompts, Hq, Hkv, window, sinks, max_ctx);
     const int64_t most = most_parts(q8, visible_pages(p.tok, window, sinks, max_ctx));  // parts of a row tile
     // (a smaller call may have all its rows in one prompt)
-    const uint64_t images = q8 && image_reuse(M, p.heads, window) >= kImageReuse
+    const uint64_t images = q8 && image_reuse(M, p.heads, window) >= kLeastReuse
                                 ? (std::min(images_of(M, n_prompts, p.heads, Hkv, d, window, sinks, max_ctx).bytes, kMostImages) + 31) / 16 * 16
                                 : 0;
     if (most < 2) return images ? kCounterBytes + images : 16;
@@ -1653,8 +1658,7 @@ cudaError_t launch_any(const WindowArgs& a, bool f32, cudaStream_t st) {
     p.rows = reinterpret_cast<int4*>(p.part + plan.tiles * plan.splits * 128 * (a.d / 4));
     p.ml = reinterpret_cast<float2*>(p.rows + plan.tiles);
     p.ended = reinterpret_cast<unsigned*>(p.ml + plan.tiles * plan.splits * 128);
-    if (SRC != kBf16 && (f32 || two_tiles(plan.tiles)) &&
-        image_reuse(a.rows / a.n_prompts, plan.heads, a.window) >= kImageReuse) {
+    if (SRC != kBf16 && image_reuse(a.rows / a.n_prompts, plan.heads, a.window) >= least_reuse(f32, plan.tiles)) {
         const Images m = images_of(a.rows, a.n_prompts, plan.heads, a.Hkv, a.d, a.window, a.sinks, a.max_ctx);
         if (m.bytes <= kMostImages && a.n_prompts * (int64_t)m.pages <= 0x7fffffff) {
             // (of the scratch's end, which the parts do not reach)
