@@ -59,6 +59,14 @@ __device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uin
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
+// The same onto zero.
+__device__ __forceinline__ void mma_first(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
+                                          uint32_t b1) {
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
+}
 // 8 x 8 transpose over the warp: lane 4 n + c gives elements (n, 2 c), (n, 2 c + 1) and
 // gets (2 c, n), (2 c + 1, n).
 __device__ __forceinline__ uint32_t transpose(uint32_t x) {
@@ -164,13 +172,17 @@ __device__ __forceinline__ void soften(const float (&s)[4], bool see0, bool see1
 template <bool F32, int PV>
 __device__ __forceinline__ void add_values(float (&o)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
                                            const uint32_t (&pb)[PV][2]) {
-    float y[4];
+    if constexpr (F32) {
+        float y[4];
+        mma_first(y, a0, a1, a2, a3, pb[PV - 1][0], pb[PV - 1][1]);
 #pragma unroll
-    for (int h = 0; h < 4; ++h) y[h] = F32 ? 0.f : o[h];
+        for (int pl = PV - 2; pl >= 0; --pl) mma(y, a0, a1, a2, a3, pb[pl][0], pb[pl][1]);
 #pragma unroll
-    for (int pl = PV - 1; pl >= 0; --pl) mma(y, a0, a1, a2, a3, pb[pl][0], pb[pl][1]);
+        for (int h = 0; h < 4; ++h) o[h] += y[h];
+    } else {
 #pragma unroll
-    for (int h = 0; h < 4; ++h) o[h] = F32 ? o[h] + y[h] : y[h];
+        for (int pl = PV - 1; pl >= 0; --pl) mma(o, a0, a1, a2, a3, pb[pl][0], pb[pl][1]);
+    }
 }
 
 // What the warps of a block share at the end: maxima, sums, and where their O lie ([8][D], a
@@ -183,7 +195,7 @@ struct Shared {
 // The end of a unit, or of a part of it: sums of the block's warps, and of the unit's `active` blocks
 // in the last one to arrive.  head: the first of the group's `heads` query heads; slot: where this
 // block's part goes; slot_of(x): where the unit's part x is.
-template <int D, typename T, typename SlotOf>
+template <int D, bool Q8, typename T, typename SlotOf>
 __device__ __forceinline__ void join(const DecodeArgs& p, Shared& sh, const float* sm_o, int pitch, const float (&m)[2],
                                      float (&l)[2], int b, int head, int heads, int active, unsigned* counter, int64_t slot,
                                      SlotOf&& slot_of) {
@@ -237,37 +249,60 @@ __device__ __forceinline__ void join(const DecodeArgs& p, Shared& sh, const floa
     __syncthreads();
     if (!sh.last) return;
     __threadfence();
-    for (int u = threadIdx.x; u < units; u += kThreads) {
-        const int h = u / (D / 4);
-        float mt = -INFINITY, lt = 0.f;
-        float4 r = make_float4(0.f, 0.f, 0.f, 0.f);
-        constexpr int BATCH = 12;  // parts whose loads are in flight together
-        for (int x0 = 0; x0 < active; x0 += BATCH) {
-            float2 ml[BATCH];
-            float4 y[BATCH];
+    // `N` units at a time, so many parts' loads in flight together.
+    auto gather = [&](auto n_units, auto n_parts) {
+        constexpr int N = decltype(n_units)::value, BATCH = decltype(n_parts)::value;
+        for (int u0 = threadIdx.x; u0 < units; u0 += N * kThreads) {
+            float mt[N], lt[N];
+            float4 r[N];
 #pragma unroll
-            for (int x = 0; x < BATCH; ++x) {
-                const int64_t at = slot_of(min(x0 + x, active - 1)) * p.plan.heads + h;
-                ml[x] = __ldcg(p.ml + at);
-                y[x] = __ldcg(reinterpret_cast<const float4*>(p.part + at * D) + u % (D / 4));
+            for (int k = 0; k < N; ++k) {
+                mt[k] = -INFINITY;
+                lt[k] = 0.f;
+                r[k] = make_float4(0.f, 0.f, 0.f, 0.f);
             }
-            float mb = mt;
+            for (int x0 = 0; x0 < active; x0 += BATCH) {
+                float2 ml[N][BATCH];
+                float4 y[N][BATCH];
 #pragma unroll
-            for (int x = 0; x < BATCH; ++x) mb = fmaxf(mb, ml[x].x);
-            const float keep = mt == -INFINITY ? 0.f : exp2f(mt - mb);
-            mt = mb;
-            lt *= keep;
-            r.x *= keep; r.y *= keep; r.z *= keep; r.w *= keep;
+                for (int x = 0; x < BATCH; ++x) {
+                    const int64_t first = slot_of(min(x0 + x, active - 1)) * p.plan.heads;
 #pragma unroll
-            for (int x = 0; x < BATCH; ++x) {
-                const float f = x0 + x < active && ml[x].x != -INFINITY ? exp2f(ml[x].x - mt) : 0.f;
-                lt = fmaf(f, ml[x].y, lt);
-                r.x = fmaf(f, y[x].x, r.x); r.y = fmaf(f, y[x].y, r.y);
-                r.z = fmaf(f, y[x].z, r.z); r.w = fmaf(f, y[x].w, r.w);
+                    for (int k = 0; k < N; ++k) {
+                        const int u = min(u0 + k * kThreads, units - 1);
+                        const int64_t at = first + u / (D / 4);
+                        ml[k][x] = __ldcg(p.ml + at);
+                        y[k][x] = __ldcg(reinterpret_cast<const float4*>(p.part + at * D) + u % (D / 4));
+                    }
+                }
+#pragma unroll
+                for (int k = 0; k < N; ++k) {
+                    float mb = mt[k];
+#pragma unroll
+                    for (int x = 0; x < BATCH; ++x) mb = fmaxf(mb, ml[k][x].x);
+                    const float keep = mt[k] == -INFINITY ? 0.f : exp2f(mt[k] - mb);
+                    mt[k] = mb;
+                    lt[k] *= keep;
+                    r[k].x *= keep; r[k].y *= keep; r[k].z *= keep; r[k].w *= keep;
+#pragma unroll
+                    for (int x = 0; x < BATCH; ++x) {
+                        const float f = x0 + x < active && ml[k][x].x != -INFINITY ? exp2f(ml[k][x].x - mt[k]) : 0.f;
+                        lt[k] = fmaf(f, ml[k][x].y, lt[k]);
+                        r[k].x = fmaf(f, y[k][x].x, r[k].x); r[k].y = fmaf(f, y[k][x].y, r[k].y);
+                        r[k].z = fmaf(f, y[k][x].z, r[k].z); r[k].w = fmaf(f, y[k][x].w, r[k].w);
+                    }
+                }
             }
+#pragma unroll
+            for (int k = 0; k < N; ++k)
+                if (u0 + k * kThreads < units) put(u0 + k * kThreads, r[k], lt[k] == 0.f ? 0.f : 1.0f / lt[k]);
         }
-        put(u, r, lt == 0.f ? 0.f : 1.0f / lt);
-    }
+    };
+    using std::integral_constant;
+    if (Q8 && units > kThreads)
+        gather(integral_constant<int, 2>{}, integral_constant<int, 9>{});
+    else
+        gather(integral_constant<int, 1>{}, integral_constant<int, 12>{});
 }
 
 // Queries into shared memory, the same for every warp: bf16 planes in the MMA's B layout, of which a
@@ -420,7 +455,7 @@ __global__ void __launch_bounds__(kThreads, kResident) window_decode_kernel(cons
                     o[4 * x + e][h], o[4 * x + e][2 + h], o[4 * x + e + 1][h], o[4 * x + e + 1][2 + h]);
     }
     const int64_t unit = (int64_t)b * gridDim.y + blockIdx.y, part0 = unit * p.plan.splits;
-    join<D, T>(p, sh, &sm_o[0][0][0], 8 * D, m, l, b, kvh * G + head0, heads, active, p.counters + unit, part0 + split,
+    join<D, false, T>(p, sh, &sm_o[0][0][0], 8 * D, m, l, b, kvh * G + head0, heads, active, p.counters + unit, part0 + split,
                [&](int x) { return part0 + x; });
 }
 
@@ -618,10 +653,6 @@ __global__ void __launch_bounds__(kThreads, kResident8) window_decode_q8_kernel(
                     constexpr int SUMS = F32 ? 1 : 2;
                     float z[PL][SUMS][4];
 #pragma unroll
-                    for (int pl = 0; pl < PL; ++pl)
-#pragma unroll
-                        for (int h = 0; h < SUMS; ++h) z[pl][h][0] = z[pl][h][1] = z[pl][h][2] = z[pl][h][3] = 0.f;
-#pragma unroll
                     for (int x = 0; x < 4 * NK; ++x) {
                         uint32_t A[2][2];
 #pragma unroll
@@ -632,7 +663,10 @@ __global__ void __launch_bounds__(kThreads, kResident8) window_decode_q8_kernel(
 #pragma unroll
                         for (int pl = 0; pl < PL; ++pl) {
                             const uint4 q = sm_q[x / 2][pl][lane];
-                            mma(z[pl][x % SUMS], A[0][0], A[1][0], A[0][1], A[1][1], x % 2 ? q.z : q.x, x % 2 ? q.w : q.y);
+                            if (x < SUMS)
+                                mma_first(z[pl][x], A[0][0], A[1][0], A[0][1], A[1][1], x % 2 ? q.z : q.x, x % 2 ? q.w : q.y);
+                            else
+                                mma(z[pl][x % SUMS], A[0][0], A[1][0], A[0][1], A[1][1], x % 2 ? q.z : q.x, x % 2 ? q.w : q.y);
                         }
                     }
 #pragma unroll
@@ -693,7 +727,7 @@ __global__ void __launch_bounds__(kThreads, kResident8) window_decode_q8_kernel(
         // A block's part of a unit that began in an earlier block is its first, of one that ends in a
         // later block its second; a unit's counter is that of the block where it begins.
         const int64_t from = unit_at / share, active = (unit_at + steps - 1) / share - from + 1;
-        join<D, T>(p, sh, reinterpret_cast<const float*>(ring), kStages * Gr::BYTES / 4, m, l, b, kvh * G + head0, heads,
+        join<D, true, T>(p, sh, reinterpret_cast<const float*>(ring), kStages * Gr::BYTES / 4, m, l, b, kvh * G + head0, heads,
                    (int)active, p.counters + from, 2 * (int64_t)blockIdx.x + (from == blockIdx.x),
                    [&](int x) { return 2 * (from + x) + (x == 0); });
         unit_at += steps;
