@@ -196,6 +196,56 @@ def run_window(iters):
               f"status {L.loip_k_attention_tc_status()}")
 
 
+def run_cache_q8(iters):
+    """The 8-bit cache: append and reading back, one-token attention and prompt attention over all of it."""
+    P, Hq, Hkv, d = 64, 64, 8, 128
+    lpb, held = L.loip_k_cache_q8_layer_bytes(Hkv, d), 2 * Hkv * d * 33 // 32
+
+    def ints(v):
+        return torch.tensor(list(v), dtype=torch.int32, device="cuda")
+
+    def cache(R, ctx):
+        """Filled by the append."""
+        pages = -(-ctx // P)
+        kv = torch.empty(R * pages * lpb, dtype=torch.uint8, device="cuda")
+        pt = (torch.randperm(R * pages, device="cuda") * lpb).view(R, pages)
+        x = torch.randn(ctx, (Hq + 2 * Hkv) * d, device="cuda").bfloat16()
+        q, pos = torch.empty(ctx, Hq * d, dtype=torch.bfloat16, device="cuda"), ints(range(ctx))
+        for r in range(R):
+            L.loip_k_qk_append_q8(x, None, None, Hq, Hkv, d, 0.0, 5e5, pos, ints([r] * ctx), q, kv, pt, pages, P, 0, lpb)
+        return kv, pt, pages
+
+    for T, dt in ((1, torch.float32), (2048, torch.bfloat16), (8192, torch.float32)):
+        kv, pt, pages = cache(1, T)
+        x = torch.randn(T, (Hq + 2 * Hkv) * d, device="cuda").to(dt)
+        q, pos, req = torch.empty(T, Hq * d, dtype=dt, device="cuda"), ints(range(T)), ints([0] * T)
+        t = _time(lambda i: L.loip_k_qk_append_q8(x, None, None, Hq, Hkv, d, 0.0, 5e5, pos, req, q, kv, pt, pages, P, 0,
+                                                  lpb), iters)
+        by = x.numel() * x.element_size() + q.numel() * q.element_size() + T * held
+        print(f"8-bit append {T} {dt} rows: {t * 1e6:9.1f} us  {by / t / 1e9:8.1f} GB/s")
+        out = torch.empty(T, 2 * Hkv * d, dtype=dt, device="cuda")
+        t = _time(lambda i: L.loip_k_cache_read_q8(kv, pt, pages, pos, req, Hkv, d, P, 0, lpb, out), iters)
+        print(f"8-bit read {T} {dt} rows: {t * 1e6:9.1f} us  {(T * held + out.nbytes) / t / 1e9:8.1f} GB/s")
+    for B, ctx, dt in ((1, 1088, torch.float32), (8, 4352, torch.float32), (64, 8192, torch.bfloat16)):
+        kv, pt, pages = cache(B, ctx)
+        q, n = torch.randn(B, Hq * d, device="cuda").to(dt), ints([ctx] * B)
+        o, args = torch.empty_like(q), (Hq, Hkv, d, P, 0, lpb, ctx, 0, ctx)
+        sc = torch.zeros(L.loip_k_window_attention_q8_scratch_bytes(B, Hq, Hkv, d, ctx, 0, ctx), dtype=torch.uint8,
+                         device="cuda")
+        t = _time(lambda i: L.loip_k_window_attention_q8(q, kv, pt, pages, n, *args, sc, o), iters)
+        print(f"8-bit attention {B} x {ctx}, {dt}: {t * 1e6:9.1f} us  {B * ctx * held / t / 1e9:8.1f} GB/s")
+    for n, rows, dt in ((4, 512, torch.float32), (1, 8192, torch.bfloat16)):
+        kv, pt, pages = cache(n, rows)
+        q, o = torch.randn(n * rows, Hq * d, device="cuda").to(dt), torch.empty(n * rows, Hq * d, dtype=dt, device="cuda")
+        starts, args = ints(range(0, n * rows + 1, rows)), (Hq, Hkv, d, P, 0, lpb, rows, 0, rows)
+        sc = torch.zeros(L.loip_k_window_prefill_q8_scratch_bytes(n * rows, n, Hq, Hkv, d, rows, 0, rows),
+                         dtype=torch.uint8, device="cuda")
+        t = _time(lambda i: L.loip_k_window_prefill_q8(q, kv, pt, pages, starts, None, *args, sc, o), iters)
+        fl = 2 * n * Hq * d * rows * (rows + 1)
+        print(f"8-bit prefill {n} x {rows}, {dt}: {t * 1e6:9.1f} us  {fl / t / 1e12:7.1f} TFLOP/s  "
+              f"status {L.loip_k_attention_tc_status()}")
+
+
 def main():
     ap = argparse.ArgumentParser()
     ap.add_argument("--only", default="")
@@ -215,6 +265,8 @@ def main():
         run_attn_tc(max(3, min(a.iters, 10)))
     if a.only in ("", "window"):
         run_window(max(3, min(a.iters, 10)))
+    if a.only in ("", "cache_q8"):
+        run_cache_q8(max(3, min(a.iters, 10)))
 
 
 if __name__ == "__main__":

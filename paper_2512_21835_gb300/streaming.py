@@ -2,13 +2,16 @@
 
     python -m paper_2512_21835_gb300.streaming [--model tiny] [--prompt N] [--new N]
                                                [--window N] [--sinks N] [--chunk N] [--batch N]
+                                               [--cache bf16|q8]
 
 A cache behind a sliding window with sinks stops growing, so its pages can be
 recycled instead of pushing weights off the device as a growing cache does.  Each
 layer appends its new tokens (loip_k_qk_append) and attends behind the window:
 prompts in chunks (loip_k_window_prefill), then one token per request and step
 (loip_k_window_attention).  A page that holds neither sinks nor positions that a later
-token sees goes back to the pool; its page-table entry is not read again.
+token sees goes back to the pool; its page-table entry is not read again.  With
+cache="q8" the cache holds 8 bits per element (loip_k_qk_append_q8 and the attentions
+of that name), in 33/64 of the memory.
 
 Weights are resident and generated (the shapes of configs.MODELS); up to 8 requests.
 """
@@ -69,12 +72,17 @@ class WindowedDecoder:
     """Greedy decoding of a resident model behind a sliding window with sinks."""
 
     def __init__(self, model: dict, batch: int, window: int, sinks: int, max_ctx: int, chunk: int = 256,
-                 n_pages: int | None = None, seed: int = configs.WEIGHT_SEED):
+                 n_pages: int | None = None, seed: int = configs.WEIGHT_SEED, cache: str = "bf16"):
         import torch
 
         from . import build, loip
         build.build()
         self.torch, self.L = torch, loip
+        if cache not in ("bf16", "q8"):
+            raise ValueError(f"the cache is bf16 or q8, not {cache}")
+        kind = "_q8" if cache == "q8" else ""
+        self.append, self.attend, self.attend_chunk = (
+            getattr(loip, f + kind) for f in ("loip_k_qk_append", "loip_k_window_attention", "loip_k_window_prefill"))
         m = self.m = dict(model)
         self.window, self.sinks, self.max_ctx, self.chunk = window, sinks, max_ctx, chunk
         H, F, d = m["hidden"], m["ffn"], m["head_dim"]
@@ -97,15 +105,16 @@ class WindowedDecoder:
                 w.update(g_q=gen((d,), t + 9, 1), g_k=gen((d,), t + 10, 1))
             self.layers.append(w)
         # a page holds every layer's keys and values of 64 tokens
-        self.layer_page_bytes = 2 * m["n_kv_heads"] * PAGE * d * 2
+        self.layer_page_bytes = (loip.loip_k_cache_q8_layer_bytes(m["n_kv_heads"], d) if cache == "q8"
+                                 else 2 * m["n_kv_heads"] * PAGE * d * 2)
         page_bytes = m["n_layers"] * self.layer_page_bytes
         if n_pages is None:
             n_pages = batch * pages_of_a_request(window, sinks, max_ctx, chunk)
         self.pool = PagePool(n_pages, batch, max_ctx, page_bytes)
         self.kv = torch.empty(n_pages * page_bytes, dtype=torch.uint8, device="cuda")
         heads = (m["n_heads"], m["n_kv_heads"], d, window, sinks, max_ctx)
-        need = max(loip.loip_k_window_attention_scratch_bytes(batch, *heads),
-                   loip.loip_k_window_prefill_scratch_bytes(chunk, 1, *heads))
+        need = max(getattr(loip, f"loip_k_window_attention{kind}_scratch_bytes")(batch, *heads),
+                   getattr(loip, f"loip_k_window_prefill{kind}_scratch_bytes")(chunk, 1, *heads))
         self.scratch = torch.zeros(need, dtype=torch.uint8, device="cuda")
         self.pos = [0] * batch
 
@@ -149,14 +158,14 @@ class WindowedDecoder:
         for l, w in enumerate(self.layers):
             qkv = torch.zeros(T, self.qd + 2 * self.kvd, device="cuda")
             self._product(self._norm(x, w["g_attn"]), w["wqkv"], qkv)
-            L.loip_k_qk_append(qkv, w["g_q"], w["g_k"], Hq, Hkv, d, eps, m["rope_theta"], positions, row_req, q, self.kv,
-                               table, self.pool.max_pages, PAGE, l, self.layer_page_bytes)
+            self.append(qkv, w["g_q"], w["g_k"], Hq, Hkv, d, eps, m["rope_theta"], positions, row_req, q, self.kv, table,
+                        self.pool.max_pages, PAGE, l, self.layer_page_bytes)
             if single:
-                L.loip_k_window_attention(q, self.kv, table_rows, self.pool.max_pages, ctx, Hq, Hkv, d, PAGE, l,
-                                          self.layer_page_bytes, self.window, self.sinks, self.max_ctx, self.scratch, o)
+                self.attend(q, self.kv, table_rows, self.pool.max_pages, ctx, Hq, Hkv, d, PAGE, l,
+                            self.layer_page_bytes, self.window, self.sinks, self.max_ctx, self.scratch, o)
             else:
-                L.loip_k_window_prefill(q, self.kv, table_rows, self.pool.max_pages, starts, first, Hq, Hkv, d, PAGE, l,
-                                        self.layer_page_bytes, self.window, self.sinks, self.max_ctx, self.scratch, o)
+                self.attend_chunk(q, self.kv, table_rows, self.pool.max_pages, starts, first, Hq, Hkv, d, PAGE, l,
+                                  self.layer_page_bytes, self.window, self.sinks, self.max_ctx, self.scratch, o)
             self._product(o, w["wo"], x)
             if T <= 8:
                 a = torch.empty(T, F, device="cuda")
@@ -237,12 +246,13 @@ def main():
     ap.add_argument("--window", type=int, default=256)
     ap.add_argument("--sinks", type=int, default=4)
     ap.add_argument("--chunk", type=int, default=128)
+    ap.add_argument("--cache", default="bf16", choices=["bf16", "q8"])
     a = ap.parse_args()
     import torch
 
     from . import inputs
     m = configs.MODELS[a.model]
-    dec = WindowedDecoder(m, a.batch, a.window, a.sinks, a.prompt + a.new, a.chunk)
+    dec = WindowedDecoder(m, a.batch, a.window, a.sinks, a.prompt + a.new, a.chunk, cache=a.cache)
     last = [int(dec.prefill(r, p)[2][0]) for r, p in
             enumerate(inputs.prompts(configs.PROMPT_SEED, a.batch, a.prompt, m["vocab"]))]
     torch.cuda.synchronize()
@@ -252,7 +262,8 @@ def main():
     dt = time.perf_counter() - t0
     full = a.batch * -(-(a.prompt + a.new) // PAGE)
     print(f"{a.model}: {a.batch} x ({a.prompt} + {a.new}) tokens behind a window of {a.window} with {a.sinks} sinks: "
-          f"{a.new * a.batch / dt:.1f} tokens/s, {dec.pool.most} pages held at most (without a window: {full})")
+          f"{a.new * a.batch / dt:.1f} tokens/s, {dec.pool.most} pages of {dec.pool.page_bytes} bytes held at most "
+          f"(without a window: {full})")
 
 
 if __name__ == "__main__":
