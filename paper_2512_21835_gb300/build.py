@@ -5,10 +5,12 @@ import concurrent.futures as cf
 import os
 import shutil
 import subprocess
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 OUT = os.path.join(HERE, "libloip.so")
+CALLS = os.path.join(HERE, "_calls.so")  # the extension module of csrc/calls.c
 BUILD = os.path.join(HERE, "_build")
 SOURCES = ["decode.cu", "prefill.cu", "gemm_tc.cu", "attn_tc.cu", "pack.cu", "runtime.cu", "plan.cpp", "hostpool.cpp", "noalloc.cu",
            "disktier.cpp", "window.cu", "window_decode.cu", "window_prefill.cu"]
@@ -23,7 +25,7 @@ def _nvcc() -> str:
 
 
 def _stale() -> bool:
-    if not os.path.exists(OUT):
+    if not (os.path.exists(OUT) and os.path.exists(CALLS)):
         return True
     t = os.path.getmtime(OUT)
     deps = [os.path.join(CSRC, f) for f in os.listdir(CSRC)] + [os.path.join(HERE, "..", "include", "loip.h")]
@@ -55,6 +57,13 @@ def build(force: bool = False, verbose: bool = False) -> str:
     if r.returncode != 0:
         raise RuntimeError(f"link failed:\n{r.stdout}\n{r.stderr}")
     os.replace(tmp, OUT)
+    tmp = CALLS + ".tmp"
+    cmd = ["gcc", "-O2", "-shared", "-fPIC", "-I", sysconfig.get_paths()["include"], os.path.join(CSRC, "calls.c"), "-o", tmp,
+           "-L", HERE, "-l:" + os.path.basename(OUT), "-Wl,-rpath,$ORIGIN", "-Wl,--allow-shlib-undefined"]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"gcc failed on calls.c:\n{r.stdout}\n{r.stderr}")
+    os.replace(tmp, CALLS)
     return OUT
 
 

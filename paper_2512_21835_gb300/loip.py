@@ -149,6 +149,11 @@ def lib():
             f = getattr(L, name)
             f.restype = res
             f.argtypes = args
+        # the windowed-serving entries, called without ctypes' conversions (csrc/calls.c)
+        from . import _calls
+        for name in dir(_calls):
+            if name.startswith("loip_k_"):
+                setattr(L, name, getattr(_calls, name))
         _lib = L
     return _lib
 

@@ -229,3 +229,27 @@ def test_arguments_are_those_of_the_bf16_calls():
         other = name.replace("_scratch_bytes", "") + "_q8" + ("_scratch_bytes" if name.endswith("_scratch_bytes") else "")
         assert loip._SIGS[name] == loip._SIGS[other]
     assert loip.loip_k_cache_q8_layer_bytes(8, 128) == 8 * 132 * 128
+
+
+def test_entries_without_ctypes(L):
+    """The extension module's functions take what the ctypes ones take, and no other number of arguments."""
+    import ctypes as C
+
+    from paper_2512_21835_gb300 import _calls
+    names = [n for n in dir(_calls) if n.startswith("loip_k_")]
+    assert len(names) == 7
+    for name in names:
+        sig = loip._SIGS[name][1]
+        assert getattr(L, name) is getattr(_calls, name)
+        zero = [0.0 if t is C.c_float else None if t is C.c_void_p else 0 for t in sig]
+        assert getattr(L, name)(*zero) == loip.ERR_INVALID and L.loip_last_error(None)
+        assert getattr(L, name)(*[C.c_void_p() if t is C.c_void_p else z for t, z in zip(sig, zero)]) == loip.ERR_INVALID
+        for wrong in (zero[1:], zero + [0]):
+            with pytest.raises(TypeError, match=f"takes {len(sig)} arguments"):
+                getattr(L, name)(*wrong)
+        for i, t in enumerate(sig):
+            for bad, error in (("x", (TypeError, AttributeError)), (1 << 70, OverflowError)):
+                if t is C.c_float and bad != "x":
+                    continue
+                with pytest.raises(error):
+                    getattr(L, name)(*zero[:i], bad, *zero[i + 1:])
