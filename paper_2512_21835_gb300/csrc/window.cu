@@ -114,7 +114,6 @@ template <int D, typename T, bool Q8>
 __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 8 : 6) qk_append_kernel(const __grid_constant__ AppendArgs p) {
     constexpr int LANES = D / 16;
     __shared__ float4 turn[4][LANES];  // cos, sin of elements 8l + 2k and 8l + 2k + 1 at [k][l]: no bank conflicts
-    pdl_trigger();
     pdl_wait();
     const int t = blockIdx.x, l = threadIdx.x % LANES, head = blockIdx.y * p.heads + threadIdx.x / LANES;
     const bool live = head < min(p.Hq + 2 * p.Hkv, (int)(blockIdx.y + 1) * p.heads);
@@ -142,6 +141,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 8 : 6) qk_append_kernel(
         reinterpret_cast<float2*>(&turn[threadIdx.x % 8 / 2][threadIdx.x / 8])[threadIdx.x % 2] = make_float2(c, s);
     }
     __syncthreads();
+    pdl_trigger();
     float a[8], b[8];
     if (live) {
         ra.values(a);
@@ -259,7 +259,6 @@ __device__ __forceinline__ void store32(void* p, const uint32_t (&u)[8]) {
 template <int D, typename T, int R>
 __global__ void __launch_bounds__(256) cache_read_kernel(const __grid_constant__ ReadArgs p, int per_block) {
     using G = q8::Granule<D>;
-    pdl_trigger();
     pdl_wait();
     const int pieces = p.Hkv * G::PIECES, row = threadIdx.x / pieces, i = blockIdx.y * 256 + threadIdx.x - row * pieces;
     if (row >= per_block || i >= pieces) return;
@@ -293,6 +292,7 @@ __global__ void __launch_bounds__(256) cache_read_kernel(const __grid_constant__
                 E[x][v] = (uint8_t)g[x][G::exponents(v, pos[x] % q8::kGranule) + c / 2];
             }
         }
+    pdl_trigger();
 #pragma unroll
     for (int x = 0; x < R; ++x) {
         const int64_t t = t0 + x * per_block;
