@@ -797,9 +797,11 @@ Plan make_plan(int B, int Hq, int Hkv, int window, int sinks, int max_ctx) {
     return p;
 }
 
-// Steps of a call over the 8-bit cache, at most.
-int64_t most_steps(int B, int Hkv, int groups, int window, int sinks, int max_ctx) {
-    return (int64_t)B * Hkv * groups * ((visible_tiles(window, sinks, max_ctx) + kWarps - 1) / kWarps);
+// Blocks of a call over the 8-bit cache: no more than it has steps.
+int blocks8(int B, int Hkv, int groups, int window, int sinks, int max_ctx) {
+    const int64_t units = (int64_t)B * Hkv * groups;
+    if (units >= kPlaces8) return kPlaces8;
+    return (int)std::min<int64_t>(kPlaces8, units * ((visible_tiles(window, sinks, max_ctx) + kWarps - 1) / kWarps));
 }
 
 template <int D, typename T>
@@ -807,7 +809,7 @@ cudaError_t launch_t(const DecodeArgs& p, bool q8, cudaStream_t st) {
     const dim3 grid((unsigned)p.a.rows * p.plan.splits, p.a.Hkv * p.plan.groups);
     if (!q8) return launch_pdl(window_decode_kernel<D, T>, grid, kThreads, 0, st, p);
     constexpr int BYTES = kWarps * kStages * q8::Granule<D>::BYTES;
-    const dim3 grid8((unsigned)std::min<int64_t>(kPlaces8, most_steps(p.a.rows, p.a.Hkv, p.plan.groups, p.a.window, p.a.sinks, p.a.max_ctx)));
+    const dim3 grid8(blocks8(p.a.rows, p.a.Hkv, p.plan.groups, p.a.window, p.a.sinks, p.a.max_ctx));
     static std::atomic<uint64_t> ready{0};
     const cudaError_t e = raise_smem_limit(window_decode_q8_kernel<D, T>, BYTES, ready);
     return e != cudaSuccess ? e : launch_pdl(window_decode_q8_kernel<D, T>, grid8, kThreads, BYTES, st, p);
@@ -818,7 +820,7 @@ cudaError_t launch_any(const WindowArgs& a, bool f32, bool q8, cudaStream_t st) 
     p.a = a;
     p.plan = make_plan(a.rows, a.Hq, a.Hkv, a.window, a.sinks, a.max_ctx);
     if ((int64_t)a.rows * p.plan.splits > 0x7fffffff) return cudaErrorInvalidValue;
-    const int64_t parts = q8 ? 2 * std::min<int64_t>(kPlaces8, most_steps(a.rows, a.Hkv, p.plan.groups, a.window, a.sinks, a.max_ctx))
+    const int64_t parts = q8 ? 2 * blocks8(a.rows, a.Hkv, p.plan.groups, a.window, a.sinks, a.max_ctx)
                              : (int64_t)a.rows * a.Hkv * p.plan.groups * p.plan.splits;
     p.counters = static_cast<unsigned*>(a.scratch);
     p.part = reinterpret_cast<float*>(p.counters + kMaxCounters);
@@ -848,7 +850,7 @@ cudaError_t launch_window_decode(const WindowArgs& a, bool f32, cudaStream_t st)
 // Two parts for each block; more blocks for more or longer requests.
 uint64_t window_decode_q8_scratch(int B, int Hq, int Hkv, int d, int window, int sinks, int max_ctx) {
     const Plan p = make_plan(B, Hq, Hkv, window, sinks, max_ctx);
-    const uint64_t blocks = std::min<int64_t>(kPlaces8, most_steps(B, Hkv, p.groups, window, sinks, max_ctx));
+    const uint64_t blocks = blocks8(B, Hkv, p.groups, window, sinks, max_ctx);
     return (kCounterBytes + blocks * 2 * p.heads * (d + 2) * sizeof(float) + 15) / 16 * 16;
 }
 cudaError_t launch_window_decode_q8(const WindowArgs& a, bool f32, cudaStream_t st) { return launch_any(a, f32, true, st); }

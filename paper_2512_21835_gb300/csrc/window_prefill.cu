@@ -1595,7 +1595,7 @@ Images images_of(int M, int n_prompts, int heads, int Hkv, int d, int window, in
     Images m{};
     const int64_t pages = visible_pages(M, window, sinks, max_ctx);
     m.pages = (int)pages;
-    m.tiles = n_prompts * pages * Hkv;
+    m.tiles = std::min(n_prompts * pages, kMostImages) * Hkv;  // (far too many, and no overflow)
     m.bytes = m.tiles * (2 * KT * (int64_t)d * 2 + (int64_t)sizeof(unsigned));
     return m;
 }

@@ -686,18 +686,21 @@ def loip_k_cache_q8_layer_bytes(Hkv, d) -> int:
     return Hkv * 132 * d
 
 
-def _on_current(x):
-    """Refuses rows on another device than the current one, whose stream the call would go to."""
+def _on_current(x, kv_base):
+    """Refuses rows on another device than the current one, whose stream the call would go to, and a cache in
+    host memory, which the prompt kernels' bulk copies do not read."""
     if not _of_torch:
         _torch()
     if x.is_cuda and x.get_device() != _of_torch[1]():
         _refuse(f"rows on device {x.get_device()} in a call on device {_of_torch[1]()}")
+    if not (isinstance(kv_base, int) or kv_base is None or kv_base.is_cuda):
+        _refuse("the 8-bit cache is in device memory")
 
 
 def loip_k_qk_append_q8(qkv, g_q, g_k, Hq, Hkv, d, eps, theta, positions, row_req, q_out, kv_base, page_offsets,
                         max_pages, page_tokens, layer, layer_page_bytes, stream=None):
     """loip_k_qk_append into the 8-bit cache."""
-    _on_current(qkv)
+    _on_current(qkv, kv_base)
     _append(lib().loip_k_qk_append_q8, qkv, g_q, g_k, Hq, Hkv, d, eps, theta, positions, row_req, q_out, kv_base,
             page_offsets, max_pages, page_tokens, layer, layer_page_bytes, stream)
 
@@ -706,7 +709,7 @@ def loip_k_cache_read_q8(kv_base, page_offsets, max_pages, positions, row_req, H
                          layer_page_bytes, out, stream=None):
     """Rows of the 8-bit cache as numbers: out [T, 2 * Hkv * d] float32 or bfloat16 (key heads, value heads) for the
     positions [T] of the requests row_req [T] (None: row t is of request t); page_offsets [requests, max_pages]."""
-    _on_current(out)
+    _on_current(out, kv_base)
     T, dtype, n_req = out.shape[0], _dtype(out, out), page_offsets.shape[0]
     if not out.is_contiguous() or out.numel() != T * 2 * Hkv * d:
         _refuse("out is contiguous [T, 2 * Hkv * d]")
@@ -725,7 +728,7 @@ def loip_k_window_attention_q8_scratch_bytes(B, Hq, Hkv, d, window, sinks, max_c
 def loip_k_window_attention_q8(q, kv_base, page_offsets, max_pages, ctx_lens, Hq, Hkv, d, page_tokens, layer,
                                layer_page_bytes, window, sinks, max_ctx, scratch, o, stream=None):
     """loip_k_window_attention over the 8-bit cache."""
-    _on_current(q)
+    _on_current(q, kv_base)
     _attention(lib().loip_k_window_attention_q8, q, kv_base, page_offsets, max_pages, ctx_lens, Hq, Hkv, d,
                page_tokens, layer, layer_page_bytes, window, sinks, max_ctx, scratch, o, stream)
 
@@ -737,6 +740,6 @@ def loip_k_window_prefill_q8_scratch_bytes(M, n_prompts, Hq, Hkv, d, window, sin
 def loip_k_window_prefill_q8(q, kv_base, page_offsets, max_pages, row_starts, first_pos, Hq, Hkv, d, page_tokens,
                              layer, layer_page_bytes, window, sinks, max_ctx, scratch, o, stream=None):
     """loip_k_window_prefill over the 8-bit cache."""
-    _on_current(q)
+    _on_current(q, kv_base)
     _prefill(lib().loip_k_window_prefill_q8, q, kv_base, page_offsets, max_pages, row_starts, first_pos, Hq, Hkv, d,
              page_tokens, layer, layer_page_bytes, window, sinks, max_ctx, scratch, o, stream)

@@ -294,6 +294,26 @@ def test_blocks_of_every_size(torch, L, d, kind):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("d,E", [(64, -60), (128, -60), (128, 60), (128, -120), (64, 110)])
+def test_decode_meets_extreme_blocks_late(torch, L, d, E, dtype):
+    """Ordinary blocks first, then values of 2^E (and keys of 2^-60) among them: what was summed before counts on."""
+    n, Hq, Hkv = 700, 6, 2
+    c = Cache8(2, 11, Hkv, d, 37)
+    rng = np.random.default_rng(38)
+    for r in range(2):
+        k, v = rng.standard_normal((2, n, Hkv, d))
+        v[400::37, :, 32:] *= 2.0 ** E
+        k[433::64, :, :32] *= 2.0 ** -60
+        c.put(r, np.arange(n), k, v)
+    q = rng.standard_normal((2, Hq * d)).astype(np.float32)
+    qd, q64 = _rows(torch, q, dtype)
+    got = _host(_decode(torch, L, c, qd, (n, 399), Hq, ALL, 0, 704))
+    for r, ctx in enumerate((n, 399)):
+        want, t32, tbf = W.attend(c, r, ctx - 1, q64[r].reshape(Hq, d), ALL, 0)
+        assert np.all(np.abs(got[r].reshape(Hq, d) - want) <= (t32 if dtype == "f32" else tbf)), r
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("kind", ["decode", "prefill"])
 def test_blocks_of_nan_that_a_row_sees(torch, L, d, dtype, kind):
@@ -523,6 +543,45 @@ def test_prefill_exponents_at_the_borders(torch, L, runs, dtype):
     for t in range(0, rows, 13):
         want, t32, tbf = W.attend(c, 0, first + t, q64[t].reshape(64, d), ALL, 2)
         assert np.all(np.abs(got[t] - want) <= (t32 if dtype == "f32" else tbf)), t
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_prompts_of_captured_calls_change(torch, L, dtype):
+    """Two captured calls on one scratch, one of them with images, replayed in turn while the prompts' rows and
+    positions change on the device; rows that no prompt has keep what they hold."""
+    Hq, Hkv, d, M, ctx = 64, 4, 64, 500, 640
+    c = Cache8(3, ctx // P, Hkv, d, 221)
+    for r in range(3):
+        c.fill_request(r, range(ctx), 222 + r)
+    kv, table = _dev(torch, c.bytes), _dev(torch, c.table)
+    qd, q64 = _rows(torch, np.random.default_rng(223).standard_normal((M, Hq * d)).astype(np.float32), dtype)
+    starts, first = torch.zeros(4, dtype=torch.int32, device="cuda"), torch.zeros(3, dtype=torch.int32, device="cuda")
+    need = max(L.loip_k_window_prefill_q8_scratch_bytes(m, 3, Hq, Hkv, d, 200, 3, ctx) for m in (M, 20))
+    scratch = torch.zeros(need, dtype=torch.uint8, device="cuda")
+    graphs = []
+    for m in (M, 20):
+        o = torch.zeros(m, Hq * d, dtype=qd.dtype, device="cuda")
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            L.loip_k_window_prefill_q8(qd[:m], kv, table, c.max_pages, starts, first, Hq, Hkv, d, P, 0, c.layer_page_bytes,
+                                       200, 3, ctx, scratch, o)
+        graphs.append((m, g, o))
+    for i, (m, rows, at) in enumerate([(M, (300, 200, 0), (0, 440, 9)), (20, (7, 0, 12), (600, 3, 50)),
+                                       (M, (1, 2, 390), (639, 0, 250)), (20, (20, 0, 0), (0, 0, 0)),
+                                       (M, (0, 0, 480), (5, 5, 160))]):
+        starts.copy_(torch.tensor([0, *np.cumsum(rows)]))
+        first.copy_(torch.tensor(at))
+        _, g, o = graphs[m != M]
+        o.fill_(7.0)
+        g.replay()
+        got = _host(o).reshape(m, Hq, d)
+        assert np.all(got[sum(rows):] == 7.0), i
+        row = 0
+        for r, (n, lo) in enumerate(zip(rows, at)):
+            for t in range(0, n, 11):
+                want, t32, tbf = W.attend(c, r, lo + t, q64[row + t].reshape(Hq, d), 200, 3)
+                assert np.all(np.abs(got[row + t] - want) <= (t32 if dtype == "f32" else tbf)), (i, r, t)
+            row += n
 
 
 def test_prefill_rows_behind_the_last_prompt(torch, L):

@@ -107,6 +107,16 @@ def test_scratch_sizes(L):
         assert g(a[0], a[1], *heads, *a[2:]) <= g(b[0], b[1], *heads, *b[2:]), (heads, a, b)
 
 
+def test_scratch_sizes_of_the_largest_arguments(L):
+    f, g = L.loip_k_window_attention_q8_scratch_bytes, L.loip_k_window_prefill_q8_scratch_bytes
+    most = (1 << 31) - 1
+    for heads in ((65536 - 3 * 8192 * 2, 8192, 128), (8, 1, 128), (64, 64, 64)):
+        for ctx in (1, 1 << 30):
+            assert f(1, *heads, most, most, ctx) <= f(most, *heads, most, most, ctx) < 1 << 30
+            small, large = g(1, 1, *heads, most, most, ctx), g(1 << 30, 1 << 20, *heads, most, most, ctx)
+            assert 16 <= small <= large < 3 << 30
+
+
 # ---------------------------------------------------------------------------
 # the binding (the library is a stand-in that records its calls, the tensors say that they are on a GPU)
 # ---------------------------------------------------------------------------
@@ -204,6 +214,17 @@ def test_tensors_of_another_device(library, op):
     heads = {b_append: HQ + 2 * HKV, b_read: 2 * HKV}.get(op, HQ)
     with pytest.raises(loip.LoipError, match="device 1"):
         op(**{name: dev(torch.zeros(7 if op is b_prefill else B, heads * D), OnAnotherGpu)})
+    assert not library.calls
+
+
+@pytest.mark.parametrize("op", OPS)
+def test_a_cache_in_host_memory(library, op):
+    class Pinned(torch.Tensor):
+        def is_pinned(self):
+            return True
+
+    with pytest.raises(loip.LoipError, match="device memory"):
+        op(kv_base=torch.zeros(1024, dtype=torch.uint8).as_subclass(Pinned))
     assert not library.calls
 
 
