@@ -605,7 +605,7 @@ def _scratch(x):
     return x.data_ptr()
 
 
-def _append(entry, qkv, g_q, g_k, Hq, Hkv, d, eps, theta, positions, row_req, q_out, kv_base, page_offsets, max_pages,
+def _append(entry, qkv, g_q, g_k, Hq, Hkv, d, eps, theta, positions, row_req, q_out, kv, page_offsets, max_pages,
             page_tokens, layer, layer_page_bytes, stream):
     (T, width), (row_stride, step) = qkv.shape, qkv.stride()
     dtype = _dtype(qkv, q_out)
@@ -616,31 +616,31 @@ def _append(entry, qkv, g_q, g_k, Hq, Hkv, d, eps, theta, positions, row_req, q_
         _refuse("qkv and q_out do not fit together")
     rc = entry(qkv.data_ptr(), dtype, row_stride, T, Hq, Hkv, d, _gain(g_q, d), _gain(g_k, d), eps, theta,
                _ints(positions, T, "positions"), None if row_req is None else _ints(row_req, T, "row_req"), n_req,
-               q_out.data_ptr(), _cache(kv_base), _pages(page_offsets, n_req, max_pages), max_pages, page_tokens, layer,
-               layer_page_bytes, _s(stream))
+               q_out.data_ptr(), kv, _pages(page_offsets, n_req, max_pages), max_pages, page_tokens, layer, layer_page_bytes,
+               _s(stream))
     if rc:
         _check(rc)
 
 
-def _attention(entry, q, kv_base, page_offsets, max_pages, ctx_lens, Hq, Hkv, d, page_tokens, layer, layer_page_bytes,
+def _attention(entry, q, kv, page_offsets, max_pages, ctx_lens, Hq, Hkv, d, page_tokens, layer, layer_page_bytes,
                window, sinks, max_ctx, scratch, o, stream):
     B, dtype = q.shape[0], _dtype(q, o)
     if not (q.is_contiguous() and o.is_contiguous()) or q.numel() != B * Hq * d or o.numel() != q.numel():
         _refuse("q and o are contiguous [B, Hq * d]")
-    rc = entry(q.data_ptr(), dtype, _cache(kv_base), _pages(page_offsets, B, max_pages), max_pages,
+    rc = entry(q.data_ptr(), dtype, kv, _pages(page_offsets, B, max_pages), max_pages,
                _ints(ctx_lens, B, "ctx_lens"), B, Hq, Hkv, d, page_tokens, layer, layer_page_bytes, window, sinks, max_ctx,
                _scratch(scratch), scratch.nbytes, o.data_ptr(), _s(stream))
     if rc:
         _check(rc)
 
 
-def _prefill(entry, q, kv_base, page_offsets, max_pages, row_starts, first_pos, Hq, Hkv, d, page_tokens, layer,
+def _prefill(entry, q, kv, page_offsets, max_pages, row_starts, first_pos, Hq, Hkv, d, page_tokens, layer,
              layer_page_bytes, window, sinks, max_ctx, scratch, o, stream):
     M, dtype = q.shape[0], _dtype(q, o)
     if not (q.is_contiguous() and o.is_contiguous()) or q.numel() != M * Hq * d or o.numel() != q.numel():
         _refuse("q and o are contiguous [M, Hq * d]")
     n = row_starts.numel() - 1
-    rc = entry(q.data_ptr(), dtype, _cache(kv_base), _pages(page_offsets, n, max_pages), max_pages,
+    rc = entry(q.data_ptr(), dtype, kv, _pages(page_offsets, n, max_pages), max_pages,
                _ints(row_starts, 1, "row_starts"), None if first_pos is None else _ints(first_pos, n, "first_pos"), n, M,
                Hq, Hkv, d, page_tokens, layer, layer_page_bytes, window, sinks, max_ctx, _scratch(scratch),
                scratch.nbytes, o.data_ptr(), _s(stream))
@@ -652,7 +652,7 @@ def loip_k_qk_append(qkv, g_q, g_k, Hq, Hkv, d, eps, theta, positions, row_req, 
                      max_pages, page_tokens, layer, layer_page_bytes, stream=None):
     """Norm of queries and keys (g_q, g_k or None), rotation (theta 0: none), append.  qkv [T, (Hq + 2 Hkv) * d]
     float32 or bfloat16 with any row stride; page_offsets [requests, max_pages]."""
-    _append(lib().loip_k_qk_append, qkv, g_q, g_k, Hq, Hkv, d, eps, theta, positions, row_req, q_out, kv_base,
+    _append(lib().loip_k_qk_append, qkv, g_q, g_k, Hq, Hkv, d, eps, theta, positions, row_req, q_out, _cache(kv_base),
             page_offsets, max_pages, page_tokens, layer, layer_page_bytes, stream)
 
 
@@ -664,7 +664,7 @@ def loip_k_window_attention(q, kv_base, page_offsets, max_pages, ctx_lens, Hq, H
                             layer_page_bytes, window, sinks, max_ctx, scratch, o, stream=None):
     """Attention of one new token per request behind a window with sinks.  scratch: a uint8 tensor of
     loip_k_window_attention_scratch_bytes(...), zero-filled once."""
-    _attention(lib().loip_k_window_attention, q, kv_base, page_offsets, max_pages, ctx_lens, Hq, Hkv, d, page_tokens,
+    _attention(lib().loip_k_window_attention, q, _cache(kv_base), page_offsets, max_pages, ctx_lens, Hq, Hkv, d, page_tokens,
                layer, layer_page_bytes, window, sinks, max_ctx, scratch, o, stream)
 
 
@@ -676,7 +676,7 @@ def loip_k_window_prefill(q, kv_base, page_offsets, max_pages, row_starts, first
                           layer_page_bytes, window, sinks, max_ctx, scratch, o, stream=None):
     """The same attention for the rows of prompts: row_starts (device int32 [prompts + 1]), first_pos (device int32
     [prompts] or None = 0)."""
-    _prefill(lib().loip_k_window_prefill, q, kv_base, page_offsets, max_pages, row_starts, first_pos, Hq, Hkv, d,
+    _prefill(lib().loip_k_window_prefill, q, _cache(kv_base), page_offsets, max_pages, row_starts, first_pos, Hq, Hkv, d,
              page_tokens, layer, layer_page_bytes, window, sinks, max_ctx, scratch, o, stream)
 
 
@@ -686,34 +686,36 @@ def loip_k_cache_q8_layer_bytes(Hkv, d) -> int:
     return Hkv * 132 * d
 
 
-def _on_current(x, kv_base):
-    """Refuses rows on another device than the current one, whose stream the call would go to, and a cache in
-    host memory, which the prompt kernels' bulk copies do not read."""
+def _cache_q8(x, rows):
+    """Address of the cache, which lies in device memory: the prompt kernels' bulk copies read no other.  Refuses
+    rows on another device than the current one, whose stream the call goes to."""
     if not _of_torch:
         _torch()
-    if x.is_cuda and x.get_device() != _of_torch[1]():
-        _refuse(f"rows on device {x.get_device()} in a call on device {_of_torch[1]()}")
-    if not (isinstance(kv_base, int) or kv_base is None or kv_base.is_cuda):
-        _refuse("the 8-bit cache is in device memory")
+    if rows.get_device() != _of_torch[1]():
+        _refuse(f"rows on device {rows.get_device()} in a call on device {_of_torch[1]()}")
+    if x is None or isinstance(x, int):
+        return x
+    if not x.is_cuda or not x.is_contiguous():
+        _refuse("the 8-bit cache is a contiguous tensor in device memory, or an address")
+    return x.data_ptr()
 
 
 def loip_k_qk_append_q8(qkv, g_q, g_k, Hq, Hkv, d, eps, theta, positions, row_req, q_out, kv_base, page_offsets,
                         max_pages, page_tokens, layer, layer_page_bytes, stream=None):
     """loip_k_qk_append into the 8-bit cache."""
-    _on_current(qkv, kv_base)
-    _append(lib().loip_k_qk_append_q8, qkv, g_q, g_k, Hq, Hkv, d, eps, theta, positions, row_req, q_out, kv_base,
-            page_offsets, max_pages, page_tokens, layer, layer_page_bytes, stream)
+    _append(lib().loip_k_qk_append_q8, qkv, g_q, g_k, Hq, Hkv, d, eps, theta, positions, row_req, q_out,
+            _cache_q8(kv_base, qkv), page_offsets, max_pages, page_tokens, layer, layer_page_bytes, stream)
 
 
 def loip_k_cache_read_q8(kv_base, page_offsets, max_pages, positions, row_req, Hkv, d, page_tokens, layer,
                          layer_page_bytes, out, stream=None):
     """Rows of the 8-bit cache as numbers: out [T, 2 * Hkv * d] float32 or bfloat16 (key heads, value heads) for the
     positions [T] of the requests row_req [T] (None: row t is of request t); page_offsets [requests, max_pages]."""
-    _on_current(out, kv_base)
-    T, dtype, n_req = out.shape[0], _dtype(out, out), page_offsets.shape[0]
-    if not out.is_contiguous() or out.numel() != T * 2 * Hkv * d:
-        _refuse("out is contiguous [T, 2 * Hkv * d]")
-    rc = lib().loip_k_cache_read_q8(_cache(kv_base), _pages(page_offsets, n_req, max_pages), max_pages,
+    kv = _cache_q8(kv_base, out)
+    T, dtype, n_req = out.shape[0], _of_torch[2].get(out.dtype), page_offsets.shape[0]
+    if dtype is None or not out.is_contiguous() or out.numel() != T * 2 * Hkv * d:
+        _refuse("out is contiguous [T, 2 * Hkv * d], float32 or bfloat16")
+    rc = lib().loip_k_cache_read_q8(kv, _pages(page_offsets, n_req, max_pages), max_pages,
                                     _ints(positions, T, "positions"),
                                     None if row_req is None else _ints(row_req, T, "row_req"), n_req, T, Hkv, d,
                                     page_tokens, layer, layer_page_bytes, out.data_ptr(), dtype, _s(stream))
@@ -728,8 +730,7 @@ def loip_k_window_attention_q8_scratch_bytes(B, Hq, Hkv, d, window, sinks, max_c
 def loip_k_window_attention_q8(q, kv_base, page_offsets, max_pages, ctx_lens, Hq, Hkv, d, page_tokens, layer,
                                layer_page_bytes, window, sinks, max_ctx, scratch, o, stream=None):
     """loip_k_window_attention over the 8-bit cache."""
-    _on_current(q, kv_base)
-    _attention(lib().loip_k_window_attention_q8, q, kv_base, page_offsets, max_pages, ctx_lens, Hq, Hkv, d,
+    _attention(lib().loip_k_window_attention_q8, q, _cache_q8(kv_base, q), page_offsets, max_pages, ctx_lens, Hq, Hkv, d,
                page_tokens, layer, layer_page_bytes, window, sinks, max_ctx, scratch, o, stream)
 
 
@@ -740,6 +741,5 @@ def loip_k_window_prefill_q8_scratch_bytes(M, n_prompts, Hq, Hkv, d, window, sin
 def loip_k_window_prefill_q8(q, kv_base, page_offsets, max_pages, row_starts, first_pos, Hq, Hkv, d, page_tokens,
                              layer, layer_page_bytes, window, sinks, max_ctx, scratch, o, stream=None):
     """loip_k_window_prefill over the 8-bit cache."""
-    _on_current(q, kv_base)
-    _prefill(lib().loip_k_window_prefill_q8, q, kv_base, page_offsets, max_pages, row_starts, first_pos, Hq, Hkv, d,
+    _prefill(lib().loip_k_window_prefill_q8, q, _cache_q8(kv_base, q), page_offsets, max_pages, row_starts, first_pos, Hq, Hkv, d,
              page_tokens, layer, layer_page_bytes, window, sinks, max_ctx, scratch, o, stream)
