@@ -21,7 +21,6 @@
 namespace loip {
 namespace q8 {
 
-constexpr int kBlock = 32;    // elements with one exponent
 constexpr int kGranule = 16;  // tokens in one contiguous piece
 constexpr int kMostExponent = 253;
 

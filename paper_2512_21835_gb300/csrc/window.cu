@@ -338,8 +338,8 @@ cudaError_t launch_read(const ReadArgs& a, cudaStream_t st) {
 bool aligned(const void* p, uintptr_t to) { return ((uintptr_t)p & (to - 1)) == 0; }
 
 // What every call on the cache has in common; null if it is in order.
-const char* cache_refusal(bool q8, int dtype, int rows, int Hq, int Hkv, int d, const void* kv_base, const int64_t* page_offsets,
-                          int max_pages, int page_tokens, int layer, uint64_t layer_page_bytes) {
+const char* cache_refusal(bool q8, int dtype, int rows, int Hq, int Hkv, int d, const void* kv_base,
+                          const int64_t* page_offsets, int max_pages, int page_tokens, int layer, uint64_t layer_page_bytes) {
     if (dtype != LOIP_F32 && dtype != LOIP_BF16) return "dtype is LOIP_F32 or LOIP_BF16";
     if (rows < 0) return "a negative number of rows";
     if (Hkv < 1 || Hq < 1 || Hq % Hkv) return "the query heads are a multiple of the kv heads";

@@ -638,7 +638,8 @@ __global__ void __launch_bounds__(kThreads, kResident8) window_decode_q8_kernel(
             }
             // An exponent of 96 to 159 is one whose shift is a test of bits.  A tile with another one takes O to
             // its own units, and from then on elements are made by two products.
-            if (!exact && __any_sync(0xffffffffu, ((ek - 0x00600060u) | (ev[0] - 0x00600060u) | (ev[1] - 0x00600060u)) & 0xffc0ffc0u)) {
+            const uint32_t off = (ek - 0x00600060u) | (ev[0] - 0x00600060u) | (ev[1] - 0x00600060u);
+            if (!exact && __any_sync(0xffffffffu, off & 0xffc0ffc0u)) {
                 exact = true;
 #pragma unroll
                 for (int e = 0; e < D / 16; ++e)
@@ -647,7 +648,9 @@ __global__ void __launch_bounds__(kThreads, kResident8) window_decode_q8_kernel(
             }
             auto tile = [&](auto exactly) {
                 constexpr bool EXACT = decltype(exactly)::value;
-                auto pair = [](uint32_t twice, uint32_t sc) { return EXACT ? q8::pair_of(twice, sc) : q8::shifted_of(twice, sc); };
+                auto pair = [](uint32_t twice, uint32_t sc) {
+                    return EXACT ? q8::pair_of(twice, sc) : q8::shifted_of(twice, sc);
+                };
                 // ---- scores, in independent sums (a chain of MMAs waits for each result)
                 float s[4];
                 {
@@ -660,7 +663,8 @@ __global__ void __launch_bounds__(kThreads, kResident8) window_decode_q8_kernel(
                             k[j][4 * x] = u.x; k[j][4 * x + 1] = u.y; k[j][4 * x + 2] = u.z; k[j][4 * x + 3] = u.w;
                         }
                     const uint32_t both = EXACT ? q8::scale2(ek) : q8::shifted2(ek);
-                    const uint32_t sc[2] = {see0 ? __byte_perm(both, 0u, 0x1010u) : 0u, see1 ? __byte_perm(both, 0u, 0x3232u) : 0u};
+                    const uint32_t sc[2] = {see0 ? __byte_perm(both, 0u, 0x1010u) : 0u,
+                                            see1 ? __byte_perm(both, 0u, 0x3232u) : 0u};
                     constexpr int SUMS = F32 ? 1 : 2;
                     float z[PL][SUMS][4];
 #pragma unroll

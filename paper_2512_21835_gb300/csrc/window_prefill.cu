@@ -212,6 +212,10 @@ __device__ __forceinline__ void bar_init(uint32_t b, uint32_t n) {
 __device__ __forceinline__ void bar_arrive(uint32_t b) {
     asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(b) : "memory");
 }
+// An arrival, and the bytes that copies will bring.
+__device__ __forceinline__ void bar_expect(uint32_t b, uint32_t bytes) {
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(b), "r"(bytes) : "memory");
+}
 // Whether the phase of that parity is complete; waits for it up to a millisecond, asleep.
 // (Without the hint the wait ended after some hundred cycles, and the waiting warps'
 // polls took issue slots and shared memory from the others.)
@@ -409,7 +413,8 @@ struct Pages {
 };
 
 template <int D, int NP, int QT, Source SRC, typename T>
-__global__ void __launch_bounds__(Cfg<D, NP, QT, SRC>::THREADS, 1) window_prefill_kernel(const __grid_constant__ PrefillArgs p) {
+__global__ void __launch_bounds__(Cfg<D, NP, QT, SRC>::THREADS, 1)
+    window_prefill_kernel(const __grid_constant__ PrefillArgs p) {
     using C = Cfg<D, NP, QT, SRC>;
     constexpr bool Q8 = C::Q8;
     const WindowArgs& a = p.a;
@@ -678,7 +683,7 @@ __global__ void __launch_bounds__(Cfg<D, NP, QT, SRC>::THREADS, 1) window_prefil
                             const int t = i - C::AHEAD;  // whose values
                             const uint32_t bar = bar_full + 8 * use.bar, dst = ring + use.slot * C::SLOT;
                             const uint32_t bytes = ((i < n) + (t >= 0)) * C::TILE;
-                            asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+                            bar_expect(bar, bytes);
                             if (i < n) copy_bulk(dst, p.images + image(i) * (2 * C::TILE), C::TILE, bar);
                             if (t >= 0) copy_bulk(dst + C::TILE, p.images + image(t) * (2 * C::TILE) + C::TILE, C::TILE, bar);
                             issued = i + 1;
@@ -688,93 +693,94 @@ __global__ void __launch_bounds__(Cfg<D, NP, QT, SRC>::THREADS, 1) window_prefil
                     if (lane == 0) {  // no copy may be in flight at the block's end
                         const uint64_t t0 = now_ns();
                         for (int i = max(0, issued - C::SLOTS); i < issued; ++i)
-                            while (!bar_try(bar_full + 8 * (i % C::CYCLE), i / C::CYCLE & 1) && now_ns() - t0 < 2000000000ull) {}
+                            while (!bar_try(bar_full + 8 * (i % C::CYCLE), i / C::CYCLE & 1) &&
+                                   now_ns() - t0 < 2000000000ull) {}
                     }
                 }
             } else {
-            // ---------------------------------------------------------------- loader
-            const int lt = tid - 256;
-            constexpr int CPR = D / 8, RPP = C::LOADERS / CPR;  // 16-byte chunks per row, rows per pass
-            constexpr int PASSES = KT / RPP;
-            const int chunk = lt % CPR, r0 = lt / CPR;
-            const char* layer = a.kv.base + (uint64_t)a.kv.layer * a.kv.layer_page_bytes;
-            const int64_t* table = a.kv.page_offsets + (int64_t)req * a.kv.max_pages;
-            const int win0 = max(0, pos0 - a.window + 1);  // (window 0: no page of it is in the list)
-            auto seen = [&](int pos) {
-                return pos < pages.last && ((pos >= win0 && a.window > 0) || pos < a.sinks);
-            };
-            // place in a slot of this thread's chunk of pass k: row r0 + k RPP, chunk ^ row % 8
-            static_assert(RPP == 4 || RPP == 8, "");
-            const uint32_t place0 = (uint32_t)((chunk >> 3) * C::KV_SLAB + r0 * 128 + (((chunk & 7) ^ (r0 & 7)) << 4));
-            const uint32_t place1 = RPP == 8 ? place0 : place0 ^ 64;  // odd passes: row % 8 differs by 4
-            auto place = [&](int k) { return (k & 1 ? place1 : place0) + k * RPP * 128; };
-            // Slots arrive at their barrier by themselves, except with values of a page that not all rows
-            // see in full: of those, the ones that are not finite are taken out first, one slot later.
-            auto checked = [&](uint32_t slot) {
-                for (int k = 0; k < PASSES; ++k) {
-                    const uint32_t w = ring + slot * C::SLOT + C::TILE + place(k);
-                    uint32_t u[4];
-                    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];"
-                                 : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3])
-                                 : "r"(w)
-                                 : "memory");
-                    bool bad = false;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        bad |= (u[i] & 0x7F80u) == 0x7F80u || (u[i] & 0x7F800000u) == 0x7F800000u;
-                    if (bad) {
-                        asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(w), "r"(0u) : "memory");
-                        *(volatile int*)&c->bad = 1;
-                    }
-                }
-                bar_arrive(bar_full + 8 * slot);
-            };
-            constexpr int STEP = RPP * D * 2;  // bytes from a pass to the next in the page
-            auto load = [&](int t, bool is_v, uint32_t dst) {
-                const int pg = page_at(t), b = pg * KT;
-                const char* src = layer + table[pg] + ((int64_t)(is_v ? a.Hkv : 0) + kvh) * (KT * D * 2) +
-                                  (r0 * D + chunk * 8) * 2;
-                if (b + KT <= pages.last && ((b >= win0 && a.window > 0) || b + KT <= a.sinks)) {  // the whole page
-#pragma unroll
-                    for (int k = 0; k < PASSES; ++k) cp_async16(dst + place(k), src + k * STEP, 16u);
-                } else {
-#pragma unroll 2
+                // ---------------------------------------------------------------- loader
+                const int lt = tid - 256;
+                constexpr int CPR = D / 8, RPP = C::LOADERS / CPR;  // 16-byte chunks per row, rows per pass
+                constexpr int PASSES = KT / RPP;
+                const int chunk = lt % CPR, r0 = lt / CPR;
+                const char* layer = a.kv.base + (uint64_t)a.kv.layer * a.kv.layer_page_bytes;
+                const int64_t* table = a.kv.page_offsets + (int64_t)req * a.kv.max_pages;
+                const int win0 = max(0, pos0 - a.window + 1);  // (window 0: no page of it is in the list)
+                auto seen = [&](int pos) {
+                    return pos < pages.last && ((pos >= win0 && a.window > 0) || pos < a.sinks);
+                };
+                // place in a slot of this thread's chunk of pass k: row r0 + k RPP, chunk ^ row % 8
+                static_assert(RPP == 4 || RPP == 8, "");
+                const uint32_t place0 = (uint32_t)((chunk >> 3) * C::KV_SLAB + r0 * 128 + (((chunk & 7) ^ (r0 & 7)) << 4));
+                const uint32_t place1 = RPP == 8 ? place0 : place0 ^ 64;  // odd passes: row % 8 differs by 4
+                auto place = [&](int k) { return (k & 1 ? place1 : place0) + k * RPP * 128; };
+                // Slots arrive at their barrier by themselves, except with values of a page that not all rows
+                // see in full: of those, the ones that are not finite are taken out first, one slot later.
+                auto checked = [&](uint32_t slot) {
                     for (int k = 0; k < PASSES; ++k) {
-                        const bool ok = seen(b + r0 + k * RPP);
-                        cp_async16(dst + place(k), ok ? src + k * STEP : layer, ok ? 16u : 0u);
+                        const uint32_t w = ring + slot * C::SLOT + C::TILE + place(k);
+                        uint32_t u[4];
+                        asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];"
+                                     : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3])
+                                     : "r"(w)
+                                     : "memory");
+                        bool bad = false;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            bad |= (u[i] & 0x7F80u) == 0x7F80u || (u[i] & 0x7F800000u) == 0x7F800000u;
+                        if (bad) {
+                            asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(w), "r"(0u) : "memory");
+                            *(volatile int*)&c->bad = 1;
+                        }
+                    }
+                    bar_arrive(bar_full + 8 * slot);
+                };
+                constexpr int STEP = RPP * D * 2;  // bytes from a pass to the next in the page
+                auto load = [&](int t, bool is_v, uint32_t dst) {
+                    const int pg = page_at(t), b = pg * KT;
+                    const char* src = layer + table[pg] + ((int64_t)(is_v ? a.Hkv : 0) + kvh) * (KT * D * 2) +
+                                      (r0 * D + chunk * 8) * 2;
+                    if (b + KT <= pages.last && ((b >= win0 && a.window > 0) || b + KT <= a.sinks)) {  // the whole page
+#pragma unroll
+                        for (int k = 0; k < PASSES; ++k) cp_async16(dst + place(k), src + k * STEP, 16u);
+                    } else {
+#pragma unroll 2
+                        for (int k = 0; k < PASSES; ++k) {
+                            const bool ok = seen(b + r0 + k * RPP);
+                            cp_async16(dst + place(k), ok ? src + k * STEP : layer, ok ? 16u : 0u);
+                        }
+                    }
+                };
+                int slot = 0, late = -1;  // late: the slot before, if it is yet to be checked
+                uint32_t free_phase = 1;  // of the ring's previous round (before the first one: complete)
+#pragma unroll 1
+                for (int i = 0; i < n + C::AHEAD && n > 0; ++i) {
+                    const int t = i - C::AHEAD;  // whose values
+                    const uint32_t dst = ring + (uint32_t)slot * C::SLOT;
+                    wait(bar_empty + 8 * slot, free_phase, 1);
+                    if (i < n) load(i, false, dst);
+                    bool some = false;
+                    if (t >= 0) {
+                        load(t, true, dst + C::TILE);
+                        const int b = page_at(t) * KT;
+                        some = !(b + KT - 1 <= pos0 && (b > pos1 - a.window || b + KT <= a.sinks));
+                    }
+                    asm volatile("cp.async.commit_group;" ::: "memory");
+                    if (!some)
+                        asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar_full + 8 * slot)
+                                     : "memory");
+                    if (late >= 0) {
+                        asm volatile("cp.async.wait_group 1;" ::: "memory");
+                        checked(late);
+                    }
+                    late = some ? slot : -1;
+                    if (++slot == C::SLOTS) {
+                        slot = 0;
+                        free_phase ^= 1;
                     }
                 }
-            };
-            int slot = 0, late = -1;  // late: the slot before, if it is yet to be checked
-            uint32_t free_phase = 1;  // of the ring's previous round (before the first one: complete)
-#pragma unroll 1
-            for (int i = 0; i < n + C::AHEAD && n > 0; ++i) {
-                const int t = i - C::AHEAD;  // whose values
-                const uint32_t dst = ring + (uint32_t)slot * C::SLOT;
-                wait(bar_empty + 8 * slot, free_phase, 1);
-                if (i < n) load(i, false, dst);
-                bool some = false;
-                if (t >= 0) {
-                    load(t, true, dst + C::TILE);
-                    const int b = page_at(t) * KT;
-                    some = !(b + KT - 1 <= pos0 && (b > pos1 - a.window || b + KT <= a.sinks));
-                }
-                asm volatile("cp.async.commit_group;" ::: "memory");
-                if (!some)
-                    asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar_full + 8 * slot)
-                                 : "memory");
-                if (late >= 0) {
-                    asm volatile("cp.async.wait_group 1;" ::: "memory");
-                    checked(late);
-                }
-                late = some ? slot : -1;
-                if (++slot == C::SLOTS) {
-                    slot = 0;
-                    free_phase ^= 1;
-                }
-            }
-            asm volatile("cp.async.wait_all;" ::: "memory");
-            if (late >= 0) checked(late);
+                asm volatile("cp.async.wait_all;" ::: "memory");
+                if (late >= 0) checked(late);
             }
         } else if (n > 0 && warp < C::MMA_WARP + 2) {
             // ---------------------------------------------------------------- MMA issue
@@ -830,56 +836,56 @@ __global__ void __launch_bounds__(Cfg<D, NP, QT, SRC>::THREADS, 1) window_prefil
                     commit(empty);
                 }
             } else {
-            if (QT == 2 || w < steps) wait(bar_full + 8 * use.bar, use.phase, 3);
-            // From P of a tile to S of the next but one the stream waits for this warp, so with two row
-            // tiles the next slot is waited for before P, and the last one released after S (467 -> 454
-            // us for 8192 rows behind 4096).  With one row tile a stream has two slots, and there the
-            // release has to come first (4 x 512 fp32 rows: 109 us, 121 the other way).
+                if (QT == 2 || w < steps) wait(bar_full + 8 * use.bar, use.phase, 3);
+                // From P of a tile to S of the next but one the stream waits for this warp, so with two row
+                // tiles the next slot is waited for before P, and the last one released after S (467 -> 454
+                // us for 8192 rows behind 4096).  With one row tile a stream has two slots, and there the
+                // release has to come first (4 x 512 fp32 rows: 109 us, 121 the other way).
 #pragma unroll 1
-            for (int i = QT == 2 ? 0 : w; i < steps; i += STRIDE) {
-                const uint32_t k_at = use.slot * (C::SLOT / 16);
-                fence_loaded();
-                if (mine(i)) {  // S = Q K^T, once the softmax has read the last one
-                    wait(bar_s_free + 8 * w, free, 4);
-                    free ^= 1;
-                    fence_after();
-                    const uint64_t k = k_desc + k_at;
+                for (int i = QT == 2 ? 0 : w; i < steps; i += STRIDE) {
+                    const uint32_t k_at = use.slot * (C::SLOT / 16);
+                    fence_loaded();
+                    if (mine(i)) {  // S = Q K^T, once the softmax has read the last one
+                        wait(bar_s_free + 8 * w, free, 4);
+                        free ^= 1;
+                        fence_after();
+                        const uint64_t k = k_desc + k_at;
 #pragma unroll
-                    for (int pl = NP - 1; pl >= 0; --pl)
+                        for (int pl = NP - 1; pl >= 0; --pl)
 #pragma unroll
-                        for (int x = 0; x < D / 64; ++x)
-                            mma_ss4(tmem + C::s_col(w), q_desc + (pl * C::Q_PLANE + x * C::Q_SLAB) / 16,
-                                    k + x * C::KV_SLAB / 16, idesc(KT, false), pl != NP - 1 || x != 0);
-                    commit(bar_s + 8 * w);
+                            for (int x = 0; x < D / 64; ++x)
+                                mma_ss4(tmem + C::s_col(w), q_desc + (pl * C::Q_PLANE + x * C::Q_SLAB) / 16,
+                                        k + x * C::KV_SLAB / 16, idesc(KT, false), pl != NP - 1 || x != 0);
+                        commit(bar_s + 8 * w);
+                    }
+                    if (QT == 2 && used >= 0) commit(bar_empty + 8 * used);
+                    used = use.bar;
+#pragma unroll
+                    for (int x = 0; x < STRIDE; ++x) use.template next<C::SLOTS, C::CYCLE>();
+                    if (QT == 2 && i + STRIDE < steps) wait(bar_full + 8 * use.bar, use.phase, 3);
+                    if (mine(i - C::AHEAD)) {  // O += P V
+                        const uint32_t buf = done & 1;
+                        wait(bar_p + 16 * w + 8 * buf, done / 2 & 1, 5);
+                        // O is one for both streams: the other one's last tile has been drained.  (This
+                        // stream's own last one has, as its P is here, so the phase is the right one.)
+                        if (NP > 1) wait(bar_o_free, (i - C::AHEAD + 1) & 1, 9);
+                        fence_after();
+                        const uint64_t v = v_desc + k_at;
+#pragma unroll
+                        for (int pl = NP - 1; pl >= 0; --pl)
+#pragma unroll
+                            for (int x = 0; x < 2; ++x)  // O is kept (bf16), or drained after every tile
+                                mma_ts2(tmem + C::o_col(w), tmem + C::p_col(w, buf, pl) + 16 * x,
+                                        v + x * (32 * 128 / 16), idesc(D, true),
+                                        pl != NP - 1 || x != 0 || (NP == 1 && done) ? 1u : 0u);
+                        commit(bar_pv + 16 * w + 8 * buf);
+                        ++done;
+                    }
+                    if (QT == 1) {
+                        commit(bar_empty + 8 * used);
+                        if (i + STRIDE < steps) wait(bar_full + 8 * use.bar, use.phase, 3);
+                    }
                 }
-                if (QT == 2 && used >= 0) commit(bar_empty + 8 * used);
-                used = use.bar;
-#pragma unroll
-                for (int x = 0; x < STRIDE; ++x) use.template next<C::SLOTS, C::CYCLE>();
-                if (QT == 2 && i + STRIDE < steps) wait(bar_full + 8 * use.bar, use.phase, 3);
-                if (mine(i - C::AHEAD)) {  // O += P V
-                    const uint32_t buf = done & 1;
-                    wait(bar_p + 16 * w + 8 * buf, done / 2 & 1, 5);
-                    // O is one for both streams: the other one's last tile has been drained.  (This
-                    // stream's own last one has, as its P is here, so the phase is the right one.)
-                    if (NP > 1) wait(bar_o_free, (i - C::AHEAD + 1) & 1, 9);
-                    fence_after();
-                    const uint64_t v = v_desc + k_at;
-#pragma unroll
-                    for (int pl = NP - 1; pl >= 0; --pl)
-#pragma unroll
-                        for (int x = 0; x < 2; ++x)  // O is kept (bf16), or drained after every tile
-                            mma_ts2(tmem + C::o_col(w), tmem + C::p_col(w, buf, pl) + 16 * x,
-                                    v + x * (32 * 128 / 16), idesc(D, true),
-                                    pl != NP - 1 || x != 0 || (NP == 1 && done) ? 1u : 0u);
-                    commit(bar_pv + 16 * w + 8 * buf);
-                    ++done;
-                }
-                if (QT == 1) {
-                    commit(bar_empty + 8 * used);
-                    if (i + STRIDE < steps) wait(bar_full + 8 * use.bar, use.phase, 3);
-                }
-            }
             }
             // nothing may be in flight when the tensor memory is released
             commit(bar_end);
@@ -901,7 +907,7 @@ __global__ void __launch_bounds__(Cfg<D, NP, QT, SRC>::THREADS, 1) window_prefil
                 __syncwarp();
                 if (lane == 0 && !wait.dead) {
                     const uint32_t bar = bar_page + 8 * stage;
-                    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "n"(C::PAGE) : "memory");
+                    bar_expect(bar, C::PAGE);
                     copy_bulk(q_smem + C::STAGE + stage * C::PAGE, from + at, C::PAGE, bar);
                     issued = t + 1;
                 }
@@ -914,7 +920,8 @@ __global__ void __launch_bounds__(Cfg<D, NP, QT, SRC>::THREADS, 1) window_prefil
             if (lane == 0) {
                 const uint64_t t0 = now_ns();
                 for (int t = max(0, issued - C::STAGES); t < issued; ++t)
-                    while (!bar_try(bar_page + 8 * (t % C::STAGES), t / C::STAGES & 1) && now_ns() - t0 < 2000000000ull) {}
+                    while (!bar_try(bar_page + 8 * (t % C::STAGES), t / C::STAGES & 1) &&
+                           now_ns() - t0 < 2000000000ull) {}
             }
         }
     } else if (tokens > 0) {
@@ -1079,18 +1086,8 @@ __global__ void __launch_bounds__(Cfg<D, NP, QT, SRC>::THREADS, 1) window_prefil
         } else
         for (int t = QT == 1 ? w : 0; t < n; t += QT == 1 ? 2 : 1) {
             if (QT == 2 && !takes(t)) continue;
-            // which positions of the page this row sees, one bit each
-            const bool masked = t < full0 || t >= full1;
-            uint32_t see[2] = {0xffffffffu, 0xffffffffu};
-            if (masked) {
-                const int b = page_at(t) * KT;
-                const uint64_t bits =
-                    live ? low_bits(min(pos, a.max_ctx - 1) - b + 1) &
-                               (~low_bits(pos - a.window + 1 - b) | low_bits(a.sinks - b))
-                         : 0ull;
-                see[0] = (uint32_t)bits;
-                see[1] = (uint32_t)(bits >> 32);
-            }
+            uint32_t see[2];
+            const bool masked = seen_of(t, see);
             const uint32_t buf = done & 1;
             wait(bar_s + 8 * w, done & 1, 6);
             __syncwarp();
@@ -1389,7 +1386,8 @@ __global__ void __launch_bounds__(Cfg<D, NP, QT, SRC>::THREADS, 1) window_prefil
     } else if (end == kPartNotFinite && warp < 8) {
         for (int i = warp; i < tokens * heads; i += 8) {
             const int64_t at = ((int64_t)(row0 + i / heads) * a.Hq + kvh * G + head0 + i % heads) * D;
-            walk_row<D, C::EIGHT, T>(a, req, kvh, pos0 + i / heads, static_cast<const T*>(a.q) + at, static_cast<T*>(a.o) + at);
+            walk_row<D, C::EIGHT, T>(a, req, kvh, pos0 + i / heads, static_cast<const T*>(a.q) + at,
+                                     static_cast<T*>(a.o) + at);
         }
     }
 }
@@ -1572,7 +1570,10 @@ Plan make_plan(bool q8, int M, int n_prompts, int Hq, int Hkv, int window, int s
     p.tok = 128 / p.heads;
     p.tiles = std::min<int64_t>((int64_t)M / p.tok + n_prompts, M) * Hkv * p.groups;
     const int64_t pages = visible_pages(p.tok, window, sinks, max_ctx);
-    p.splits = p.tiles < kSms ? (int)std::max<int64_t>(1, std::min<int64_t>(kSms / std::max<int64_t>(p.tiles, 1), most_parts(q8, pages))) : 1;
+    p.splits = 1;
+    if (p.tiles < kSms)
+        p.splits = (int)std::max<int64_t>(
+            1, std::min<int64_t>(kSms / std::max<int64_t>(p.tiles, 1), most_parts(q8, pages)));
     return p;
 }
 
@@ -1582,8 +1583,8 @@ bool two_tiles(int64_t tiles) { return tiles >= 2 * kSms; }
 // flags.  They are made where a page meets enough row tiles, and take kMostImages at most (else the
 // row tiles' loaders convert).  With images and without, us, by the row tiles that meet a page:
 //   fp32 rows                 1.5: 20.5 17.3   2: 35 41   4: 50 70   8: 68 108   16: 106 197
-//   bf16, one tile a block    2.5: 44.7 44.7   4: 29 32   8: 38 46   16: 46 68
-//   bf16, two                 5.6: 178 160     8: 59 56   12: 73 72  20: 127 135  32: 83 134  256: 1050 1364
+//   bf16, one tile a block    2.5: 44.7 44.7   4: 29 32   8: 38 46   16: 46 68   32: 83 134
+//   bf16, two                 5.6: 178 160     8: 59 56   12: 73 72  20: 127 135  256: 1050 1364
 constexpr int64_t kMostImages = 1ll << 30;
 constexpr int64_t kLeastReuse = 2;
 int64_t least_reuse(bool f32, int64_t tiles) { return f32 ? kLeastReuse : two_tiles(tiles) ? 12 : 4; }
@@ -1591,7 +1592,7 @@ struct Images {
     int pages;
     int64_t tiles, bytes;
 };
-Images images_of(int M, int n_prompts, int heads, int Hkv, int d, int window, int sinks, int max_ctx) {
+Images images_of(int M, int n_prompts, int Hkv, int d, int window, int sinks, int max_ctx) {
     Images m{};
     const int64_t pages = visible_pages(M, window, sinks, max_ctx);
     m.pages = (int)pages;
@@ -1600,7 +1601,9 @@ Images images_of(int M, int n_prompts, int heads, int Hkv, int d, int window, in
     return m;
 }
 // Row tiles that meet a page, about, when a prompt has `rows` rows.
-int64_t image_reuse(int64_t rows, int heads, int window) { return std::min<int64_t>(rows, (int64_t)window + KT) * heads / 128; }
+int64_t image_reuse(int64_t rows, int heads, int window) {
+    return std::min<int64_t>(rows, (int64_t)window + KT) * heads / 128;
+}
 
 template <int D, int NP, int QT, Source SRC, typename T>
 cudaError_t launch_t(const PrefillArgs& p, cudaStream_t st) {
@@ -1614,15 +1617,16 @@ cudaError_t launch_t(const PrefillArgs& p, cudaStream_t st) {
     if (blocks > 0x7fffffff) return cudaErrorInvalidValue;
     e = launch_pdl(window_prefill_kernel<D, NP, QT, SRC, T>, dim3((unsigned)blocks), C::THREADS, C::BYTES, st, p);
     if (e != cudaSuccess || p.splits == 1) return e;
-    return launch_pdl(window_join_kernel<D, Q8, T>, dim3((unsigned)(blocks / p.splits) * (D / (8 * kJoinVectors<Q8>))), 256, 0, st, p);
+    const dim3 joins((unsigned)(blocks / p.splits) * (D / (8 * kJoinVectors<Q8>)));
+    return launch_pdl(window_join_kernel<D, Q8, T>, joins, 256, 0, st, p);
 }
 
 template <int D, Source SRC>
 cudaError_t launch_d(const PrefillArgs& p, bool f32, int64_t tiles, cudaStream_t st) {
     if constexpr (SRC != kBf16) {
         if (p.images) {
-            const cudaError_t e = launch_pdl(window_image_kernel<D>, dim3((unsigned)(p.a.n_prompts * (int64_t)p.image_pages), p.a.Hkv),
-                                             256, 0, st, p);
+            const dim3 pages((unsigned)(p.a.n_prompts * (int64_t)p.image_pages), p.a.Hkv);
+            const cudaError_t e = launch_pdl(window_image_kernel<D>, pages, 256, 0, st, p);
             if (e != cudaSuccess) return e;
             return f32                ? launch_t<D, 3, 1, kImages, float>(p, st)
                    : two_tiles(tiles) ? launch_t<D, 1, 2, kImages, __nv_bfloat16>(p, st)
@@ -1643,9 +1647,9 @@ static uint64_t scratch_of(bool q8, int M, int n_prompts, int Hq, int Hkv, int d
     const Plan p = make_plan(q8, M, n_prompts, Hq, Hkv, window, sinks, max_ctx);
     const int64_t most = most_parts(q8, visible_pages(p.tok, window, sinks, max_ctx));  // parts of a row tile
     // (a smaller call may have all its rows in one prompt)
-    const uint64_t images = q8 && image_reuse(M, p.heads, window) >= kLeastReuse
-                                ? (std::min(images_of(M, n_prompts, p.heads, Hkv, d, window, sinks, max_ctx).bytes, kMostImages) + 31) / 16 * 16
-                                : 0;
+    uint64_t images = 0;
+    if (q8 && image_reuse(M, p.heads, window) >= kLeastReuse)
+        images = (std::min(images_of(M, n_prompts, Hkv, d, window, sinks, max_ctx).bytes, kMostImages) + 31) / 16 * 16;
     if (most < 2) return images ? kCounterBytes + images : 16;
     const uint64_t parts = std::min<int64_t>(kSms, p.tiles * most), tiles = std::min<int64_t>(kSms, p.tiles);
     const uint64_t n = kCounterBytes + tiles * 16 + parts * (128 * (d + 2) * sizeof(float) + sizeof(unsigned));
@@ -1677,7 +1681,7 @@ cudaError_t launch_any(const WindowArgs& a, bool f32, cudaStream_t st) {
     p.ml = reinterpret_cast<float2*>(p.rows + plan.tiles);
     p.ended = reinterpret_cast<unsigned*>(p.ml + plan.tiles * plan.splits * 128);
     if (SRC != kBf16 && image_reuse(a.rows / a.n_prompts, plan.heads, a.window) >= least_reuse(f32, plan.tiles)) {
-        const Images m = images_of(a.rows, a.n_prompts, plan.heads, a.Hkv, a.d, a.window, a.sinks, a.max_ctx);
+        const Images m = images_of(a.rows, a.n_prompts, a.Hkv, a.d, a.window, a.sinks, a.max_ctx);
         if (m.bytes <= kMostImages && a.n_prompts * (int64_t)m.pages <= 0x7fffffff) {
             // (of the scratch's end, which the parts do not reach)
             char* behind = reinterpret_cast<char*>(p.ended + plan.tiles * plan.splits);
