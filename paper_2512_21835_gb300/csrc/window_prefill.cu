@@ -71,7 +71,7 @@
 // queue does not run dry over their answers (1168 -> 1055 us).
 // Measured: 8192 bf16 rows of 32 heads of 128 behind 8192, all visible: 1055 us in a graph, 1563 TFLOP/s
 // (tensor pipe active 68%, 1500 cycles a step of which the tensor core works 1280), with the images' 17;
-// with kCodes 1356.  4999 ragged rows of 40 heads in 7 prompts, window 1024: 159 us (920 blocks, 17
+// with kCodes 1356.  4999 ragged rows of 40 heads in 7 prompts, window 1024: 157 us (920 blocks, 17
 // pages each: 17 us of pages, 10 us around them: launch and tensor memory 2, first tile 4.5, outputs
 // 3.3).  fp32: 2048 rows behind 6144 570 us, 422 TFLOP/s (bound by the softmax: three planes of P and O
 // drained every tile); 47 rows behind 1041 17.2 us (two launches and a chain of latencies).
@@ -130,7 +130,8 @@ struct Cfg {
     static constexpr int TILE = SLABS * KV_SLAB;       // one tile of keys or of values
     static constexpr int SLOT = 2 * TILE;              // the keys of one tile, the values of an earlier one
     static constexpr int PAGE = Q8 ? 4 * q8::Granule<D>::BYTES : 0;  // a page's part of a kv head, as it is cached
-    static constexpr int STAGES = Q8 && NP == 1 ? 3 : 2;             // of those
+    // of those; with two row tiles a fourth slot of the ring does more than a third page (159.7 -> 157.4 us)
+    static constexpr int STAGES = Q8 && NP == 1 && QT == 1 ? 3 : 2;
     static constexpr int ROOM = 227 * 1024 - 1024 - 512 - Q_BYTES - STAGES * PAGE;
     static constexpr int LIMIT = EIGHT ? 5 : 12;
     static constexpr int MOST = ROOM / SLOT < LIMIT ? ROOM / SLOT : LIMIT;
