@@ -686,32 +686,40 @@ def loip_k_cache_q8_layer_bytes(Hkv, d) -> int:
     return Hkv * 132 * d
 
 
-def _cache_q8(x, rows):
+def _cache_q8(x, rows, *others):
     """Address of the cache, which lies in device memory: the prompt kernels' bulk copies read no other.  Refuses
-    rows on another device than the current one, whose stream the call goes to."""
+    tensors of another device than the current one, whose stream the call goes to: the rows, the cache, and the
+    others that are tensors of some device at all."""
     if not _of_torch:
         _torch()
-    if rows.get_device() != _of_torch[1]():
-        _refuse(f"rows on device {rows.get_device()} in a call on device {_of_torch[1]()}")
+    here = _of_torch[1]()
+    if rows.get_device() != here:
+        _refuse(f"rows on device {rows.get_device()} in a call on device {here}")
+    for y in others:
+        if y is not None and not isinstance(y, (int, np.ndarray)) and y.get_device() not in (here, -1):
+            _refuse(f"a tensor on device {y.get_device()} in a call on device {here}")
     if x is None or isinstance(x, int):
         return x
     if not x.is_cuda or not x.is_contiguous():
         _refuse("the 8-bit cache is a contiguous tensor in device memory, or an address")
+    if x.get_device() != here:
+        _refuse(f"a cache on device {x.get_device()} in a call on device {here}")
     return x.data_ptr()
 
 
 def loip_k_qk_append_q8(qkv, g_q, g_k, Hq, Hkv, d, eps, theta, positions, row_req, q_out, kv_base, page_offsets,
                         max_pages, page_tokens, layer, layer_page_bytes, stream=None):
     """loip_k_qk_append into the 8-bit cache."""
-    _append(lib().loip_k_qk_append_q8, qkv, g_q, g_k, Hq, Hkv, d, eps, theta, positions, row_req, q_out,
-            _cache_q8(kv_base, qkv), page_offsets, max_pages, page_tokens, layer, layer_page_bytes, stream)
+    kv = _cache_q8(kv_base, qkv, q_out, g_q, g_k, positions, row_req, page_offsets)
+    _append(lib().loip_k_qk_append_q8, qkv, g_q, g_k, Hq, Hkv, d, eps, theta, positions, row_req, q_out, kv, page_offsets,
+            max_pages, page_tokens, layer, layer_page_bytes, stream)
 
 
 def loip_k_cache_read_q8(kv_base, page_offsets, max_pages, positions, row_req, Hkv, d, page_tokens, layer,
                          layer_page_bytes, out, stream=None):
     """Rows of the 8-bit cache as numbers: out [T, 2 * Hkv * d] float32 or bfloat16 (key heads, value heads) for the
     positions [T] of the requests row_req [T] (None: row t is of request t); page_offsets [requests, max_pages]."""
-    kv = _cache_q8(kv_base, out)
+    kv = _cache_q8(kv_base, out, page_offsets, positions, row_req)
     T, dtype, n_req = out.shape[0], _of_torch[2].get(out.dtype), page_offsets.shape[0]
     if dtype is None or not out.is_contiguous() or out.numel() != T * 2 * Hkv * d:
         _refuse("out is contiguous [T, 2 * Hkv * d], float32 or bfloat16")
@@ -730,8 +738,9 @@ def loip_k_window_attention_q8_scratch_bytes(B, Hq, Hkv, d, window, sinks, max_c
 def loip_k_window_attention_q8(q, kv_base, page_offsets, max_pages, ctx_lens, Hq, Hkv, d, page_tokens, layer,
                                layer_page_bytes, window, sinks, max_ctx, scratch, o, stream=None):
     """loip_k_window_attention over the 8-bit cache."""
-    _attention(lib().loip_k_window_attention_q8, q, _cache_q8(kv_base, q), page_offsets, max_pages, ctx_lens, Hq, Hkv, d,
-               page_tokens, layer, layer_page_bytes, window, sinks, max_ctx, scratch, o, stream)
+    _attention(lib().loip_k_window_attention_q8, q, _cache_q8(kv_base, q, o, page_offsets, ctx_lens, scratch), page_offsets,
+               max_pages, ctx_lens, Hq, Hkv, d, page_tokens, layer, layer_page_bytes, window, sinks, max_ctx, scratch, o,
+               stream)
 
 
 def loip_k_window_prefill_q8_scratch_bytes(M, n_prompts, Hq, Hkv, d, window, sinks, max_ctx) -> int:
@@ -741,5 +750,6 @@ def loip_k_window_prefill_q8_scratch_bytes(M, n_prompts, Hq, Hkv, d, window, sin
 def loip_k_window_prefill_q8(q, kv_base, page_offsets, max_pages, row_starts, first_pos, Hq, Hkv, d, page_tokens,
                              layer, layer_page_bytes, window, sinks, max_ctx, scratch, o, stream=None):
     """loip_k_window_prefill over the 8-bit cache."""
-    _prefill(lib().loip_k_window_prefill_q8, q, _cache_q8(kv_base, q), page_offsets, max_pages, row_starts, first_pos, Hq, Hkv, d,
-             page_tokens, layer, layer_page_bytes, window, sinks, max_ctx, scratch, o, stream)
+    kv = _cache_q8(kv_base, q, o, page_offsets, row_starts, first_pos, scratch)
+    _prefill(lib().loip_k_window_prefill_q8, q, kv, page_offsets, max_pages, row_starts, first_pos, Hq, Hkv, d, page_tokens,
+             layer, layer_page_bytes, window, sinks, max_ctx, scratch, o, stream)
