@@ -10,7 +10,7 @@ import sysconfig
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 OUT = os.path.join(HERE, "libloip.so")
-CALLS = os.path.join(HERE, "_calls.so")  # the extension module of csrc/calls.c
+CALLS = os.path.join(HERE, "_calls" + sysconfig.get_config_var("EXT_SUFFIX"))  # the extension module of csrc/calls.c
 BUILD = os.path.join(HERE, "_build")
 SOURCES = ["decode.cu", "prefill.cu", "gemm_tc.cu", "attn_tc.cu", "pack.cu", "runtime.cu", "plan.cpp", "hostpool.cpp", "noalloc.cu",
            "disktier.cpp", "window.cu", "window_decode.cu", "window_prefill.cu"]
@@ -27,7 +27,7 @@ def _nvcc() -> str:
 def _stale() -> bool:
     if not (os.path.exists(OUT) and os.path.exists(CALLS)):
         return True
-    t = os.path.getmtime(OUT)
+    t = min(os.path.getmtime(OUT), os.path.getmtime(CALLS))
     deps = [os.path.join(CSRC, f) for f in os.listdir(CSRC)] + [os.path.join(HERE, "..", "include", "loip.h")]
     return any(os.path.getmtime(p) > t for p in deps if os.path.exists(p))
 
@@ -51,19 +51,22 @@ def build(force: bool = False, verbose: bool = False) -> str:
 
     with cf.ThreadPoolExecutor(max_workers=len(SOURCES)) as ex:
         objs = list(ex.map(compile_one, SOURCES))
-    tmp = OUT + ".tmp"
-    cmd = [nvcc] + ARCH + ["-shared", "-cudart", "shared", "-o", tmp] + objs
-    r = subprocess.run(cmd, capture_output=True, text=True)
-    if r.returncode != 0:
-        raise RuntimeError(f"link failed:\n{r.stdout}\n{r.stderr}")
-    os.replace(tmp, OUT)
-    tmp = CALLS + ".tmp"
-    cmd = ["gcc", "-O2", "-shared", "-fPIC", "-I", sysconfig.get_paths()["include"], os.path.join(CSRC, "calls.c"), "-o", tmp,
-           "-L", HERE, "-l:" + os.path.basename(OUT), "-Wl,-rpath,$ORIGIN", "-Wl,--allow-shlib-undefined"]
-    r = subprocess.run(cmd, capture_output=True, text=True)
-    if r.returncode != 0:
-        raise RuntimeError(f"gcc failed on calls.c:\n{r.stdout}\n{r.stderr}")
-    os.replace(tmp, CALLS)
+    # Both files are made before either takes its place: an extension module never meets a library of other sources.
+    lib, calls = os.path.join(BUILD, os.path.basename(OUT)), os.path.join(BUILD, os.path.basename(CALLS))
+
+    def link(what, cmd):
+        r = subprocess.run([nvcc] + cmd, capture_output=True, text=True)
+        if r.returncode != 0:
+            raise RuntimeError(f"nvcc failed on {what}:\n{r.stdout}\n{r.stderr}")
+
+    link("the library", ARCH + ["-shared", "-cudart", "shared", "-o", lib] + objs)
+    link("calls.c", ["-shared", "-cudart", "none", "-O2", "-Xcompiler", "-fPIC", "-I", sysconfig.get_paths()["include"],
+                     os.path.join(CSRC, "calls.c"), "-o", calls, "-L", BUILD, "-lloip", "-Xlinker", "-rpath=$ORIGIN",
+                     "-Xlinker", "--allow-shlib-undefined"])
+    if os.path.exists(CALLS):
+        os.remove(CALLS)
+    os.replace(lib, OUT)
+    os.replace(calls, CALLS)
     return OUT
 
 
