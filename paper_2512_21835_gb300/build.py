@@ -24,10 +24,16 @@ def _nvcc() -> str:
     raise RuntimeError("nvcc not found: the CUDA toolkit is required to build libloip")
 
 
+def _made() -> list:
+    """What a build makes: the library, and the extension module where Python's headers are installed (without
+    it the same entries are called through ctypes, a microsecond slower)."""
+    return [OUT, CALLS] if os.path.exists(os.path.join(sysconfig.get_paths()["include"], "Python.h")) else [OUT]
+
+
 def _stale() -> bool:
-    if not (os.path.exists(OUT) and os.path.exists(CALLS)):
+    if not all(os.path.exists(f) for f in _made()):
         return True
-    t = min(os.path.getmtime(OUT), os.path.getmtime(CALLS))
+    t = min(os.path.getmtime(f) for f in _made())
     deps = [os.path.join(CSRC, f) for f in os.listdir(CSRC)] + [os.path.join(HERE, "..", "include", "loip.h")]
     return any(os.path.getmtime(p) > t for p in deps if os.path.exists(p))
 
@@ -60,13 +66,15 @@ def build(force: bool = False, verbose: bool = False) -> str:
             raise RuntimeError(f"nvcc failed on {what}:\n{r.stdout}\n{r.stderr}")
 
     link("the library", ARCH + ["-shared", "-cudart", "shared", "-o", lib] + objs)
-    link("calls.c", ["-shared", "-cudart", "none", "-O2", "-Xcompiler", "-fPIC", "-I", sysconfig.get_paths()["include"],
-                     os.path.join(CSRC, "calls.c"), "-o", calls, "-L", BUILD, "-lloip", "-Xlinker", "-rpath=$ORIGIN",
-                     "-Xlinker", "--allow-shlib-undefined"])
+    if CALLS in _made():
+        link("calls.c", ["-shared", "-cudart", "none", "-O2", "-Xcompiler", "-fPIC", "-I", sysconfig.get_paths()["include"],
+                         os.path.join(CSRC, "calls.c"), "-o", calls, "-L", BUILD, "-lloip", "-Xlinker", "-rpath=$ORIGIN",
+                         "-Xlinker", "--allow-shlib-undefined"])
     if os.path.exists(CALLS):
         os.remove(CALLS)
     os.replace(lib, OUT)
-    os.replace(calls, CALLS)
+    if CALLS in _made():
+        os.replace(calls, CALLS)
     return OUT
 
 

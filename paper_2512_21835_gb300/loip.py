@@ -12,6 +12,8 @@ import os
 
 import numpy as np
 
+from . import build
+
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libloip.so")
 
@@ -149,11 +151,12 @@ def lib():
             f = getattr(L, name)
             f.restype = res
             f.argtypes = args
-        # the windowed-serving entries, called without ctypes' conversions (csrc/calls.c)
-        from . import _calls
-        for name in dir(_calls):
-            if name.startswith("loip_k_"):
-                setattr(L, name, getattr(_calls, name))
+        # the windowed-serving entries, called without ctypes' conversions (csrc/calls.c) where that was built
+        if os.path.exists(build.CALLS):
+            from . import _calls
+            for name in dir(_calls):
+                if name.startswith("loip_k_"):
+                    setattr(L, name, getattr(_calls, name))
         _lib = L
     return _lib
 

@@ -82,3 +82,33 @@ def test_one_compiler(tree, monkeypatch):
     commands = compiler(monkeypatch)
     B.build()
     assert {c[0] for c in commands} == {"nvcc"}
+
+
+def test_without_python_headers(tree, monkeypatch):
+    """The library is built all the same, and no module of an earlier build stays beside it."""
+    commands = compiler(monkeypatch)
+    B.build()
+    monkeypatch.setattr(B.sysconfig, "get_paths", lambda: dict(include=str(tree / "nowhere")))
+    os.utime(tree / "csrc" / "a.cu", (os.path.getmtime(B.OUT) + 10,) * 2)
+    commands.clear()
+    B.build()
+    assert commands and not any("calls.c" in c for cmd in commands for c in cmd)
+    assert os.path.exists(B.OUT) and not os.path.exists(B.CALLS)
+    age(tree / "csrc" / "a.cu", 1000)
+    age(tree / "csrc" / "calls.c", 1000)
+    assert not B._stale()
+
+
+def test_entries_without_the_extension(monkeypatch):
+    """Without it the windowed-serving entries are called through ctypes, with the same refusals."""
+    import ctypes as C
+
+    from paper_2512_21835_gb300 import loip
+    B.build()
+    monkeypatch.setattr(B, "CALLS", B.CALLS + ".missing")
+    monkeypatch.setattr(loip, "_lib", None)
+    L = loip.lib()
+    for name in ("loip_k_qk_append", "loip_k_window_attention_q8", "loip_k_cache_read_q8"):
+        sig = loip._SIGS[name][1]
+        zero = [0.0 if t is C.c_float else None if t is C.c_void_p else 0 for t in sig]
+        assert isinstance(getattr(L, name), C._CFuncPtr) and getattr(L, name)(*zero) == loip.ERR_INVALID
