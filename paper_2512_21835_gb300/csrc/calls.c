@@ -40,8 +40,10 @@ static int64_t i64(PyObject* o, int* bad) {
     return v;
 }
 static uint64_t u64(PyObject* o, int* bad) {
-    const unsigned long long v = PyLong_AsUnsignedLongLong(o);
+    PyObject* whole = PyNumber_Index(o); /* (unlike the signed conversion, the unsigned one asks for an int) */
+    const unsigned long long v = whole ? PyLong_AsUnsignedLongLong(whole) : (unsigned long long)-1;
     if (v == (unsigned long long)-1 && PyErr_Occurred()) *bad = 1;
+    Py_XDECREF(whole);
     return v;
 }
 static float f32(PyObject* o, int* bad) {

@@ -1,0 +1,31 @@
+"""What the extension module of the windowed-serving entries does with arguments that do not convert, and what the
+binding makes of it (host only)."""
+import ctypes as C
+
+import numpy as np
+import pytest
+
+from paper_2512_21835_gb300 import loip
+
+NAMES = [n + s for s in ("", "_q8") for n in ("loip_k_qk_append", "loip_k_window_attention", "loip_k_window_prefill")]
+NAMES.append("loip_k_cache_read_q8")
+
+
+@pytest.fixture(scope="module")
+def calls():
+    from paper_2512_21835_gb300 import build
+    build.build()
+    loip.lib()
+    return pytest.importorskip("paper_2512_21835_gb300._calls")
+
+
+def zeros(name):
+    return [0.0 if t is C.c_float else None if t is C.c_void_p else 0 for t in loip._SIGS[name][1]]
+
+
+@pytest.mark.parametrize("number", [np.int64, np.uint64, np.int32, bool])
+@pytest.mark.parametrize("name", NAMES)
+def test_whole_numbers_of_other_types(calls, name, number):
+    """Numbers that are not Python's own (a size that numpy has worked out), as ctypes takes them."""
+    args = [0.0 if t is C.c_float else None if t is C.c_void_p else number(0) for t in loip._SIGS[name][1]]
+    assert getattr(calls, name)(*args) == loip.ERR_INVALID
