@@ -11,9 +11,9 @@
 
 #include "../../include/loip.h"
 
-/* Each sets *bad where Python has raised an error. */
+/* Each sets *bad where Python has raised an error, and does nothing where it has before. */
 static void* ptr(PyObject* o, int* bad) {
-    if (o == Py_None) return NULL;
+    if (*bad || o == Py_None) return NULL;
     if (!PyLong_Check(o)) {
         PyObject* v = PyObject_GetAttrString(o, "value"); /* c_void_p and the like */
         void* p = v ? ptr(v, bad) : (*bad = 1, NULL);
@@ -25,6 +25,7 @@ static void* ptr(PyObject* o, int* bad) {
     return p;
 }
 static int32_t i32(PyObject* o, int* bad) {
+    if (*bad) return 0;
     const long long v = PyLong_AsLongLong(o);
     if (v == -1 && PyErr_Occurred()) {
         *bad = 1;
@@ -35,11 +36,13 @@ static int32_t i32(PyObject* o, int* bad) {
     return (int32_t)v;
 }
 static int64_t i64(PyObject* o, int* bad) {
+    if (*bad) return 0;
     const long long v = PyLong_AsLongLong(o);
     if (v == -1 && PyErr_Occurred()) *bad = 1;
     return v;
 }
 static uint64_t u64(PyObject* o, int* bad) {
+    if (*bad) return 0;
     PyObject* whole = PyNumber_Index(o); /* (unlike the signed conversion, the unsigned one asks for an int) */
     const unsigned long long v = whole ? PyLong_AsUnsignedLongLong(whole) : (unsigned long long)-1;
     if (v == (unsigned long long)-1 && PyErr_Occurred()) *bad = 1;
@@ -47,6 +50,7 @@ static uint64_t u64(PyObject* o, int* bad) {
     return v;
 }
 static float f32(PyObject* o, int* bad) {
+    if (*bad) return 0.f;
     const double v = PyFloat_AsDouble(o);
     if (v == -1.0 && PyErr_Occurred()) *bad = 1;
     return (float)v;

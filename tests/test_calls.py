@@ -29,3 +29,32 @@ def test_whole_numbers_of_other_types(calls, name, number):
     """Numbers that are not Python's own (a size that numpy has worked out), as ctypes takes them."""
     args = [0.0 if t is C.c_float else None if t is C.c_void_p else number(0) for t in loip._SIGS[name][1]]
     assert getattr(calls, name)(*args) == loip.ERR_INVALID
+
+
+class Number:
+    """A whole number and a float that say when they are looked at."""
+
+    def __init__(self, seen, error=None):
+        self.seen, self.error = seen, error
+
+    def __index__(self):
+        self.seen.append(self)
+        if self.error:
+            raise self.error
+        return 0
+
+    def __float__(self):
+        return float(self.__index__())
+
+
+@pytest.mark.parametrize("name", NAMES)
+def test_nothing_is_converted_behind_an_error(calls, name):
+    sig = loip._SIGS[name][1]
+    numbers = [i for i, t in enumerate(sig) if t is not C.c_void_p]
+    for first in numbers:
+        seen, args = [], zeros(name)
+        for i in numbers:
+            args[i] = Number(seen, ZeroDivisionError(f"argument {i}") if i >= first else None)
+        with pytest.raises(ZeroDivisionError, match=f"argument {first}$"):
+            getattr(calls, name)(*args)
+        assert len(seen) == numbers.index(first) + 1
