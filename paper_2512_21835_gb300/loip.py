@@ -602,6 +602,16 @@ def _cache(x):
     return x.data_ptr()
 
 
+def _call(entry, *args):
+    """An entry of the windowed operators; what does not fit its arguments' types is refused as everything else is."""
+    try:
+        rc = entry(*args)
+    except OverflowError as e:
+        _refuse(str(e))
+    if rc:
+        _check(rc)
+
+
 def _scratch(x):
     if not x.is_cuda or not x.is_contiguous():
         _refuse("the scratch is a contiguous CUDA tensor")
@@ -617,12 +627,10 @@ def _append(entry, qkv, g_q, g_k, Hq, Hkv, d, eps, theta, positions, row_req, q_
     n_req = page_offsets.shape[0]
     if q_out.numel() != T * Hq * d or width != (Hq + 2 * Hkv) * d:
         _refuse("qkv and q_out do not fit together")
-    rc = entry(qkv.data_ptr(), dtype, row_stride, T, Hq, Hkv, d, _gain(g_q, d), _gain(g_k, d), eps, theta,
-               _ints(positions, T, "positions"), None if row_req is None else _ints(row_req, T, "row_req"), n_req,
-               q_out.data_ptr(), kv, _pages(page_offsets, n_req, max_pages), max_pages, page_tokens, layer, layer_page_bytes,
-               _s(stream))
-    if rc:
-        _check(rc)
+    _call(entry, qkv.data_ptr(), dtype, row_stride, T, Hq, Hkv, d, _gain(g_q, d), _gain(g_k, d), eps, theta,
+          _ints(positions, T, "positions"), None if row_req is None else _ints(row_req, T, "row_req"), n_req,
+          q_out.data_ptr(), kv, _pages(page_offsets, n_req, max_pages), max_pages, page_tokens, layer, layer_page_bytes,
+          _s(stream))
 
 
 def _attention(entry, q, kv, page_offsets, max_pages, ctx_lens, Hq, Hkv, d, page_tokens, layer, layer_page_bytes,
@@ -630,11 +638,9 @@ def _attention(entry, q, kv, page_offsets, max_pages, ctx_lens, Hq, Hkv, d, page
     B, dtype = q.shape[0], _dtype(q, o)
     if not (q.is_contiguous() and o.is_contiguous()) or q.numel() != B * Hq * d or o.numel() != q.numel():
         _refuse("q and o are contiguous [B, Hq * d]")
-    rc = entry(q.data_ptr(), dtype, kv, _pages(page_offsets, B, max_pages), max_pages,
-               _ints(ctx_lens, B, "ctx_lens"), B, Hq, Hkv, d, page_tokens, layer, layer_page_bytes, window, sinks, max_ctx,
-               _scratch(scratch), scratch.nbytes, o.data_ptr(), _s(stream))
-    if rc:
-        _check(rc)
+    _call(entry, q.data_ptr(), dtype, kv, _pages(page_offsets, B, max_pages), max_pages,
+          _ints(ctx_lens, B, "ctx_lens"), B, Hq, Hkv, d, page_tokens, layer, layer_page_bytes, window, sinks, max_ctx,
+          _scratch(scratch), scratch.nbytes, o.data_ptr(), _s(stream))
 
 
 def _prefill(entry, q, kv, page_offsets, max_pages, row_starts, first_pos, Hq, Hkv, d, page_tokens, layer,
@@ -643,12 +649,10 @@ def _prefill(entry, q, kv, page_offsets, max_pages, row_starts, first_pos, Hq, H
     if not (q.is_contiguous() and o.is_contiguous()) or q.numel() != M * Hq * d or o.numel() != q.numel():
         _refuse("q and o are contiguous [M, Hq * d]")
     n = row_starts.numel() - 1
-    rc = entry(q.data_ptr(), dtype, kv, _pages(page_offsets, n, max_pages), max_pages,
-               _ints(row_starts, 1, "row_starts"), None if first_pos is None else _ints(first_pos, n, "first_pos"), n, M,
-               Hq, Hkv, d, page_tokens, layer, layer_page_bytes, window, sinks, max_ctx, _scratch(scratch),
-               scratch.nbytes, o.data_ptr(), _s(stream))
-    if rc:
-        _check(rc)
+    _call(entry, q.data_ptr(), dtype, kv, _pages(page_offsets, n, max_pages), max_pages,
+          _ints(row_starts, 1, "row_starts"), None if first_pos is None else _ints(first_pos, n, "first_pos"), n, M,
+          Hq, Hkv, d, page_tokens, layer, layer_page_bytes, window, sinks, max_ctx, _scratch(scratch),
+          scratch.nbytes, o.data_ptr(), _s(stream))
 
 
 def loip_k_qk_append(qkv, g_q, g_k, Hq, Hkv, d, eps, theta, positions, row_req, q_out, kv_base, page_offsets,
@@ -726,12 +730,9 @@ def loip_k_cache_read_q8(kv_base, page_offsets, max_pages, positions, row_req, H
     T, dtype, n_req = out.shape[0], _of_torch[2].get(out.dtype), page_offsets.shape[0]
     if dtype is None or not out.is_contiguous() or out.numel() != T * 2 * Hkv * d:
         _refuse("out is contiguous [T, 2 * Hkv * d], float32 or bfloat16")
-    rc = lib().loip_k_cache_read_q8(kv, _pages(page_offsets, n_req, max_pages), max_pages,
-                                    _ints(positions, T, "positions"),
-                                    None if row_req is None else _ints(row_req, T, "row_req"), n_req, T, Hkv, d,
-                                    page_tokens, layer, layer_page_bytes, out.data_ptr(), dtype, _s(stream))
-    if rc:
-        _check(rc)
+    _call(lib().loip_k_cache_read_q8, kv, _pages(page_offsets, n_req, max_pages), max_pages,
+          _ints(positions, T, "positions"), None if row_req is None else _ints(row_req, T, "row_req"), n_req, T, Hkv, d,
+          page_tokens, layer, layer_page_bytes, out.data_ptr(), dtype, _s(stream))
 
 
 def loip_k_window_attention_q8_scratch_bytes(B, Hq, Hkv, d, window, sinks, max_ctx) -> int:

@@ -58,3 +58,36 @@ def test_nothing_is_converted_behind_an_error(calls, name):
         with pytest.raises(ZeroDivisionError, match=f"argument {first}$"):
             getattr(calls, name)(*args)
         assert len(seen) == numbers.index(first) + 1
+
+
+class Overflowing:
+    """A library whose entries find a number that does not fit."""
+
+    def __getattr__(self, name):
+        def entry(*a):
+            raise OverflowError("an argument does not fit into 32 bits")
+        return entry
+
+
+def test_numbers_past_their_type_are_refusals(monkeypatch):
+    """The binding's error is that of every other refusal."""
+    import test_q8_refusals as R
+    import test_window_binding as W
+    loip._torch()
+    monkeypatch.setattr(loip, "_of_torch", [loip._of_torch[0], lambda: 0, *loip._of_torch[2:]])  # device 0 is current
+    monkeypatch.setattr(loip, "lib", lambda: Overflowing())
+    for call in (W.append, W.attention, W.prefill, R.b_append, R.b_read, R.b_attention, R.b_prefill):
+        with pytest.raises(loip.LoipError, match="32 bits") as e:
+            call()
+        assert e.value.code == loip.ERR_INVALID
+
+
+@pytest.mark.parametrize("number", [1 << 31, -(1 << 31) - 1, 1 << 32, 1 << 70])
+@pytest.mark.parametrize("name", NAMES)
+def test_numbers_past_their_type(calls, name, number):
+    """Not cut off to another number, which the library may accept."""
+    sig = loip._SIGS[name][1]
+    for i, t in enumerate(sig):
+        if t is C.c_int32 or (t is C.c_uint64 and number < 0):
+            with pytest.raises(OverflowError):
+                getattr(calls, name)(*zeros(name)[:i], number, *zeros(name)[i + 1:])
