@@ -3,7 +3,9 @@
  * The smallest calls of these operators take the GPU two or three microseconds, and ctypes takes
  * one and a half to convert their fifteen to twenty-two arguments.  Here an argument is one C API
  * call.  Arguments and results are those of the ctypes functions, which these take the place of:
- * whole numbers, floats, and addresses as whole numbers, None or ctypes pointers. */
+ * whole numbers, floats, and addresses as whole numbers, None or whatever ctypes takes for a pointer
+ * (but text).  Two things differ: a number past its type is an OverflowError and not cut off, and what is no
+ * number is a TypeError where ctypes has an ArgumentError. */
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 #include <limits.h>
@@ -14,13 +16,22 @@
 /* Each sets *bad where Python has raised an error, and does nothing where it has before. */
 static void* ptr(PyObject* o, int* bad) {
     if (*bad || o == Py_None) return NULL;
-    if (!PyLong_Check(o)) {
-        PyObject* v = PyObject_GetAttrString(o, "value"); /* c_void_p and the like */
-        void* p = v ? ptr(v, bad) : (*bad = 1, NULL);
+    void* p = NULL;
+    if (PyLong_Check(o)) {
+        p = PyLong_AsVoidPtr(o);
+    } else if (PyUnicode_Check(o) || PyBytes_Check(o)) {
+        PyErr_SetString(PyExc_TypeError, "an address is a number, None or a ctypes pointer");
+    } else { /* the address that ctypes would pass */
+        PyObject* ctypes = PyImport_ImportModule("ctypes");
+        PyObject* type = ctypes ? PyObject_GetAttrString(ctypes, "c_void_p") : NULL;
+        PyObject* at = type ? PyObject_CallMethod(ctypes, "cast", "OO", o, type) : NULL;
+        PyObject* v = at ? PyObject_GetAttrString(at, "value") : NULL;
+        if (v && v != Py_None) p = PyLong_AsVoidPtr(v);
         Py_XDECREF(v);
-        return p;
+        Py_XDECREF(at);
+        Py_XDECREF(type);
+        Py_XDECREF(ctypes);
     }
-    void* p = PyLong_AsVoidPtr(o);
     if (!p && PyErr_Occurred()) *bad = 1;
     return p;
 }

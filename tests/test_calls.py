@@ -91,3 +91,38 @@ def test_numbers_past_their_type(calls, name, number):
         if t is C.c_int32 or (t is C.c_uint64 and number < 0):
             with pytest.raises(OverflowError):
                 getattr(calls, name)(*zeros(name)[:i], number, *zeros(name)[i + 1:])
+
+
+def pointers(name):
+    return [i for i, t in enumerate(loip._SIGS[name][1]) if t is C.c_void_p]
+
+
+@pytest.mark.parametrize("name", NAMES)
+def test_addresses_of_every_kind(calls, name):
+    """What ctypes takes as an address: arrays, pointers and references are theirs; the number in an int object is none."""
+    number, array = C.c_int(64), (C.c_int * 4)()
+    for i in pointers(name):
+        for good in (C.c_void_p(64), C.c_void_p(), array, C.pointer(number), C.byref(number), True):
+            args = zeros(name)
+            args[i] = good
+            assert getattr(calls, name)(*args) == loip.ERR_INVALID
+        for bad in (number, C.c_uint64(64), C.c_float(1), 1.0, np.float64(1), np.int64(64), "x", b"x", object()):
+            args = zeros(name)
+            args[i] = bad
+            with pytest.raises((TypeError, C.ArgumentError)):
+                getattr(calls, name)(*args)
+
+
+def test_an_address_is_the_objects_own(calls):
+    """The check of alignment sees the address that ctypes would pass."""
+    raw = C.create_string_buffer(64)
+    at = C.addressof(raw)
+    at16, odd = at + -at % 16, at + -at % 16 + 4
+    name = "loip_k_cache_read_q8"  # kv_base and page_offsets come first; the shape is right, T is 0
+    def read(kv, table=16):
+        return getattr(calls, name)(kv, table, 1, None, None, 1, 0, 1, 64, 64, 0, 132 * 64, None, 0, None)
+    for make in (C.c_void_p, lambda a: (C.c_int * 4).from_address(a), lambda a: C.pointer(C.c_int.from_address(a)),
+                 lambda a: C.byref(C.c_int.from_address(a)), int):
+        assert read(make(at16)) == loip.OK
+        assert read(make(odd)) == loip.ERR_INVALID
+        assert read(make(at16), make(odd)) == loip.ERR_INVALID
