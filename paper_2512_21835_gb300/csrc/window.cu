@@ -109,12 +109,18 @@ __device__ __forceinline__ void store8(__nv_bfloat16* p, const float (&v)[8]) {
 // the bank conflicts went: eight blocks per SM 18.3, six 20.7, two tokens per block 19.9,
 // one wave of blocks that walk over the tokens with the next one's loads in flight 28.7).
 //
+// The next launch may come from the start for fp32 rows into the bf16 cache, and once the loads are done for the others
+// (in a graph, late and early: 76 fp32 rows of 48 heads 2.57 and 2.20 us, 304 4.49 and 3.73; 304 bf16 ones 2.69 and
+// 3.10; 1 to 40 rows and 512 and more alike).
+//
 // Q8: keys and values go to the 8-bit cache (q8.h); the four lanes that hold a block's 32 elements find its
 // exponent with two shuffles.  8191 fp32 tokens of 120 heads of 128: 119 us, 6.4 TB/s.
 template <int D, typename T, bool Q8>
 __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 8 : 6) qk_append_kernel(const __grid_constant__ AppendArgs p) {
     constexpr int LANES = D / 16;
     __shared__ float4 turn[4][LANES];  // cos, sin of elements 8l + 2k and 8l + 2k + 1 at [k][l]: no bank conflicts
+    constexpr bool EARLY = !Q8 && sizeof(T) == 4;
+    if (EARLY) pdl_trigger();
     pdl_wait();
     const int t = blockIdx.x, l = threadIdx.x % LANES, head = blockIdx.y * p.heads + threadIdx.x / LANES;
     const bool live = head < min(p.Hq + 2 * p.Hkv, (int)(blockIdx.y + 1) * p.heads);
@@ -142,7 +148,7 @@ __global__ void __launch_bounds__(256, sizeof(T) == 2 ? 8 : 6) qk_append_kernel(
         reinterpret_cast<float2*>(&turn[threadIdx.x % 8 / 2][threadIdx.x / 8])[threadIdx.x % 2] = make_float2(c, s);
     }
     __syncthreads();
-    pdl_trigger();
+    if (!EARLY) pdl_trigger();
     float a[8], b[8];
     if (live) {
         ra.values(a);
