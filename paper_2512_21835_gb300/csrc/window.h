@@ -20,9 +20,9 @@ constexpr int kMaxCounters = 16384;
 constexpr uint64_t kCounterBytes = kMaxCounters * sizeof(unsigned);
 
 // Programmatic dependent launch: a kernel of this family lets its successor in the stream
-// be launched once all its own blocks are at work (from pdl_trigger on), and reads or writes global memory only
-// after pdl_wait, which returns when the predecessor is complete and its writes are
-// visible.  What overlaps is the launch and the set-up of a block.  The read-only path
+// be launched once all its own blocks are at work (from pdl_trigger on, or at their end),
+// and reads or writes global memory only after pdl_wait, which returns when the
+// predecessor is complete and its writes are visible.  What overlaps is the launch and the set-up of a block.  The read-only path
 // (ld.global.nc, __ldg) is not used for anything that a predecessor may write: the kernel
 // may have been resident while that was written.
 #ifdef __CUDACC__

@@ -26,8 +26,8 @@
 //
 // Measured (GB300, in a graph): 64 requests behind a 4096-token window, 64 heads of 128: 175
 // us, 6.0 TB/s (fp32 183, 5.7 TB/s; heads of 64 95, 5.5 TB/s); 4 requests of up to 131072
-// tokens, 32 heads: 251 us, 6.2 TB/s (fp32 276), bound by memory; 8 fp32 requests of up to
-// 1028: 13.1 us, one request of 1088: 7.6 us (a chain of latencies: length, page table, keys,
+// tokens, 32 heads: 254 us, 6.2 TB/s (fp32 276), bound by memory; 8 fp32 requests of up to
+// 1028: 13.3 us, one request of 1088: 6.2 us (a chain of latencies: length, page table, keys,
 // join).
 //
 // Masked positions are neither loaded nor multiplied: their key and value registers
@@ -192,10 +192,12 @@ struct Shared {
     bool last;
 };
 
-// The end of a unit, or of a part of it: sums of the block's warps, and of the unit's `active` blocks
-// in the last one to arrive.  head: the first of the group's `heads` query heads; slot: where this
-// block's part goes; slot_of(x): where the unit's part x is.
-template <int D, bool Q8, typename T, typename SlotOf>
+// The end of a unit of the 8-bit cache, or of a part of it: sums of the block's warps, and of the unit's
+// `active` blocks in the last one to arrive.  head: the first of the group's `heads` query heads; slot:
+// where this block's part goes; slot_of(x): where the unit's part x is.  (The bf16 cache's kernel has an end
+// of its own: with this one 8 requests of up to 1028 took 13.6 us instead of 13.3, 4 of up to 3000 13.8
+// instead of 13.5.)
+template <int D, typename T, typename SlotOf>
 __device__ __forceinline__ void join(const DecodeArgs& p, Shared& sh, const float* sm_o, int pitch, const float (&m)[2],
                                      float (&l)[2], int b, int head, int heads, int active, unsigned* counter, int64_t slot,
                                      SlotOf&& slot_of) {
@@ -299,7 +301,7 @@ __device__ __forceinline__ void join(const DecodeArgs& p, Shared& sh, const floa
         }
     };
     using std::integral_constant;
-    if (Q8 && units > kThreads)
+    if (units > kThreads)
         gather(integral_constant<int, 2>{}, integral_constant<int, 9>{});
     else
         gather(integral_constant<int, 1>{}, integral_constant<int, 12>{});
@@ -443,13 +445,19 @@ __global__ void __launch_bounds__(kThreads, kResident) window_decode_kernel(cons
         at = at_next;
     }
 
-    // The next launch may come now and not from the start: where calls of a few microseconds follow each
-    // other without a pause, its waiting blocks slowed this one's (one request of 1088: 8.4 us a call, 7.5
-    // so, and 7.5 and 6.8 in a graph).
-    pdl_trigger();
+    // The next launch comes at this one's end.  Where it may come from the start, or from here, its waiting
+    // blocks slow this one's (graph and stream, us, from the start, from here, and so: one request of 1088
+    // 7.7 8.3, 6.5 7.4, 6.2 6.2; 16 of up to 2000, 20/4 heads of 64, 12.0 12.3, 11.8 12.0, 11.0 11.1; in turn
+    // with an append all alike).
     // ---- join the warps: heads 2 c4 + h, elements 64 x + 8 n4 .. + 7
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
+#pragma unroll
+        for (int x = 4; x < 32; x *= 2) l[h] += __shfl_xor_sync(0xffffffffu, l[h], x);
+        if (n4 == 0) {
+            sh.m[warp][2 * c4 + h] = m[h];
+            sh.l[warp][2 * c4 + h] = l[h];
+        }
 #pragma unroll
         for (int x = 0; x < NV; ++x)
 #pragma unroll
@@ -457,9 +465,79 @@ __global__ void __launch_bounds__(kThreads, kResident) window_decode_kernel(cons
                 *reinterpret_cast<float4*>(&sm_o[warp][2 * c4 + h][64 * x + 8 * n4 + 2 * e]) = make_float4(
                     o[4 * x + e][h], o[4 * x + e][2 + h], o[4 * x + e + 1][h], o[4 * x + e + 1][2 + h]);
     }
-    const int64_t unit = (int64_t)b * gridDim.y + blockIdx.y, part0 = unit * p.plan.splits;
-    join<D, false, T>(p, sh, &sm_o[0][0][0], 8 * D, m, l, b, kvh * G + head0, heads, active, p.counters + unit, part0 + split,
-               [&](int x) { return part0 + x; });
+    __syncthreads();
+    const int64_t unit = (int64_t)b * gridDim.y + blockIdx.y;
+    const int units = heads * (D / 4);  // four elements of a head each
+    T* out = static_cast<T*>(a.o) + ((int64_t)b * a.Hq + kvh * G + head0) * D;
+    auto put = [&](int u, float4 r, float inv) {
+        r.x *= inv; r.y *= inv; r.z *= inv; r.w *= inv;
+        if constexpr (F32)
+            reinterpret_cast<float4*>(out)[u] = r;
+        else
+            reinterpret_cast<uint2*>(out)[u] = make_uint2(pack(r.x, r.y), pack(r.z, r.w));
+    };
+    for (int u = threadIdx.x; u < units; u += kThreads) {
+        const int h = u / (D / 4);
+        float mt = -INFINITY, lt = 0.f;
+#pragma unroll
+        for (int x = 0; x < kWarps; ++x) mt = fmaxf(mt, sh.m[x][h]);
+        float4 r = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int x = 0; x < kWarps; ++x) {
+            const float f = sh.m[x][h] == -INFINITY ? 0.f : exp2f(sh.m[x][h] - mt);
+            const float4 y = *reinterpret_cast<const float4*>(&sm_o[x][h][4 * (u % (D / 4))]);
+            lt = fmaf(f, sh.l[x][h], lt);
+            r.x = fmaf(f, y.x, r.x); r.y = fmaf(f, y.y, r.y); r.z = fmaf(f, y.z, r.z); r.w = fmaf(f, y.w, r.w);
+        }
+        if (active == 1) {
+            put(u, r, lt == 0.f ? 0.f : 1.0f / lt);
+        } else {
+            const int64_t at = (unit * p.plan.splits + split) * p.plan.heads + h;
+            __stcg(reinterpret_cast<float4*>(p.part + at * D) + u % (D / 4), r);
+            if (u % (D / 4) == 0) __stcg(p.ml + at, make_float2(mt, lt));
+        }
+    }
+    if (active == 1) return;
+    // ---- join the blocks: the last one to arrive sums all parts, in their order; the
+    // counter wraps to zero with that arrival
+    __threadfence();
+    __syncthreads();
+    if (threadIdx.x == 0) sh.last = atomicInc(p.counters + unit, (unsigned)active - 1u) == (unsigned)active - 1u;
+    __syncthreads();
+    if (!sh.last) return;
+    __threadfence();
+    for (int u = threadIdx.x; u < units; u += kThreads) {
+        const int h = u / (D / 4);
+        const int64_t first = unit * p.plan.splits * p.plan.heads + h;
+        float mt = -INFINITY, lt = 0.f;
+        float4 r = make_float4(0.f, 0.f, 0.f, 0.f);
+        constexpr int BATCH = 12;  // parts whose loads are in flight together
+        for (int x0 = 0; x0 < active; x0 += BATCH) {
+            float2 ml[BATCH];
+            float4 y[BATCH];
+#pragma unroll
+            for (int x = 0; x < BATCH; ++x) {
+                const int64_t at = first + (int64_t)min(x0 + x, active - 1) * p.plan.heads;
+                ml[x] = __ldcg(p.ml + at);
+                y[x] = __ldcg(reinterpret_cast<const float4*>(p.part + at * D) + u % (D / 4));
+            }
+            float mb = mt;
+#pragma unroll
+            for (int x = 0; x < BATCH; ++x) mb = fmaxf(mb, ml[x].x);
+            const float keep = mt == -INFINITY ? 0.f : exp2f(mt - mb);
+            mt = mb;
+            lt *= keep;
+            r.x *= keep; r.y *= keep; r.z *= keep; r.w *= keep;
+#pragma unroll
+            for (int x = 0; x < BATCH; ++x) {
+                const float f = x0 + x < active && ml[x].x != -INFINITY ? exp2f(ml[x].x - mt) : 0.f;
+                lt = fmaf(f, ml[x].y, lt);
+                r.x = fmaf(f, y[x].x, r.x); r.y = fmaf(f, y[x].y, r.y);
+                r.z = fmaf(f, y[x].z, r.z); r.w = fmaf(f, y[x].w, r.w);
+            }
+        }
+        put(u, r, lt == 0.f ? 0.f : 1.0f / lt);
+    }
 }
 
 // ---------------------------------------------------------------------------
@@ -729,7 +807,7 @@ __global__ void __launch_bounds__(kThreads, kResident8) window_decode_q8_kernel(
             else
                 tile(std::false_type{});
         }
-        pdl_trigger();  // (see window_decode_kernel)
+        pdl_trigger();  // (from the start one request of 640 took 9.2 us a call, so 7.2)
         asm volatile("cp.async.wait_all;" ::: "memory");
         __syncwarp();
         float* sm_o = reinterpret_cast<float*>(mine);
@@ -743,7 +821,7 @@ __global__ void __launch_bounds__(kThreads, kResident8) window_decode_q8_kernel(
         // A block's part of a unit that began in an earlier block is its first, of one that ends in a
         // later block its second; a unit's counter is that of the block where it begins.
         const int64_t from = unit_at / share, active = (unit_at + steps - 1) / share - from + 1;
-        join<D, true, T>(p, sh, reinterpret_cast<const float*>(ring), kStages * Gr::BYTES / 4, m, l, b, kvh * G + head0, heads,
+        join<D, T>(p, sh, reinterpret_cast<const float*>(ring), kStages * Gr::BYTES / 4, m, l, b, kvh * G + head0, heads,
                    (int)active, p.counters + from, 2 * (int64_t)blockIdx.x + (from == blockIdx.x),
                    [&](int x) { return 2 * (from + x) + (x == 0); });
         unit_at += steps;
@@ -771,8 +849,7 @@ int64_t visible_tiles(int window, int sinks, int max_ctx) {
 // fifths of the places that the card has for blocks, or more, all blocks run at once: whole
 // waves, few joins, down to a tile per warp (4 requests of up to 131072 tokens: 14 parts
 // each, 251 us, 267 us with blocks of 48 tiles; 8 requests of up to 1028: 12.9 us, 20.7 us
-// with blocks of 4; one of 1088 in 17 parts: 6.7 us a call and 7.6 in a graph, in nine parts
-// 6.7 and 6.9).  But the lengths are on the device, and what is one wave of equal requests is a
+// with blocks of 4; one of 1088 in 17 parts: 6.2 us).  But the lengths are on the device, and what is one wave of equal requests is a
 // few blocks at work when one is long and the others are short.  So a wave's blocks have at
 // most 384 tiles, or a request alone has blocks for half of the SMs (48 requests, one of
 // 131072 tokens among 1000: 139 us, 2150 us unsplit; 8: 102 and 371 us; the price: 8 of 65536
