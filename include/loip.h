@@ -674,9 +674,9 @@ int loip_k_cache_read_q8(const void* kv_base, const int64_t* page_offsets, int32
  * value's block the 32 elements.  The scratch rules are the same, and one scratch
  * serves the calls on both kinds of cache; a prompt call whose pages meet many rows
  * keeps them there as bf16 tiles (up to 1 GiB, which the size function counts).  Prompt
- * rows are computed one by one, slowly, where a tile of theirs meets NaN in a value that
- * only some of them see, or a block that is not zero with E below 71 or above 191
- * (elements below 2^-62, or of 2^58 and more).  The cache is in device memory. */
+ * rows are computed one by one, slowly, where a tile of theirs meets NaN in a value of a
+ * page that not all of them see in full, or a block that is not zero with E below 71 or
+ * above 191 (elements below 2^-62, or of 2^58 and more).  The cache is in device memory. */
 int loip_k_window_attention_q8(const void* q, int32_t dtype, const void* kv_base, const int64_t* page_offsets,
                                int32_t max_pages, const int32_t* ctx_lens, int32_t B, int32_t Hq, int32_t Hkv,
                                int32_t d, int32_t page_tokens, int32_t layer, uint64_t layer_page_bytes,

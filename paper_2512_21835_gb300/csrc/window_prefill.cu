@@ -199,6 +199,10 @@ struct Use {
     }
 };
 
+// Of an image: it lacks blocks whose exponents it has no form for, so that rows that see the page are walked; it
+// has values of NaN, so that they are walked where not all rows of their tiles see the whole page.
+enum ImageFlags : unsigned { kImageLacks = 1, kImageNan = 2 };
+
 struct PrefillArgs {
     WindowArgs a;
     int heads, groups;  // query heads per row tile, groups per kv head
@@ -212,7 +216,7 @@ struct PrefillArgs {
     unsigned* ended;    // [unit][split]: PartEnd
     // in scratch, with images; a prompt's pages in the order of its list
     uint8_t* images;    // [prompt][image_pages][kv head][keys, values]: tiles as they lie in shared memory
-    unsigned* flags;    // [prompt][image_pages][kv head]: whether rows that see the page are walked
+    unsigned* flags;    // [prompt][image_pages][kv head]: ImageFlags
     int image_pages;
 };
 
@@ -568,6 +572,9 @@ __global__ void __launch_bounds__(Cfg<D, NP, QT, SRC>::THREADS, 1)
         return k;
     };
 
+    // whether every row of the block sees the whole page that begins at position b
+    auto shared = [&](int b) { return b + KT - 1 <= pos0 && (b > pos1 - a.window || b + KT <= a.sinks); };
+
     Waiter wait{c, false};
     auto stopped = [&] { return *(volatile int*)&c->abort != 0; };
     if (warp >= 8) {
@@ -608,7 +615,7 @@ __global__ void __launch_bounds__(Cfg<D, NP, QT, SRC>::THREADS, 1)
                 auto put = [&](int b, uint32_t to, auto which) {
                     constexpr int V = decltype(which)::value;
                     const bool whole = b + KT <= pages.last && ((b >= win0 && a.window > 0) || b + KT <= a.sinks);
-                    const bool shared = b + KT - 1 <= pos0 && (b > pos1 - a.window || b + KT <= a.sinks);
+                    const bool some = V && !shared(b);  // values that not all rows of the block see
                     uint32_t scale[PASSES];
 #pragma unroll
                     for (int k = 0; k < PASSES; ++k) {
@@ -617,7 +624,7 @@ __global__ void __launch_bounds__(Cfg<D, NP, QT, SRC>::THREADS, 1)
                         if (!whole && !(pos < pages.last && ((pos >= win0 && a.window > 0) || pos < a.sinks))) {
                             scale[k] = 0u;
                         } else if (!q8::shift_holds(exp[V][k])) {
-                            scale[k] = unheld(code[V][k], exp[V][k], V && !shared);
+                            scale[k] = unheld(code[V][k], exp[V][k], some);
                         }
                     }
 #pragma unroll
@@ -678,15 +685,18 @@ __global__ void __launch_bounds__(Cfg<D, NP, QT, SRC>::THREADS, 1)
                     }
                 }
             } else if constexpr (C::IMG) {
-                if (warp == 8 && n > 0) {
+                const Pages all(a, c->prompt0, c->prompt1);
+                auto image = [&](int t) {  // of tile t, counted in kv heads of pages
+                    const int j = page_at(t);
+                    return ((int64_t)req * p.image_pages + (j < all.sink ? j : j - all.win + all.sink)) * a.Hkv + kvh;
+                };
+                if (warp == 9) {
+                    for (int t = lane; t < n; t += 32) {
+                        const unsigned flags = p.flags[image(t)];
+                        if (flags & kImageLacks || (flags & kImageNan && !shared(page_at(t) * KT))) *(volatile int*)&c->bad = 1;
+                    }
+                } else if (n > 0) {
                     // -------------------------------------------------------- loader, images
-                    const Pages all(a, c->prompt0, c->prompt1);
-                    auto image = [&](int t) {  // of tile t, counted in kv heads of pages
-                        const int j = page_at(t);
-                        return ((int64_t)req * p.image_pages + (j < all.sink ? j : j - all.win + all.sink)) * a.Hkv + kvh;
-                    };
-                    for (int t = lane; t < n; t += 32)
-                        if (p.flags[image(t)]) *(volatile int*)&c->bad = 1;
                     Use use{0, 0, 0}, freed{0, 0, 0};
                     int issued = 0;
 #pragma unroll 1
@@ -779,8 +789,7 @@ __global__ void __launch_bounds__(Cfg<D, NP, QT, SRC>::THREADS, 1)
                     bool some = false;
                     if (t >= 0) {
                         load(t, true, dst + C::TILE);
-                        const int b = page_at(t) * KT;
-                        some = !(b + KT - 1 <= pos0 && (b > pos1 - a.window || b + KT <= a.sinks));
+                        some = !shared(page_at(t) * KT);
                     }
                     asm volatile("cp.async.commit_group;" ::: "memory");
                     if (!some)
@@ -1413,7 +1422,7 @@ __global__ void __launch_bounds__(Cfg<D, NP, QT, SRC>::THREADS, 1)
 // Images of the pages that some row of a prompt sees, a block per page and kv head: codes to bf16 times
 // 2^-kShift, as the tiles lie in shared memory, so that a plain copy fetches them (made where enough row
 // tiles meet a page, least_reuse).
-// What no row of the prompt sees is zero.  Values of NaN, and extreme exponents, flag the page.
+// What no row of the prompt sees is zero.  Extreme exponents, and NaN in values, flag the page.
 template <int D>
 __global__ void __launch_bounds__(256) window_image_kernel(const __grid_constant__ PrefillArgs p) {
     using Gr = q8::Granule<D>;
@@ -1444,7 +1453,7 @@ __global__ void __launch_bounds__(256) window_image_kernel(const __grid_constant
             code[v][k] = *reinterpret_cast<const uint4*>(g + Gr::piece(v, r % 16, ch));
             exp[v][k] = *reinterpret_cast<const uint8_t*>(g + Gr::exponents(v, r % 16) + ch / 2);
         }
-    bool flag = false;
+    unsigned flags = 0;
 #pragma unroll
     for (int v = 0; v < 2; ++v)
 #pragma unroll
@@ -1456,8 +1465,9 @@ __global__ void __launch_bounds__(256) window_image_kernel(const __grid_constant
                 scale = 0u;
             } else if (!q8::shift_holds(E)) {
                 const bool nan = E > q8::kMostExponent;
-                scale = nan && !v ? 0x7fc07fc0u : 0u;
-                flag |= nan ? v : ((x[0] | x[1] | x[2] | x[3]) & 0x7f7f7f7fu) != 0u;
+                scale = nan ? 0x7fc07fc0u : 0u;
+                if (nan && v) flags |= kImageNan;
+                if (!nan && ((x[0] | x[1] | x[2] | x[3]) & 0x7f7f7f7fu)) flags |= kImageLacks;
             }
             uint32_t u[8];
 #pragma unroll
@@ -1471,8 +1481,8 @@ __global__ void __launch_bounds__(256) window_image_kernel(const __grid_constant
                          "r"(u[3]), "r"(u[4]), "r"(u[5]), "r"(u[6]), "r"(u[7])
                          : "memory");
         }
-    const int any = __syncthreads_or(flag);
-    if (threadIdx.x == 0) p.flags[at] = any != 0;
+    flags = (__syncthreads_or(flags & kImageLacks) ? kImageLacks : 0u) | (__syncthreads_or(flags & kImageNan) ? kImageNan : 0u);
+    if (threadIdx.x == 0) p.flags[at] = flags;
 }
 
 // The parts of a row tile, in their order: a block per unit and 16 columns, a thread per row

@@ -125,3 +125,22 @@ def test_equal_prompts_give_equal_bits(torch, L, Hq, Hkv, d, runs, dtype):
     assert bool(torch.isfinite(first).all())
     for _ in range(4):
         assert torch.equal(_prefill(torch, L, c, qd, runs, Hq, ALL, 0, c.max_pages * P), first)
+
+
+# values of NaN that every row sees: the other columns are computed as without them, bit for bit
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("Hq,Hkv,d,runs,window,j", [
+    (16, 4, 64, [(12, 130)], ALL, 40), (64, 4, 128, [(150, 130)], ALL, 40), (64, 4, 64, [(640, 130)], ALL, 127),
+    (64, 4, 64, [(150, 130)], 500, 0), (64, 4, 128, [(150, 130)], 0, 1)])
+def test_a_value_of_nan_that_all_rows_see(torch, L, Hq, Hkv, d, runs, window, j, dtype):
+    sinks = 0 if window else 64
+    n = max(rows + first for rows, first in runs)
+    c, sizes = filled(1, n, Hkv, d, 341, 120, 130, zeros=True)
+    M = sum(rows for rows, _ in runs)
+    qd, _ = _rows(torch, queries(M, Hq, d, sizes, 342), dtype)
+    plain = _host(_prefill(torch, L, c, qd, runs, Hq, window, sinks, c.max_pages * P)).reshape(M, Hkv, -1, d)
+    c.bytes[c.slot(0, j, 1)[1][1, 1]] = 255
+    got = _host(_prefill(torch, L, c, qd, runs, Hq, window, sinks, c.max_pages * P)).reshape(M, Hkv, -1, d)
+    assert np.all(np.isnan(got[:, 1, :, 32:64])) and np.all(np.isfinite(plain))
+    got[:, 1, :, 32:64] = plain[:, 1, :, 32:64]
+    assert np.array_equal(got, plain)
