@@ -568,7 +568,9 @@ uint64_t loip_k_lm_head_scratch_bytes(int32_t B, int32_t V);
  * for prompts, whose outputs are off by 0.0021 of their size (root mean square)
  * instead of the 0.0017 of their own rounding (a caller who wants more passes
  * fp32 rows).  An infinity that a row sees answers as by the definition, its
- * weights being fp32 numbers (one below their range is zero, and 0 x inf NaN).
+ * weights being fp32 numbers (one below their range is zero, and 0 x inf NaN).  A sum of
+ * weights times values past fp32's range is infinite, whatever their mean (the largest
+ * weight is 1; in prompts of bf16 rows it may be 2^8).
  * d = 64 or 128; any Hq / Hkv.  Zero rows are allowed and launch nothing.  Every
  * call is async on `stream`, allocates nothing and can be captured in a CUDA graph;
  * a refusal (LOIP_ERR_INVALID, message in loip_last_error(NULL)) comes before

@@ -32,7 +32,7 @@
 // 1240 TFLOP/s, tensor pipe active 54%; bound by the chain from P of a tile to S of the
 // next but one (waits, issue and answer, 1700 cycles per tile of which the tensor core
 // works 1280).  4 x 512 fp32 rows of 64 heads 111 us: half of a block's time is its
-// queries, its join and its outputs.  8192 fp32 rows 1330 us.  The registers (168) do not
+// queries, its join and its outputs.  8192 fp32 rows 1326 us.  The registers (168) do not
 // hold everything: in the tile loop a softmax warp reloads two or three spilled words a tile
 // and stores none.
 //
@@ -69,9 +69,9 @@
 // the order P V (t), S (t + 2) every S is there when the softmax gets to it, and P needs no wait at all.
 // The issuing warps ask for the next step's barriers between this step's MMAs, so that the tensor core's
 // queue does not run dry over their answers (1168 -> 1055 us).
-// Measured: 8192 bf16 rows of 32 heads of 128 behind 8192, all visible: 1055 us in a graph, 1563 TFLOP/s
-// (tensor pipe active 68%, 1500 cycles a step of which the tensor core works 1280), with the images' 17;
-// with kCodes 1356.  4999 ragged rows of 40 heads in 7 prompts, window 1024: 157 us (920 blocks, 17
+// Measured: 8192 bf16 rows of 32 heads of 128 behind 8192, all visible: 1049 to 1119 us by the clock, 1570
+// to 1470 TFLOP/s (tensor pipe active 68%, 1500 cycles a step of which the tensor core works 1280), with the
+// images' 17; with kCodes 1356 where that was 1055.  4999 ragged rows of 40 heads in 7 prompts, window 1024: 157 us (920 blocks, 17
 // pages each: 17 us of pages, 10 us around them: launch and tensor memory 2, first tile 4.5, outputs
 // 3.3).  fp32: 2048 rows behind 6144 570 us, 422 TFLOP/s (bound by the softmax: three planes of P and O
 // drained every tile); 47 rows behind 1041 17.2 us (two launches and a chain of latencies).

@@ -144,3 +144,26 @@ def test_a_value_of_nan_that_all_rows_see(torch, L, Hq, Hkv, d, runs, window, j,
     assert np.all(np.isnan(got[:, 1, :, 32:64])) and np.all(np.isfinite(plain))
     got[:, 1, :, 32:64] = plain[:, 1, :, 32:64]
     assert np.array_equal(got, plain)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("d,rows", [(128, 150), (64, 640)])
+def test_a_value_of_nan_that_the_first_rows_do_not_see(torch, L, d, rows, dtype):
+    """Rows before it are finite; the row tiles behind its page are computed as without it, bit for bit."""
+    Hq, Hkv, first, j = 64, 4, 30, 40
+    c, sizes = filled(1, rows + first, Hkv, d, 351, 120, 130, zeros=True)
+    qd, q64 = _rows(torch, queries(rows, Hq, d, sizes, 352), dtype)
+    plain = _host(_prefill(torch, L, c, qd, [(rows, first)], Hq, ALL, 0, c.max_pages * P)).reshape(rows, Hkv, -1, d)
+    c.bytes[c.slot(0, j, 1)[1][1, 1]] = 255
+    got = _host(_prefill(torch, L, c, qd, [(rows, first)], Hq, ALL, 0, c.max_pages * P)).reshape(rows, Hkv, -1, d)
+    nan = np.zeros(got.shape, dtype=bool)
+    nan[j - first:, 1, :, 32:64] = True
+    assert np.array_equal(np.isnan(got), nan)
+    for t in range(j - first):
+        want, t32, tbf = W.attend(c, 0, first + t, q64[t].reshape(Hq, d), ALL, 0)
+        assert np.all(np.abs(got[t].reshape(Hq, d) - want) <= (t32 if dtype == "f32" else tbf)), t
+    behind = P - 1 - first + 16  # two row tiles of eight positions further on
+    got[nan] = plain[nan]
+    assert np.array_equal(got[behind:], plain[behind:])
+    others = [0, 2, 3]
+    assert np.array_equal(got[:, others], plain[:, others])
