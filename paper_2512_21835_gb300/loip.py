@@ -416,7 +416,8 @@ def _s(stream):
     return stream
 
 
-_of_torch = []  # current raw stream of a device, current device, types of rows, int32, int64, types of bf16 and its bits
+# current raw stream of a device, current device, types of rows, int32, int64, types of bf16 and its bits, tensors
+_of_torch = []
 
 
 def _torch():
@@ -425,7 +426,7 @@ def _torch():
     if not _of_torch:
         _of_torch.extend([torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice,
                           {torch.float32: F32_ROWS, torch.bfloat16: BF16_ROWS}, torch.int32, torch.int64,
-                          (torch.bfloat16, torch.int16, torch.uint16)])
+                          (torch.bfloat16, torch.int16, torch.uint16), torch.Tensor])
     return torch
 
 
@@ -703,7 +704,7 @@ def _cache_q8(x, rows, *others):
     if rows.get_device() != here:
         _refuse(f"rows on device {rows.get_device()} in a call on device {here}")
     for y in others:
-        if y is not None and not isinstance(y, (int, np.ndarray)) and y.get_device() not in (here, -1):
+        if isinstance(y, _of_torch[6]) and y.get_device() not in (here, -1):
             _refuse(f"a tensor on device {y.get_device()} in a call on device {here}")
     if x is None or isinstance(x, int):
         return x

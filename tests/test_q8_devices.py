@@ -26,3 +26,16 @@ def test_every_tensor_is_of_the_current_device(library, op, name):  # noqa: F811
     with pytest.raises(loip.LoipError, match="device 1") as e:
         op(**{name: OTHERS[op][name]}, **more)
     assert e.value.code == loip.ERR_INVALID and not library.calls
+
+
+class Foreign:
+    """An array of another library on the GPU: no tensor, whatever else it has."""
+    dtype, shape, device, is_cuda = "int32", (B,), "cuda:1", True
+
+
+@pytest.mark.parametrize("op,name", [(op, name) for op, names in OTHERS.items() for name in names
+                                     if name in ("positions", "row_req", "ctx_lens", "first_pos", "page_offsets")])
+def test_what_is_no_tensor_is_refused_by_its_own_check(library, op, name):  # noqa: F811
+    with pytest.raises(loip.LoipError) as e:
+        op(**{name: Foreign()})
+    assert e.value.code == loip.ERR_INVALID and not library.calls
